@@ -48,6 +48,7 @@ typedef int optima_status;
 #define OPTIMA_DTYPE_F32 0
 #define OPTIMA_DTYPE_BF16 1
 #define OPTIMA_DTYPE_F64 2
+#define OPTIMA_DTYPE_I8 3 /* 8-bit codes with scales (optima_rms_norm, optima_w4_*) */
 
 /* Arithmetic of the solver's per-iteration H-products (optima_solver_opts).
  * FP32: v_mfma_f32_16x16x4_f32, fp32 products and sums.
@@ -415,6 +416,124 @@ optima_status optima_qp_solve_batched(const float* H, int64_t d,
                                       const optima_solve_stats* stats,
                                       optima_solve_info* info,
                                       hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Feed-forward half of a decoder block.
+ *
+ * The inputs of the gate and up projections are the RMS norm of the residual
+ * stream, those of the down projection the gated product of the two: the X whose
+ * Hessians the calls above form (Algorithm 1; the paper prunes every linear layer
+ * of a block). The calls below compute both for calibration, their gradients for
+ * recovery steps under the masks, and their few-token forms with 4-bit weights
+ * for serving the pruned block.
+ *
+ * Conventions of these calls: token matrices have a row pitch in elements (ldx,
+ * ...; at least the row's length) and need only the alignment of an element;
+ * weights are contiguous. All are asynchronous on `stream`, record no memset and
+ * synchronise nothing, so that they can be captured in a HIP graph. NaN and
+ * infinities go through the arithmetic. Every sum is fp32 or wider (whole numbers:
+ * int32) and is taken in an order that depends on the sizes only. With no tokens
+ * nothing is read of token matrices. Outputs overlap neither inputs nor each other
+ * except where stated.
+ * ------------------------------------------------------------------------- */
+
+/* RMS norm with the residual's addition.
+ *   s = x + r (r = 0 where R is NULL), y = s * weight / sqrt(mean(s^2) + eps)
+ * over rows of d <= OPTIMA_NORM_MAX_DIM values (larger: OPTIMA_E_UNSUPPORTED).
+ * X, R and S are of `dtype` (F32 or BF16), weight of w_dtype. S (nullable)
+ * receives s rounded to dtype; the norm is taken of the fp32 s. S may be X or R
+ * themselves (same pointer and pitch), and so may Y if it has their type.
+ * Y: y_dtype F32, BF16, or I8: codes q = rne(y / scale) within +-127 with
+ *   scale = max |y| / 127 over each group of `group` consecutive values (32, 64 or
+ *   128; the last group of a row may be shorter) or over the row (group = 0).
+ *   scales[n_tok][ceil(d / group)] (one a row for group = 0) is required then. A
+ *   group of zeros has scale 0; one with a NaN or infinity has codes 0 and a NaN
+ *   or infinite scale. For other types scales is NULL and group 0.
+ * eps > 0. */
+#define OPTIMA_NORM_MAX_DIM 16384
+optima_status optima_rms_norm(const void* X, int64_t ldx, const void* R, int64_t ldr, int dtype,
+                              int64_t n_tok, int64_t d, const void* weight, int w_dtype,
+                              float eps, void* S, int64_t lds, void* Y, int64_t ldy, int y_dtype,
+                              float* scales, int64_t group, hipStream_t stream);
+
+/* Gradient of the RMS norm at S, the sum that the forward call stored. With
+ * rstd = 1 / sqrt(mean(s^2) + eps), xh = s rstd and p = weight * dy:
+ *   dX = dS + rstd (p - xh mean(p xh)),   dweight = sum over tokens of dy xh.
+ * dS (nullable) is the gradient that reaches s from the residual stream; dX is the
+ * gradient of both x and r, and may be dY or dS themselves. S, dY, dS and dX are of
+ * `dtype`. dweight (nullable): fp32 [d], added to what it holds with accumulate = 1.
+ * ws: optima_rms_norm_backward_workspace_bytes(n_tok, d) bytes, unless dweight is
+ * NULL. */
+size_t optima_rms_norm_backward_workspace_bytes(int64_t n_tok, int64_t d);
+optima_status optima_rms_norm_backward(const void* S, int64_t lds, const void* weight, int w_dtype,
+                                       const void* dY, int64_t lddy, const void* dS, int64_t ldds,
+                                       int dtype, int64_t n_tok, int64_t d, float eps, void* dX,
+                                       int64_t lddx, float* dweight, int accumulate, void* ws,
+                                       size_t ws_bytes, hipStream_t stream);
+
+/* Gated feed-forward product.
+ *   G = X Wg^T, U = X Wu^T, H = act(G) * U element by element
+ * X: [n_tok][d_in] bf16, any d_in >= 1; Wg, Wu: [d_ff][d_in] bf16 (16-byte aligned
+ * where d_in % 64 == 0). H: h_dtype BF16 or F32. G and U (nullable): bf16
+ * [n_tok][d_ff], what the gradient takes; H is formed of the unrounded sums.
+ * act: OPTIMA_ACT_SILU or OPTIMA_ACT_NONE.
+ * ws: optima_gated_forward_workspace_bytes(n_tok, d_in, d_ff) bytes (0 for few
+ * tokens): copies of operands whose rows do not suit wide loads. */
+size_t optima_gated_forward_workspace_bytes(int64_t n_tok, int64_t d_in, int64_t d_ff);
+optima_status optima_gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d_in,
+                                   const void* Wg, const void* Wu, int64_t d_ff, int act, void* H,
+                                   int64_t ldh, int h_dtype, void* G, int64_t ldg, void* U,
+                                   int64_t ldu, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradient of the gated product.
+ *   dU = dH * act(G), dG = dH * U * act'(G), each rounded to bf16 for the products
+ *   dX = dG Wg + dU Wu,  dWg = mask_g * (dG^T X),  dWu = mask_u * (dU^T X)
+ * X, Wg, Wu, act as in the forward call, G and U what it stored, dH bf16. dX
+ * (nullable): dx_dtype BF16 or F32. dWg and dWu (both or neither): [d_ff][d_in] of
+ * dw_dtype, added to what they hold with accumulate = 1. mask_g, mask_u (each
+ * nullable): uint8 [d_ff][d_in]; where 0, the weight is pruned and its gradient is
+ * exactly 0, so that a step along it keeps the pattern.
+ * ws: optima_gated_backward_workspace_bytes(n_tok, d_in, d_ff) bytes. */
+size_t optima_gated_backward_workspace_bytes(int64_t n_tok, int64_t d_in, int64_t d_ff);
+optima_status optima_gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t d_in,
+                                    const void* Wg, const void* Wu, int64_t d_ff, int act,
+                                    const void* G, int64_t ldg, const void* U, int64_t ldu,
+                                    const void* dH, int64_t lddh, void* dX, int64_t lddx,
+                                    int dx_dtype, void* dWg, void* dWu, int dw_dtype,
+                                    const uint8_t* mask_g, const uint8_t* mask_u, int accumulate,
+                                    void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* 4-bit weights with group scales.
+ * W: [n][d] F32 or BF16. Groups of `group` (32, 64 or 128) consecutive values of a
+ * row have scale = bf16(max |w| / 7) and codes clamp(rne(w / scale), -7, 7): a zero
+ * weight, as every pruned one is, stays exactly zero. A group with a NaN or infinity
+ * has codes 0 and a NaN or infinite scale.
+ * Q: [n][optima_w4_row_bytes(d)], 16-byte aligned. A chunk of 128 codes takes 64
+ *   bytes: dword j of its 16-byte block b holds codes 32 j + 8 b .. + 7, the even ones
+ *   in nibbles 0..3 and the odd ones in nibbles 4..7, each as code + 8; rows are
+ *   padded to whole chunks with zero codes.
+ * scales: bf16 [n][ceil(d / group)]. */
+size_t optima_w4_row_bytes(int64_t d);
+optima_status optima_w4_pack(const void* W, int dtype, int64_t n, int64_t d, int64_t group,
+                             void* Q, void* scales, hipStream_t stream);
+
+/* Y = X deq(Q)^T for the tokens of decoding steps: the weights are streamed once for
+ * every 64 tokens.
+ * X: [n_tok][d] of x_dtype BF16, or I8 with x_scales: fp32 [n_tok][ceil(d / x_group)]
+ * with x_group = group, or one a token with x_group = 0 (as optima_rms_norm writes
+ * them). Y: [n_tok][d_out] BF16 or F32. 8-bit codes are multiplied exactly within a
+ * group. */
+optima_status optima_w4_linear(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
+                               int64_t x_group, int64_t n_tok, int64_t d, const void* Q,
+                               const void* scales, int64_t group, int64_t d_out, void* Y,
+                               int64_t ldy, int y_dtype, hipStream_t stream);
+
+/* The gated product with 4-bit weights: H = act(X deq(Qg)^T) * (X deq(Qu)^T). */
+optima_status optima_w4_gated(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
+                              int64_t x_group, int64_t n_tok, int64_t d, const void* Qg,
+                              const void* scales_g, const void* Qu, const void* scales_u,
+                              int64_t group, int64_t d_ff, int act, void* H, int64_t ldh,
+                              int h_dtype, hipStream_t stream);
 
 #ifdef __cplusplus
 }

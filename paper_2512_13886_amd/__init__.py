@@ -17,7 +17,12 @@ from ._lib import (OptimaError, SolverOpts, DTYPE_F32, DTYPE_BF16, DTYPE_F64, PR
                    optima_spectral_lanczos_workspace_bytes, optima_spectral_lanczos,
                    optima_wanda_mask, optima_qp_workspace_bytes,
                    optima_qp_solve_batched, ACT_NONE, ACT_SILU,
-                   optima_linear_forward_workspace_bytes, optima_linear_forward)
+                   optima_linear_forward_workspace_bytes, optima_linear_forward, DTYPE_I8,
+                   NORM_MAX_DIM, optima_rms_norm, optima_rms_norm_backward_workspace_bytes,
+                   optima_rms_norm_backward, optima_gated_forward_workspace_bytes,
+                   optima_gated_forward, optima_gated_backward_workspace_bytes,
+                   optima_gated_backward, optima_w4_row_bytes, optima_w4_pack,
+                   optima_w4_linear, optima_w4_gated)
 
 __all__ = [
     "OptimaError", "SolverOpts", "DTYPE_F32", "DTYPE_BF16", "DTYPE_F64", "PREC_FP32",
@@ -29,5 +34,9 @@ __all__ = [
     "SPECTRAL_NOALLOC_MAX_DIM", "optima_spectral_norm_noalloc",
     "optima_spectral_lanczos_workspace_bytes", "optima_spectral_lanczos", "optima_wanda_mask",
     "optima_qp_workspace_bytes", "optima_qp_solve_batched", "ACT_NONE", "ACT_SILU",
-    "optima_linear_forward_workspace_bytes", "optima_linear_forward",
+    "optima_linear_forward_workspace_bytes", "optima_linear_forward", "DTYPE_I8",
+    "NORM_MAX_DIM", "optima_rms_norm", "optima_rms_norm_backward_workspace_bytes",
+    "optima_rms_norm_backward", "optima_gated_forward_workspace_bytes", "optima_gated_forward",
+    "optima_gated_backward_workspace_bytes", "optima_gated_backward", "optima_w4_row_bytes",
+    "optima_w4_pack", "optima_w4_linear", "optima_w4_gated",
 ]

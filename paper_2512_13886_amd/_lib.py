@@ -27,6 +27,7 @@ OPTIMA_E_UNSUPPORTED = -5
 DTYPE_F32 = 0
 DTYPE_BF16 = 1
 DTYPE_F64 = 2
+DTYPE_I8 = 3
 METHOD_RAPDHG = 0
 METHOD_CG = 1
 PREC_FP32 = 0
@@ -82,7 +83,7 @@ def _sig(name, res, args):
 _status_string = _sig("optima_status_string", ctypes.c_char_p, [_i32])
 _abi_version = _sig("optima_abi_version", _i32, [])
 # The structs above mirror include/optima.h at this ABI version.
-ABI_VERSION = 11
+ABI_VERSION = 12
 if _abi_version() != ABI_VERSION:
     raise ImportError(f"{_LIB_PATH} has ABI version {_abi_version()}, the binding expects "
                       f"{ABI_VERSION}: rebuild the library")
@@ -109,6 +110,29 @@ _qp_ws = _sig("optima_qp_workspace_bytes", _sz, [_i64, _i64])
 _qp_solve = _sig("optima_qp_solve_batched", _i32,
                  [_vp, _i64, _vp, _vp, _vp, _i64, ctypes.POINTER(_Opts), _vp, _sz, _vp,
                   ctypes.POINTER(_Stats), ctypes.POINTER(_Info), _vp])
+_norm = _sig("optima_rms_norm", _i32,
+             [_vp, _i64, _vp, _i64, _i32, _i64, _i64, _vp, _i32, _f32, _vp, _i64, _vp, _i64, _i32,
+              _vp, _i64, _vp])
+_norm_bwd_ws = _sig("optima_rms_norm_backward_workspace_bytes", _sz, [_i64, _i64])
+_norm_bwd = _sig("optima_rms_norm_backward", _i32,
+                 [_vp, _i64, _vp, _i32, _vp, _i64, _vp, _i64, _i32, _i64, _i64, _f32, _vp, _i64,
+                  _vp, _i32, _vp, _sz, _vp])
+_gated_ws = _sig("optima_gated_forward_workspace_bytes", _sz, [_i64, _i64, _i64])
+_gated = _sig("optima_gated_forward", _i32,
+              [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64,
+               _vp, _sz, _vp])
+_gated_bwd_ws = _sig("optima_gated_backward_workspace_bytes", _sz, [_i64, _i64, _i64])
+_gated_bwd = _sig("optima_gated_backward", _i32,
+                  [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64,
+                   _vp, _i64, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _sz, _vp])
+_w4_row = _sig("optima_w4_row_bytes", _sz, [_i64])
+_w4_pack = _sig("optima_w4_pack", _i32, [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp])
+_w4_linear = _sig("optima_w4_linear", _i32,
+                  [_vp, _i64, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _i32,
+                   _vp])
+_w4_gated = _sig("optima_w4_gated", _i32,
+                 [_vp, _i64, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _i64, _i32,
+                  _vp, _i64, _i32, _vp])
 
 
 def library_path() -> str:
@@ -435,3 +459,232 @@ def optima_qp_solve_batched(H: torch.Tensor, lambda_max: torch.Tensor | None, W0
                      ctypes.byref(c_opts), _ptr(ws), nbytes, _ptr(W_out), ctypes.byref(st),
                      ctypes.byref(info), _stream(stream)))
     return {f[0]: getattr(info, f[0]) for f in _Info._fields_}
+
+
+_ROW_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.int8: DTYPE_I8}
+
+
+def _rows(name, t, shape, dtypes):
+    """(address, row pitch, dtype code) of a token matrix: rows of consecutive elements,
+    any pitch. The address of a matrix without rows is NULL."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be one of {dtypes}, got {t.dtype}")
+    n, d = shape
+    ld = t.stride(0) if n > 1 else d
+    if (d > 1 and t.stride(1) != 1) or ld < d:
+        raise ValueError(f"{name} must have rows of consecutive elements that do not overlap")
+    return (t.data_ptr() if n else None), ld, _ROW_DTYPES[t.dtype]
+
+
+def _opt_rows(name, t, shape, dtypes):
+    return (None, shape[1], 0) if t is None else _rows(name, t, shape, dtypes)
+
+
+def _need_shape(name, t, shape, dtypes):
+    _need_cuda(name, t)
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be one of {dtypes}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+_F = (torch.float32, torch.bfloat16)
+_B = (torch.bfloat16,)
+NORM_MAX_DIM = 16384
+
+
+def optima_rms_norm(X: torch.Tensor, weight: torch.Tensor, Y: torch.Tensor, eps: float = 1e-6,
+                    R: torch.Tensor | None = None, S: torch.Tensor | None = None,
+                    scales: torch.Tensor | None = None, group: int = 0, stream=None) -> None:
+    """Y = s * weight / sqrt(mean(s^2) + eps) with s = X + R, row by row; S receives s.
+
+    X, R, S [n_tok, d] float32 or bfloat16 (one type); weight [d] float32 or bfloat16; Y
+    float32, bfloat16, or int8 codes with scales (float32 [n_tok, ceil(d / group)], or
+    [n_tok, 1] with group = 0). S may be X or R. Rows may have any pitch."""
+    if X.dim() != 2:
+        raise ValueError("X must be [n_tok, d]")
+    n, d = X.shape
+    x, ldx, dt = _rows("X", X, (n, d), _F)
+    r, ldr, _ = _opt_rows("R", R, (n, d), (X.dtype,))
+    s, lds, _ = _opt_rows("S", S, (n, d), (X.dtype,))
+    y, ldy, y_dt = _rows("Y", Y, (n, d), (*_F, torch.int8))
+    _need_shape("weight", weight, (d,), _F)
+    if (Y.dtype == torch.int8) != (scales is not None):
+        raise ValueError("scales go with an int8 Y")
+    if scales is not None:
+        groups = -(-d // group) if group > 0 else 1
+        _need_shape("scales", scales, (n, groups), (torch.float32,))
+    _check(_norm(x, ldx, r, ldr, dt, n, d, _ptr(weight), _ROW_DTYPES[weight.dtype], float(eps), s,
+                 lds, y, ldy, y_dt, _ptr(scales), int(group), _stream(stream)))
+
+
+def optima_rms_norm_backward_workspace_bytes(n_tok: int, d: int) -> int:
+    return int(_norm_bwd_ws(n_tok, d))
+
+
+def optima_rms_norm_backward(S: torch.Tensor, weight: torch.Tensor, dY: torch.Tensor,
+                             dX: torch.Tensor, eps: float = 1e-6, dS: torch.Tensor | None = None,
+                             dweight: torch.Tensor | None = None, accumulate: bool = False,
+                             ws: torch.Tensor | None = None, stream=None) -> None:
+    """dX, the gradient of X and of R, and dweight (float32 [d]; + what it holds with
+    accumulate) of optima_rms_norm at the S it stored, from dY and the gradient dS that
+    reaches S itself. S, dY, dS and dX are [n_tok, d] of one type; dX may be dY or dS."""
+    if S.dim() != 2:
+        raise ValueError("S must be [n_tok, d]")
+    n, d = S.shape
+    s, lds, dt = _rows("S", S, (n, d), _F)
+    dy, lddy, _ = _rows("dY", dY, (n, d), (S.dtype,))
+    ds, ldds, _ = _opt_rows("dS", dS, (n, d), (S.dtype,))
+    dx, lddx, _ = _rows("dX", dX, (n, d), (S.dtype,))
+    _need_shape("weight", weight, (d,), _F)
+    nbytes = 0
+    if dweight is not None:
+        _need_shape("dweight", dweight, (d,), (torch.float32,))
+        ws, nbytes = _workspace(optima_rms_norm_backward_workspace_bytes(n, d), ws, S.device,
+                                stream)
+    _check(_norm_bwd(s, lds, _ptr(weight), _ROW_DTYPES[weight.dtype], dy, lddy, ds, ldds, dt, n, d,
+                     float(eps), dx, lddx, _ptr(dweight), int(bool(accumulate)), _ptr(ws), nbytes,
+                     _stream(stream)))
+
+
+def optima_gated_forward_workspace_bytes(n_tok: int, d_in: int, d_ff: int) -> int:
+    return int(_gated_ws(n_tok, d_in, d_ff))
+
+
+def _gated_weights(X, Wg, Wu):
+    if X.dim() != 2 or Wg.dim() != 2:
+        raise ValueError("X must be [n_tok, d_in] and Wg, Wu [d_ff, d_in]")
+    n, d = X.shape
+    ff = Wg.shape[0]
+    _need_shape("Wg", Wg, (ff, d), _B)
+    _need_shape("Wu", Wu, (ff, d), _B)
+    return n, d, ff
+
+
+def optima_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, H: torch.Tensor,
+                         act: int = ACT_SILU, G: torch.Tensor | None = None,
+                         U: torch.Tensor | None = None, ws: torch.Tensor | None = None,
+                         stream=None) -> None:
+    """H = act(X Wg^T) * (X Wu^T) for X [n_tok, d_in] and Wg, Wu [d_ff, d_in] bfloat16; H
+    bfloat16 or float32 [n_tok, d_ff]. G and U (bfloat16) receive the two products, which
+    optima_gated_backward takes."""
+    n, d, ff = _gated_weights(X, Wg, Wu)
+    x, ldx, _ = _rows("X", X, (n, d), _B)
+    h, ldh, h_dt = _rows("H", H, (n, ff), _F)
+    g, ldg, _ = _opt_rows("G", G, (n, ff), _B)
+    u, ldu, _ = _opt_rows("U", U, (n, ff), _B)
+    need = optima_gated_forward_workspace_bytes(n, d, ff)
+    nbytes = 0
+    if need or ws is not None:
+        ws, nbytes = _workspace(need, ws, X.device, stream)
+    _check(_gated(x, ldx, n, d, _ptr(Wg), _ptr(Wu), ff, int(act), h, ldh, h_dt, g, ldg, u, ldu,
+                  _ptr(ws), nbytes, _stream(stream)))
+
+
+def optima_gated_backward_workspace_bytes(n_tok: int, d_in: int, d_ff: int) -> int:
+    return int(_gated_bwd_ws(n_tok, d_in, d_ff))
+
+
+def optima_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: torch.Tensor,
+                          U: torch.Tensor, dH: torch.Tensor, dX: torch.Tensor | None = None,
+                          dWg: torch.Tensor | None = None, dWu: torch.Tensor | None = None,
+                          act: int = ACT_SILU, mask_g: torch.Tensor | None = None,
+                          mask_u: torch.Tensor | None = None, accumulate: bool = False,
+                          ws: torch.Tensor | None = None, stream=None) -> None:
+    """Gradients of optima_gated_forward: dX [n_tok, d_in] and dWg, dWu [d_ff, d_in], each
+    bfloat16 or float32 (dWg and dWu of one type, + what they hold with accumulate). Where
+    mask_g or mask_u (uint8 [d_ff, d_in]) is 0 the weight's gradient is exactly 0."""
+    n, d, ff = _gated_weights(X, Wg, Wu)
+    x, ldx, _ = _rows("X", X, (n, d), _B)
+    g, ldg, _ = _rows("G", G, (n, ff), _B)
+    u, ldu, _ = _rows("U", U, (n, ff), _B)
+    dh, lddh, _ = _rows("dH", dH, (n, ff), _B)
+    dx, lddx, dx_dt = _opt_rows("dX", dX, (n, d), _F)
+    if (dWg is None) != (dWu is None):
+        raise ValueError("dWg and dWu go together")
+    dw_dt = 0
+    if dWg is not None:
+        _need_shape("dWg", dWg, (ff, d), _F)
+        _need_shape("dWu", dWu, (ff, d), (dWg.dtype,))
+        dw_dt = _ROW_DTYPES[dWg.dtype]
+    for name, m in (("mask_g", mask_g), ("mask_u", mask_u)):
+        if m is not None:
+            _need_shape(name, m, (ff, d), (torch.uint8,))
+    ws, nbytes = _workspace(optima_gated_backward_workspace_bytes(n, d, ff), ws, X.device, stream)
+    _check(_gated_bwd(x, ldx, n, d, _ptr(Wg), _ptr(Wu), ff, int(act), g, ldg, u, ldu, dh, lddh, dx,
+                      lddx, dx_dt, _ptr(dWg), _ptr(dWu), dw_dt, _ptr(mask_g), _ptr(mask_u),
+                      int(bool(accumulate)), _ptr(ws), nbytes, _stream(stream)))
+
+
+def optima_w4_row_bytes(d: int) -> int:
+    return int(_w4_row(d))
+
+
+def optima_w4_pack(W: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, group: int = 128,
+                   stream=None) -> None:
+    """4-bit codes and scales of W [n, d] (float32 or bfloat16): Q uint8
+    [n, optima_w4_row_bytes(d)], scales bfloat16 [n, ceil(d / group)], group 32, 64 or
+    128. Zero weights stay exactly zero."""
+    if W.dim() != 2:
+        raise ValueError("W must be [n, d]")
+    n, d = W.shape
+    _need_shape("W", W, (n, d), _F)
+    _w4_weights("Q", Q, "scales", scales, n, d, group)
+    _check(_w4_pack(_ptr(W), _ROW_DTYPES[W.dtype], n, d, int(group), _ptr(Q), _ptr(scales),
+                    _stream(stream)))
+
+
+def _w4_weights(q_name, Q, s_name, scales, n, d, group):
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    _need_shape(q_name, Q, (n, -(-d // 128) * 64), (torch.uint8,))
+    _need_shape(s_name, scales, (n, -(-d // group)), _B)
+
+
+def _w4_tokens(X, x_scales, x_group, group):
+    if X.dim() != 2:
+        raise ValueError("X must be [n_tok, d]")
+    n, d = X.shape
+    x, ldx, x_dt = _rows("X", X, (n, d), (torch.bfloat16, torch.int8))
+    if (X.dtype == torch.int8) != (x_scales is not None):
+        raise ValueError("x_scales go with an int8 X")
+    if x_scales is not None:
+        if x_group not in (0, group):
+            raise ValueError("x_group must be the weights' group, or 0 (one scale a token)")
+        _need_shape("x_scales", x_scales, (n, -(-d // x_group) if x_group else 1),
+                    (torch.float32,))
+    return n, d, x, ldx, x_dt
+
+
+def optima_w4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y: torch.Tensor,
+                     group: int = 128, x_scales: torch.Tensor | None = None, x_group: int = 0,
+                     stream=None) -> None:
+    """Y = X W^T for the weights W [d_out, d] that Q and scales stand for (optima_w4_pack).
+    X [n_tok, d] bfloat16, or int8 with x_scales as optima_rms_norm writes them (x_group is
+    its group: the weights' group, or 0); Y [n_tok, d_out] bfloat16 or float32."""
+    n, d, x, ldx, x_dt = _w4_tokens(X, x_scales, x_group, group)
+    n_out = Q.shape[0]
+    _w4_weights("Q", Q, "scales", scales, n_out, d, group)
+    y, ldy, y_dt = _rows("Y", Y, (n, n_out), _F)
+    _check(_w4_linear(x, ldx, x_dt, _ptr(x_scales), int(x_group), n, d, _ptr(Q), _ptr(scales),
+                      int(group), n_out, y, ldy, y_dt, _stream(stream)))
+
+
+def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Qu: torch.Tensor,
+                    scales_u: torch.Tensor, H: torch.Tensor, group: int = 128,
+                    act: int = ACT_SILU, x_scales: torch.Tensor | None = None, x_group: int = 0,
+                    stream=None) -> None:
+    """H = act(X Wg^T) * (X Wu^T) with both weights in 4 bits; arguments as in
+    optima_w4_linear."""
+    n, d, x, ldx, x_dt = _w4_tokens(X, x_scales, x_group, group)
+    ff = Qg.shape[0]
+    _w4_weights("Qg", Qg, "scales_g", scales_g, ff, d, group)
+    _w4_weights("Qu", Qu, "scales_u", scales_u, ff, d, group)
+    h, ldh, h_dt = _rows("H", H, (n, ff), _F)
+    _check(_w4_gated(x, ldx, x_dt, _ptr(x_scales), int(x_group), n, d, _ptr(Qg), _ptr(scales_g),
+                     _ptr(Qu), _ptr(scales_u), int(group), ff, int(act), h, ldh, h_dt,
+                     _stream(stream)))

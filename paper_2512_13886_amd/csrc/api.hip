@@ -1,5 +1,5 @@
 // extern "C" entry points of liboptima.so: argument validation, then the
-// launch sequences in hessian.hip, spectral.hip and solver.hip.
+// launch sequences in the other sources.
 #include "common.h"
 
 namespace optima {
@@ -31,6 +31,32 @@ optima_status qp_solve(const float* H, int64_t d, const float* lambda_max, const
                        const uint8_t* mask, int64_t n_cols, const optima_solver_opts& o, void* ws,
                        float* W_out, const optima_solve_stats& stats, optima_solve_info* info,
                        hipStream_t s);
+optima_status rms_norm(const void* X, int64_t ldx, const void* R, int64_t ldr, int dtype, int64_t n,
+                       int64_t d, const void* w, int w_dtype, float eps, void* S, int64_t lds,
+                       void* Y, int64_t ldy, int y_dtype, float* scales, int64_t group,
+                       hipStream_t s);
+size_t rms_norm_backward_workspace_bytes(int64_t n, int64_t d);
+optima_status rms_norm_backward(const void* S, int64_t lds, const void* w, int w_dtype,
+                                const void* dY, int64_t lddy, const void* dS, int64_t ldds,
+                                int dtype, int64_t n, int64_t d, float eps, void* dX, int64_t lddx,
+                                float* dweight, int accumulate, void* ws, hipStream_t s);
+size_t gated_forward_workspace_bytes(int64_t n_tok, int64_t d, int64_t ff);
+optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d, const void* Wg,
+                            const void* Wu, int64_t ff, int act, void* H, int64_t ldh, int h_dtype,
+                            void* G, int64_t ldg, void* U, int64_t ldu, void* ws, hipStream_t s);
+size_t gated_backward_workspace_bytes(int64_t n_tok, int64_t d, int64_t ff);
+optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t d, const void* Wg,
+                             const void* Wu, int64_t ff, int act, const void* G, int64_t ldg,
+                             const void* U, int64_t ldu, const void* dH, int64_t lddh, void* dX,
+                             int64_t lddx, int dx_dtype, void* dWg, void* dWu, int dw_dtype,
+                             const uint8_t* mask_g, const uint8_t* mask_u, int accumulate, void* ws,
+                             hipStream_t s);
+optima_status w4_pack(const void* W, int dtype, int64_t n, int64_t d, int64_t group, void* Q,
+                      void* scales, hipStream_t s);
+optima_status w4_linear(const void* X, int64_t ldx, const float* x_scales, int64_t x_group,
+                        int64_t n_tok, int64_t d, const void* Q, const void* sc, const void* Q2,
+                        const void* sc2, int64_t group, int64_t d_out, int act, void* Y,
+                        int64_t ldy, int y_dtype, hipStream_t s);
 }  // namespace optima
 
 namespace {
@@ -41,6 +67,71 @@ constexpr int64_t kMaxCols = int64_t(1) << 24;
 bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
+}
+
+// A token matrix or another array as a call sees it: `rows` rows of `cols`
+// elements of `esz` bytes, `ld` elements apart.
+struct Span {
+  const void* p;
+  int64_t rows, cols, ld;
+  int64_t esz;
+  size_t bytes() const {
+    return !p || rows < 1 ? 0 : (size_t(rows - 1) * size_t(ld) + size_t(cols)) * size_t(esz);
+  }
+  bool aligned() const { return reinterpret_cast<uintptr_t>(p) % size_t(esz) == 0; }
+  // A pointer where there are rows, elements aligned, and rows that do not overlap.
+  bool good() const {
+    return ld >= cols && ld < (int64_t(1) << 31) && (rows < 1 || p) && aligned();
+  }
+  bool meets(const Span& o) const {
+    return bytes() && o.bytes() && overlaps(p, bytes(), o.p, o.bytes());
+  }
+  // The same elements in the same places: a kernel that reads a row before it
+  // writes it may work in place.
+  bool same(const Span& o) const { return p == o.p && ld == o.ld && esz == o.esz; }
+};
+
+constexpr int64_t kMaxTok = (int64_t(1) << 31) - 1;
+
+int64_t esize(int dtype) {
+  return dtype == OPTIMA_DTYPE_F32 ? 4 : dtype == OPTIMA_DTYPE_BF16 ? 2 : 1;
+}
+bool f32_or_bf16(int dtype) { return dtype == OPTIMA_DTYPE_F32 || dtype == OPTIMA_DTYPE_BF16; }
+bool group_ok(int64_t group) { return group == 32 || group == 64 || group == 128; }
+
+// Sizes of the gated product: tiles of tokens by values stay below 2^31.
+bool gated_sizes(int64_t n_tok, int64_t d_in, int64_t d_ff) {
+  return n_tok >= 0 && n_tok <= kMaxTok && d_in >= 1 && d_in <= kMaxDim && d_ff >= 1 &&
+         d_ff <= kMaxDim &&
+         (n_tok / 64 + 1) * (std::max(d_in, d_ff) / 64 + 1) < (int64_t(1) << 30);
+}
+
+optima_status w4_call(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
+                      int64_t x_group, int64_t n_tok, int64_t d, const void* Q, const void* scales,
+                      const void* Q2, const void* scales2, int64_t group, int64_t d_out, int act,
+                      void* Y, int64_t ldy, int y_dtype, hipStream_t stream) {
+  if (x_dtype != OPTIMA_DTYPE_BF16 && x_dtype != OPTIMA_DTYPE_I8) return OPTIMA_E_UNSUPPORTED;
+  if (!f32_or_bf16(y_dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (n_tok < 0 || n_tok > (int64_t(1) << 21) || d < 1 || d > kMaxDim || d_out < 1 ||
+      d_out > kMaxCols || !group_ok(group))
+    return OPTIMA_E_INVAL;
+  const bool i8 = x_dtype == OPTIMA_DTYPE_I8;
+  if (i8 ? x_group != 0 && x_group != group : x_group != 0 || x_scales) return OPTIMA_E_INVAL;
+  if (!Q || !scales || !optima::aligned16(Q) || !optima::aligned16(Q2)) return OPTIMA_E_INVAL;
+  const int64_t groups = (d + group - 1) / group, x_groups = x_group ? groups : 1;
+  const Span x{X, n_tok, d, ldx, esize(x_dtype)}, y{Y, n_tok, d_out, ldy, esize(y_dtype)};
+  const Span xs{x_scales, n_tok, x_groups, x_groups, 4};
+  if (!x.good() || !y.good() || (i8 && !xs.good())) return OPTIMA_E_INVAL;
+  const int64_t row = int64_t(optima_w4_row_bytes(d));
+  for (int k = 0; k < 2; ++k) {
+    const Span q{k ? Q2 : Q, d_out, row, row, 1};
+    const Span sc{k ? scales2 : scales, d_out, groups, groups, 2};
+    if (!sc.aligned() || y.meets(q) || y.meets(sc)) return OPTIMA_E_INVAL;
+  }
+  if (y.meets(x) || (i8 && y.meets(xs))) return OPTIMA_E_INVAL;
+  if (n_tok == 0) return OPTIMA_OK;
+  return optima::w4_linear(X, ldx, i8 ? x_scales : nullptr, x_group, n_tok, d, Q, scales, Q2,
+                           scales2, group, d_out, act, Y, ldy, y_dtype, stream);
 }
 }  // namespace
 
@@ -58,7 +149,7 @@ const char* optima_status_string(optima_status status) {
   }
 }
 
-int optima_abi_version(void) { return 11; }
+int optima_abi_version(void) { return 12; }
 
 size_t optima_hessian_workspace_bytes(int64_t n_tok, int64_t d, int dtype) {
   if (n_tok < 0 || d < 1 || d > kMaxDim) return 0;
@@ -266,6 +357,162 @@ optima_status optima_qp_solve_batched(const float* H, int64_t d, const float* la
   optima_solve_stats st{};
   if (stats) st = *stats;
   return optima::qp_solve(H, d, lambda_max, W0, mask, n_cols, o, ws, W_out, st, info, stream);
+}
+
+optima_status optima_rms_norm(const void* X, int64_t ldx, const void* R, int64_t ldr, int dtype,
+                              int64_t n_tok, int64_t d, const void* weight, int w_dtype,
+                              float eps, void* S, int64_t lds, void* Y, int64_t ldy, int y_dtype,
+                              float* scales, int64_t group, hipStream_t stream) {
+  if (!f32_or_bf16(dtype) || !f32_or_bf16(w_dtype)) return OPTIMA_E_UNSUPPORTED;
+  const bool i8 = y_dtype == OPTIMA_DTYPE_I8;
+  if (!i8 && !f32_or_bf16(y_dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (n_tok < 0 || n_tok > kMaxTok || d < 1 || !(eps > 0.f) || !weight) return OPTIMA_E_INVAL;
+  if (d > OPTIMA_NORM_MAX_DIM) return OPTIMA_E_UNSUPPORTED;
+  if (i8 ? group != 0 && !group_ok(group) : group != 0 || scales) return OPTIMA_E_INVAL;
+  const int64_t e = esize(dtype), groups = group ? (d + group - 1) / group : 1;
+  const Span x{X, n_tok, d, ldx, e}, r{R, n_tok, d, ldr, e}, w{weight, 1, d, d, esize(w_dtype)};
+  const Span s{S, n_tok, d, lds, e}, y{Y, n_tok, d, ldy, esize(y_dtype)};
+  const Span sc{scales, n_tok, groups, groups, 4};
+  if (!x.good() || !y.good() || !w.aligned() || (R && !r.good()) || (S && !s.good()) ||
+      (i8 && !sc.good()))
+    return OPTIMA_E_INVAL;
+  for (const Span& o : {s, y}) {
+    if ((o.meets(x) && !o.same(x)) || (o.meets(r) && !o.same(r)) || o.meets(w)) return OPTIMA_E_INVAL;
+    if (sc.meets(o)) return OPTIMA_E_INVAL;
+  }
+  if (s.meets(y) || sc.meets(x) || sc.meets(r) || sc.meets(w)) return OPTIMA_E_INVAL;
+  if (n_tok == 0) return OPTIMA_OK;
+  return optima::rms_norm(X, ldx, R, ldr, dtype, n_tok, d, weight, w_dtype, eps, S, lds, Y, ldy,
+                          y_dtype, scales, group, stream);
+}
+
+size_t optima_rms_norm_backward_workspace_bytes(int64_t n_tok, int64_t d) {
+  if (n_tok < 0 || n_tok > kMaxTok || d < 1 || d > OPTIMA_NORM_MAX_DIM) return 0;
+  return optima::rms_norm_backward_workspace_bytes(n_tok, d);
+}
+
+optima_status optima_rms_norm_backward(const void* S, int64_t lds, const void* weight, int w_dtype,
+                                       const void* dY, int64_t lddy, const void* dS, int64_t ldds,
+                                       int dtype, int64_t n_tok, int64_t d, float eps, void* dX,
+                                       int64_t lddx, float* dweight, int accumulate, void* ws,
+                                       size_t ws_bytes, hipStream_t stream) {
+  if (!f32_or_bf16(dtype) || !f32_or_bf16(w_dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (n_tok < 0 || n_tok > kMaxTok || d < 1 || !(eps > 0.f) || !weight) return OPTIMA_E_INVAL;
+  if (d > OPTIMA_NORM_MAX_DIM) return OPTIMA_E_UNSUPPORTED;
+  const int64_t e = esize(dtype);
+  const Span s{S, n_tok, d, lds, e}, dy{dY, n_tok, d, lddy, e}, ds{dS, n_tok, d, ldds, e};
+  const Span dx{dX, n_tok, d, lddx, e}, w{weight, 1, d, d, esize(w_dtype)}, dw{dweight, 1, d, d, 4};
+  if (!s.good() || !dy.good() || !dx.good() || (dS && !ds.good()) || !w.aligned() || !dw.aligned())
+    return OPTIMA_E_INVAL;
+  if (dx.meets(s) || dx.meets(w) || (dx.meets(dy) && !dx.same(dy)) || (dx.meets(ds) && !dx.same(ds)))
+    return OPTIMA_E_INVAL;
+  for (const Span& o : {s, dy, ds, dx, w})
+    if (dw.meets(o)) return OPTIMA_E_INVAL;
+  if (dweight && n_tok > 0 &&
+      (!ws || (reinterpret_cast<uintptr_t>(ws) & 3) ||
+       ws_bytes < optima::rms_norm_backward_workspace_bytes(n_tok, d)))
+    return OPTIMA_E_WORKSPACE;
+  return optima::rms_norm_backward(S, lds, weight, w_dtype, dY, lddy, dS, ldds, dtype, n_tok, d, eps,
+                                   dX, lddx, dweight, accumulate ? 1 : 0, ws, stream);
+}
+
+size_t optima_gated_forward_workspace_bytes(int64_t n_tok, int64_t d_in, int64_t d_ff) {
+  if (!gated_sizes(n_tok, d_in, d_ff)) return 0;
+  return optima::gated_forward_workspace_bytes(n_tok, d_in, d_ff);
+}
+
+optima_status optima_gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d_in,
+                                   const void* Wg, const void* Wu, int64_t d_ff, int act, void* H,
+                                   int64_t ldh, int h_dtype, void* G, int64_t ldg, void* U,
+                                   int64_t ldu, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!gated_sizes(n_tok, d_in, d_ff) || !Wg || !Wu) return OPTIMA_E_INVAL;
+  if (act != OPTIMA_ACT_NONE && act != OPTIMA_ACT_SILU) return OPTIMA_E_INVAL;
+  if (!f32_or_bf16(h_dtype)) return OPTIMA_E_UNSUPPORTED;
+  const Span x{X, n_tok, d_in, ldx, 2}, wg{Wg, d_ff, d_in, d_in, 2}, wu{Wu, d_ff, d_in, d_in, 2};
+  const Span h{H, n_tok, d_ff, ldh, esize(h_dtype)}, g{G, n_tok, d_ff, ldg, 2};
+  const Span u{U, n_tok, d_ff, ldu, 2};
+  if (!x.good() || !wg.good() || !wu.good() || !h.good() || (G && !g.good()) || (U && !u.good()))
+    return OPTIMA_E_INVAL;
+  if (d_in % 64 == 0 && (!optima::aligned16(Wg) || !optima::aligned16(Wu))) return OPTIMA_E_INVAL;
+  for (const Span& o : {h, g, u})
+    if (o.meets(x) || o.meets(wg) || o.meets(wu)) return OPTIMA_E_INVAL;
+  if (h.meets(g) || h.meets(u) || g.meets(u)) return OPTIMA_E_INVAL;
+  const size_t need = optima::gated_forward_workspace_bytes(n_tok, d_in, d_ff);
+  if (need && (!ws || !optima::aligned16(ws) || ws_bytes < need)) return OPTIMA_E_WORKSPACE;
+  if (n_tok == 0) return OPTIMA_OK;
+  return optima::gated_forward(X, ldx, n_tok, d_in, Wg, Wu, d_ff, act, H, ldh, h_dtype, G, ldg, U,
+                               ldu, ws, stream);
+}
+
+size_t optima_gated_backward_workspace_bytes(int64_t n_tok, int64_t d_in, int64_t d_ff) {
+  if (!gated_sizes(n_tok, d_in, d_ff)) return 0;
+  return optima::gated_backward_workspace_bytes(n_tok, d_in, d_ff);
+}
+
+optima_status optima_gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t d_in,
+                                    const void* Wg, const void* Wu, int64_t d_ff, int act,
+                                    const void* G, int64_t ldg, const void* U, int64_t ldu,
+                                    const void* dH, int64_t lddh, void* dX, int64_t lddx,
+                                    int dx_dtype, void* dWg, void* dWu, int dw_dtype,
+                                    const uint8_t* mask_g, const uint8_t* mask_u, int accumulate,
+                                    void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!gated_sizes(n_tok, d_in, d_ff) || !Wg || !Wu) return OPTIMA_E_INVAL;
+  if (act != OPTIMA_ACT_NONE && act != OPTIMA_ACT_SILU) return OPTIMA_E_INVAL;
+  if ((!dX && !dWg) || !dWg != !dWu || ((mask_g || mask_u) && !dWg)) return OPTIMA_E_INVAL;
+  if ((dX && !f32_or_bf16(dx_dtype)) || (dWg && !f32_or_bf16(dw_dtype)))
+    return OPTIMA_E_UNSUPPORTED;
+  const Span x{X, n_tok, d_in, ldx, 2}, wg{Wg, d_ff, d_in, d_in, 2}, wu{Wu, d_ff, d_in, d_in, 2};
+  const Span g{G, n_tok, d_ff, ldg, 2}, u{U, n_tok, d_ff, ldu, 2}, dh{dH, n_tok, d_ff, lddh, 2};
+  const Span dx{dX, n_tok, d_in, lddx, esize(dx_dtype)};
+  const Span dwg{dWg, d_ff, d_in, d_in, esize(dw_dtype)}, dwu{dWu, d_ff, d_in, d_in, esize(dw_dtype)};
+  const Span mg{mask_g, d_ff, d_in, d_in, 1}, mu{mask_u, d_ff, d_in, d_in, 1};
+  for (const Span& i : {x, wg, wu, g, u, dh})
+    if (!i.good()) return OPTIMA_E_INVAL;
+  if ((dX && !dx.good()) || (dWg && (!dwg.good() || !dwu.good()))) return OPTIMA_E_INVAL;
+  for (const Span& o : {dx, dwg, dwu})
+    for (const Span& i : {x, wg, wu, g, u, dh, mg, mu})
+      if (o.meets(i)) return OPTIMA_E_INVAL;
+  if (dx.meets(dwg) || dx.meets(dwu) || dwg.meets(dwu)) return OPTIMA_E_INVAL;
+  const size_t need = optima::gated_backward_workspace_bytes(n_tok, d_in, d_ff);
+  if (!ws || !optima::aligned16(ws) || ws_bytes < need) return OPTIMA_E_WORKSPACE;
+  return optima::gated_backward(X, ldx, n_tok, d_in, Wg, Wu, d_ff, act, G, ldg, U, ldu, dH, lddh, dX,
+                                lddx, dx_dtype, dWg, dWu, dw_dtype, mask_g, mask_u,
+                                accumulate ? 1 : 0, ws, stream);
+}
+
+size_t optima_w4_row_bytes(int64_t d) {
+  return d < 1 || d > kMaxDim ? 0 : size_t((d + 127) / 128) * 64;
+}
+
+optima_status optima_w4_pack(const void* W, int dtype, int64_t n, int64_t d, int64_t group,
+                             void* Q, void* scales, hipStream_t stream) {
+  if (!f32_or_bf16(dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (n < 0 || n > kMaxCols || d < 1 || d > kMaxDim || !group_ok(group)) return OPTIMA_E_INVAL;
+  const int64_t groups = (d + group - 1) / group, row = int64_t(optima_w4_row_bytes(d));
+  if (n * (row / 64) >= int64_t(1) << 34) return OPTIMA_E_INVAL;  // 16 chunks a workgroup
+  const Span w{W, n, d, d, esize(dtype)}, q{Q, n, row, row, 1}, sc{scales, n, groups, groups, 2};
+  if (!w.good() || !q.good() || !sc.good() || !optima::aligned16(Q)) return OPTIMA_E_INVAL;
+  if (q.meets(w) || sc.meets(w) || q.meets(sc)) return OPTIMA_E_INVAL;
+  if (n == 0) return OPTIMA_OK;
+  return optima::w4_pack(W, dtype, n, d, group, Q, scales, stream);
+}
+
+optima_status optima_w4_linear(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
+                               int64_t x_group, int64_t n_tok, int64_t d, const void* Q,
+                               const void* scales, int64_t group, int64_t d_out, void* Y,
+                               int64_t ldy, int y_dtype, hipStream_t stream) {
+  return w4_call(X, ldx, x_dtype, x_scales, x_group, n_tok, d, Q, scales, nullptr, nullptr, group,
+                 d_out, OPTIMA_ACT_NONE, Y, ldy, y_dtype, stream);
+}
+
+optima_status optima_w4_gated(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
+                              int64_t x_group, int64_t n_tok, int64_t d, const void* Qg,
+                              const void* scales_g, const void* Qu, const void* scales_u,
+                              int64_t group, int64_t d_ff, int act, void* H, int64_t ldh,
+                              int h_dtype, hipStream_t stream) {
+  if (!Qu || !scales_u || (act != OPTIMA_ACT_NONE && act != OPTIMA_ACT_SILU)) return OPTIMA_E_INVAL;
+  return w4_call(X, ldx, x_dtype, x_scales, x_group, n_tok, d, Qg, scales_g, Qu, scales_u, group,
+                 d_ff, act, H, ldh, h_dtype, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,685 @@
+// The gated feed-forward product of a decoder block and its gradient.
+//
+// Forward: g = X Wg^T, u = X Wu^T, h = act(g) o u, with X [n_tok][d] and Wg, Wu
+// [ff][d] in bf16. A tile multiplies the same token rows with rows of both weights,
+// so that g and u of an output meet in one lane's registers.
+// Up to 64 tokens: bound by the weights' way from HBM, k_gated_few streams them once.
+//
+// Backward: dU = dH o act(g), dG = dH o u o act'(g), then
+//   dX = [dG dU] [Wg; Wu],  [dWg; dWu] = [dG dU]^T X  (o masks).
+// dG and dU are rounded to bf16, the type that the matrix instructions take. The
+// products want the contraction contiguous in both operands, so the element-wise
+// kernel writes [dG dU] and its transpose, and X and the weights are transposed.
+#include "common.h"
+#include "gemm128.h"
+#include "gemm256.h"
+#include "gemm_core.h"
+#include "vec8.h"
+
+namespace optima {
+namespace {
+
+constexpr int kFewTokens = 64;
+constexpr int kFewWaves = 8;
+constexpr int64_t kCus = 256;
+
+__device__ inline int cdiv(int64_t a, int b) { return int((a + b - 1) / b); }
+
+__device__ inline float gate_act(int act, float z) {
+  return act == OPTIMA_ACT_SILU ? z / (1.f + expf(-z)) : z;
+}
+// act(z) and its derivative.
+__device__ inline void gate_act_slope(int act, float z, float* a, float* slope) {
+  if (act == OPTIMA_ACT_SILU) {
+    const float sig = 1.f / (1.f + expf(-z));
+    *a = z * sig;
+    *slope = sig * (1.f + z * (1.f - sig));
+  } else {
+    *a = z;
+    *slope = 1.f;
+  }
+}
+
+struct GatedArgs {
+  const char *x, *wg, *wu;  // rows of bf16
+  void* h;
+  bf16_t *g, *u;                // or NULL
+  int64_t n_tok, d, ff;
+  int64_t ldx, ldw, ldh, ldg, ldu;  // in elements
+  int h_f32, act;
+};
+
+__device__ inline void store_h(const GatedArgs& a, int64_t tok, int64_t n, const float (&h)[8],
+                               int left) {
+  if (a.h_f32)
+    store_upto8(static_cast<float*>(a.h) + tok * a.ldh + n, h, left);
+  else
+    store_upto8(static_cast<bf16_t*>(a.h) + tok * a.ldh + n, h, left);
+}
+
+// ---------------------------------------------------------------------------
+// Few tokens: 16 outputs a workgroup; wave w takes every eighth 64-value piece
+// of the 32 weight rows, and the waves' sums are joined in LDS in their order.
+// Lane (q, i) reads values 16 q .. + 15 of a piece of row i: two MFMA operands,
+// and with the other lanes whole 128-byte lines.
+// ---------------------------------------------------------------------------
+template <int NT>
+__global__ void __launch_bounds__(64 * kFewWaves) k_gated_few(GatedArgs a) {
+  __shared__ float part[kFewWaves][2][NT][4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int q = lane >> 4, i = lane & 15;
+  const int64_t n0 = int64_t(blockIdx.x) * 16;
+  const int64_t n = std::min(n0 + i, a.ff - 1);
+  const bf16_t* wg = reinterpret_cast<const bf16_t*>(a.wg) + n * a.ldw;
+  const bf16_t* wu = reinterpret_cast<const bf16_t*>(a.wu) + n * a.ldw;
+  const bf16_t* x[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    x[t] = reinterpret_cast<const bf16_t*>(a.x) + std::min<int64_t>(16 * t + i, a.n_tok - 1) * a.ldx;
+  f4 acc[2][NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) acc[0][t] = acc[1][t] = f4{0.f, 0.f, 0.f, 0.f};
+  const int pieces = cdiv(a.d, 64);
+  for (int c = wave; c < pieces; c += kFewWaves) {
+    const int k = 64 * c + 16 * q, left = int(a.d) - k;
+    Raw8<bf16_t> rg[2], ru[2], rx[NT][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      load_upto8(rg[e], wg + k + 8 * e, left - 8 * e);
+      load_upto8(ru[e], wu + k + 8 * e, left - 8 * e);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) load_upto8(rx[t][e], x[t] + k + 8 * e, left - 8 * e);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const bf16x8 xv = __builtin_bit_cast(bf16x8, rx[t][e].w);
+        acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            xv, __builtin_bit_cast(bf16x8, rg[e].w), acc[0][t], 0, 0, 0);
+        acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            xv, __builtin_bit_cast(bf16x8, ru[e].w), acc[1][t], 0, 0, 0);
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[wave][m][t][e][lane] = acc[m][t][e];
+  __syncthreads();
+  for (int o = threadIdx.x; o < 256 * NT; o += 64 * kFewWaves) {
+    const int nn = o & 15, m16 = (o >> 4) & 15, t = o >> 8;
+    const int64_t tok = 16 * t + m16, at = n0 + nn;
+    if (tok >= a.n_tok || at >= a.ff) continue;
+    float v[2] = {0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) v[m] += part[w][m][t][m16 & 3][(m16 >> 2) * 16 + nn];
+    const float h = gate_act(a.act, v[0]) * v[1];
+    if (a.h_f32)
+      static_cast<float*>(a.h)[tok * a.ldh + at] = h;
+    else
+      store1(static_cast<bf16_t*>(a.h) + tok * a.ldh + at, h);
+    if (a.g) store1(a.g + tok * a.ldg + at, v[0]);
+    if (a.u) store1(a.u + tok * a.ldu + at, v[1]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles. Operand rows are 16-byte aligned with whole 64-value stages.
+// ---------------------------------------------------------------------------
+
+// 256 tokens x 128 outputs on the 256 x 256 tile: half B0 holds rows of Wg, half
+// B1 the same rows of Wu, so quadrants (qa, 0) and (qa, 1) of a lane are g and u of
+// the same outputs.
+__global__ void __launch_bounds__(Tile256::kThreads) k_gated256(GatedArgs a) {
+  __shared__ __attribute__((aligned(1024))) char l0[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l1[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l2[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l3[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l4[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l5[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l6[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l7[Tile256::kHalfBytes];
+  const int tiles_m = cdiv(a.n_tok, 256), tiles_n = cdiv(a.ff, 128);
+  int tm, tn;
+  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 128;
+  Operands256 src;
+#pragma unroll
+  for (int i = 0; i < Tile256::kHalfLoads; ++i) {
+    const int r = t256_load_row(i), seg = t256_seg_bytes(i);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      src.a[h][i] = a.x + std::min(m0 + 128 * h + r, a.n_tok - 1) * (2 * a.ldx) + seg;
+      src.b[h][i] = (h ? a.wu : a.wg) + std::min(n0 + r, a.ff - 1) * (2 * a.ldw) + seg;
+    }
+  }
+  Acc256 acc;
+  gemm256_mainloop<Bf16Tag>(acc, src, int(a.d / 64), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
+
+  // g and u, where they are kept, then h, each through the stage buffers.
+#pragma unroll
+  for (int out = 0; out < 3; ++out) {
+    if (out == 0 && !a.g) continue;
+    if (out == 1 && !a.u) continue;
+#pragma unroll
+    for (int qa = 0; qa < 2; ++qa)
+#pragma unroll
+      for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = t256_row(qa, mi, k);
+#pragma unroll
+          for (int ni = 0; ni < 2; ++ni) {
+            const int c = t256_col(0, ni);
+            const float g = acc.q[qa][0][mi][ni][k], u = acc.q[qa][1][mi][ni][k];
+            *reinterpret_cast<float*>(t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r) +
+                                      ((c >> 2) ^ (r & 31)) * 16 + (c & 3) * 4) =
+                out == 0 ? g : out == 1 ? u : gate_act(a.act, g) * u;
+          }
+        }
+    __syncthreads();
+#pragma unroll 2
+    for (int p = threadIdx.x; p < 256 * 16; p += Tile256::kThreads) {
+      const int r = p >> 4, c = 2 * (p & 15);
+      const int64_t tok = m0 + r, n = n0 + 4 * c;
+      if (tok >= a.n_tok || n >= a.ff) continue;
+      const char* row = t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r);
+      const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
+      const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
+      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      const int left = int(std::min<int64_t>(a.ff - n, 8));
+      if (out == 0) store_upto8(a.g + tok * a.ldg + n, v, left);
+      else if (out == 1) store_upto8(a.u + tok * a.ldu + n, v, left);
+      else store_h(a, tok, n, v, left);
+    }
+    if (out < 2) __syncthreads();
+  }
+}
+
+// 128 tokens x 64 outputs on the 128 x 128 ring tile: 16-row blocks of B are rows
+// of Wg and Wu in turn, so that blocks 0 and 1 of a wave are g and u.
+__global__ void __launch_bounds__(Ring128::kThreads) k_gated_ring(GatedArgs a) {
+  __shared__ __attribute__((aligned(1024))) char b0[Ring128::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b1[Ring128::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b2[Ring128::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b3[Ring128::kBufBytes];
+  const int tiles_m = cdiv(a.n_tok, 128), tiles_n = cdiv(a.ff, 64);
+  int tm, tn;
+  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  const int64_t m0 = int64_t(tm) * 128, n0 = int64_t(tn) * 64;
+  OperandsR128 src;
+#pragma unroll
+  for (int i = 0; i < Ring128::kLoads; ++i) {
+    const int r = t256_load_row(i), seg = t256_seg_bytes(i);
+    src.a[i] = a.x + std::min(m0 + r, a.n_tok - 1) * (2 * a.ldx) + seg;
+    const int64_t n = n0 + 16 * (r >> 5) + (r & 15);
+    src.b[i] = ((r & 16) ? a.wu : a.wg) + std::min(n, a.ff - 1) * (2 * a.ldw) + seg;
+  }
+  AccR128<false> acc;
+  r128_mainloop<Bf16Tag>(acc, src, SumShape{0, 0, 0}, int(a.d / 64), b0, b1, b2, b3, [] {});
+
+  const int wn = (threadIdx.x >> 6) & 3;
+#pragma unroll
+  for (int out = 0; out < 3; ++out) {
+    if (out == 0 && !a.g) continue;
+    if (out == 1 && !a.u) continue;
+#pragma unroll
+    for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = r128_row(mi, k), c = wn * 16 + (threadIdx.x & 15);
+        const float g = acc.q[mi][0][k], u = acc.q[mi][1][k];
+        *reinterpret_cast<float*>(r128_stage_row(b0, b1, r) + ((c >> 2) ^ (r & 31)) * 16 +
+                                  (c & 3) * 4) =
+            out == 0 ? g : out == 1 ? u : gate_act(a.act, g) * u;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int p = threadIdx.x; p < 128 * 8; p += Ring128::kThreads) {
+      const int r = p >> 3, c = 2 * (p & 7);
+      const int64_t tok = m0 + r, n = n0 + 4 * c;
+      if (tok >= a.n_tok || n >= a.ff) continue;
+      const char* row = r128_stage_row(b0, b1, r);
+      const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
+      const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
+      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      const int left = int(std::min<int64_t>(a.ff - n, 8));
+      if (out == 0) store_upto8(a.g + tok * a.ldg + n, v, left);
+      else if (out == 1) store_upto8(a.u + tok * a.ldu + n, v, left);
+      else store_h(a, tok, n, v, left);
+    }
+    if (out < 2) __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Layout
+// ---------------------------------------------------------------------------
+
+// dst [rows][pitch] = src [rows][cols] with zeros up to the pitch (a multiple of 8).
+__global__ void __launch_bounds__(kThreads) k_pad_rows(const bf16_t* src, int64_t ld, int64_t rows,
+                                                       int64_t cols, int64_t pitch, bf16_t* dst) {
+  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t per = pitch / 8, r = i / per, c = 8 * (i - r * per);
+  if (r >= rows) return;
+  Raw8<bf16_t> v;
+  load_upto8(v, src + r * ld + c, int(std::max<int64_t>(std::min<int64_t>(cols - c, 8), 0)));
+  *reinterpret_cast<u32x4*>(dst + r * pitch + c) = v.w;
+}
+
+// 64 x 64 values of a tile in LDS, rows 66 apart: the transposing reads below
+// (eight rows of a column a lane) are free of bank conflicts.
+constexpr int kTrPitch = 66;
+
+__device__ inline void tr_put(uint16_t* tile, int r, int c, const u32x4& w) {
+  uint32_t* p = reinterpret_cast<uint32_t*>(tile + r * kTrPitch + c);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = w[i];
+}
+__device__ inline u32x4 tr_get(const uint16_t* tile, int r, int c) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = tile[(r + 2 * i) * kTrPitch + c] | (uint32_t(tile[(r + 2 * i + 1) * kTrPitch + c]) << 16);
+  return w;
+}
+
+// dst [cols][pitch] = src^T, src [rows][cols], with zeros from `rows` up to the
+// next multiple of 64 of a dst row. pitch and dst are multiples of 8 values.
+__global__ void __launch_bounds__(kThreads) k_transpose_bf16(const bf16_t* src, int64_t ld,
+                                                             int64_t rows, int64_t cols,
+                                                             int64_t pitch, bf16_t* dst) {
+  __shared__ uint16_t tile[64 * kTrPitch];
+  const int tiles_c = cdiv(cols, 64), tr = blockIdx.x / tiles_c;
+  const int64_t r0 = int64_t(tr) * 64, c0 = int64_t(blockIdx.x - tr * tiles_c) * 64;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int p = threadIdx.x + k * kThreads, r = p >> 3, c = 8 * (p & 7);
+    Raw8<bf16_t> v;
+    const int64_t left = r0 + r < rows ? cols - c0 - c : 0;
+    load_upto8(v, src + (r0 + r) * ld + c0 + c, int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
+    tr_put(tile, r, c, v.w);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int p = threadIdx.x + k * kThreads, c = p >> 3, r = 8 * (p & 7);
+    if (c0 + c < cols) *reinterpret_cast<u32x4*>(dst + (c0 + c) * pitch + r0 + r) = tr_get(tile, r, c);
+  }
+}
+
+struct GateGradArgs {
+  const bf16_t *g, *u, *dh;
+  int64_t ldg, ldu, lddh, n_tok, ff;
+  bf16_t* p;       // [n_tok][2 ffp]: dG, dU, zeros in between, or NULL
+  bf16_t* pt;      // [2 ff][tp]: dG^T, dU^T, zeros from n_tok on, or NULL
+  int64_t ffp, tp;
+  int act;
+};
+
+// 64 tokens x 64 values of dG and dU.
+__global__ void __launch_bounds__(kThreads) k_gate_grad(GateGradArgs a) {
+  __shared__ uint16_t tile[2][64 * kTrPitch];
+  const int tiles_f = int(a.ffp / 64), tt = blockIdx.x / tiles_f;
+  const int64_t t0 = int64_t(tt) * 64, f0 = int64_t(blockIdx.x - tt * tiles_f) * 64;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = threadIdx.x + k * kThreads, r = i >> 3, c = 8 * (i & 7);
+    const int64_t t = t0 + r, f = f0 + c;
+    const int left = int(std::max<int64_t>(std::min<int64_t>(t < a.n_tok ? a.ff - f : 0, 8), 0));
+    Raw8<bf16_t> rg, ru, rh;
+    load_upto8(rg, a.g + t * a.ldg + f, left);
+    load_upto8(ru, a.u + t * a.ldu + f, left);
+    load_upto8(rh, a.dh + t * a.lddh + f, left);
+    float g[8], u[8], dh[8], dg[8], du[8];
+    values8(rg, g);
+    values8(ru, u);
+    values8(rh, dh);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float act, slope;
+      gate_act_slope(a.act, g[e], &act, &slope);
+      du[e] = dh[e] * act;
+      dg[e] = dh[e] * u[e] * slope;
+    }
+    u32x4 wg, wu;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      wg[e] = pack_bf16(dg[2 * e], dg[2 * e + 1]);
+      wu[e] = pack_bf16(du[2 * e], du[2 * e + 1]);
+    }
+    if (a.p && t < a.n_tok) {
+      *reinterpret_cast<u32x4*>(a.p + t * (2 * a.ffp) + f) = wg;
+      *reinterpret_cast<u32x4*>(a.p + t * (2 * a.ffp) + a.ffp + f) = wu;
+    }
+    if (a.pt) {
+      tr_put(tile[0], r, c, wg);
+      tr_put(tile[1], r, c, wu);
+    }
+  }
+  if (!a.pt) return;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = threadIdx.x + k * kThreads, c = i >> 3, r = 8 * (i & 7);
+    if (f0 + c >= a.ff) continue;
+    *reinterpret_cast<u32x4*>(a.pt + (f0 + c) * a.tp + t0 + r) = tr_get(tile[0], r, c);
+    *reinterpret_cast<u32x4*>(a.pt + (a.ff + f0 + c) * a.tp + t0 + r) = tr_get(tile[1], r, c);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// C = A B^T into one or two outputs
+// ---------------------------------------------------------------------------
+
+// Rows from `split` on go to y[1]. A zero in a mask makes the product's value +0
+// there. accumulate adds to what the output holds.
+struct NtOut {
+  void* y[2];
+  const uint8_t* mask[2];
+  int64_t split, ld, rows, cols;
+  int f32, accumulate;
+};
+struct NtArgs {
+  const char *a, *b;
+  int64_t pitch_a, pitch_b;  // bytes, multiples of 16
+  int64_t stages;            // of 64 values
+  NtOut out;
+};
+
+template <typename T>
+__device__ inline void nt_put(T* y, float (&v)[8], int left, int accumulate) {
+  if (accumulate) {
+    Raw8<T> raw;
+    float old[8];
+    load_upto8(raw, y, left);
+    values8(raw, old);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += old[i];
+  }
+  store_upto8(y, v, left);
+}
+
+__device__ inline void nt_store(const NtOut& o, int64_t row, int64_t col, float (&v)[8]) {
+  if (row >= o.rows || col >= o.cols) return;
+  const int which = row >= o.split;
+  const int64_t r = which ? row - o.split : row, at = r * o.ld + col;
+  const int left = int(std::min<int64_t>(o.cols - col, 8));
+  if (o.mask[which]) {
+    const uint8_t* m = o.mask[which] + r * o.cols + col;
+    uint32_t w[2] = {0, 0};
+    if (left == 8) {
+      const u32x2 q = *reinterpret_cast<const u32x2_1*>(m);
+      w[0] = q[0], w[1] = q[1];
+    } else {
+      for (int i = 0; i < left; ++i) w[i >> 2] |= uint32_t(m[i]) << (8 * (i & 3));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!((w[i >> 2] >> (8 * (i & 3))) & 255u)) v[i] = 0.f;
+  }
+  if (o.f32)
+    nt_put(static_cast<float*>(o.y[which]) + at, v, left, o.accumulate);
+  else
+    nt_put(static_cast<bf16_t*>(o.y[which]) + at, v, left, o.accumulate);
+}
+
+__global__ void __launch_bounds__(Tile256::kThreads) k_nt256(NtArgs a) {
+  __shared__ __attribute__((aligned(1024))) char l0[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l1[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l2[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l3[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l4[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l5[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l6[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l7[Tile256::kHalfBytes];
+  const int tiles_m = cdiv(a.out.rows, 256), tiles_n = cdiv(a.out.cols, 256);
+  int tm, tn;
+  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 256;
+  Operands256 src;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < Tile256::kHalfLoads; ++i) {
+      const int64_t r = 128 * h + t256_load_row(i);
+      src.a[h][i] = a.a + std::min(m0 + r, a.out.rows - 1) * a.pitch_a + t256_seg_bytes(i);
+      src.b[h][i] = a.b + std::min(n0 + r, a.out.cols - 1) * a.pitch_b + t256_seg_bytes(i);
+    }
+  Acc256 acc;
+  gemm256_mainloop<Bf16Tag>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
+#pragma unroll
+  for (int qb = 0; qb < 2; ++qb) {
+    if (qb) __syncthreads();
+#pragma unroll
+    for (int qa = 0; qa < 2; ++qa)
+#pragma unroll
+      for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = t256_row(qa, mi, k);
+#pragma unroll
+          for (int ni = 0; ni < 2; ++ni) {
+            const int c = t256_col(0, ni);
+            *reinterpret_cast<float*>(t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r) +
+                                      ((c >> 2) ^ (r & 31)) * 16 + (c & 3) * 4) =
+                acc.q[qa][qb][mi][ni][k];
+          }
+        }
+    __syncthreads();
+#pragma unroll 2
+    for (int p = threadIdx.x; p < 256 * 16; p += Tile256::kThreads) {
+      const int r = p >> 4, c = 2 * (p & 15);
+      const char* row = t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r);
+      const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
+      const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      nt_store(a.out, m0 + r, n0 + 128 * qb + 4 * c, v);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(Ring128::kThreads) k_nt_ring(NtArgs a) {
+  __shared__ __attribute__((aligned(1024))) char b0[Ring128::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b1[Ring128::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b2[Ring128::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b3[Ring128::kBufBytes];
+  const int tiles_m = cdiv(a.out.rows, 128), tiles_n = cdiv(a.out.cols, 128);
+  int tm, tn;
+  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  const int64_t m0 = int64_t(tm) * 128, n0 = int64_t(tn) * 128;
+  OperandsR128 src;
+#pragma unroll
+  for (int i = 0; i < Ring128::kLoads; ++i) {
+    const int r = t256_load_row(i), seg = t256_seg_bytes(i);
+    src.a[i] = a.a + std::min(m0 + r, a.out.rows - 1) * a.pitch_a + seg;
+    src.b[i] = a.b + std::min(n0 + r, a.out.cols - 1) * a.pitch_b + seg;
+  }
+  AccR128<false> acc;
+  r128_mainloop<Bf16Tag>(acc, src, SumShape{0, 0, 0}, int(a.stages), b0, b1, b2, b3, [] {});
+#pragma unroll
+  for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r128_row(mi, k);
+#pragma unroll
+      for (int ni = 0; ni < 2; ++ni) {
+        const int c = r128_col(ni);
+        *reinterpret_cast<float*>(r128_stage_row(b0, b1, r) + ((c >> 2) ^ (r & 31)) * 16 +
+                                  (c & 3) * 4) = acc.q[mi][ni][k];
+      }
+    }
+  __syncthreads();
+#pragma unroll
+  for (int p = threadIdx.x; p < 128 * 16; p += Ring128::kThreads) {
+    const int r = p >> 4, c = 2 * (p & 15);
+    const char* row = r128_stage_row(b0, b1, r);
+    const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
+    const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
+    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    nt_store(a.out, m0 + r, n0 + 4 * c, v);
+  }
+}
+
+// A round of 256 x 256 tiles over the CUs against one of 128 x 128 tiles, a
+// quarter of the outputs: 1.4 against 0.56 us a stage of 64.
+bool wide_tiles(int64_t wide, int64_t small) {
+  return 5 * ceil_div(wide, kCus) <= 2 * ceil_div(small, kCus);
+}
+
+optima_status nt_product(const NtArgs& a, hipStream_t s) {
+  const int64_t wide = ceil_div(a.out.rows, 256) * ceil_div(a.out.cols, 256);
+  const int64_t small = ceil_div(a.out.rows, 128) * ceil_div(a.out.cols, 128);
+  if (wide_tiles(wide, small))
+    hipLaunchKernelGGL(k_nt256, dim3(unsigned(wide)), dim3(Tile256::kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL(k_nt_ring, dim3(unsigned(small)), dim3(Ring128::kThreads), 0, s, a);
+  OPTIMA_LAUNCH_CHECK();
+  return OPTIMA_OK;
+}
+
+struct GatedLayout {
+  bf16_t *x, *wg, *wu;
+};
+GatedLayout carve_gated(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* bytes) {
+  Carver c(ws);
+  GatedLayout l{};
+  if (n_tok > kFewTokens) {
+    const int64_t dp = round_up(d, 64);
+    l.x = c.take<bf16_t>(size_t(n_tok) * size_t(dp));
+    if (dp != d) {
+      l.wg = c.take<bf16_t>(size_t(ff) * size_t(dp));
+      l.wu = c.take<bf16_t>(size_t(ff) * size_t(dp));
+    }
+  }
+  if (bytes) *bytes = c.bytes();
+  return l;
+}
+
+struct GradLayout {
+  bf16_t *p, *pt, *wt, *xt;
+};
+GradLayout carve_grad(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* bytes) {
+  Carver c(ws);
+  GradLayout l{};
+  const size_t ffp = size_t(round_up(ff, 64)), tp = size_t(round_up(n_tok, 64));
+  l.p = c.take<bf16_t>(size_t(n_tok) * 2 * ffp);
+  l.wt = c.take<bf16_t>(size_t(d) * 2 * ffp);
+  l.pt = c.take<bf16_t>(2 * size_t(ff) * tp);
+  l.xt = c.take<bf16_t>(size_t(d) * tp);
+  if (bytes) *bytes = c.bytes();
+  return l;
+}
+
+void pad_rows(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, bf16_t* dst,
+              hipStream_t s) {
+  hipLaunchKernelGGL(k_pad_rows, dim3(unsigned(ceil_div(rows * (pitch / 8), kThreads))),
+                     dim3(kThreads), 0, s, static_cast<const bf16_t*>(src), ld, rows, cols, pitch,
+                     dst);
+}
+void transpose(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, bf16_t* dst,
+               hipStream_t s) {
+  hipLaunchKernelGGL(k_transpose_bf16, dim3(unsigned(ceil_div(cols, 64) * ceil_div(rows, 64))),
+                     dim3(kThreads), 0, s, static_cast<const bf16_t*>(src), ld, rows, cols, pitch,
+                     dst);
+}
+
+}  // namespace
+
+size_t gated_forward_workspace_bytes(int64_t n_tok, int64_t d, int64_t ff) {
+  size_t b = 0;
+  carve_gated(nullptr, n_tok, d, ff, &b);
+  return b;
+}
+
+optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d, const void* Wg,
+                            const void* Wu, int64_t ff, int act, void* H, int64_t ldh, int h_dtype,
+                            void* G, int64_t ldg, void* U, int64_t ldu, void* ws, hipStream_t s) {
+  GatedArgs a{static_cast<const char*>(X), static_cast<const char*>(Wg),
+              static_cast<const char*>(Wu), H, static_cast<bf16_t*>(G), static_cast<bf16_t*>(U),
+              n_tok, d, ff, ldx, d, ldh, ldg, ldu, h_dtype == OPTIMA_DTYPE_F32, act};
+  if (n_tok <= kFewTokens) {
+    const dim3 grid(unsigned(ceil_div(ff, 16))), wg(64 * kFewWaves);
+    if (n_tok <= 16) hipLaunchKernelGGL(k_gated_few<1>, grid, wg, 0, s, a);
+    else if (n_tok <= 32) hipLaunchKernelGGL(k_gated_few<2>, grid, wg, 0, s, a);
+    else hipLaunchKernelGGL(k_gated_few<4>, grid, wg, 0, s, a);
+    OPTIMA_LAUNCH_CHECK();
+    return OPTIMA_OK;
+  }
+  const GatedLayout l = carve_gated(ws, n_tok, d, ff, nullptr);
+  const int64_t dp = round_up(d, 64);
+  if (dp != d || !aligned16(X) || ldx % 8) {
+    pad_rows(X, ldx, n_tok, d, dp, l.x, s);
+    a.x = reinterpret_cast<const char*>(l.x);
+    a.ldx = dp;
+  }
+  if (dp != d) {
+    pad_rows(Wg, d, ff, d, dp, l.wg, s);
+    pad_rows(Wu, d, ff, d, dp, l.wu, s);
+    a.wg = reinterpret_cast<const char*>(l.wg);
+    a.wu = reinterpret_cast<const char*>(l.wu);
+    a.ldw = dp;
+  }
+  a.d = dp;
+  OPTIMA_LAUNCH_CHECK();
+  const int64_t wide = ceil_div(n_tok, 256) * ceil_div(ff, 128);
+  const int64_t small = ceil_div(n_tok, 128) * ceil_div(ff, 64);
+  if (wide_tiles(wide, small))
+    hipLaunchKernelGGL(k_gated256, dim3(unsigned(wide)), dim3(Tile256::kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL(k_gated_ring, dim3(unsigned(small)), dim3(Ring128::kThreads), 0, s, a);
+  OPTIMA_LAUNCH_CHECK();
+  return OPTIMA_OK;
+}
+
+size_t gated_backward_workspace_bytes(int64_t n_tok, int64_t d, int64_t ff) {
+  size_t b = 0;
+  carve_grad(nullptr, n_tok, d, ff, &b);
+  return b;
+}
+
+optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t d, const void* Wg,
+                             const void* Wu, int64_t ff, int act, const void* G, int64_t ldg,
+                             const void* U, int64_t ldu, const void* dH, int64_t lddh, void* dX,
+                             int64_t lddx, int dx_dtype, void* dWg, void* dWu, int dw_dtype,
+                             const uint8_t* mask_g, const uint8_t* mask_u, int accumulate, void* ws,
+                             hipStream_t s) {
+  const GradLayout l = carve_grad(ws, n_tok, d, ff, nullptr);
+  const int64_t ffp = round_up(ff, 64), tp = round_up(n_tok, 64);
+  if (n_tok > 0) {
+    const GateGradArgs a{static_cast<const bf16_t*>(G), static_cast<const bf16_t*>(U),
+                         static_cast<const bf16_t*>(dH), ldg, ldu, lddh, n_tok, ff,
+                         dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, act};
+    hipLaunchKernelGGL(k_gate_grad, dim3(unsigned(ffp / 64 * (tp / 64))), dim3(kThreads), 0,
+                       s, a);
+    OPTIMA_LAUNCH_CHECK();
+  }
+  if (dX && n_tok > 0) {
+    transpose(Wg, d, ff, d, 2 * ffp, l.wt, s);
+    transpose(Wu, d, ff, d, 2 * ffp, l.wt + ffp, s);
+    OPTIMA_LAUNCH_CHECK();
+    NtArgs a{reinterpret_cast<const char*>(l.p), reinterpret_cast<const char*>(l.wt), 4 * ffp,
+             4 * ffp, 2 * ffp / 64, {}};
+    a.out = NtOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, lddx, n_tok, d,
+                  dx_dtype == OPTIMA_DTYPE_F32, 0};
+    const optima_status st = nt_product(a, s);
+    if (st != OPTIMA_OK) return st;
+  }
+  if (dWg) {
+    // No tokens: no stages, and the products are zero.
+    if (n_tok > 0) transpose(X, ldx, n_tok, d, tp, l.xt, s);
+    OPTIMA_LAUNCH_CHECK();
+    NtArgs a{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt), 2 * tp,
+             2 * tp, tp / 64, {}};
+    a.out = NtOut{{dWg, dWu}, {mask_g, mask_u}, ff, d, 2 * ff, d, dw_dtype == OPTIMA_DTYPE_F32,
+                  accumulate};
+    return nt_product(a, s);
+  }
+  return OPTIMA_OK;
+}
+
+}  // namespace optima
