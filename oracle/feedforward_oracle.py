@@ -82,10 +82,10 @@ def gated_backward(x, wg, wu, g, u, dh, name):
 
 
 def w4_quantize(w: np.ndarray, group: int):
-    """(codes [n, d] int, scales [n, groups]) by the rule scale = bf16(max|w| / 7),
-    code = clamp(rne(w / scale), -7, 7), with the fp32 quotients the rule names."""
+    """(codes [n, d] int, scales [n, groups]) by the rule scale = bf16(max|w| * (1 / 7)),
+    code = clamp(rne(w / scale), -7, 7), in fp32 as the rule names it."""
     w = np.asarray(w, np.float32)
-    scales = bf16(group_max(w, group).astype(np.float32) / np.float32(7.0)).astype(np.float32)
+    scales = bf16(group_max(w, group).astype(np.float32) * np.float32(1.0 / 7.0)).astype(np.float32)
     each = scales[:, groups_of(w.shape[1], group)]
     with np.errstate(divide="ignore", invalid="ignore"):
         codes = np.where(each > 0, np.clip(np.rint(w / each), -7, 7), 0)

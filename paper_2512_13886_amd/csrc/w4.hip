@@ -1,7 +1,7 @@
 // Products with 4-bit weights: packing, and Y = X deq(Q)^T of a few tokens, plain
 // or gated.
 //
-// Packing: one scale = bf16(max |w| / 7) for each group of 32, 64 or 128 values of
+// Packing: one scale = bf16(max |w| * (1 / 7)) for each group of 32, 64 or 128 values of
 // a row, code = clamp(rne(w / scale), -7, 7), stored as code + 8. A zero weight has
 // code 0, so that pruned entries stay exactly zero.
 //
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kThreads) k_w4_pack(const T* W, int64_t total,
 #pragma unroll
   for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(w[e]) & 0x7FFFFFFFu);
   for (int o = 1; o < group / 8; o <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), o, 64)));
-  const uint32_t sb = pack_bf16(__uint_as_float(m) / 7.f, 0.f) & 0xFFFFu;
+  const uint32_t sb = pack_bf16(__uint_as_float(m) * (1.f / 7.f), 0.f) & 0xFFFFu;
   const float s = bf16_low(sb);
   if (live && (k & (group - 1)) == 0 && k < d) scales[n * groups + k / group].bits = uint16_t(sb);
   // A group with an infinity or NaN has codes 0 and that scale: NaN as values.
