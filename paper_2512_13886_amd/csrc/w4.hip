@@ -30,7 +30,6 @@ namespace {
 
 constexpr int kChunk = 128;       // codes
 constexpr int kChunkBytes = 64;
-constexpr int kW4Waves = 8;
 constexpr int kW4Tokens = 64;     // a workgroup's
 
 typedef int i4 __attribute__((ext_vector_type(4)));
@@ -127,99 +126,213 @@ struct XFrag<true> {
   }
 };
 
-// 16 outputs of each of MATS matrices for up to 16 NT tokens.
-template <bool I8, int MATS, int NT>
-__global__ void __launch_bounds__(64 * kW4Waves) k_w4(W4Args a) {
-  __shared__ float part[kW4Waves][MATS][NT][4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Lane 4 k + e's value in the four lanes 4 k .. 4 k + 3.
+template <int E>
+__device__ inline float quad_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), E * 0x55, 0xF, 0xF, true));
+}
+
+// N (even) consecutive scales from group g on, two a word; zeros past the row's `groups`.
+template <int N>
+__device__ inline void load_scales(uint32_t (&v)[N / 2], const bf16_t* row, int g, int groups) {
+  if (g + N <= groups) {
+    struct __attribute__((packed, aligned(2))) Packed {
+      uint32_t w[N / 2];
+    } q;
+    __builtin_memcpy(&q, row + g, sizeof(q));
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = q.w[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      v[i] = g + 2 * i < groups ? row[g + 2 * i].bits : 0u;
+      if (g + 2 * i + 1 < groups) v[i] |= uint32_t(row[g + 2 * i + 1].bits) << 16;
+    }
+  }
+}
+__device__ inline float scale_of(uint32_t w, int odd) { return odd ? bf16_high(w) : bf16_low(w); }
+template <int N>
+__device__ inline void load_scales(float (&v)[N], const float* row, int g, int groups) {
+  if (g + N <= groups) {
+    struct __attribute__((packed, aligned(4))) Packed {
+      float f[N];
+    } q;
+    __builtin_memcpy(&q, row + g, sizeof(q));
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = q.f[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = g + i < groups ? row[g + i] : 0.f;
+  }
+}
+
+// Chunks that a wave takes at once, their loads together, and waves of a workgroup.
+constexpr int w4_batch(int nt) { return nt == 1 ? 4 : nt == 2 ? 2 : 1; }
+constexpr int w4_waves(int mats, int nt) { return mats * nt == 1 ? 16 : 8; }  // at most
+// Bytes of one token's values of a batch in LDS (NT = 1), with 64 bytes between
+// rows that keep the reads of several tokens off each other's banks.
+constexpr int w4_x_pitch(bool i8) { return 4 * kChunk * (i8 ? 1 : 2) + 64; }
+
+// 16 outputs of each of MATS matrices for up to 16 NT tokens; GP groups a chunk.
+// Up to 16 tokens (NT = 1) a wave brings the tokens' values of its batch through
+// LDS: the operand layout would read every value 16 times over, 16 / n_tok times
+// for nothing.
+template <bool I8, int MATS, int NT, int GP>
+__global__ void __launch_bounds__(64 * w4_waves(MATS, NT)) k_w4(W4Args a) {
+  constexpr int kBatch = w4_batch(NT), kPer = 4 / GP, kGroups = kBatch * GP;
+  constexpr bool kStaged = NT == 1;
+  constexpr int kPitch = w4_x_pitch(I8), kEsz = I8 ? 1 : 2;
+  typedef typename std::conditional<I8, i4, f4>::type acc_t;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  float* part = reinterpret_cast<float*>(lds);  // [wave][MATS][NT][4][64], at the end
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int b = lane >> 4, i = lane & 15;
   const int64_t n0 = int64_t(blockIdx.x) * 16, t0 = int64_t(blockIdx.y) * kW4Tokens;
   const int64_t n = std::min(n0 + i, a.d_out - 1);
-  const char* x[NT];
+  const int tokens = int(std::min<int64_t>(a.n_tok - t0, 16 * NT));
+  const char* x = static_cast<const char*>(a.x) + t0 * a.ldx * kEsz;
+  const char* rows[NT];
+  const float* xs[NT];  // of token 4 b + i % 4
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-    x[t] = static_cast<const char*>(a.x) +
-           std::min(t0 + 16 * t + i, a.n_tok - 1) * a.ldx * (I8 ? 1 : 2);
+  for (int t = 0; t < NT; ++t) {
+    rows[t] = x + std::min(16 * t + i, tokens - 1) * a.ldx * kEsz;
+    xs[t] = a.xs + (t0 + std::min(16 * t + 4 * b + (i & 3), tokens - 1)) * a.x_groups;
+  }
+  char* mine = lds + wave * tokens * kPitch;
   f4 sum[MATS][NT];
 #pragma unroll
   for (int m = 0; m < MATS; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t) sum[m][t] = f4{0.f, 0.f, 0.f, 0.f};
-  const int per = a.group / 32;  // dwords of a chunk in a group: 1, 2 or 4
-  for (int c = wave; c < a.chunks; c += kW4Waves) {
-    u32x4 w[MATS];
+  for (int c0 = kBatch * wave; c0 < a.chunks; c0 += kBatch * waves) {
+    u32x4 w[kBatch][MATS];
+    uint32_t s[MATS][(kGroups + 1) / 2];
+    float sx[NT][kGroups];
+    // Lane l takes values 8 l .. of a token's batch, eight tokens at a time.
+    XFrag<I8> row[kStaged ? 8 : 1];
+    const int xk = c0 * kChunk + 8 * lane;
+    if constexpr (kStaged)
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (r < tokens) row[r].load(x + r * a.ldx * kEsz, xk, a.d - xk);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      // Past the last chunk: its codes again, with scales and tokens of zeros.
+      const int c = std::min(c0 + u, a.chunks - 1);
+#pragma unroll
+      for (int m = 0; m < MATS; ++m)
+        w[u][m] = *reinterpret_cast<const u32x4*>(a.q[m] + (n * a.chunks + c) * kChunkBytes + b * 16);
+    }
 #pragma unroll
     for (int m = 0; m < MATS; ++m)
-      w[m] = *reinterpret_cast<const u32x4*>(a.q[m] + (n * a.chunks + c) * kChunkBytes + b * 16);
-    XFrag<I8> f[NT][4];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int k = c * kChunk + 32 * j + 8 * b;
-        f[t][j].load(x[t], k, a.d - k);
-      }
-    typedef typename std::conditional<I8, i4, f4>::type acc_t;
-    acc_t acc[MATS][NT];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
+      load_scales<(kGroups + 1) / 2 * 2>(s[m], a.s[m] + n * a.groups, c0 * GP, a.groups);
+    if constexpr (I8)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        acc_t base = {};
-        if constexpr (I8) {
-          base = __builtin_amdgcn_mfma_i32_16x16x32_i8(f[t][j].v, long(0xF8F8F8F8F8F8F8F8ull), base,
-                                                       0, 0, 0);
-        } else {
-          const bf16x8 k24 = __builtin_bit_cast(
-              bf16x8, u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u});
-          base = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t][j].v, k24, base, 0, 0, 0);
-        }
+        if (a.x_groups > 1)
+          load_scales<kGroups>(sx[t], xs[t], c0 * GP, a.groups);
+        else
 #pragma unroll
-        for (int m = 0; m < MATS; ++m) {
-          acc_t v = base;
-          if constexpr (I8)
-            v = __builtin_amdgcn_mfma_i32_16x16x32_i8(f[t][j].v, codes_i8(w[m][j]), v, 0, 0, 0);
-          else
-            v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t][j].v, codes_bf16(w[m][j]), v, 0, 0, 0);
-          acc[m][t] = j % per == 0 ? v : acc[m][t] + v;
-        }
+          for (int g = 0; g < kGroups; ++g) sx[t][g] = 1.f;
       }
-      if ((j + 1) % per) continue;
-      const int g = (c * 4 + j) / per;  // the group that ends here
-      if (g >= a.groups) continue;      // padding
+    if constexpr (kStaged) {
+      for (int r0 = 0;; r0 += 8) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        float xs[4] = {1.f, 1.f, 1.f, 1.f};
-        if (I8 && a.x_groups > 1)
+        for (int r = 0; r < 8; ++r)
+          if (r0 + r < tokens)
+            *reinterpret_cast<decltype(row[r].v)*>(mine + (r0 + r) * kPitch + lane * 8 * kEsz) = row[r].v;
+        if (r0 + 8 >= tokens) break;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            xs[e] = a.xs[std::min(t0 + 16 * t + 4 * b + e, a.n_tok - 1) * a.x_groups + g];
-#pragma unroll
-        for (int m = 0; m < MATS; ++m) {
-          const float s = bf16_low(a.s[m][n * a.groups + g].bits);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[m][t][e] += float(acc[m][t][e]) * (s * xs[e]);
-        }
+        for (int r = 0; r < 8; ++r)
+          if (r0 + 8 + r < tokens) row[r].load(x + (r0 + 8 + r) * a.ldx * kEsz, xk, a.d - xk);
       }
+      // The wave's own rows: its LDS accesses are served in order.
+      __builtin_amdgcn_wave_barrier();
     }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      XFrag<I8> f[NT][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (kStaged) {
+            f[t][j].v = *reinterpret_cast<const decltype(f[t][j].v)*>(
+                mine + std::min(i, tokens - 1) * kPitch + (u * kChunk + 32 * j + 8 * b) * kEsz);
+          } else {
+            const int k = (c0 + u) * kChunk + 32 * j + 8 * b;
+            f[t][j].load(rows[t], k, a.d - k);
+          }
+        }
+#pragma unroll
+      for (int g = 0; g < GP; ++g)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          acc_t acc[MATS], base = {};
+#pragma unroll
+          for (int j = g * kPer; j < (g + 1) * kPer; ++j) {
+            if constexpr (I8) {
+              base = __builtin_amdgcn_mfma_i32_16x16x32_i8(
+                  f[t][j].v, long(0xF8F8F8F8F8F8F8F8ull), base, 0, 0, 0);
+            } else {
+              const bf16x8 k24 = __builtin_bit_cast(
+                  bf16x8, u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u});
+              base = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t][j].v, k24, base, 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int m = 0; m < MATS; ++m) {
+            acc[m] = base;
+#pragma unroll
+            for (int j = g * kPer; j < (g + 1) * kPer; ++j) {
+              if constexpr (I8)
+                acc[m] = __builtin_amdgcn_mfma_i32_16x16x32_i8(f[t][j].v, codes_i8(w[u][m][j]),
+                                                               acc[m], 0, 0, 0);
+              else
+                acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    f[t][j].v, codes_bf16(w[u][m][j]), acc[m], 0, 0, 0);
+            }
+          }
+          const int gi = u * GP + g;
+          float sc[MATS];
+#pragma unroll
+          for (int m = 0; m < MATS; ++m) sc[m] = scale_of(s[m][gi >> 1], gi & 1);
+          float r[4] = {1.f, 1.f, 1.f, 1.f};
+          if constexpr (I8) {
+            r[0] = quad_lane<0>(sx[t][gi]);
+            r[1] = quad_lane<1>(sx[t][gi]);
+            r[2] = quad_lane<2>(sx[t][gi]);
+            r[3] = quad_lane<3>(sx[t][gi]);
+          }
+#pragma unroll
+          for (int m = 0; m < MATS; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sum[m][t][e] += float(acc[m][e]) * (I8 ? sc[m] * r[e] : sc[m]);
+        }
+    }
+    if constexpr (kStaged) __builtin_amdgcn_wave_barrier();
   }
+  constexpr int kPart = MATS * NT * 256;
+  __syncthreads();  // the staged values' place
 #pragma unroll
   for (int m = 0; m < MATS; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) part[wave][m][t][e][lane] = sum[m][t][e];
+      for (int e = 0; e < 4; ++e)
+        part[wave * kPart + ((m * NT + t) * 4 + e) * 64 + lane] = sum[m][t][e];
   __syncthreads();
-  for (int o = threadIdx.x; o < 256 * NT; o += 64 * kW4Waves) {
+  for (int o = threadIdx.x; o < 256 * NT; o += blockDim.x) {
     const int nn = o & 15, m16 = (o >> 4) & 15, t = o >> 8;
     const int64_t tok = t0 + 16 * t + m16;
     if (tok >= a.n_tok || n0 + nn >= a.d_out) continue;
     float v[MATS];
 #pragma unroll
     for (int m = 0; m < MATS; ++m) {
+      const float* p = part + ((m * NT + t) * 4 + (m16 & 3)) * 64 + (m16 >> 2) * 16 + nn;
       v[m] = 0.f;
-#pragma unroll
-      for (int w = 0; w < kW4Waves; ++w) v[m] += part[w][m][t][m16 & 3][(m16 >> 2) * 16 + nn];
+      for (int w = 0; w < waves; ++w) v[m] += p[w * kPart];
       if (I8 && a.x_groups == 1) v[m] *= a.xs[tok];
     }
     const float y = MATS == 2 ? w4_act(a.act, v[0]) * v[MATS - 1] : v[0];
@@ -231,13 +344,29 @@ __global__ void __launch_bounds__(64 * kW4Waves) k_w4(W4Args a) {
   }
 }
 
+template <bool I8, int MATS, int NT, int GP>
+void launch_w4(const W4Args& a, hipStream_t s) {
+  // Few enough waves that each has a batch of chunks to load together.
+  const int64_t batches = ceil_div(a.chunks, w4_batch(NT));
+  const size_t stage = NT == 1 ? size_t(std::min<int64_t>(a.n_tok, 16)) * w4_x_pitch(I8) : 0;
+  const size_t each = std::max(stage, size_t(MATS) * NT * 1024);
+  // 64 KiB of LDS
+  const int most = int(std::min<size_t>(w4_waves(MATS, NT), 65536 / each));
+  const int waves = int(std::min<int64_t>(std::max<int64_t>(batches, 1), most));
+  const dim3 grid(unsigned(ceil_div(a.d_out, 16)), unsigned(ceil_div(a.n_tok, kW4Tokens)));
+  hipLaunchKernelGGL((k_w4<I8, MATS, NT, GP>), grid, dim3(64 * waves), waves * each, s, a);
+}
+template <bool I8, int MATS, int NT>
+void launch_w4(const W4Args& a, hipStream_t s) {
+  if (a.group == 32) launch_w4<I8, MATS, NT, 4>(a, s);
+  else if (a.group == 64) launch_w4<I8, MATS, NT, 2>(a, s);
+  else launch_w4<I8, MATS, NT, 1>(a, s);
+}
 template <bool I8, int MATS>
 void launch_w4(const W4Args& a, hipStream_t s) {
-  const dim3 grid(unsigned(ceil_div(a.d_out, 16)), unsigned(ceil_div(a.n_tok, kW4Tokens)));
-  const dim3 wg(64 * kW4Waves);
-  if (a.n_tok <= 16) hipLaunchKernelGGL((k_w4<I8, MATS, 1>), grid, wg, 0, s, a);
-  else if (a.n_tok <= 32) hipLaunchKernelGGL((k_w4<I8, MATS, 2>), grid, wg, 0, s, a);
-  else hipLaunchKernelGGL((k_w4<I8, MATS, 4>), grid, wg, 0, s, a);
+  if (a.n_tok <= 16) launch_w4<I8, MATS, 1>(a, s);
+  else if (a.n_tok <= 32) launch_w4<I8, MATS, 2>(a, s);
+  else launch_w4<I8, MATS, 4>(a, s);
 }
 
 }  // namespace
