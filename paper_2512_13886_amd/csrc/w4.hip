@@ -350,8 +350,8 @@ void launch_w4(const W4Args& a, hipStream_t s) {
   const int64_t batches = ceil_div(a.chunks, w4_batch(NT));
   const size_t stage = NT == 1 ? size_t(std::min<int64_t>(a.n_tok, 16)) * w4_x_pitch(I8) : 0;
   const size_t each = std::max(stage, size_t(MATS) * NT * 1024);
-  // 64 KiB of LDS
-  const int most = int(std::min<size_t>(w4_waves(MATS, NT), 65536 / each));
+  constexpr size_t kLds = 136 << 10;
+  const int most = int(std::min<size_t>(w4_waves(MATS, NT), kLds / each));
   const int waves = int(std::min<int64_t>(std::max<int64_t>(batches, 1), most));
   const dim3 grid(unsigned(ceil_div(a.d_out, 16)), unsigned(ceil_div(a.n_tok, kW4Tokens)));
   hipLaunchKernelGGL((k_w4<I8, MATS, NT, GP>), grid, dim3(64 * waves), waves * each, s, a);
