@@ -49,14 +49,6 @@ struct GatedArgs {
   int h_f32, act;
 };
 
-__device__ inline void store_h(const GatedArgs& a, int64_t tok, int64_t n, const float (&h)[8],
-                               int left) {
-  if (a.h_f32)
-    store_upto8(static_cast<float*>(a.h) + tok * a.ldh + n, h, left);
-  else
-    store_upto8(static_cast<bf16_t*>(a.h) + tok * a.ldh + n, h, left);
-}
-
 // ---------------------------------------------------------------------------
 // Few tokens: 16 outputs a workgroup; wave w takes every eighth 64-value piece
 // of the 32 weight rows, and the waves' sums are joined in LDS in their order.
@@ -154,50 +146,35 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_gated256(GatedArgs a) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       src.a[h][i] = a.x + std::min(m0 + 128 * h + r, a.n_tok - 1) * (2 * a.ldx) + seg;
-      src.b[h][i] = (h ? a.wu : a.wg) + std::min(n0 + r, a.ff - 1) * (2 * a.ldw) + seg;
+      src.b[h][i] = (h ? a.wu : a.wg) +
+                    std::min(n0 + t256_rows_source(r), a.ff - 1) * (2 * a.ldw) + seg;
     }
   }
   Acc256 acc;
-  gemm256_mainloop<Bf16Tag>(acc, src, int(a.d / 64), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
+  gemm256_mainloop<Bf16RowsTag>(acc, src, int(a.d / 64), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
 
-  // g and u, where they are kept, then h, each through the stage buffers.
+  const int64_t n = n0 + t256_rows_col(0);
+  const int left = int(std::max<int64_t>(std::min<int64_t>(a.ff - n, 8), 0));
 #pragma unroll
-  for (int out = 0; out < 3; ++out) {
-    if (out == 0 && !a.g) continue;
-    if (out == 1 && !a.u) continue;
+  for (int qa = 0; qa < 2; ++qa)
 #pragma unroll
-    for (int qa = 0; qa < 2; ++qa)
+    for (int mi = 0; mi < 4; ++mi) {
+      const int64_t tok = m0 + t256_rows_row(qa, mi);
+      if (tok >= a.n_tok) continue;
+      float g[8], u[8], h[8];
 #pragma unroll
-      for (int mi = 0; mi < 4; ++mi)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int r = t256_row(qa, mi, k);
-#pragma unroll
-          for (int ni = 0; ni < 2; ++ni) {
-            const int c = t256_col(0, ni);
-            const float g = acc.q[qa][0][mi][ni][k], u = acc.q[qa][1][mi][ni][k];
-            *reinterpret_cast<float*>(t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r) +
-                                      ((c >> 2) ^ (r & 31)) * 16 + (c & 3) * 4) =
-                out == 0 ? g : out == 1 ? u : gate_act(a.act, g) * u;
-          }
-        }
-    __syncthreads();
-#pragma unroll 2
-    for (int p = threadIdx.x; p < 256 * 16; p += Tile256::kThreads) {
-      const int r = p >> 4, c = 2 * (p & 15);
-      const int64_t tok = m0 + r, n = n0 + 4 * c;
-      if (tok >= a.n_tok || n >= a.ff) continue;
-      const char* row = t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r);
-      const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
-      const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
-      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      const int left = int(std::min<int64_t>(a.ff - n, 8));
-      if (out == 0) store_upto8(a.g + tok * a.ldg + n, v, left);
-      else if (out == 1) store_upto8(a.u + tok * a.ldu + n, v, left);
-      else store_h(a, tok, n, v, left);
+      for (int e = 0; e < 8; ++e) {
+        g[e] = acc.q[qa][0][mi][e >> 2][e & 3];
+        u[e] = acc.q[qa][1][mi][e >> 2][e & 3];
+        h[e] = gate_act(a.act, g[e]) * u[e];
+      }
+      if (a.g) store_upto8(a.g + tok * a.ldg + n, g, left);
+      if (a.u) store_upto8(a.u + tok * a.ldu + n, u, left);
+      if (a.h_f32)
+        store_upto8(static_cast<float*>(a.h) + tok * a.ldh + n, h, left);
+      else
+        store_upto8(static_cast<bf16_t*>(a.h) + tok * a.ldh + n, h, left);
     }
-    if (out < 2) __syncthreads();
-  }
 }
 
 // 128 tokens x 64 outputs on the 128 x 128 ring tile: 16-row blocks of B are rows
@@ -220,39 +197,27 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_gated_ring(GatedArgs a) {
     src.b[i] = ((r & 16) ? a.wu : a.wg) + std::min(n, a.ff - 1) * (2 * a.ldw) + seg;
   }
   AccR128<false> acc;
-  r128_mainloop<Bf16Tag>(acc, src, SumShape{0, 0, 0}, int(a.d / 64), b0, b1, b2, b3, [] {});
+  r128_mainloop<Bf16RowsTag>(acc, src, SumShape{0, 0, 0}, int(a.d / 64), b0, b1, b2, b3, [] {});
 
-  const int wn = (threadIdx.x >> 6) & 3;
+  const int64_t n = n0 + 16 * ((threadIdx.x >> 6) & 3) + 4 * ((threadIdx.x >> 4) & 3);
+  const int left = int(std::max<int64_t>(std::min<int64_t>(a.ff - n, 4), 0));
 #pragma unroll
-  for (int out = 0; out < 3; ++out) {
-    if (out == 0 && !a.g) continue;
-    if (out == 1 && !a.u) continue;
+  for (int mi = 0; mi < 4; ++mi) {
+    const int64_t tok = m0 + t256_rows_row(0, mi);
+    if (tok >= a.n_tok) continue;
+    float g[4], u[4], h[4];
 #pragma unroll
-    for (int mi = 0; mi < 4; ++mi)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = r128_row(mi, k), c = wn * 16 + (threadIdx.x & 15);
-        const float g = acc.q[mi][0][k], u = acc.q[mi][1][k];
-        *reinterpret_cast<float*>(r128_stage_row(b0, b1, r) + ((c >> 2) ^ (r & 31)) * 16 +
-                                  (c & 3) * 4) =
-            out == 0 ? g : out == 1 ? u : gate_act(a.act, g) * u;
-      }
-    __syncthreads();
-#pragma unroll
-    for (int p = threadIdx.x; p < 128 * 8; p += Ring128::kThreads) {
-      const int r = p >> 3, c = 2 * (p & 7);
-      const int64_t tok = m0 + r, n = n0 + 4 * c;
-      if (tok >= a.n_tok || n >= a.ff) continue;
-      const char* row = r128_stage_row(b0, b1, r);
-      const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
-      const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
-      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      const int left = int(std::min<int64_t>(a.ff - n, 8));
-      if (out == 0) store_upto8(a.g + tok * a.ldg + n, v, left);
-      else if (out == 1) store_upto8(a.u + tok * a.ldu + n, v, left);
-      else store_h(a, tok, n, v, left);
+    for (int e = 0; e < 4; ++e) {
+      g[e] = acc.q[mi][0][e];
+      u[e] = acc.q[mi][1][e];
+      h[e] = gate_act(a.act, g[e]) * u[e];
     }
-    if (out < 2) __syncthreads();
+    if (a.g) store_upto4(a.g + tok * a.ldg + n, g, left);
+    if (a.u) store_upto4(a.u + tok * a.ldu + n, u, left);
+    if (a.h_f32)
+      store_upto4(static_cast<float*>(a.h) + tok * a.ldh + n, h, left);
+    else
+      store_upto4(static_cast<bf16_t*>(a.h) + tok * a.ldh + n, h, left);
   }
 }
 
@@ -446,41 +411,23 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_nt256(NtArgs a) {
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int i = 0; i < Tile256::kHalfLoads; ++i) {
-      const int64_t r = 128 * h + t256_load_row(i);
-      src.a[h][i] = a.a + std::min(m0 + r, a.out.rows - 1) * a.pitch_a + t256_seg_bytes(i);
-      src.b[h][i] = a.b + std::min(n0 + r, a.out.cols - 1) * a.pitch_b + t256_seg_bytes(i);
+      const int r = t256_load_row(i), seg = t256_seg_bytes(i);
+      src.a[h][i] = a.a + std::min(m0 + 128 * h + r, a.out.rows - 1) * a.pitch_a + seg;
+      src.b[h][i] = a.b + std::min(n0 + 128 * h + t256_rows_source(r), a.out.cols - 1) * a.pitch_b + seg;
     }
   Acc256 acc;
-  gemm256_mainloop<Bf16Tag>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
+  gemm256_mainloop<Bf16RowsTag>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
 #pragma unroll
-  for (int qb = 0; qb < 2; ++qb) {
-    if (qb) __syncthreads();
+  for (int qa = 0; qa < 2; ++qa)
 #pragma unroll
-    for (int qa = 0; qa < 2; ++qa)
+    for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
-      for (int mi = 0; mi < 4; ++mi)
+      for (int mi = 0; mi < 4; ++mi) {
+        float v[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int r = t256_row(qa, mi, k);
-#pragma unroll
-          for (int ni = 0; ni < 2; ++ni) {
-            const int c = t256_col(0, ni);
-            *reinterpret_cast<float*>(t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r) +
-                                      ((c >> 2) ^ (r & 31)) * 16 + (c & 3) * 4) =
-                acc.q[qa][qb][mi][ni][k];
-          }
-        }
-    __syncthreads();
-#pragma unroll 2
-    for (int p = threadIdx.x; p < 256 * 16; p += Tile256::kThreads) {
-      const int r = p >> 4, c = 2 * (p & 15);
-      const char* row = t256_stage_row(l0, l1, l2, l3, l4, l5, l6, l7, r);
-      const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
-      const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
-      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      nt_store(a.out, m0 + r, n0 + 128 * qb + 4 * c, v);
-    }
-  }
+        for (int e = 0; e < 8; ++e) v[e] = acc.q[qa][qb][mi][e >> 2][e & 3];
+        nt_store(a.out, m0 + t256_rows_row(qa, mi), n0 + t256_rows_col(qb), v);
+      }
 }
 
 __global__ void __launch_bounds__(Ring128::kThreads) k_nt_ring(NtArgs a) {
@@ -497,31 +444,16 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_nt_ring(NtArgs a) {
   for (int i = 0; i < Ring128::kLoads; ++i) {
     const int r = t256_load_row(i), seg = t256_seg_bytes(i);
     src.a[i] = a.a + std::min(m0 + r, a.out.rows - 1) * a.pitch_a + seg;
-    src.b[i] = a.b + std::min(n0 + r, a.out.cols - 1) * a.pitch_b + seg;
+    src.b[i] = a.b + std::min(n0 + t256_rows_source(r), a.out.cols - 1) * a.pitch_b + seg;
   }
   AccR128<false> acc;
-  r128_mainloop<Bf16Tag>(acc, src, SumShape{0, 0, 0}, int(a.stages), b0, b1, b2, b3, [] {});
+  r128_mainloop<Bf16RowsTag>(acc, src, SumShape{0, 0, 0}, int(a.stages), b0, b1, b2, b3, [] {});
 #pragma unroll
-  for (int mi = 0; mi < 4; ++mi)
+  for (int mi = 0; mi < 4; ++mi) {
+    float v[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r128_row(mi, k);
-#pragma unroll
-      for (int ni = 0; ni < 2; ++ni) {
-        const int c = r128_col(ni);
-        *reinterpret_cast<float*>(r128_stage_row(b0, b1, r) + ((c >> 2) ^ (r & 31)) * 16 +
-                                  (c & 3) * 4) = acc.q[mi][ni][k];
-      }
-    }
-  __syncthreads();
-#pragma unroll
-  for (int p = threadIdx.x; p < 128 * 16; p += Ring128::kThreads) {
-    const int r = p >> 4, c = 2 * (p & 15);
-    const char* row = r128_stage_row(b0, b1, r);
-    const f4 lo = *reinterpret_cast<const f4*>(row + ((c ^ (r & 31)) * 16));
-    const f4 hi = *reinterpret_cast<const f4*>(row + (((c + 1) ^ (r & 31)) * 16));
-    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    nt_store(a.out, m0 + r, n0 + 4 * c, v);
+    for (int e = 0; e < 8; ++e) v[e] = acc.q[mi][e >> 2][e & 3];
+    nt_store(a.out, m0 + t256_rows_row(0, mi), n0 + t256_rows_col(0), v);
   }
 }
 

@@ -74,6 +74,20 @@ __device__ inline int t256_col(int qb, int ni) {
   return qb * 128 + wn * 32 + ni * 16 + (lane & 15);
 }
 
+// The same with Bf16RowsTag. A lane holds row t256_rows_row(qa, mi), and of the two
+// blocks of a wave's 32 columns eight consecutive ones from t256_rows_col(qb) on,
+// block 0's four first, if LDS row r of a half tile of B is fetched from column
+// t256_rows_source(r) of the half.
+__device__ inline int t256_rows_row(int qa, int mi) {
+  return qa * 128 + int(threadIdx.x >> 8) * 64 + mi * 16 + int(threadIdx.x & 15);
+}
+__device__ inline int t256_rows_col(int qb) {
+  return qb * 128 + int((threadIdx.x >> 6) & 3) * 32 + 8 * int((threadIdx.x >> 4) & 3);
+}
+__device__ inline int t256_rows_source(int r) {
+  return (r & ~31) + 8 * ((r >> 2) & 3) + 4 * ((r >> 4) & 1) + (r & 3);
+}
+
 namespace t256 {
 
 __device__ inline void fetch(const char* const (&src)[Tile256::kHalfLoads], int64_t off, char* half) {
@@ -106,6 +120,7 @@ template <typename T>
 __device__ inline void quadrant(f4 (&c)[4][2], f4 (&cross)[4][2], const bf16x8 (&a)[4][2],
                                 const bf16x8 (&b)[2][2]) {
   constexpr bool kSplit = std::is_same<T, Bf16x3Tag>::value;
+  constexpr bool kRows = std::is_same<T, Bf16RowsTag>::value;
 #pragma unroll
   for (int p = 0; p < (kSplit ? 3 : 2); ++p) {
     // bf16: both K steps; split planes: hi hi, hi lo, lo hi.
@@ -115,7 +130,9 @@ __device__ inline void quadrant(f4 (&c)[4][2], f4 (&cross)[4][2], const bf16x8 (
     for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
       for (int ni = 0; ni < 2; ++ni)
-        to[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[mi][pa], b[ni][pb], to[mi][ni], 0, 0, 0);
+        to[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kRows ? b[ni][pb] : a[mi][pa],
+                                                             kRows ? a[mi][pa] : b[ni][pb],
+                                                             to[mi][ni], 0, 0, 0);
   }
 }
 

@@ -69,6 +69,10 @@ __device__ inline void mfma_bf16_blocks(f4 (&acc)[MB][NB], const uint4 (&a)[MB],
 }
 
 struct Bf16Tag {};
+// bf16 with the MFMA's operands exchanged (the main loops of gemm256.h and
+// gemm128.h): a lane then holds four consecutive columns of one row of a 16 x 16
+// block, row lane % 16, columns 4 * (lane / 16) + e, which can be stored as they are.
+struct Bf16RowsTag {};
 
 // fp32 emulated by bf16 MFMAs: every value v is stored as two bf16 planes,
 // hi = rne(v) and lo = rne(v - hi), and a product a*b is formed as

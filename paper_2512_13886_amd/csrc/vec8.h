@@ -91,6 +91,31 @@ __device__ inline void store8(float* p, const float (&v)[8]) {
   *reinterpret_cast<u32x4_4*>(p) = a;
   *reinterpret_cast<u32x4_4*>(p + 4) = b;
 }
+typedef u32x2 u32x2_2 __attribute__((aligned(2)));
+// The first n (0 .. 4) of four values.
+__device__ inline void store1(bf16_t* p, float v) { p->bits = uint16_t(pack_bf16(v, v)); }
+__device__ inline void store1(float* p, float v) { *p = v; }
+__device__ inline void store_upto4(bf16_t* p, const float (&v)[4], int n) {
+  if (n >= 4) {
+    *reinterpret_cast<u32x2_2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) store1(p + i, v[i]);
+}
+__device__ inline void store_upto4(float* p, const float (&v)[4], int n) {
+  if (n >= 4) {
+    u32x4 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(v[i]);
+    *reinterpret_cast<u32x4_4*>(p) = a;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) store1(p + i, v[i]);
+}
 // Whole numbers within int8.
 __device__ inline void store8(int8_t* p, const float (&v)[8]) {
   uint32_t w[2] = {0, 0};
@@ -98,8 +123,6 @@ __device__ inline void store8(int8_t* p, const float (&v)[8]) {
   for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t(int(v[i])) & 255u) << (8 * (i & 3));
   *reinterpret_cast<u32x2_1*>(p) = u32x2{w[0], w[1]};
 }
-__device__ inline void store1(bf16_t* p, float v) { p->bits = uint16_t(pack_bf16(v, v)); }
-__device__ inline void store1(float* p, float v) { *p = v; }
 __device__ inline void store1(int8_t* p, float v) { *p = int8_t(int(v)); }
 // The first n (0 .. 8) of eight values.
 template <typename T>
