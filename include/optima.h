@@ -474,7 +474,7 @@ optima_status optima_rms_norm_backward(const void* S, int64_t lds, const void* w
 /* Gated feed-forward product.
  *   G = X Wg^T, U = X Wu^T, H = act(G) * U element by element
  * X: [n_tok][d_in] bf16, any d_in >= 1; Wg, Wu: [d_ff][d_in] bf16 (16-byte aligned
- * where d_in % 64 == 0). H: h_dtype BF16 or F32. G and U (nullable): bf16
+ * where d_in % 8 == 0). H: h_dtype BF16 or F32. G and U (nullable): bf16
  * [n_tok][d_ff], what the gradient takes; H is formed of the unrounded sums.
  * act: OPTIMA_ACT_SILU or OPTIMA_ACT_NONE.
  * ws: optima_gated_forward_workspace_bytes(n_tok, d_in, d_ff) bytes (0 for few

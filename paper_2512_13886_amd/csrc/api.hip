@@ -433,7 +433,7 @@ optima_status optima_gated_forward(const void* X, int64_t ldx, int64_t n_tok, in
   const Span u{U, n_tok, d_ff, ldu, 2};
   if (!x.good() || !wg.good() || !wu.good() || !h.good() || (G && !g.good()) || (U && !u.good()))
     return OPTIMA_E_INVAL;
-  if (d_in % 64 == 0 && (!optima::aligned16(Wg) || !optima::aligned16(Wu))) return OPTIMA_E_INVAL;
+  if (d_in % 8 == 0 && (!optima::aligned16(Wg) || !optima::aligned16(Wu))) return OPTIMA_E_INVAL;
   for (const Span& o : {h, g, u})
     if (o.meets(x) || o.meets(wg) || o.meets(wu)) return OPTIMA_E_INVAL;
   if (h.meets(g) || h.meets(u) || g.meets(u)) return OPTIMA_E_INVAL;
@@ -468,6 +468,7 @@ optima_status optima_gated_backward(const void* X, int64_t ldx, int64_t n_tok, i
   const Span mg{mask_g, d_ff, d_in, d_in, 1}, mu{mask_u, d_ff, d_in, d_in, 1};
   for (const Span& i : {x, wg, wu, g, u, dh})
     if (!i.good()) return OPTIMA_E_INVAL;
+  if (d_in % 8 == 0 && (!optima::aligned16(Wg) || !optima::aligned16(Wu))) return OPTIMA_E_INVAL;
   if ((dX && !dx.good()) || (dWg && (!dwg.good() || !dwu.good()))) return OPTIMA_E_INVAL;
   for (const Span& o : {dx, dwg, dwu})
     for (const Span& i : {x, wg, wu, g, u, dh, mg, mu})

@@ -7,9 +7,7 @@
 //
 // Backward: dU = dH o act(g), dG = dH o u o act'(g), then
 //   dX = [dG dU] [Wg; Wu],  [dWg; dWu] = [dG dU]^T X  (o masks).
-// dG and dU are rounded to bf16, the type that the matrix instructions take. The
-// products want the contraction contiguous in both operands, so the element-wise
-// kernel writes [dG dU] and its transpose, and X and the weights are transposed.
+// P = [dG dU] is rounded to bf16, the type that the matrix instructions take.
 #include "common.h"
 #include "gemm128.h"
 #include "gemm256.h"
@@ -151,7 +149,7 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_gated256(GatedArgs a) {
     }
   }
   Acc256 acc;
-  gemm256_mainloop<Bf16RowsTag>(acc, src, int(a.d / 64), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
+  gemm256_mainloop<Bf16Rows<false>>(acc, src, int(a.d / 64), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
 
   const int64_t n = n0 + t256_rows_col(0);
   const int left = int(std::max<int64_t>(std::min<int64_t>(a.ff - n, 8), 0));
@@ -197,7 +195,7 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_gated_ring(GatedArgs a) {
     src.b[i] = ((r & 16) ? a.wu : a.wg) + std::min(n, a.ff - 1) * (2 * a.ldw) + seg;
   }
   AccR128<false> acc;
-  r128_mainloop<Bf16RowsTag>(acc, src, SumShape{0, 0, 0}, int(a.d / 64), b0, b1, b2, b3, [] {});
+  r128_mainloop<Bf16Rows<false>>(acc, src, SumShape{0, 0, 0}, int(a.d / 64), b0, b1, b2, b3, [] {});
 
   const int64_t n = n0 + 16 * ((threadIdx.x >> 6) & 3) + 4 * ((threadIdx.x >> 4) & 3);
   const int left = int(std::max<int64_t>(std::min<int64_t>(a.ff - n, 4), 0));
@@ -225,14 +223,16 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_gated_ring(GatedArgs a) {
 // Layout
 // ---------------------------------------------------------------------------
 
-// dst [rows][pitch] = src [rows][cols] with zeros up to the pitch (a multiple of 8).
+// dst [rows_out][pitch] = src [rows][cols] with zeros around it; pitch is a multiple of 8.
 __global__ void __launch_bounds__(kThreads) k_pad_rows(const bf16_t* src, int64_t ld, int64_t rows,
-                                                       int64_t cols, int64_t pitch, bf16_t* dst) {
+                                                       int64_t cols, int64_t rows_out,
+                                                       int64_t pitch, bf16_t* dst) {
   const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
   const int64_t per = pitch / 8, r = i / per, c = 8 * (i - r * per);
-  if (r >= rows) return;
+  if (r >= rows_out) return;
   Raw8<bf16_t> v;
-  load_upto8(v, src + r * ld + c, int(std::max<int64_t>(std::min<int64_t>(cols - c, 8), 0)));
+  const int64_t left = r < rows ? cols - c : 0;
+  load_upto8(v, src + r * ld + c, int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
   *reinterpret_cast<u32x4*>(dst + r * pitch + c) = v.w;
 }
 
@@ -280,13 +280,13 @@ __global__ void __launch_bounds__(kThreads) k_transpose_bf16(const bf16_t* src, 
 struct GateGradArgs {
   const bf16_t *g, *u, *dh;
   int64_t ldg, ldu, lddh, n_tok, ff;
-  bf16_t* p;       // [n_tok][2 ffp]: dG, dU, zeros in between, or NULL
-  bf16_t* pt;      // [2 ff][tp]: dG^T, dU^T, zeros from n_tok on, or NULL
+  bf16_t* p;   // [n_tok][2 ffp]: dG, dU, each with zeros up to ffp, or NULL
+  bf16_t* pt;  // [2 ff][tp]: their transpose with zeros from n_tok to tp, or NULL
   int64_t ffp, tp;
   int act;
 };
 
-// 64 tokens x 64 values of dG and dU.
+// 64 tokens x 64 values of dG and dU. Bound by HBM: 14 bytes a value.
 __global__ void __launch_bounds__(kThreads) k_gate_grad(GateGradArgs a) {
   __shared__ uint16_t tile[2][64 * kTrPitch];
   const int tiles_f = int(a.ffp / 64), tt = blockIdx.x / tiles_f;
@@ -338,62 +338,119 @@ __global__ void __launch_bounds__(kThreads) k_gate_grad(GateGradArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// C = A B^T into one or two outputs
+// The gradient's products, dX = P [Wg; Wu] and [dWg; dWu] = P^T X. A is P or P^T, both
+// written by k_gate_grad, with the contraction contiguous in its rows. dX takes the
+// weights as they are, with the contraction along their rows, through the transposing
+// LDS reads of gemm256.h (TB); dW takes X^T, transposed in memory.
+// Measured at 4096 tokens, 4096 -> 14336, of 962 GFLOP each: dX 701 us with TB, 670 and
+// 114 for the transposed weights without; dW 767 us with TB, 670 and 14 for X^T without,
+// and 840 us with both operands read through LDS that way (46 us less to write in
+// k_gate_grad).
 // ---------------------------------------------------------------------------
 
-// Rows from `split` on go to y[1]. A zero in a mask makes the product's value +0
-// there. accumulate adds to what the output holds.
-struct NtOut {
+// Rows of the product below `part` go to y[0], those from `split` to split + part to
+// y[1]. A zero in a mask makes the product's value +0 there. accumulate adds to what
+// the output holds.
+struct GradOut {
   void* y[2];
   const uint8_t* mask[2];
-  int64_t split, ld, rows, cols;
+  int64_t split, part, ld, cols;
   int f32, accumulate;
 };
-struct NtArgs {
+struct GradArgs {
   const char *a, *b;
   int64_t pitch_a, pitch_b;  // bytes, multiples of 16
-  int64_t stages;            // of 64 values
-  NtOut out;
+  int64_t rows, cols8;       // of the product; its columns rounded up to 8
+  int64_t stages;            // of 64 values of the contraction
+  int64_t s1, jump;          // TB: from stage s1 on B continues `jump` bytes further
+  GradOut out;
 };
 
-template <typename T>
-__device__ inline void nt_put(T* y, float (&v)[8], int left, int accumulate) {
-  if (accumulate) {
-    Raw8<T> raw;
-    float old[8];
-    load_upto8(raw, y, left);
-    values8(raw, old);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += old[i];
+template <bool TB>
+struct GradSteps {
+  int64_t pitch_b, jump;
+  int s1;
+  __device__ inline int64_t a(int s) const { return int64_t(s) * 128; }
+  __device__ inline int64_t b(int s) const {
+    return TB ? int64_t(s) * 64 * pitch_b + (s >= s1 ? jump : 0) : int64_t(s) * 128;
   }
-  store_upto8(y, v, left);
+};
+
+template <typename T, int N>
+__device__ inline void grad_put(T* y, float (&v)[N], int left, int accumulate) {
+  if (accumulate) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < left) {
+        if constexpr (sizeof(T) == 2)
+          v[i] += bf16_low(y[i].bits);
+        else
+          v[i] += y[i];
+      }
+  }
+  if constexpr (N == 8)
+    store_upto8(y, v, left);
+  else
+    store_upto4(y, v, left);
 }
 
-__device__ inline void nt_store(const NtOut& o, int64_t row, int64_t col, float (&v)[8]) {
-  if (row >= o.rows || col >= o.cols) return;
+// N consecutive values of a row of the product.
+template <int N>
+__device__ inline void grad_store(const GradOut& o, int64_t row, int64_t col, float (&v)[N]) {
   const int which = row >= o.split;
   const int64_t r = which ? row - o.split : row, at = r * o.ld + col;
-  const int left = int(std::min<int64_t>(o.cols - col, 8));
+  const int left = int(std::min<int64_t>(o.cols - col, N));
+  if (r >= o.part || left <= 0) return;
   if (o.mask[which]) {
     const uint8_t* m = o.mask[which] + r * o.cols + col;
-    uint32_t w[2] = {0, 0};
-    if (left == 8) {
-      const u32x2 q = *reinterpret_cast<const u32x2_1*>(m);
-      w[0] = q[0], w[1] = q[1];
-    } else {
-      for (int i = 0; i < left; ++i) w[i >> 2] |= uint32_t(m[i]) << (8 * (i & 3));
-    }
+    uint8_t keep[N];
+    if (left == N)
+      __builtin_memcpy(keep, m, N);
+    else
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (!((w[i >> 2] >> (8 * (i & 3))) & 255u)) v[i] = 0.f;
+      for (int i = 0; i < N; ++i) keep[i] = i < left ? m[i] : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (!keep[i]) v[i] = 0.f;
   }
   if (o.f32)
-    nt_put(static_cast<float*>(o.y[which]) + at, v, left, o.accumulate);
+    grad_put(static_cast<float*>(o.y[which]) + at, v, left, o.accumulate);
   else
-    nt_put(static_cast<bf16_t*>(o.y[which]) + at, v, left, o.accumulate);
+    grad_put(static_cast<bf16_t*>(o.y[which]) + at, v, left, o.accumulate);
+}
+// The two blocks of a wave's 32 columns from c0 on, of one row.
+template <bool TB>
+__device__ inline void grad_store_blocks(const GradOut& o, int64_t row, int64_t c0,
+                                         const f4 (&c)[2]) {
+  const int q = (threadIdx.x >> 4) & 3;
+  if (TB) {
+#pragma unroll
+    for (int ni = 0; ni < 2; ++ni) {
+      float v[4] = {c[ni][0], c[ni][1], c[ni][2], c[ni][3]};
+      grad_store<4>(o, row, c0 + 16 * ni + 4 * q, v);
+    }
+  } else {
+    float v[8] = {c[0][0], c[0][1], c[0][2], c[0][3], c[1][0], c[1][1], c[1][2], c[1][3]};
+    grad_store<8>(o, row, c0 + 8 * q, v);
+  }
 }
 
-__global__ void __launch_bounds__(Tile256::kThreads) k_nt256(NtArgs a) {
+// This thread's first-stage address of load i of A's rows from r0 on, and of B's
+// columns from c0 on.
+__device__ inline const char* grad_a(const GradArgs& a, int64_t r0, int i) {
+  return a.a + std::min(r0 + t256_load_row(i), a.rows - 1) * a.pitch_a + t256_seg_bytes(i);
+}
+template <bool TB>
+__device__ inline const char* grad_b(const GradArgs& a, int64_t c0, int i) {
+  if (TB)
+    return a.b + tr_load_row(i) * a.pitch_b +
+           2 * std::min<int64_t>(c0 + tr_seg_bytes() / 2, a.cols8 - 8);
+  return a.b + std::min(c0 + t256_rows_source(t256_load_row(i)), a.out.cols - 1) * a.pitch_b +
+         t256_seg_bytes(i);
+}
+
+template <bool TB>
+__global__ void __launch_bounds__(Tile256::kThreads) k_grad256(GradArgs a) {
   __shared__ __attribute__((aligned(1024))) char l0[Tile256::kHalfBytes];
   __shared__ __attribute__((aligned(1024))) char l1[Tile256::kHalfBytes];
   __shared__ __attribute__((aligned(1024))) char l2[Tile256::kHalfBytes];
@@ -402,7 +459,7 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_nt256(NtArgs a) {
   __shared__ __attribute__((aligned(1024))) char l5[Tile256::kHalfBytes];
   __shared__ __attribute__((aligned(1024))) char l6[Tile256::kHalfBytes];
   __shared__ __attribute__((aligned(1024))) char l7[Tile256::kHalfBytes];
-  const int tiles_m = cdiv(a.out.rows, 256), tiles_n = cdiv(a.out.cols, 256);
+  const int tiles_m = cdiv(a.rows, 256), tiles_n = cdiv(a.out.cols, 256);
   int tm, tn;
   tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 256;
@@ -411,50 +468,47 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_nt256(NtArgs a) {
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int i = 0; i < Tile256::kHalfLoads; ++i) {
-      const int r = t256_load_row(i), seg = t256_seg_bytes(i);
-      src.a[h][i] = a.a + std::min(m0 + 128 * h + r, a.out.rows - 1) * a.pitch_a + seg;
-      src.b[h][i] = a.b + std::min(n0 + 128 * h + t256_rows_source(r), a.out.cols - 1) * a.pitch_b + seg;
+      src.a[h][i] = grad_a(a, m0 + 128 * h, i);
+      src.b[h][i] = grad_b<TB>(a, n0 + 128 * h, i);
     }
   Acc256 acc;
-  gemm256_mainloop<Bf16RowsTag>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1)};
+  gemm256_mainloop<Bf16Rows<TB>>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7,
+                                       [] {}, steps);
 #pragma unroll
   for (int qa = 0; qa < 2; ++qa)
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb)
+    for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
-      for (int mi = 0; mi < 4; ++mi) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = acc.q[qa][qb][mi][e >> 2][e & 3];
-        nt_store(a.out, m0 + t256_rows_row(qa, mi), n0 + t256_rows_col(qb), v);
-      }
+      for (int qb = 0; qb < 2; ++qb)
+        grad_store_blocks<TB>(a.out, m0 + t256_rows_row(qa, mi),
+                              n0 + 128 * qb + 32 * ((threadIdx.x >> 6) & 3), acc.q[qa][qb][mi]);
 }
 
-__global__ void __launch_bounds__(Ring128::kThreads) k_nt_ring(NtArgs a) {
+template <bool TB>
+__global__ void __launch_bounds__(Ring128::kThreads) k_grad_ring(GradArgs a) {
   __shared__ __attribute__((aligned(1024))) char b0[Ring128::kBufBytes];
   __shared__ __attribute__((aligned(1024))) char b1[Ring128::kBufBytes];
   __shared__ __attribute__((aligned(1024))) char b2[Ring128::kBufBytes];
   __shared__ __attribute__((aligned(1024))) char b3[Ring128::kBufBytes];
-  const int tiles_m = cdiv(a.out.rows, 128), tiles_n = cdiv(a.out.cols, 128);
+  const int tiles_m = cdiv(a.rows, 128), tiles_n = cdiv(a.out.cols, 128);
   int tm, tn;
   tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = int64_t(tm) * 128, n0 = int64_t(tn) * 128;
   OperandsR128 src;
 #pragma unroll
   for (int i = 0; i < Ring128::kLoads; ++i) {
-    const int r = t256_load_row(i), seg = t256_seg_bytes(i);
-    src.a[i] = a.a + std::min(m0 + r, a.out.rows - 1) * a.pitch_a + seg;
-    src.b[i] = a.b + std::min(n0 + t256_rows_source(r), a.out.cols - 1) * a.pitch_b + seg;
+    src.a[i] = grad_a(a, m0, i);
+    src.b[i] = grad_b<TB>(a, n0, i);
   }
   AccR128<false> acc;
-  r128_mainloop<Bf16RowsTag>(acc, src, SumShape{0, 0, 0}, int(a.stages), b0, b1, b2, b3, [] {});
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1)};
+  r128_mainloop<Bf16Rows<TB>>(acc, src, SumShape{0, 0, 0}, int(a.stages), b0, b1, b2, b3,
+                                    [] {}, steps);
 #pragma unroll
-  for (int mi = 0; mi < 4; ++mi) {
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = acc.q[mi][e >> 2][e & 3];
-    nt_store(a.out, m0 + t256_rows_row(0, mi), n0 + t256_rows_col(0), v);
-  }
+  for (int mi = 0; mi < 4; ++mi)
+    grad_store_blocks<TB>(a.out, m0 + t256_rows_row(0, mi), n0 + 32 * ((threadIdx.x >> 6) & 3),
+                          acc.q[mi]);
 }
 
 // A round of 256 x 256 tiles over the CUs against one of 128 x 128 tiles, a
@@ -463,13 +517,14 @@ bool wide_tiles(int64_t wide, int64_t small) {
   return 5 * ceil_div(wide, kCus) <= 2 * ceil_div(small, kCus);
 }
 
-optima_status nt_product(const NtArgs& a, hipStream_t s) {
-  const int64_t wide = ceil_div(a.out.rows, 256) * ceil_div(a.out.cols, 256);
-  const int64_t small = ceil_div(a.out.rows, 128) * ceil_div(a.out.cols, 128);
+template <bool TB>
+optima_status grad_product(const GradArgs& a, hipStream_t s) {
+  const int64_t wide = ceil_div(a.rows, 256) * ceil_div(a.out.cols, 256);
+  const int64_t small = ceil_div(a.rows, 128) * ceil_div(a.out.cols, 128);
   if (wide_tiles(wide, small))
-    hipLaunchKernelGGL(k_nt256, dim3(unsigned(wide)), dim3(Tile256::kThreads), 0, s, a);
+    hipLaunchKernelGGL(k_grad256<TB>, dim3(unsigned(wide)), dim3(Tile256::kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL(k_nt_ring, dim3(unsigned(small)), dim3(Ring128::kThreads), 0, s, a);
+    hipLaunchKernelGGL(k_grad_ring<TB>, dim3(unsigned(small)), dim3(Ring128::kThreads), 0, s, a);
   OPTIMA_LAUNCH_CHECK();
   return OPTIMA_OK;
 }
@@ -493,26 +548,34 @@ GatedLayout carve_gated(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* 
 }
 
 struct GradLayout {
-  bf16_t *p, *pt, *wt, *xt;
+  bf16_t *p, *pt, *xt, *wg, *wu;
 };
+// Whether the weights' rows suit the products as they are: whole stages of rows,
+// 16-byte pieces.
+bool weights_suit(int64_t d, int64_t ff) { return ff % 64 == 0 && d % 8 == 0; }
 GradLayout carve_grad(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* bytes) {
   Carver c(ws);
   GradLayout l{};
   const size_t ffp = size_t(round_up(ff, 64)), tp = size_t(round_up(n_tok, 64));
+  const size_t dp = size_t(round_up(d, 8));
   l.p = c.take<bf16_t>(size_t(n_tok) * 2 * ffp);
-  l.wt = c.take<bf16_t>(size_t(d) * 2 * ffp);
   l.pt = c.take<bf16_t>(2 * size_t(ff) * tp);
   l.xt = c.take<bf16_t>(size_t(d) * tp);
+  if (!weights_suit(d, ff)) {
+    l.wg = c.take<bf16_t>(ffp * dp);
+    l.wu = c.take<bf16_t>(ffp * dp);
+  }
   if (bytes) *bytes = c.bytes();
   return l;
 }
 
-void pad_rows(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, bf16_t* dst,
-              hipStream_t s) {
-  hipLaunchKernelGGL(k_pad_rows, dim3(unsigned(ceil_div(rows * (pitch / 8), kThreads))),
-                     dim3(kThreads), 0, s, static_cast<const bf16_t*>(src), ld, rows, cols, pitch,
-                     dst);
+void pad_rows(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t rows_out,
+              int64_t pitch, bf16_t* dst, hipStream_t s) {
+  hipLaunchKernelGGL(k_pad_rows, dim3(unsigned(ceil_div(rows_out * (pitch / 8), kThreads))),
+                     dim3(kThreads), 0, s, static_cast<const bf16_t*>(src), ld, rows, cols,
+                     rows_out, pitch, dst);
 }
+
 void transpose(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, bf16_t* dst,
                hipStream_t s) {
   hipLaunchKernelGGL(k_transpose_bf16, dim3(unsigned(ceil_div(cols, 64) * ceil_div(rows, 64))),
@@ -545,13 +608,13 @@ optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d
   const GatedLayout l = carve_gated(ws, n_tok, d, ff, nullptr);
   const int64_t dp = round_up(d, 64);
   if (dp != d || !aligned16(X) || ldx % 8) {
-    pad_rows(X, ldx, n_tok, d, dp, l.x, s);
+    pad_rows(X, ldx, n_tok, d, n_tok, dp, l.x, s);
     a.x = reinterpret_cast<const char*>(l.x);
     a.ldx = dp;
   }
   if (dp != d) {
-    pad_rows(Wg, d, ff, d, dp, l.wg, s);
-    pad_rows(Wu, d, ff, d, dp, l.wu, s);
+    pad_rows(Wg, d, ff, d, ff, dp, l.wg, s);
+    pad_rows(Wu, d, ff, d, ff, dp, l.wu, s);
     a.wg = reinterpret_cast<const char*>(l.wg);
     a.wu = reinterpret_cast<const char*>(l.wu);
     a.ldw = dp;
@@ -581,35 +644,41 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
                              const uint8_t* mask_g, const uint8_t* mask_u, int accumulate, void* ws,
                              hipStream_t s) {
   const GradLayout l = carve_grad(ws, n_tok, d, ff, nullptr);
-  const int64_t ffp = round_up(ff, 64), tp = round_up(n_tok, 64);
+  const int64_t ffp = round_up(ff, 64), tp = round_up(n_tok, 64), dp = round_up(d, 8);
   if (n_tok > 0) {
     const GateGradArgs a{static_cast<const bf16_t*>(G), static_cast<const bf16_t*>(U),
                          static_cast<const bf16_t*>(dH), ldg, ldu, lddh, n_tok, ff,
                          dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, act};
-    hipLaunchKernelGGL(k_gate_grad, dim3(unsigned(ffp / 64 * (tp / 64))), dim3(kThreads), 0,
-                       s, a);
+    hipLaunchKernelGGL(k_gate_grad, dim3(unsigned(ffp / 64 * (tp / 64))), dim3(kThreads), 0, s, a);
     OPTIMA_LAUNCH_CHECK();
   }
   if (dX && n_tok > 0) {
-    transpose(Wg, d, ff, d, 2 * ffp, l.wt, s);
-    transpose(Wu, d, ff, d, 2 * ffp, l.wt + ffp, s);
-    OPTIMA_LAUNCH_CHECK();
-    NtArgs a{reinterpret_cast<const char*>(l.p), reinterpret_cast<const char*>(l.wt), 4 * ffp,
-             4 * ffp, 2 * ffp / 64, {}};
-    a.out = NtOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, lddx, n_tok, d,
-                  dx_dtype == OPTIMA_DTYPE_F32, 0};
-    const optima_status st = nt_product(a, s);
+    const void *wg = Wg, *wu = Wu;
+    if (!weights_suit(d, ff)) {
+      pad_rows(Wg, d, ff, d, ffp, dp, l.wg, s);
+      pad_rows(Wu, d, ff, d, ffp, dp, l.wu, s);
+      OPTIMA_LAUNCH_CHECK();
+      wg = l.wg;
+      wu = l.wu;
+    }
+    // P [dG dU] times Wg, then Wu.
+    const int64_t s1 = ffp / 64;
+    const int64_t jump = static_cast<const char*>(wu) - static_cast<const char*>(wg) - 2 * ffp * dp;
+    GradArgs a{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg), 4 * ffp, 2 * dp, n_tok, dp, 2 * s1, s1, jump, {}};
+    a.out = GradOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, n_tok, lddx, d,
+                    dx_dtype == OPTIMA_DTYPE_F32, 0};
+    const optima_status st = grad_product<true>(a, s);
     if (st != OPTIMA_OK) return st;
   }
   if (dWg) {
     // No tokens: no stages, and the products are zero.
     if (n_tok > 0) transpose(X, ldx, n_tok, d, tp, l.xt, s);
     OPTIMA_LAUNCH_CHECK();
-    NtArgs a{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt), 2 * tp,
-             2 * tp, tp / 64, {}};
-    a.out = NtOut{{dWg, dWu}, {mask_g, mask_u}, ff, d, 2 * ff, d, dw_dtype == OPTIMA_DTYPE_F32,
-                  accumulate};
-    return nt_product(a, s);
+    GradArgs a{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt), 2 * tp,
+               2 * tp, 2 * ff, dp, tp / 64, 0, 0, {}};
+    a.out = GradOut{{dWg, dWu}, {mask_g, mask_u}, ff, ff, d, d, dw_dtype == OPTIMA_DTYPE_F32,
+                    accumulate};
+    return grad_product<false>(a, s);
   }
   return OPTIMA_OK;
 }

@@ -87,18 +87,17 @@ __device__ inline int r128_col(int ni) { return t256_col(0, ni); }
 
 // LEFT: stages left, this one included (4: or more); the last three fetch
 // nothing, and wait for what is in flight.
-template <typename T, int LEFT, bool RANGES>
+template <typename T, int LEFT, bool RANGES, typename Steps>
 __device__ inline void r128_stage(AccR128<RANGES>& acc, const OperandsR128& src, SumRanges& ranges,
-                                  int s, char* cur, char* nxt) {
+                                  const Steps& steps, int s, char* cur, char* nxt) {
   constexpr int kStage = 2 * Ring128::kLoads;
   const int wm = threadIdx.x >> 8, wn = (threadIdx.x >> 6) & 3;
   bf16x8 fa[4][2], fb[2][2];
   t256::read<4>(fa, cur, wm * 64);
-  t256::read<2>(fb, cur + 128 * Ring128::kSRB, wn * 32);
+  t256::read_operand<2, MfmaOperands<T>::kTb>(fb, cur + 128 * Ring128::kSRB, wn * 32);
   if constexpr (LEFT >= 4) {
-    const int64_t off = int64_t(s + 3) * Ring128::kSRB;
-    t256::fetch(src.a, off, nxt);
-    t256::fetch(src.b, off, nxt + 128 * Ring128::kSRB);
+    t256::fetch(src.a, steps.a(s + 3), nxt);
+    t256::fetch(src.b, steps.b(s + 3), nxt + 128 * Ring128::kSRB);
   }
   t256::end_memory<LEFT >= 4 ? 2 * kStage : LEFT == 3 ? kStage : LEFT == 2 ? 0 : -1>();
   t256::quadrant<T>(acc.q, RANGES ? acc.q : acc.other, fa, fb);
@@ -113,28 +112,29 @@ __device__ inline void r128_stage(AccR128<RANGES>& acc, const OperandsR128& src,
 }
 
 // The last three stages, from buffers c0, c1, c2.
-template <typename T, bool RANGES>
+template <typename T, bool RANGES, typename Steps>
 __device__ inline void r128_last3(AccR128<RANGES>& acc, const OperandsR128& src, SumRanges& ranges,
-                                  char* c0, char* c1, char* c2) {
-  r128_stage<T, 3>(acc, src, ranges, 0, c0, nullptr);
-  r128_stage<T, 2>(acc, src, ranges, 0, c1, nullptr);
-  r128_stage<T, 1>(acc, src, ranges, 0, c2, nullptr);
+                                  const Steps& steps, char* c0, char* c1, char* c2) {
+  r128_stage<T, 3>(acc, src, ranges, steps, 0, c0, nullptr);
+  r128_stage<T, 2>(acc, src, ranges, steps, 0, c1, nullptr);
+  r128_stage<T, 1>(acc, src, ranges, steps, 0, c2, nullptr);
 }
 
 // n stages (n >= 0) of a sum, with RANGES its ranges as `shape` has them. b0..b3 are
 // distinct __shared__ arrays of Ring128::kBufBytes. `aside` runs once the first
-// fetches are out.
-template <typename T, bool RANGES, typename Aside>
+// fetches are out; `steps` says where a stage's operands are.
+template <typename T, bool RANGES, typename Aside, typename Steps = RowSteps>
 __device__ inline void r128_mainloop(AccR128<RANGES>& acc, const OperandsR128& src, SumShape shape,
-                                     int n, char* b0, char* b1, char* b2, char* b3, Aside aside) {
+                                     int n, char* b0, char* b1, char* b2, char* b3, Aside aside,
+                                     const Steps& steps = Steps{}) {
   constexpr int kStage = 2 * Ring128::kLoads;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     acc.q[i >> 1][i & 1] = acc.other[i >> 1][i & 1] = f4{0.f, 0.f, 0.f, 0.f};
   if (n <= 0) return;
   auto fetch = [&](int s, char* buf) {
-    t256::fetch(src.a, int64_t(s) * Ring128::kSRB, buf);
-    t256::fetch(src.b, int64_t(s) * Ring128::kSRB, buf + 128 * Ring128::kSRB);
+    t256::fetch(src.a, steps.a(s), buf);
+    t256::fetch(src.b, steps.b(s), buf + 128 * Ring128::kSRB);
   };
   const bool behind = threadIdx.x >= 256;  // waves 4-7
   fetch(0, b0);
@@ -149,10 +149,10 @@ __device__ inline void r128_mainloop(AccR128<RANGES>& acc, const OperandsR128& s
     }
     if (behind) t256::barrier();
     if (n == 2) {
-      r128_stage<T, 2>(acc, src, ranges, 0, b0, nullptr);
-      r128_stage<T, 1>(acc, src, ranges, 0, b1, nullptr);
+      r128_stage<T, 2>(acc, src, ranges, steps, 0, b0, nullptr);
+      r128_stage<T, 1>(acc, src, ranges, steps, 0, b1, nullptr);
     } else {
-      r128_stage<T, 1>(acc, src, ranges, 0, b0, nullptr);
+      r128_stage<T, 1>(acc, src, ranges, steps, 0, b0, nullptr);
     }
   } else {
     fetch(1, b1);
@@ -163,26 +163,26 @@ __device__ inline void r128_mainloop(AccR128<RANGES>& acc, const OperandsR128& s
     if (behind) t256::barrier();
     int s = 0;
     for (; s + 7 <= n; s += 4) {
-      r128_stage<T, 4>(acc, src, ranges, s, b0, b3);
-      r128_stage<T, 4>(acc, src, ranges, s + 1, b1, b0);
-      r128_stage<T, 4>(acc, src, ranges, s + 2, b2, b1);
-      r128_stage<T, 4>(acc, src, ranges, s + 3, b3, b2);
+      r128_stage<T, 4>(acc, src, ranges, steps, s, b0, b3);
+      r128_stage<T, 4>(acc, src, ranges, steps, s + 1, b1, b0);
+      r128_stage<T, 4>(acc, src, ranges, steps, s + 2, b2, b1);
+      r128_stage<T, 4>(acc, src, ranges, steps, s + 3, b3, b2);
     }
     // 3 to 6 stages are left.
     if (n - s == 3) {
-      r128_last3<T>(acc, src, ranges, b0, b1, b2);
+      r128_last3<T>(acc, src, ranges, steps, b0, b1, b2);
     } else if (n - s == 4) {
-      r128_stage<T, 4>(acc, src, ranges, s, b0, b3);
-      r128_last3<T>(acc, src, ranges, b1, b2, b3);
+      r128_stage<T, 4>(acc, src, ranges, steps, s, b0, b3);
+      r128_last3<T>(acc, src, ranges, steps, b1, b2, b3);
     } else if (n - s == 5) {
-      r128_stage<T, 4>(acc, src, ranges, s, b0, b3);
-      r128_stage<T, 4>(acc, src, ranges, s + 1, b1, b0);
-      r128_last3<T>(acc, src, ranges, b2, b3, b0);
+      r128_stage<T, 4>(acc, src, ranges, steps, s, b0, b3);
+      r128_stage<T, 4>(acc, src, ranges, steps, s + 1, b1, b0);
+      r128_last3<T>(acc, src, ranges, steps, b2, b3, b0);
     } else {
-      r128_stage<T, 4>(acc, src, ranges, s, b0, b3);
-      r128_stage<T, 4>(acc, src, ranges, s + 1, b1, b0);
-      r128_stage<T, 4>(acc, src, ranges, s + 2, b2, b1);
-      r128_last3<T>(acc, src, ranges, b3, b0, b1);
+      r128_stage<T, 4>(acc, src, ranges, steps, s, b0, b3);
+      r128_stage<T, 4>(acc, src, ranges, steps, s + 1, b1, b0);
+      r128_stage<T, 4>(acc, src, ranges, steps, s + 2, b2, b1);
+      r128_last3<T>(acc, src, ranges, steps, b3, b0, b1);
     }
   }
   if (!behind) t256::barrier();

@@ -59,6 +59,24 @@ __device__ inline int t256_seg_bytes(int i) {
   return (int(threadIdx.x & 7) ^ (t256_load_row(i) & 7)) * 16;
 }
 
+// Bytes from a thread's first-stage addresses to those of stage s.
+struct RowSteps {
+  __device__ inline int64_t a(int s) const { return int64_t(s) * Tile256::kSRB; }
+  __device__ inline int64_t b(int s) const { return int64_t(s) * Tile256::kSRB; }
+};
+
+// Half tiles of a B with the contraction along its rows: 64 rows (k) of 128 columns,
+// 256 bytes each. Load i of this thread fetches row tr_load_row(i), byte
+// tr_seg_bytes() of its 256. 16-byte segment g of row r sits at physical segment
+// g ^ tr_swz(r), so that the transposing reads meet no bank twice.
+__device__ inline int tr_load_row(int i) {
+  return (i * Tile256::kWaves + int(threadIdx.x >> 6)) * 4 + int((threadIdx.x & 63) >> 4);
+}
+__device__ inline int tr_swz(int r) { return 2 * ((r & 3) | (((r >> 3) & 1) << 2)); }
+__device__ inline int tr_seg_bytes() {
+  return (int(threadIdx.x & 15) ^ tr_swz(tr_load_row(0))) * 16;  // the same for every i
+}
+
 struct Acc256 {
   f4 q[2][2][4][2];  // [A half][B half][16-row block][16-column block]
 };
@@ -74,7 +92,7 @@ __device__ inline int t256_col(int qb, int ni) {
   return qb * 128 + wn * 32 + ni * 16 + (lane & 15);
 }
 
-// The same with Bf16RowsTag. A lane holds row t256_rows_row(qa, mi), and of the two
+// The same with Bf16Rows. A lane holds row t256_rows_row(qa, mi), and of the two
 // blocks of a wave's 32 columns eight consecutive ones from t256_rows_col(qb) on,
 // block 0's four first, if LDS row r of a half tile of B is fetched from column
 // t256_rows_source(r) of the half.
@@ -115,12 +133,44 @@ __device__ inline void read(bf16x8 (&f)[NBLK][2], const char* half, int r0) {
   }
 }
 
+// The same of a half tile with the contraction along its rows: columns c0 on.
+// ds_read_b64_tr_b16 treats the eight-byte reads of 16 lanes as a 4 x 16 matrix of
+// 16-bit values (lane j supplies row j / 4, columns 4 (j % 4) .. + 3) and returns
+// column i to lane i: two of them give a lane eight consecutive k of its column.
+template <int NBLK>
+__device__ inline void read_tr(bf16x8 (&f)[NBLK][2], const char* half, int c0) {
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+  const int row = 8 * g + (j >> 2), sw = tr_swz(row);
+  // One offset from the array: through a chain of them the compiler loses track of the
+  // array and waits for the other arrays' loads in flight.
+  auto at = [half](int off) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(half + off));
+  };
+#pragma unroll
+  for (int m = 0; m < NBLK; ++m) {
+    const int off = row * 256 + 8 * (j & 1) + (((c0 >> 3) + 2 * m + ((j & 3) >> 1)) ^ sw) * 16;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const v4s lo = at(off + k * 8192), hi = at(off + k * 8192 + 1024);
+      f[m][k] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+}
+template <int NBLK, bool TR>
+__device__ inline void read_operand(bf16x8 (&f)[NBLK][2], const char* half, int r0) {
+  if constexpr (TR)
+    read_tr<NBLK>(f, half, r0);
+  else
+    read<NBLK>(f, half, r0);
+}
+
 // The second and third products of split planes go to `cross`, which may be c.
 template <typename T>
 __device__ inline void quadrant(f4 (&c)[4][2], f4 (&cross)[4][2], const bf16x8 (&a)[4][2],
                                 const bf16x8 (&b)[2][2]) {
   constexpr bool kSplit = std::is_same<T, Bf16x3Tag>::value;
-  constexpr bool kRows = std::is_same<T, Bf16RowsTag>::value;
+  constexpr bool kRows = MfmaOperands<T>::kRows;
 #pragma unroll
   for (int p = 0; p < (kSplit ? 3 : 2); ++p) {
     // bf16: both K steps; split planes: hi hi, hi lo, lo hi.
@@ -158,27 +208,28 @@ __device__ inline void end_memory() {
 
 // One stage from buffers a0, a1, b0, b1; na1 is the other A1 buffer.
 template <typename T>
-__device__ inline void stage(Acc256& acc, const Operands256& src, int64_t off1, int64_t off2,
-                             char* a0, char* a1, char* b0, char* b1, char* na1) {
+__device__ inline void stage(Acc256& acc, const Operands256& src, int64_t a_off1, int64_t a_off2,
+                             int64_t b_off2, char* a0, char* a1, char* b0, char* b1, char* na1) {
+  constexpr bool kTb = MfmaOperands<T>::kTb;
   const int wm = threadIdx.x >> 8, wn = (threadIdx.x >> 6) & 3;
   bf16x8 fa[4][2], fb0[2][2], fb1[2][2];
   read<4>(fa, a0, wm * 64);
-  read<2>(fb0, b0, wn * 32);
-  fetch(src.a[1], off1, na1);
+  read_operand<2, kTb>(fb0, b0, wn * 32);
+  fetch(src.a[1], a_off1, na1);
   end_memory<-1>();
   quadrant<T>(acc.q[0][0], acc.q[0][0], fa, fb0);
   barrier();
-  read<2>(fb1, b1, wn * 32);
-  fetch(src.a[0], off2, a0);
+  read_operand<2, kTb>(fb1, b1, wn * 32);
+  fetch(src.a[0], a_off2, a0);
   end_memory<-1>();
   quadrant<T>(acc.q[0][1], acc.q[0][1], fa, fb1);
   barrier();
   read<4>(fa, a1, wm * 64);
-  fetch(src.b[0], off2, b0);
+  fetch(src.b[0], b_off2, b0);
   end_memory<-1>();
   quadrant<T>(acc.q[1][1], acc.q[1][1], fa, fb1);
   barrier();
-  fetch(src.b[1], off2, b1);
+  fetch(src.b[1], b_off2, b1);
   end_memory<3 * Tile256::kHalfLoads>();
   quadrant<T>(acc.q[1][0], acc.q[1][0], fa, fb0);
   barrier();
@@ -189,32 +240,35 @@ __device__ inline void stage(Acc256& acc, const Operands256& src, int64_t off1, 
 // n stages (n >= 0) of tile products. The LDS arguments are distinct
 // __shared__ arrays of Tile256::kHalfBytes; fetches past the last stage repeat
 // it, into buffers that nobody reads again. `aside` runs once the first fetches
-// are out.
-template <typename T, typename Aside>
+// are out. `steps` says where a stage's operands are.
+template <typename T, typename Aside, typename Steps = RowSteps>
 __device__ inline void gemm256_mainloop(Acc256& acc, const Operands256& src, int n, char* a00,
                                         char* a01, char* b00, char* b01, char* a10, char* a11,
-                                        char* b10, char* b11, Aside aside) {
+                                        char* b10, char* b11, Aside aside,
+                                        const Steps& steps = Steps{}) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) acc.q[i >> 4][(i >> 3) & 1][(i >> 1) & 3][i & 1] = f4{0.f, 0.f, 0.f, 0.f};
   if (n <= 0) return;
-  auto at = [n](int s) { return int64_t(s < n ? s : n - 1) * Tile256::kSRB; };
-  t256::fetch(src.a[0], 0, a00);
-  t256::fetch(src.b[0], 0, b00);
-  t256::fetch(src.b[1], 0, b01);
-  t256::fetch(src.a[1], 0, a01);
-  t256::fetch(src.a[0], at(1), a10);
-  t256::fetch(src.b[0], at(1), b10);
-  t256::fetch(src.b[1], at(1), b11);
+  auto a_at = [n, &steps](int s) { return steps.a(s < n ? s : n - 1); };
+  auto b_at = [n, &steps](int s) { return steps.b(s < n ? s : n - 1); };
+  t256::fetch(src.a[0], a_at(0), a00);
+  t256::fetch(src.b[0], b_at(0), b00);
+  t256::fetch(src.b[1], b_at(0), b01);
+  t256::fetch(src.a[1], a_at(0), a01);
+  t256::fetch(src.a[0], a_at(1), a10);
+  t256::fetch(src.b[0], b_at(1), b10);
+  t256::fetch(src.b[1], b_at(1), b11);
   aside();
   t256::end_memory<3 * Tile256::kHalfLoads>();
   const bool behind = threadIdx.x >= 256;  // waves 4-7
   if (behind) t256::barrier();
   int s = 0;
   for (; s + 1 < n; s += 2) {
-    t256::stage<T>(acc, src, at(s + 1), at(s + 2), a00, a01, b00, b01, a11);
-    t256::stage<T>(acc, src, at(s + 2), at(s + 3), a10, a11, b10, b11, a01);
+    t256::stage<T>(acc, src, a_at(s + 1), a_at(s + 2), b_at(s + 2), a00, a01, b00, b01, a11);
+    t256::stage<T>(acc, src, a_at(s + 2), a_at(s + 3), b_at(s + 3), a10, a11, b10, b11, a01);
   }
-  if (s < n) t256::stage<T>(acc, src, at(s + 1), at(s + 2), a00, a01, b00, b01, a11);
+  if (s < n)
+    t256::stage<T>(acc, src, a_at(s + 1), a_at(s + 2), b_at(s + 2), a00, a01, b00, b01, a11);
   if (!behind) t256::barrier();
   // No load may still be writing LDS when the workgroup moves on.
   wait_vmcnt<0>();

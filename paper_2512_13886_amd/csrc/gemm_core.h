@@ -72,7 +72,17 @@ struct Bf16Tag {};
 // bf16 with the MFMA's operands exchanged (the main loops of gemm256.h and
 // gemm128.h): a lane then holds four consecutive columns of one row of a 16 x 16
 // block, row lane % 16, columns 4 * (lane / 16) + e, which can be stored as they are.
-struct Bf16RowsTag {};
+// TB: B is stored with the contraction along its rows (C = A B).
+template <bool TB>
+struct Bf16Rows {};
+template <typename T>
+struct MfmaOperands {
+  static constexpr bool kRows = false, kTb = false;
+};
+template <bool TB>
+struct MfmaOperands<Bf16Rows<TB>> {
+  static constexpr bool kRows = true, kTb = TB;
+};
 
 // fp32 emulated by bf16 MFMAs: every value v is stored as two bf16 planes,
 // hi = rne(v) and lo = rne(v - hi), and a product a*b is formed as
