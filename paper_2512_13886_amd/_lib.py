@@ -480,6 +480,24 @@ def _rows(name, t, shape, dtypes):
     return (t.data_ptr() if n else None), ld, _ROW_DTYPES[t.dtype]
 
 
+def _launch_stream(stream):
+    """The stream's address, as _stream's. The decoding calls take a few microseconds, of
+    which making a Stream object would be two or three."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(_current_device())
+
+
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else \
+    torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _opt_rows(name, t, shape, dtypes):
     return (None, shape[1], 0) if t is None else _rows(name, t, shape, dtypes)
 
@@ -518,8 +536,8 @@ def optima_rms_norm(X: torch.Tensor, weight: torch.Tensor, Y: torch.Tensor, eps:
     if scales is not None:
         groups = -(-d // group) if group > 0 else 1
         _need_shape("scales", scales, (n, groups), (torch.float32,))
-    _check(_norm(x, ldx, r, ldr, dt, n, d, _ptr(weight), _ROW_DTYPES[weight.dtype], float(eps), s,
-                 lds, y, ldy, y_dt, _ptr(scales), int(group), _stream(stream)))
+    _check(_norm(x, ldx, r, ldr, dt, n, d, _addr(weight), _ROW_DTYPES[weight.dtype], float(eps), s,
+                 lds, y, ldy, y_dt, _addr(scales), int(group), _launch_stream(stream)))
 
 
 def optima_rms_norm_backward_workspace_bytes(n_tok: int, d: int) -> int:
@@ -546,9 +564,9 @@ def optima_rms_norm_backward(S: torch.Tensor, weight: torch.Tensor, dY: torch.Te
         _need_shape("dweight", dweight, (d,), (torch.float32,))
         ws, nbytes = _workspace(optima_rms_norm_backward_workspace_bytes(n, d), ws, S.device,
                                 stream)
-    _check(_norm_bwd(s, lds, _ptr(weight), _ROW_DTYPES[weight.dtype], dy, lddy, ds, ldds, dt, n, d,
-                     float(eps), dx, lddx, _ptr(dweight), int(bool(accumulate)), _ptr(ws), nbytes,
-                     _stream(stream)))
+    _check(_norm_bwd(s, lds, _addr(weight), _ROW_DTYPES[weight.dtype], dy, lddy, ds, ldds, dt, n, d,
+                     float(eps), dx, lddx, _addr(dweight), int(bool(accumulate)), _addr(ws), nbytes,
+                     _launch_stream(stream)))
 
 
 def optima_gated_forward_workspace_bytes(n_tok: int, d_in: int, d_ff: int) -> int:
@@ -581,8 +599,8 @@ def optima_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, H:
     nbytes = 0
     if need or ws is not None:
         ws, nbytes = _workspace(need, ws, X.device, stream)
-    _check(_gated(x, ldx, n, d, _ptr(Wg), _ptr(Wu), ff, int(act), h, ldh, h_dt, g, ldg, u, ldu,
-                  _ptr(ws), nbytes, _stream(stream)))
+    _check(_gated(x, ldx, n, d, _addr(Wg), _addr(Wu), ff, int(act), h, ldh, h_dt, g, ldg, u, ldu,
+                  _addr(ws), nbytes, _launch_stream(stream)))
 
 
 def optima_gated_backward_workspace_bytes(n_tok: int, d_in: int, d_ff: int) -> int:
@@ -615,9 +633,9 @@ def optima_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G
         if m is not None:
             _need_shape(name, m, (ff, d), (torch.uint8,))
     ws, nbytes = _workspace(optima_gated_backward_workspace_bytes(n, d, ff), ws, X.device, stream)
-    _check(_gated_bwd(x, ldx, n, d, _ptr(Wg), _ptr(Wu), ff, int(act), g, ldg, u, ldu, dh, lddh, dx,
-                      lddx, dx_dt, _ptr(dWg), _ptr(dWu), dw_dt, _ptr(mask_g), _ptr(mask_u),
-                      int(bool(accumulate)), _ptr(ws), nbytes, _stream(stream)))
+    _check(_gated_bwd(x, ldx, n, d, _addr(Wg), _addr(Wu), ff, int(act), g, ldg, u, ldu, dh, lddh, dx,
+                      lddx, dx_dt, _addr(dWg), _addr(dWu), dw_dt, _addr(mask_g), _addr(mask_u),
+                      int(bool(accumulate)), _addr(ws), nbytes, _launch_stream(stream)))
 
 
 def optima_w4_row_bytes(d: int) -> int:
@@ -634,8 +652,8 @@ def optima_w4_pack(W: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, group
     n, d = W.shape
     _need_shape("W", W, (n, d), _F)
     _w4_weights("Q", Q, "scales", scales, n, d, group)
-    _check(_w4_pack(_ptr(W), _ROW_DTYPES[W.dtype], n, d, int(group), _ptr(Q), _ptr(scales),
-                    _stream(stream)))
+    _check(_w4_pack(_addr(W), _ROW_DTYPES[W.dtype], n, d, int(group), _addr(Q), _addr(scales),
+                    _launch_stream(stream)))
 
 
 def _w4_weights(q_name, Q, s_name, scales, n, d, group):
@@ -670,8 +688,8 @@ def optima_w4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y: 
     n_out = Q.shape[0]
     _w4_weights("Q", Q, "scales", scales, n_out, d, group)
     y, ldy, y_dt = _rows("Y", Y, (n, n_out), _F)
-    _check(_w4_linear(x, ldx, x_dt, _ptr(x_scales), int(x_group), n, d, _ptr(Q), _ptr(scales),
-                      int(group), n_out, y, ldy, y_dt, _stream(stream)))
+    _check(_w4_linear(x, ldx, x_dt, _addr(x_scales), int(x_group), n, d, _addr(Q), _addr(scales),
+                      int(group), n_out, y, ldy, y_dt, _launch_stream(stream)))
 
 
 def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Qu: torch.Tensor,
@@ -685,6 +703,6 @@ def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Q
     _w4_weights("Qg", Qg, "scales_g", scales_g, ff, d, group)
     _w4_weights("Qu", Qu, "scales_u", scales_u, ff, d, group)
     h, ldh, h_dt = _rows("H", H, (n, ff), _F)
-    _check(_w4_gated(x, ldx, x_dt, _ptr(x_scales), int(x_group), n, d, _ptr(Qg), _ptr(scales_g),
-                     _ptr(Qu), _ptr(scales_u), int(group), ff, int(act), h, ldh, h_dt,
-                     _stream(stream)))
+    _check(_w4_gated(x, ldx, x_dt, _addr(x_scales), int(x_group), n, d, _addr(Qg), _addr(scales_g),
+                     _addr(Qu), _addr(scales_u), int(group), ff, int(act), h, ldh, h_dt,
+                     _launch_stream(stream)))
