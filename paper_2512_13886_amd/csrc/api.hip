@@ -103,7 +103,7 @@ bool group_ok(int64_t group) { return group == 32 || group == 64 || group == 128
 bool gated_sizes(int64_t n_tok, int64_t d_in, int64_t d_ff) {
   return n_tok >= 0 && n_tok <= kMaxTok && d_in >= 1 && d_in <= kMaxDim && d_ff >= 1 &&
          d_ff <= kMaxDim &&
-         (n_tok / 64 + 1) * (std::max(d_in, d_ff) / 64 + 1) < (int64_t(1) << 30);
+         (n_tok / 64 + 1) * (std::max(d_in, d_ff) / 64 + 1) < (int64_t(1) << 28);
 }
 
 optima_status w4_call(const void* X, int64_t ldx, int x_dtype, const float* x_scales,

@@ -224,16 +224,20 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_gated_ring(GatedArgs a) {
 // ---------------------------------------------------------------------------
 
 // dst [rows_out][pitch] = src [rows][cols] with zeros around it; pitch is a multiple of 8.
-__global__ void __launch_bounds__(kThreads) k_pad_rows(const bf16_t* src, int64_t ld, int64_t rows,
-                                                       int64_t cols, int64_t rows_out,
-                                                       int64_t pitch, bf16_t* dst) {
-  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t per = pitch / 8, r = i / per, c = 8 * (i - r * per);
-  if (r >= rows_out) return;
+struct PadRows {
+  const bf16_t* src;
+  int64_t ld, rows, cols, rows_out, pitch;
+  bf16_t* dst;
+  int64_t blocks() const { return src ? ceil_div(rows_out * (pitch / 8), kThreads) : 0; }
+};
+__device__ inline void pad_rows(const PadRows& a, int64_t block) {
+  const int64_t i = block * kThreads + threadIdx.x;
+  const int64_t per = a.pitch / 8, r = i / per, c = 8 * (i - r * per);
+  if (r >= a.rows_out) return;
   Raw8<bf16_t> v;
-  const int64_t left = r < rows ? cols - c : 0;
-  load_upto8(v, src + r * ld + c, int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
-  *reinterpret_cast<u32x4*>(dst + r * pitch + c) = v.w;
+  const int64_t left = r < a.rows ? a.cols - c : 0;
+  load_upto8(v, a.src + r * a.ld + c, int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
+  *reinterpret_cast<u32x4*>(a.dst + r * a.pitch + c) = v.w;
 }
 
 // 64 x 64 values of a tile in LDS, rows 66 apart: the transposing reads below
@@ -255,25 +259,30 @@ __device__ inline u32x4 tr_get(const uint16_t* tile, int r, int c) {
 
 // dst [cols][pitch] = src^T, src [rows][cols], with zeros from `rows` up to the
 // next multiple of 64 of a dst row. pitch and dst are multiples of 8 values.
-__global__ void __launch_bounds__(kThreads) k_transpose_bf16(const bf16_t* src, int64_t ld,
-                                                             int64_t rows, int64_t cols,
-                                                             int64_t pitch, bf16_t* dst) {
-  __shared__ uint16_t tile[64 * kTrPitch];
-  const int tiles_c = cdiv(cols, 64), tr = blockIdx.x / tiles_c;
-  const int64_t r0 = int64_t(tr) * 64, c0 = int64_t(blockIdx.x - tr * tiles_c) * 64;
+struct Transpose {
+  const bf16_t* src;
+  int64_t ld, rows, cols, pitch;
+  bf16_t* dst;
+  int64_t blocks() const { return src ? ceil_div(rows, 64) * ceil_div(cols, 64) : 0; }
+};
+__device__ inline void transpose_tile(const Transpose& a, int block, uint16_t* tile) {
+  const int tiles_c = cdiv(a.cols, 64), tr = block / tiles_c;
+  const int64_t r0 = int64_t(tr) * 64, c0 = int64_t(block - tr * tiles_c) * 64;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int p = threadIdx.x + k * kThreads, r = p >> 3, c = 8 * (p & 7);
     Raw8<bf16_t> v;
-    const int64_t left = r0 + r < rows ? cols - c0 - c : 0;
-    load_upto8(v, src + (r0 + r) * ld + c0 + c, int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
+    const int64_t left = r0 + r < a.rows ? a.cols - c0 - c : 0;
+    load_upto8(v, a.src + (r0 + r) * a.ld + c0 + c,
+               int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
     tr_put(tile, r, c, v.w);
   }
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int p = threadIdx.x + k * kThreads, c = p >> 3, r = 8 * (p & 7);
-    if (c0 + c < cols) *reinterpret_cast<u32x4*>(dst + (c0 + c) * pitch + r0 + r) = tr_get(tile, r, c);
+    if (c0 + c < a.cols)
+      *reinterpret_cast<u32x4*>(a.dst + (c0 + c) * a.pitch + r0 + r) = tr_get(tile, r, c);
   }
 }
 
@@ -284,13 +293,14 @@ struct GateGradArgs {
   bf16_t* pt;  // [2 ff][tp]: their transpose with zeros from n_tok to tp, or NULL
   int64_t ffp, tp;
   int act;
+  int64_t blocks() const { return ffp / 64 * (tp / 64); }
 };
 
 // 64 tokens x 64 values of dG and dU. Bound by HBM: 14 bytes a value.
-__global__ void __launch_bounds__(kThreads) k_gate_grad(GateGradArgs a) {
-  __shared__ uint16_t tile[2][64 * kTrPitch];
-  const int tiles_f = int(a.ffp / 64), tt = blockIdx.x / tiles_f;
-  const int64_t t0 = int64_t(tt) * 64, f0 = int64_t(blockIdx.x - tt * tiles_f) * 64;
+__device__ inline void gate_grad_tile(const GateGradArgs& a, int block,
+                                      uint16_t (&tile)[2][64 * kTrPitch]) {
+  const int tiles_f = int(a.ffp / 64), tt = block / tiles_f;
+  const int64_t t0 = int64_t(tt) * 64, f0 = int64_t(block - tt * tiles_f) * 64;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int i = threadIdx.x + k * kThreads, r = i >> 3, c = 8 * (i & 7);
@@ -337,15 +347,47 @@ __global__ void __launch_bounds__(kThreads) k_gate_grad(GateGradArgs a) {
   }
 }
 
+// All that the products wait for, in one launch: P and P^T, X^T, and copies of weights
+// whose rows do not suit them.
+struct GradPrep {
+  GateGradArgs gate;
+  Transpose x;
+  PadRows w[2];
+  int64_t gate_blocks, x_blocks, w_blocks;
+};
+__global__ void __launch_bounds__(kThreads) k_gated_grad_prep(GradPrep a) {
+  __shared__ uint16_t tile[2][64 * kTrPitch];
+  int64_t b = blockIdx.x;
+  if (b < a.gate_blocks) return gate_grad_tile(a.gate, int(b), tile);
+  b -= a.gate_blocks;
+  if (b < a.x_blocks) return transpose_tile(a.x, int(b), tile[0]);
+  b -= a.x_blocks;
+  const int k = b >= a.w_blocks;
+  pad_rows(a.w[k], k ? b - a.w_blocks : b);
+}
+
+// The operands of the forward product whose rows do not suit wide loads.
+struct ForwardPrep {
+  PadRows m[3];
+  int64_t first[3];  // block of the launch
+};
+__global__ void __launch_bounds__(kThreads) k_gated_prep(ForwardPrep a) {
+  const int64_t b = blockIdx.x;
+  const int k = b >= a.first[2] ? 2 : b >= a.first[1] ? 1 : 0;
+  pad_rows(a.m[k], b - a.first[k]);
+}
+
 // ---------------------------------------------------------------------------
 // The gradient's products, dX = P [Wg; Wu] and [dWg; dWu] = P^T X. A is P or P^T, both
-// written by k_gate_grad, with the contraction contiguous in its rows. dX takes the
+// written by k_gated_grad_prep, with the contraction contiguous in its rows. dX takes the
 // weights as they are, with the contraction along their rows, through the transposing
 // LDS reads of gemm256.h (TB); dW takes X^T, transposed in memory.
 // Measured at 4096 tokens, 4096 -> 14336, of 962 GFLOP each: dX 701 us with TB, 670 and
 // 114 for the transposed weights without; dW 767 us with TB, 670 and 14 for X^T without,
-// and 840 us with both operands read through LDS that way (46 us less to write in
-// k_gate_grad).
+// and 840 us with both operands read through LDS that way (46 us less to write before).
+// Both run in one launch, the longer sums first, so that the tiles of one fill the CUs
+// that the other leaves. A long sum over few tiles is split, and joined by
+// k_grad_join.
 // ---------------------------------------------------------------------------
 
 // Rows of the product below `part` go to y[0], those from `split` to split + part to
@@ -369,10 +411,10 @@ struct GradArgs {
 template <bool TB>
 struct GradSteps {
   int64_t pitch_b, jump;
-  int s1;
-  __device__ inline int64_t a(int s) const { return int64_t(s) * 128; }
+  int s1, s0;  // the workgroup's first stage
+  __device__ inline int64_t a(int s) const { return int64_t(s0 + s) * 128; }
   __device__ inline int64_t b(int s) const {
-    return TB ? int64_t(s) * 64 * pitch_b + (s >= s1 ? jump : 0) : int64_t(s) * 128;
+    return TB ? int64_t(s0 + s) * 64 * pitch_b + (s0 + s >= s1 ? jump : 0) : int64_t(s0 + s) * 128;
   }
 };
 
@@ -449,19 +491,21 @@ __device__ inline const char* grad_b(const GradArgs& a, int64_t c0, int i) {
          t256_seg_bytes(i);
 }
 
+struct GradPair {
+  GradArgs x, w;         // dX, dW; of a product that is not wanted, no tiles
+  int64_t x_blocks;      // of dX: tiles, times `splits` ranges of its sum
+  int splits;
+  float* part;           // [split][tile][128][128] where there are several
+};
+
+#define GRAD_LDS(name, bytes) __shared__ __attribute__((aligned(1024))) char name[bytes]
+
 template <bool TB>
-__global__ void __launch_bounds__(Tile256::kThreads) k_grad256(GradArgs a) {
-  __shared__ __attribute__((aligned(1024))) char l0[Tile256::kHalfBytes];
-  __shared__ __attribute__((aligned(1024))) char l1[Tile256::kHalfBytes];
-  __shared__ __attribute__((aligned(1024))) char l2[Tile256::kHalfBytes];
-  __shared__ __attribute__((aligned(1024))) char l3[Tile256::kHalfBytes];
-  __shared__ __attribute__((aligned(1024))) char l4[Tile256::kHalfBytes];
-  __shared__ __attribute__((aligned(1024))) char l5[Tile256::kHalfBytes];
-  __shared__ __attribute__((aligned(1024))) char l6[Tile256::kHalfBytes];
-  __shared__ __attribute__((aligned(1024))) char l7[Tile256::kHalfBytes];
+__device__ inline void grad256_tile(const GradArgs& a, int block, char* l0, char* l1, char* l2,
+                                    char* l3, char* l4, char* l5, char* l6, char* l7) {
   const int tiles_m = cdiv(a.rows, 256), tiles_n = cdiv(a.out.cols, 256);
   int tm, tn;
-  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  tile_of_block(block, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 256;
   Operands256 src;
 #pragma unroll
@@ -472,9 +516,9 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_grad256(GradArgs a) {
       src.b[h][i] = grad_b<TB>(a, n0 + 128 * h, i);
     }
   Acc256 acc;
-  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1)};
-  gemm256_mainloop<Bf16Rows<TB>>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7,
-                                       [] {}, steps);
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), 0};
+  gemm256_mainloop<Bf16Rows<TB>>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7, [] {},
+                                 steps);
 #pragma unroll
   for (int qa = 0; qa < 2; ++qa)
 #pragma unroll
@@ -485,15 +529,28 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_grad256(GradArgs a) {
                               n0 + 128 * qb + 32 * ((threadIdx.x >> 6) & 3), acc.q[qa][qb][mi]);
 }
 
+__global__ void __launch_bounds__(Tile256::kThreads) k_grad256(GradPair p) {
+  GRAD_LDS(l0, Tile256::kHalfBytes);
+  GRAD_LDS(l1, Tile256::kHalfBytes);
+  GRAD_LDS(l2, Tile256::kHalfBytes);
+  GRAD_LDS(l3, Tile256::kHalfBytes);
+  GRAD_LDS(l4, Tile256::kHalfBytes);
+  GRAD_LDS(l5, Tile256::kHalfBytes);
+  GRAD_LDS(l6, Tile256::kHalfBytes);
+  GRAD_LDS(l7, Tile256::kHalfBytes);
+  if (blockIdx.x < p.x_blocks)
+    grad256_tile<true>(p.x, blockIdx.x, l0, l1, l2, l3, l4, l5, l6, l7);
+  else
+    grad256_tile<false>(p.w, blockIdx.x - int(p.x_blocks), l0, l1, l2, l3, l4, l5, l6, l7);
+}
+
+// Stages [s0, s1) of the sum of a 128 x 128 tile; to `part` where that is not NULL.
 template <bool TB>
-__global__ void __launch_bounds__(Ring128::kThreads) k_grad_ring(GradArgs a) {
-  __shared__ __attribute__((aligned(1024))) char b0[Ring128::kBufBytes];
-  __shared__ __attribute__((aligned(1024))) char b1[Ring128::kBufBytes];
-  __shared__ __attribute__((aligned(1024))) char b2[Ring128::kBufBytes];
-  __shared__ __attribute__((aligned(1024))) char b3[Ring128::kBufBytes];
+__device__ inline void grad_ring_tile(const GradArgs& a, int tile, int s0, int s1, float* part,
+                                      char* b0, char* b1, char* b2, char* b3) {
   const int tiles_m = cdiv(a.rows, 128), tiles_n = cdiv(a.out.cols, 128);
   int tm, tn;
-  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  tile_of_block(tile, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = int64_t(tm) * 128, n0 = int64_t(tn) * 128;
   OperandsR128 src;
 #pragma unroll
@@ -502,13 +559,57 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_grad_ring(GradArgs a) {
     src.b[i] = grad_b<TB>(a, n0, i);
   }
   AccR128<false> acc;
-  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1)};
-  r128_mainloop<Bf16Rows<TB>>(acc, src, SumShape{0, 0, 0}, int(a.stages), b0, b1, b2, b3,
-                                    [] {}, steps);
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), s0};
+  r128_mainloop<Bf16Rows<TB>>(acc, src, SumShape{0, 0, 0}, s1 - s0, b0, b1, b2, b3, [] {}, steps);
+  const int wn = (threadIdx.x >> 6) & 3;
+  if (part) {
+    float* q = part + 32 * wn + 4 * ((threadIdx.x >> 4) & 3);
+#pragma unroll
+    for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < 2; ++ni)
+        *reinterpret_cast<f4*>(q + t256_rows_row(0, mi) * 128 + 16 * ni) = acc.q[mi][ni];
+    return;
+  }
 #pragma unroll
   for (int mi = 0; mi < 4; ++mi)
-    grad_store_blocks<TB>(a.out, m0 + t256_rows_row(0, mi), n0 + 32 * ((threadIdx.x >> 6) & 3),
-                          acc.q[mi]);
+    grad_store_blocks<TB>(a.out, m0 + t256_rows_row(0, mi), n0 + 32 * wn, acc.q[mi]);
+}
+
+__global__ void __launch_bounds__(Ring128::kThreads) k_grad_ring(GradPair p) {
+  GRAD_LDS(b0, Ring128::kBufBytes);
+  GRAD_LDS(b1, Ring128::kBufBytes);
+  GRAD_LDS(b2, Ring128::kBufBytes);
+  GRAD_LDS(b3, Ring128::kBufBytes);
+  if (blockIdx.x < p.x_blocks) {
+    const int tiles = int(p.x_blocks) / p.splits, sp = blockIdx.x / tiles;
+    const int s0 = int(p.x.stages * sp / p.splits), s1 = int(p.x.stages * (sp + 1) / p.splits);
+    grad_ring_tile<true>(p.x, blockIdx.x - sp * tiles, s0, s1,
+                         p.splits > 1 ? p.part + size_t(blockIdx.x) * 16384 : nullptr, b0, b1, b2,
+                         b3);
+  } else {
+    grad_ring_tile<false>(p.w, blockIdx.x - int(p.x_blocks), 0, int(p.w.stages), nullptr, b0, b1,
+                          b2, b3);
+  }
+}
+#undef GRAD_LDS
+
+// dX from the ranges' partial sums, in their order: four values a thread, a sixteenth
+// of a tile a workgroup.
+__global__ void __launch_bounds__(kThreads) k_grad_join(GradPair p) {
+  const int tiles_m = cdiv(p.x.rows, 128), tiles_n = cdiv(p.x.out.cols, 128);
+  const int tiles = tiles_m * tiles_n, tile = blockIdx.x >> 4;
+  int tm, tn;
+  tile_of_block(tile, tiles, tiles_m, tiles_n, &tm, &tn);
+  const int at = (blockIdx.x & 15) * 1024 + 4 * threadIdx.x;
+  const int64_t row = int64_t(tm) * 128 + (at >> 7), col = int64_t(tn) * 128 + (at & 127);
+  if (row >= p.x.rows) return;
+  f4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int sp = 0; sp < p.splits; ++sp)
+    sum += *reinterpret_cast<const f4*>(p.part + (size_t(sp) * tiles + tile) * 16384 + at);
+  float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+  grad_store<4>(p.x.out, row, col, v);
 }
 
 // A round of 256 x 256 tiles over the CUs against one of 128 x 128 tiles, a
@@ -517,15 +618,44 @@ bool wide_tiles(int64_t wide, int64_t small) {
   return 5 * ceil_div(wide, kCus) <= 2 * ceil_div(small, kCus);
 }
 
-template <bool TB>
-optima_status grad_product(const GradArgs& a, hipStream_t s) {
-  const int64_t wide = ceil_div(a.rows, 256) * ceil_div(a.out.cols, 256);
-  const int64_t small = ceil_div(a.rows, 128) * ceil_div(a.out.cols, 128);
-  if (wide_tiles(wide, small))
-    hipLaunchKernelGGL(k_grad256<TB>, dim3(unsigned(wide)), dim3(Tile256::kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL(k_grad_ring<TB>, dim3(unsigned(small)), dim3(Ring128::kThreads), 0, s, a);
+// Partial sums of at most kPartTiles tiles.
+constexpr int64_t kPartTiles = 512;
+
+// The tiles of both products over the CUs, by the time the plan should take: a stage
+// takes 1.4 us of a 256 x 256 tile and 0.56 of a 128 x 128 one, of which dX may be
+// split so that it takes no longer than the rest (5 us for the join).
+optima_status grad_products(GradPair& p, hipStream_t s) {
+  const int64_t xs = p.x.stages, wst = p.w.stages;
+  auto tiles = [](const GradArgs& a, int64_t side) {
+    return ceil_div(a.rows, side) * ceil_div(a.out.cols, side);
+  };
+  const int64_t x256 = tiles(p.x, 256), w256 = tiles(p.w, 256);
+  const int64_t x128 = tiles(p.x, 128), w128 = tiles(p.w, 128);
+  const int64_t even256 = ceil_div(x256 * xs + w256 * wst, kCus);
+  const int64_t even128 = ceil_div(x128 * xs + w128 * wst, kCus);
+  const int64_t wide = 140 * std::max({even256, x256 ? xs : 0, w256 ? wst : 0});
+  int64_t splits = 1;
+  if (x128 && xs > even128)
+    splits = std::min({ceil_div(xs, std::max<int64_t>(even128, 8)), kPartTiles / x128, xs});
+  splits = std::max<int64_t>(splits, 1);
+  const int64_t small = 56 * std::max({even128, x128 ? ceil_div(xs, splits) : 0, w128 ? wst : 0}) +
+                        (splits > 1 ? 500 : 0);
+  if (wide <= small) {
+    p.x_blocks = x256;
+    p.splits = 1;
+    hipLaunchKernelGGL(k_grad256, dim3(unsigned(x256 + w256)), dim3(Tile256::kThreads), 0, s, p);
+    OPTIMA_LAUNCH_CHECK();
+    return OPTIMA_OK;
+  }
+  p.splits = int(splits);
+  p.x_blocks = x128 * splits;
+  hipLaunchKernelGGL(k_grad_ring, dim3(unsigned(p.x_blocks + w128)), dim3(Ring128::kThreads), 0, s,
+                     p);
   OPTIMA_LAUNCH_CHECK();
+  if (splits > 1) {
+    hipLaunchKernelGGL(k_grad_join, dim3(unsigned(16 * x128)), dim3(kThreads), 0, s, p);
+    OPTIMA_LAUNCH_CHECK();
+  }
   return OPTIMA_OK;
 }
 
@@ -549,6 +679,7 @@ GatedLayout carve_gated(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* 
 
 struct GradLayout {
   bf16_t *p, *pt, *xt, *wg, *wu;
+  float* part;
 };
 // Whether the weights' rows suit the products as they are: whole stages of rows,
 // 16-byte pieces.
@@ -565,22 +696,11 @@ GradLayout carve_grad(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* by
     l.wg = c.take<bf16_t>(ffp * dp);
     l.wu = c.take<bf16_t>(ffp * dp);
   }
+  // At most a range for every stage of dX's sum.
+  const int64_t x_tiles = ceil_div(n_tok, 128) * ceil_div(d, 128);
+  l.part = c.take<float>(16384 * size_t(std::min(kPartTiles, x_tiles * int64_t(2 * ffp / 64))));
   if (bytes) *bytes = c.bytes();
   return l;
-}
-
-void pad_rows(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t rows_out,
-              int64_t pitch, bf16_t* dst, hipStream_t s) {
-  hipLaunchKernelGGL(k_pad_rows, dim3(unsigned(ceil_div(rows_out * (pitch / 8), kThreads))),
-                     dim3(kThreads), 0, s, static_cast<const bf16_t*>(src), ld, rows, cols,
-                     rows_out, pitch, dst);
-}
-
-void transpose(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, bf16_t* dst,
-               hipStream_t s) {
-  hipLaunchKernelGGL(k_transpose_bf16, dim3(unsigned(ceil_div(cols, 64) * ceil_div(rows, 64))),
-                     dim3(kThreads), 0, s, static_cast<const bf16_t*>(src), ld, rows, cols, pitch,
-                     dst);
 }
 
 }  // namespace
@@ -607,17 +727,28 @@ optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d
   }
   const GatedLayout l = carve_gated(ws, n_tok, d, ff, nullptr);
   const int64_t dp = round_up(d, 64);
+  ForwardPrep prep{};
+  int64_t blocks = 0;
   if (dp != d || !aligned16(X) || ldx % 8) {
-    pad_rows(X, ldx, n_tok, d, n_tok, dp, l.x, s);
+    prep.m[0] = PadRows{static_cast<const bf16_t*>(X), ldx, n_tok, d, n_tok, dp, l.x};
+    blocks = prep.m[0].blocks();
     a.x = reinterpret_cast<const char*>(l.x);
     a.ldx = dp;
   }
+  prep.first[1] = prep.first[2] = blocks;
   if (dp != d) {
-    pad_rows(Wg, d, ff, d, ff, dp, l.wg, s);
-    pad_rows(Wu, d, ff, d, ff, dp, l.wu, s);
+    prep.m[1] = PadRows{static_cast<const bf16_t*>(Wg), d, ff, d, ff, dp, l.wg};
+    prep.m[2] = PadRows{static_cast<const bf16_t*>(Wu), d, ff, d, ff, dp, l.wu};
+    prep.first[2] += prep.m[1].blocks();
+    blocks = prep.first[2] + prep.m[2].blocks();
     a.wg = reinterpret_cast<const char*>(l.wg);
     a.wu = reinterpret_cast<const char*>(l.wu);
     a.ldw = dp;
+  }
+  if (blocks) {
+    // Without weights to copy, no block is theirs.
+    if (dp == d) prep.first[1] = prep.first[2] = INT64_MAX;
+    hipLaunchKernelGGL(k_gated_prep, dim3(unsigned(blocks)), dim3(kThreads), 0, s, prep);
   }
   a.d = dp;
   OPTIMA_LAUNCH_CHECK();
@@ -645,42 +776,46 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
                              hipStream_t s) {
   const GradLayout l = carve_grad(ws, n_tok, d, ff, nullptr);
   const int64_t ffp = round_up(ff, 64), tp = round_up(n_tok, 64), dp = round_up(d, 8);
-  if (n_tok > 0) {
-    const GateGradArgs a{static_cast<const bf16_t*>(G), static_cast<const bf16_t*>(U),
-                         static_cast<const bf16_t*>(dH), ldg, ldu, lddh, n_tok, ff,
-                         dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, act};
-    hipLaunchKernelGGL(k_gate_grad, dim3(unsigned(ffp / 64 * (tp / 64))), dim3(kThreads), 0, s, a);
-    OPTIMA_LAUNCH_CHECK();
-  }
+  GradPrep prep{};
+  GradPair pair{};
+  pair.part = l.part;
+  const void *wg = Wg, *wu = Wu;
   if (dX && n_tok > 0) {
-    const void *wg = Wg, *wu = Wu;
     if (!weights_suit(d, ff)) {
-      pad_rows(Wg, d, ff, d, ffp, dp, l.wg, s);
-      pad_rows(Wu, d, ff, d, ffp, dp, l.wu, s);
-      OPTIMA_LAUNCH_CHECK();
+      prep.w[0] = PadRows{static_cast<const bf16_t*>(Wg), d, ff, d, ffp, dp, l.wg};
+      prep.w[1] = PadRows{static_cast<const bf16_t*>(Wu), d, ff, d, ffp, dp, l.wu};
       wg = l.wg;
       wu = l.wu;
     }
     // P [dG dU] times Wg, then Wu.
     const int64_t s1 = ffp / 64;
     const int64_t jump = static_cast<const char*>(wu) - static_cast<const char*>(wg) - 2 * ffp * dp;
-    GradArgs a{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg), 4 * ffp, 2 * dp, n_tok, dp, 2 * s1, s1, jump, {}};
-    a.out = GradOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, n_tok, lddx, d,
-                    dx_dtype == OPTIMA_DTYPE_F32, 0};
-    const optima_status st = grad_product<true>(a, s);
-    if (st != OPTIMA_OK) return st;
+    pair.x = GradArgs{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg), 4 * ffp,
+                      2 * dp, n_tok, dp, 2 * s1, s1, jump,
+                      GradOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, n_tok, lddx, d,
+                              dx_dtype == OPTIMA_DTYPE_F32, 0}};
   }
   if (dWg) {
     // No tokens: no stages, and the products are zero.
-    if (n_tok > 0) transpose(X, ldx, n_tok, d, tp, l.xt, s);
-    OPTIMA_LAUNCH_CHECK();
-    GradArgs a{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt), 2 * tp,
-               2 * tp, 2 * ff, dp, tp / 64, 0, 0, {}};
-    a.out = GradOut{{dWg, dWu}, {mask_g, mask_u}, ff, ff, d, d, dw_dtype == OPTIMA_DTYPE_F32,
-                    accumulate};
-    return grad_product<false>(a, s);
+    if (n_tok > 0) prep.x = Transpose{static_cast<const bf16_t*>(X), ldx, n_tok, d, tp, l.xt};
+    pair.w = GradArgs{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt),
+                      2 * tp, 2 * tp, 2 * ff, dp, tp / 64, 0, 0,
+                      GradOut{{dWg, dWu}, {mask_g, mask_u}, ff, ff, d, d,
+                              dw_dtype == OPTIMA_DTYPE_F32, accumulate}};
   }
-  return OPTIMA_OK;
+  if (n_tok > 0) {
+    prep.gate = GateGradArgs{static_cast<const bf16_t*>(G), static_cast<const bf16_t*>(U),
+                             static_cast<const bf16_t*>(dH), ldg, ldu, lddh, n_tok, ff,
+                             dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, act};
+    prep.gate_blocks = prep.gate.blocks();
+    prep.x_blocks = prep.x.blocks();
+    prep.w_blocks = prep.w[0].blocks();
+    const int64_t blocks = prep.gate_blocks + prep.x_blocks + 2 * prep.w_blocks;
+    hipLaunchKernelGGL(k_gated_grad_prep, dim3(unsigned(blocks)), dim3(kThreads), 0, s, prep);
+    OPTIMA_LAUNCH_CHECK();
+  }
+  if (n_tok == 0 && !dWg) return OPTIMA_OK;
+  return grad_products(pair, s);
 }
 
 }  // namespace optima
