@@ -18,7 +18,6 @@ namespace optima {
 namespace {
 
 constexpr int kFewTokens = 64;
-constexpr int kFewWaves = 8;
 constexpr int64_t kCus = 256;
 
 __device__ inline int cdiv(int64_t a, int b) { return int((a + b - 1) / b); }
@@ -48,65 +47,99 @@ struct GatedArgs {
 };
 
 // ---------------------------------------------------------------------------
-// Few tokens: 16 outputs a workgroup; wave w takes every eighth 64-value piece
-// of the 32 weight rows, and the waves' sums are joined in LDS in their order.
-// Lane (q, i) reads values 16 q .. + 15 of a piece of row i: two MFMA operands,
-// and with the other lanes whole 128-byte lines.
+// Few tokens: the waves of a workgroup take the 64-value pieces of its weight rows in
+// turn, and their sums are joined in LDS in their order. Lane (q, i) reads
+// values 16 q .. + 15 of a piece of row i: two MFMA operands, and with the other
+// lanes whole 128-byte lines. The 16 rows of an operand are MATS = 1: 8 of Wg and
+// the same 8 of Wu; MATS = 2: 16 of each, in two operands that share the tokens'.
 // ---------------------------------------------------------------------------
-template <int NT>
-__global__ void __launch_bounds__(64 * kFewWaves) k_gated_few(GatedArgs a) {
-  __shared__ float part[kFewWaves][2][NT][4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+constexpr int few_waves(int mats) { return mats == 1 ? 16 : 8; }  // at most
+// Pieces that a wave loads together.
+constexpr int few_batch(int nt) { return nt <= 2 ? 2 : 1; }
+
+__device__ inline f4 few_mfma(const Raw8<bf16_t>& x, const Raw8<bf16_t>& w, const f4& acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.w),
+                                                 __builtin_bit_cast(bf16x8, w.w), acc, 0, 0, 0);
+}
+
+template <int MATS, int NT>
+__global__ void __launch_bounds__(64 * few_waves(MATS)) k_gated_few(GatedArgs a) {
+  constexpr int kBatch = few_batch(NT), kOut = 8 * MATS;
+  __shared__ float part[few_waves(MATS)][MATS][NT][4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int q = lane >> 4, i = lane & 15;
-  const int64_t n0 = int64_t(blockIdx.x) * 16;
-  const int64_t n = std::min(n0 + i, a.ff - 1);
-  const bf16_t* wg = reinterpret_cast<const bf16_t*>(a.wg) + n * a.ldw;
-  const bf16_t* wu = reinterpret_cast<const bf16_t*>(a.wu) + n * a.ldw;
+  const int64_t n0 = int64_t(blockIdx.x) * kOut;
+  const int64_t n = std::min(n0 + (i & (kOut - 1)), a.ff - 1);
+  const bf16_t* w[MATS];
+#pragma unroll
+  for (int m = 0; m < MATS; ++m)
+    w[m] = reinterpret_cast<const bf16_t*>((MATS == 1 ? i >= 8 : m) ? a.wu : a.wg) + n * a.ldw;
   const bf16_t* x[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
     x[t] = reinterpret_cast<const bf16_t*>(a.x) + std::min<int64_t>(16 * t + i, a.n_tok - 1) * a.ldx;
-  f4 acc[2][NT];
+  f4 acc[MATS][NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) acc[0][t] = acc[1][t] = f4{0.f, 0.f, 0.f, 0.f};
-  const int pieces = cdiv(a.d, 64);
-  for (int c = wave; c < pieces; c += kFewWaves) {
-    const int k = 64 * c + 16 * q, left = int(a.d) - k;
-    Raw8<bf16_t> rg[2], ru[2], rx[NT][2];
+  for (int m = 0; m < MATS; ++m)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      load_upto8(rg[e], wg + k + 8 * e, left - 8 * e);
-      load_upto8(ru[e], wu + k + 8 * e, left - 8 * e);
+    for (int t = 0; t < NT; ++t) acc[m][t] = f4{0.f, 0.f, 0.f, 0.f};
+  const int pieces = int(a.d / 64);  // whole ones
+  for (int c0 = wave; c0 < pieces; c0 += waves * kBatch) {
+    Raw8<bf16_t> rw[kBatch][MATS][2], rx[kBatch][NT][2];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) load_upto8(rx[t][e], x[t] + k + 8 * e, left - 8 * e);
+    for (int v = 0; v < kBatch; ++v) {
+      const int k = 64 * (c0 + v * waves) + 16 * q;
+      if (c0 + v * waves >= pieces) break;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) load8(rw[v][m][e], w[m] + k + 8 * e);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) load8(rx[v][t][e], x[t] + k + 8 * e);
+      }
     }
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int v = 0; v < kBatch; ++v) {
+      if (c0 + v * waves >= pieces) break;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int m = 0; m < MATS; ++m) acc[m][t] = few_mfma(rx[v][t][e], rw[v][m][e], acc[m][t]);
+    }
+  }
+  if (a.d % 64 && wave == pieces % waves) {  // the rest, by the wave whose turn it is
+    const int k = 64 * pieces + 16 * q, left = int(a.d) - k;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      Raw8<bf16_t> rw[MATS], rx;
+#pragma unroll
+      for (int m = 0; m < MATS; ++m) load_upto8(rw[m], w[m] + k + 8 * e, left - 8 * e);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const bf16x8 xv = __builtin_bit_cast(bf16x8, rx[t][e].w);
-        acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            xv, __builtin_bit_cast(bf16x8, rg[e].w), acc[0][t], 0, 0, 0);
-        acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            xv, __builtin_bit_cast(bf16x8, ru[e].w), acc[1][t], 0, 0, 0);
+        load_upto8(rx, x[t] + k + 8 * e, left - 8 * e);
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) acc[m][t] = few_mfma(rx, rw[m], acc[m][t]);
       }
+    }
   }
 #pragma unroll
-  for (int m = 0; m < 2; ++m)
+  for (int m = 0; m < MATS; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) part[wave][m][t][e][lane] = acc[m][t][e];
   __syncthreads();
-  for (int o = threadIdx.x; o < 256 * NT; o += 64 * kFewWaves) {
-    const int nn = o & 15, m16 = (o >> 4) & 15, t = o >> 8;
+  for (int o = threadIdx.x; o < 16 * kOut * NT; o += blockDim.x) {
+    const int nn = o % kOut, m16 = o / kOut & 15, t = o / (16 * kOut);
     const int64_t tok = 16 * t + m16, at = n0 + nn;
     if (tok >= a.n_tok || at >= a.ff) continue;
     float v[2] = {0.f, 0.f};
+    for (int w = 0; w < waves; ++w)
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) v[m] += part[w][m][t][m16 & 3][(m16 >> 2) * 16 + nn];
+      for (int m = 0; m < 2; ++m)
+        v[m] += part[w][MATS == 1 ? 0 : m][t][m16 & 3][(m16 >> 2) * 16 + (MATS == 1 ? 8 * m : 0) + nn];
     const float h = gate_act(a.act, v[0]) * v[1];
     if (a.h_f32)
       static_cast<float*>(a.h)[tok * a.ldh + at] = h;
@@ -115,6 +148,14 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_gated_few(GatedArgs a) {
     if (a.g) store1(a.g + tok * a.ldg + at, v[0]);
     if (a.u) store1(a.u + tok * a.ldu + at, v[1]);
   }
+}
+
+template <int MATS, int NT>
+void launch_few(const GatedArgs& a, hipStream_t s) {
+  // Enough pieces for sixteen waves to have a batch each.
+  const int waves = MATS == 1 && a.d >= 2048 ? 16 : 8;
+  hipLaunchKernelGGL((k_gated_few<MATS, NT>), dim3(unsigned(ceil_div(a.ff, 8 * MATS))),
+                     dim3(64 * waves), 0, s, a);
 }
 
 // ---------------------------------------------------------------------------
@@ -659,13 +700,30 @@ optima_status grad_products(GradPair& p, hipStream_t s) {
   return OPTIMA_OK;
 }
 
+// Whether the weights are streamed once for all tokens, or tiles take them. Streamed
+// they come at 6 TB/s, and every 16 outputs read all tokens again, at 10 TB/s out of
+// the caches. A round of 64-output tiles takes 0.56 us for 64 values of d and 3.5 us
+// around them, at most 5.5 TB/s, and rows that do not suit them are copied first.
+// Measured, streamed against tiles: 4096 -> 14336, 4 tokens 39 to 42 us, 16 tokens 49 to
+// 43, 64 tokens 91 to 45; 1024 -> 8192, 32 tokens 10.7 to 12.2, 64 tokens 15.1 to 13.1;
+// 4096 -> 2048, 64 tokens 27 to 34; 1001 -> 2731, 64 tokens 17 to 21.
+bool few_tokens(int64_t n_tok, int64_t d, int64_t ff) {
+  if (n_tok > kFewTokens) return false;
+  const double weights = 4e-6 * double(d) * double(ff);  // MB
+  const double streamed = weights / 6 + double(n_tok) * weights / 320;
+  const double rounds = double(ceil_div(ceil_div(ff, 64), kCus));
+  const double tiles = std::max(rounds * (0.56 * double(ceil_div(d, 64)) + 3.5), weights / 5.5 + 1);
+  return streamed <= tiles + (d % 64 ? 2 * weights / 5 + 4 : 0);
+}
+
 struct GatedLayout {
   bf16_t *x, *wg, *wu;
 };
 GatedLayout carve_gated(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* bytes) {
   Carver c(ws);
   GatedLayout l{};
-  if (n_tok > kFewTokens) {
+  // Sized for tiles wherever more tokens may take them.
+  if (!few_tokens(n_tok, d, ff)) {
     const int64_t dp = round_up(d, 64);
     l.x = c.take<bf16_t>(size_t(n_tok) * size_t(dp));
     if (dp != d) {
@@ -717,11 +775,14 @@ optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d
   GatedArgs a{static_cast<const char*>(X), static_cast<const char*>(Wg),
               static_cast<const char*>(Wu), H, static_cast<bf16_t*>(G), static_cast<bf16_t*>(U),
               n_tok, d, ff, ldx, d, ldh, ldg, ldu, h_dtype == OPTIMA_DTYPE_F32, act};
-  if (n_tok <= kFewTokens) {
-    const dim3 grid(unsigned(ceil_div(ff, 16))), wg(64 * kFewWaves);
-    if (n_tok <= 16) hipLaunchKernelGGL(k_gated_few<1>, grid, wg, 0, s, a);
-    else if (n_tok <= 32) hipLaunchKernelGGL(k_gated_few<2>, grid, wg, 0, s, a);
-    else hipLaunchKernelGGL(k_gated_few<4>, grid, wg, 0, s, a);
+  if (few_tokens(n_tok, d, ff)) {
+    // Half the outputs a workgroup where that makes the launch, or its reads of the
+    // tokens are few: 4096 -> 2048, 16 tokens, 10.3 against 13.9 us, 4096 -> 14336, 4
+    // tokens, 39.4 against 45.1; but 1024 -> 8192, 16 tokens, 11.9 against 8.7.
+    if (n_tok <= 16 && (n_tok <= 8 || ff < 4096)) launch_few<1, 1>(a, s);
+    else if (n_tok <= 16) launch_few<2, 1>(a, s);
+    else if (n_tok <= 32) launch_few<2, 2>(a, s);
+    else launch_few<2, 4>(a, s);
     OPTIMA_LAUNCH_CHECK();
     return OPTIMA_OK;
   }

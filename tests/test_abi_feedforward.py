@@ -121,7 +121,7 @@ def test_gated_backward_refusals(lib, change, status):
 
 def test_gated_workspace_queries():
     import paper_2512_13886_amd as L
-    assert L.optima_gated_forward_workspace_bytes(64, 4096, 14336) == 0
+    assert L.optima_gated_forward_workspace_bytes(1, 4096, 14336) == 0
     assert L.optima_gated_forward_workspace_bytes(100, 128, 32) >= 100 * 128 * 2
     assert L.optima_gated_forward_workspace_bytes(100, 100, 32) >= (100 + 64) * 128 * 2
     assert L.optima_gated_forward_workspace_bytes(-1, 128, 32) == 0
