@@ -522,18 +522,22 @@ optima_status optima_w4_pack(const void* W, int dtype, int64_t n, int64_t d, int
  * X: [n_tok][d] of x_dtype BF16, or I8 with x_scales: fp32 [n_tok][ceil(d / x_group)]
  * with x_group = group, or one a token with x_group = 0 (as optima_rms_norm writes
  * them). Y: [n_tok][d_out] BF16 or F32. 8-bit codes are multiplied exactly within a
- * group. */
+ * group.
+ * ws: optima_w4_workspace_bytes(n_tok, d, d_out, n_mats) bytes, with n_mats 1 here and 2
+ * for the gated product: 0 up to 16 tokens, and never less for more tokens. */
+size_t optima_w4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out, int n_mats);
 optima_status optima_w4_linear(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
                                int64_t x_group, int64_t n_tok, int64_t d, const void* Q,
                                const void* scales, int64_t group, int64_t d_out, void* Y,
-                               int64_t ldy, int y_dtype, hipStream_t stream);
+                               int64_t ldy, int y_dtype, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
 
 /* The gated product with 4-bit weights: H = act(X deq(Qg)^T) * (X deq(Qu)^T). */
 optima_status optima_w4_gated(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
                               int64_t x_group, int64_t n_tok, int64_t d, const void* Qg,
                               const void* scales_g, const void* Qu, const void* scales_u,
                               int64_t group, int64_t d_ff, int act, void* H, int64_t ldh,
-                              int h_dtype, hipStream_t stream);
+                              int h_dtype, void* ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -22,7 +22,7 @@ from ._lib import (OptimaError, SolverOpts, DTYPE_F32, DTYPE_BF16, DTYPE_F64, PR
                    optima_rms_norm_backward, optima_gated_forward_workspace_bytes,
                    optima_gated_forward, optima_gated_backward_workspace_bytes,
                    optima_gated_backward, optima_w4_row_bytes, optima_w4_pack,
-                   optima_w4_linear, optima_w4_gated)
+                   optima_w4_workspace_bytes, optima_w4_linear, optima_w4_gated)
 
 __all__ = [
     "OptimaError", "SolverOpts", "DTYPE_F32", "DTYPE_BF16", "DTYPE_F64", "PREC_FP32",
@@ -38,5 +38,5 @@ __all__ = [
     "NORM_MAX_DIM", "optima_rms_norm", "optima_rms_norm_backward_workspace_bytes",
     "optima_rms_norm_backward", "optima_gated_forward_workspace_bytes", "optima_gated_forward",
     "optima_gated_backward_workspace_bytes", "optima_gated_backward", "optima_w4_row_bytes",
-    "optima_w4_pack", "optima_w4_linear", "optima_w4_gated",
+    "optima_w4_pack", "optima_w4_workspace_bytes", "optima_w4_linear", "optima_w4_gated",
 ]

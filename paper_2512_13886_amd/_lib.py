@@ -129,10 +129,11 @@ _w4_row = _sig("optima_w4_row_bytes", _sz, [_i64])
 _w4_pack = _sig("optima_w4_pack", _i32, [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp])
 _w4_linear = _sig("optima_w4_linear", _i32,
                   [_vp, _i64, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _i32,
-                   _vp])
+                   _vp, _sz, _vp])
+_w4_ws = _sig("optima_w4_workspace_bytes", _sz, [_i64, _i64, _i64, _i32])
 _w4_gated = _sig("optima_w4_gated", _i32,
                  [_vp, _i64, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _i64, _i32,
-                  _vp, _i64, _i32, _vp])
+                  _vp, _i64, _i32, _vp, _sz, _vp])
 
 
 def library_path() -> str:
@@ -678,9 +679,23 @@ def _w4_tokens(X, x_scales, x_group, group):
     return n, d, x, ldx, x_dt
 
 
+def optima_w4_workspace_bytes(n_tok: int, d: int, d_out: int, n_mats: int = 1) -> int:
+    return int(_w4_ws(n_tok, d, d_out, n_mats))
+
+
+def _w4_space(n, d, n_out, mats, ws, device, stream):
+    """(address, bytes) of the workspace; up to 16 tokens need none. One made here is
+    freed when the call returns, for later work on the stream (see _workspace)."""
+    need = optima_w4_workspace_bytes(n, d, n_out, mats) if n > 16 else 0
+    if not need and ws is None:
+        return None, 0
+    ws, nbytes = _workspace(need, ws, device, stream)
+    return ws.data_ptr(), nbytes
+
+
 def optima_w4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y: torch.Tensor,
                      group: int = 128, x_scales: torch.Tensor | None = None, x_group: int = 0,
-                     stream=None) -> None:
+                     ws: torch.Tensor | None = None, stream=None) -> None:
     """Y = X W^T for the weights W [d_out, d] that Q and scales stand for (optima_w4_pack).
     X [n_tok, d] bfloat16, or int8 with x_scales as optima_rms_norm writes them (x_group is
     its group: the weights' group, or 0); Y [n_tok, d_out] bfloat16 or float32."""
@@ -688,14 +703,15 @@ def optima_w4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y: 
     n_out = Q.shape[0]
     _w4_weights("Q", Q, "scales", scales, n_out, d, group)
     y, ldy, y_dt = _rows("Y", Y, (n, n_out), _F)
+    ws, nbytes = _w4_space(n, d, n_out, 1, ws, X.device, stream)
     _check(_w4_linear(x, ldx, x_dt, _addr(x_scales), int(x_group), n, d, _addr(Q), _addr(scales),
-                      int(group), n_out, y, ldy, y_dt, _launch_stream(stream)))
+                      int(group), n_out, y, ldy, y_dt, ws, nbytes, _launch_stream(stream)))
 
 
 def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Qu: torch.Tensor,
                     scales_u: torch.Tensor, H: torch.Tensor, group: int = 128,
                     act: int = ACT_SILU, x_scales: torch.Tensor | None = None, x_group: int = 0,
-                    stream=None) -> None:
+                    ws: torch.Tensor | None = None, stream=None) -> None:
     """H = act(X Wg^T) * (X Wu^T) with both weights in 4 bits; arguments as in
     optima_w4_linear."""
     n, d, x, ldx, x_dt = _w4_tokens(X, x_scales, x_group, group)
@@ -703,6 +719,7 @@ def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Q
     _w4_weights("Qg", Qg, "scales_g", scales_g, ff, d, group)
     _w4_weights("Qu", Qu, "scales_u", scales_u, ff, d, group)
     h, ldh, h_dt = _rows("H", H, (n, ff), _F)
+    ws, nbytes = _w4_space(n, d, ff, 2, ws, X.device, stream)
     _check(_w4_gated(x, ldx, x_dt, _addr(x_scales), int(x_group), n, d, _addr(Qg), _addr(scales_g),
-                     _addr(Qu), _addr(scales_u), int(group), ff, int(act), h, ldh, h_dt,
-                     _launch_stream(stream)))
+                     _addr(Qu), _addr(scales_u), int(group), ff, int(act), h, ldh, h_dt, ws,
+                     nbytes, _launch_stream(stream)))

@@ -56,7 +56,8 @@ optima_status w4_pack(const void* W, int dtype, int64_t n, int64_t d, int64_t gr
 optima_status w4_linear(const void* X, int64_t ldx, const float* x_scales, int64_t x_group,
                         int64_t n_tok, int64_t d, const void* Q, const void* sc, const void* Q2,
                         const void* sc2, int64_t group, int64_t d_out, int act, void* Y,
-                        int64_t ldy, int y_dtype, hipStream_t s);
+                        int64_t ldy, int y_dtype, void* ws, hipStream_t s);
+size_t w4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out, int mats);
 }  // namespace optima
 
 namespace {
@@ -109,7 +110,8 @@ bool gated_sizes(int64_t n_tok, int64_t d_in, int64_t d_ff) {
 optima_status w4_call(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
                       int64_t x_group, int64_t n_tok, int64_t d, const void* Q, const void* scales,
                       const void* Q2, const void* scales2, int64_t group, int64_t d_out, int act,
-                      void* Y, int64_t ldy, int y_dtype, hipStream_t stream) {
+                      void* Y, int64_t ldy, int y_dtype, void* ws, size_t ws_bytes,
+                      hipStream_t stream) {
   if (x_dtype != OPTIMA_DTYPE_BF16 && x_dtype != OPTIMA_DTYPE_I8) return OPTIMA_E_UNSUPPORTED;
   if (!f32_or_bf16(y_dtype)) return OPTIMA_E_UNSUPPORTED;
   if (n_tok < 0 || n_tok > (int64_t(1) << 21) || d < 1 || d > kMaxDim || d_out < 1 ||
@@ -129,9 +131,11 @@ optima_status w4_call(const void* X, int64_t ldx, int x_dtype, const float* x_sc
     if (!sc.aligned() || y.meets(q) || y.meets(sc)) return OPTIMA_E_INVAL;
   }
   if (y.meets(x) || (i8 && y.meets(xs))) return OPTIMA_E_INVAL;
+  const size_t need = optima::w4_workspace_bytes(n_tok, d, d_out, Q2 ? 2 : 1);
+  if (need && (!ws || !optima::aligned16(ws) || ws_bytes < need)) return OPTIMA_E_WORKSPACE;
   if (n_tok == 0) return OPTIMA_OK;
   return optima::w4_linear(X, ldx, i8 ? x_scales : nullptr, x_group, n_tok, d, Q, scales, Q2,
-                           scales2, group, d_out, act, Y, ldy, y_dtype, stream);
+                           scales2, group, d_out, act, Y, ldy, y_dtype, ws, stream);
 }
 }  // namespace
 
@@ -498,22 +502,30 @@ optima_status optima_w4_pack(const void* W, int dtype, int64_t n, int64_t d, int
   return optima::w4_pack(W, dtype, n, d, group, Q, scales, stream);
 }
 
+size_t optima_w4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out, int n_mats) {
+  if (n_tok < 0 || n_tok > (int64_t(1) << 21) || d < 1 || d > kMaxDim || d_out < 1 ||
+      d_out > kMaxCols || (n_mats != 1 && n_mats != 2))
+    return 0;
+  return optima::w4_workspace_bytes(n_tok, d, d_out, n_mats);
+}
+
 optima_status optima_w4_linear(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
                                int64_t x_group, int64_t n_tok, int64_t d, const void* Q,
                                const void* scales, int64_t group, int64_t d_out, void* Y,
-                               int64_t ldy, int y_dtype, hipStream_t stream) {
+                               int64_t ldy, int y_dtype, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
   return w4_call(X, ldx, x_dtype, x_scales, x_group, n_tok, d, Q, scales, nullptr, nullptr, group,
-                 d_out, OPTIMA_ACT_NONE, Y, ldy, y_dtype, stream);
+                 d_out, OPTIMA_ACT_NONE, Y, ldy, y_dtype, ws, ws_bytes, stream);
 }
 
 optima_status optima_w4_gated(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
                               int64_t x_group, int64_t n_tok, int64_t d, const void* Qg,
                               const void* scales_g, const void* Qu, const void* scales_u,
                               int64_t group, int64_t d_ff, int act, void* H, int64_t ldh,
-                              int h_dtype, hipStream_t stream) {
+                              int h_dtype, void* ws, size_t ws_bytes, hipStream_t stream) {
   if (!Qu || !scales_u || (act != OPTIMA_ACT_NONE && act != OPTIMA_ACT_SILU)) return OPTIMA_E_INVAL;
   return w4_call(X, ldx, x_dtype, x_scales, x_group, n_tok, d, Qg, scales_g, Qu, scales_u, group,
-                 d_ff, act, H, ldh, h_dtype, stream);
+                 d_ff, act, H, ldh, h_dtype, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -17,9 +17,9 @@
 // whose result starts the sum of the group. Sums over a group are fp32 (int8: exact
 // in int32), the sum over groups, each times its scales, is fp32.
 //
-// Bound by the codes' way from HBM, once per call for up to 64 tokens: a workgroup
-// takes 16 rows, its eight waves every eighth chunk of them, and the waves' sums
-// are joined in LDS in their order.
+// Bound by the codes' way from HBM, once per call for up to 64 tokens. Up to 16 tokens
+// a workgroup takes 16 rows, its waves batches of their chunks, and the waves' sums are
+// joined in LDS in their order; more tokens share what is read of them.
 #include <type_traits>
 
 #include "common.h"
@@ -30,7 +30,6 @@ namespace {
 
 constexpr int kChunk = 128;       // codes
 constexpr int kChunkBytes = 64;
-constexpr int kW4Tokens = 64;     // a workgroup's
 
 typedef int i4 __attribute__((ext_vector_type(4)));
 
@@ -75,12 +74,48 @@ struct W4Args {
   const uint8_t* q[2];
   const bf16_t* s[2];
   void* y;
+  f4* part;
   int64_t n_tok, d_out, ldx, ldy;
   int d, chunks, group, groups, x_groups, y_f32, act;
 };
 
 __device__ inline float w4_act(int act, float z) {
   return act == OPTIMA_ACT_SILU ? z / (1.f + expf(-z)) : z;
+}
+
+// Output n of a token from its sum (gated: sums) of products.
+template <bool I8, int MATS>
+__device__ inline void w4_store(const W4Args& a, int64_t tok, int64_t n, float (&v)[MATS]) {
+#pragma unroll
+  for (int m = 0; m < MATS; ++m)
+    if (I8 && a.x_groups == 1) v[m] *= a.xs[tok];
+  const float y = MATS == 2 ? w4_act(a.act, v[0]) * v[MATS - 1] : v[0];
+  const int64_t at = tok * a.ldy + n;
+  if (a.y_f32)
+    static_cast<float*>(a.y)[at] = y;
+  else
+    store1(static_cast<bf16_t*>(a.y) + at, y);
+}
+// The outputs of a wave's two operands from row n0 on: 16 of both matrices, or 32.
+template <bool I8, int MATS, int NT>
+__device__ inline void slab_store(const W4Args& a, const f4 (&sum)[2][NT], int64_t n0, int64_t t0) {
+  const int b = (threadIdx.x & 63) >> 4, i = threadIdx.x & 15;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t tok = t0 + 16 * t + 4 * b + e;
+      if (tok >= a.n_tok) continue;
+#pragma unroll
+      for (int r = 0; r < 2 / MATS; ++r) {
+        const int64_t n = n0 + 16 * r + i;
+        if (n >= a.d_out) continue;
+        float v[MATS];
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) v[m] = sum[MATS == 2 ? m : r][t][e];
+        w4_store<I8, MATS>(a, tok, n, v);
+      }
+    }
 }
 
 // Eight codes as bf16 values code + 24, in the order of their indices.
@@ -166,55 +201,95 @@ __device__ inline void load_scales(float (&v)[N], const float* row, int g, int g
   }
 }
 
-// Chunks that a wave takes at once, their loads together, and waves of a workgroup.
-constexpr int w4_batch(int nt) { return nt == 1 ? 4 : nt == 2 ? 2 : 1; }
-constexpr int w4_waves(int mats, int nt) { return mats * nt == 1 ? 16 : 8; }  // at most
-// Bytes of one token's values of a batch in LDS (NT = 1), with 64 bytes between
-// rows that keep the reads of several tokens off each other's banks.
-constexpr int w4_x_pitch(bool i8) { return 4 * kChunk * (i8 ? 1 : 2) + 64; }
+// The sum of one group's products of 16 tokens with the 16 rows of each of OPS
+// operands. acc's layout: lane (b, i) holds tokens 4 b + e of row i.
+template <bool I8, int OPS, int PER>
+__device__ inline void group_sums(typename std::conditional<I8, i4, f4>::type (&acc)[OPS],
+                                  const XFrag<I8> (&f)[4], const u32x4 (&w)[OPS], int j0) {
+  typename std::conditional<I8, i4, f4>::type base = {};
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    if constexpr (I8) {
+      base = __builtin_amdgcn_mfma_i32_16x16x32_i8(f[j0 + j].v, long(0xF8F8F8F8F8F8F8F8ull), base,
+                                                   0, 0, 0);
+    } else {
+      const bf16x8 k24 = __builtin_bit_cast(
+          bf16x8, u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u});
+      base = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j0 + j].v, k24, base, 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < OPS; ++m) {
+    acc[m] = base;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if constexpr (I8)
+        acc[m] = __builtin_amdgcn_mfma_i32_16x16x32_i8(f[j0 + j].v, codes_i8(w[m][j0 + j]), acc[m],
+                                                       0, 0, 0);
+      else
+        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j0 + j].v, codes_bf16(w[m][j0 + j]),
+                                                         acc[m], 0, 0, 0);
+    }
+  }
+}
 
-// 16 outputs of each of MATS matrices for up to 16 NT tokens; GP groups a chunk.
-// Up to 16 tokens (NT = 1) a wave brings the tokens' values of its batch through
-// LDS: the operand layout would read every value 16 times over, 16 / n_tok times
-// for nothing.
-template <bool I8, int MATS, int NT, int GP>
-__global__ void __launch_bounds__(64 * w4_waves(MATS, NT)) k_w4(W4Args a) {
-  constexpr int kBatch = w4_batch(NT), kPer = 4 / GP, kGroups = kBatch * GP;
-  constexpr bool kStaged = NT == 1;
-  constexpr int kPitch = w4_x_pitch(I8), kEsz = I8 ? 1 : 2;
+// Eight consecutive values of a token as they lie in LDS.
+template <bool I8>
+__device__ inline void put_x(char* p, const XFrag<I8>& f) {
+  *reinterpret_cast<decltype(f.v)*>(p) = f.v;
+}
+template <bool I8>
+__device__ inline void get_x(XFrag<I8>& f, const char* p) {
+  f.v = *reinterpret_cast<const decltype(f.v)*>(p);
+}
+
+constexpr int kBatch = 4;                 // chunks whose loads go out together
+constexpr int kBatchK = kBatch * kChunk;  // 512 values
+
+// ---------------------------------------------------------------------------
+// Up to 16 tokens
+// ---------------------------------------------------------------------------
+
+constexpr int kFew = 16;
+// Waves of a workgroup at most, where a wave loads `rows` tokens at once: four for up to
+// four tokens, which leaves the gated kernels registers for more waves a SIMD (one token,
+// 4096 -> 14336, 16-bit: 23.4 us with eight, 18.4 with four), eight for more (eight
+// tokens: 24.5 and 26.7).
+constexpr int few_waves(int mats, int rows) { return mats == 1 || rows == 4 ? 16 : 8; }
+// Bytes of one token's values of a batch in LDS, with 64 bytes between rows that keep
+// the reads of several tokens off each other's banks.
+constexpr int few_pitch(bool i8) { return kBatchK * (i8 ? 1 : 2) + 64; }
+
+// 16 outputs of each of MATS matrices; GP groups a chunk. A wave takes every waves-th
+// batch and brings the tokens' values of it through LDS: the operand layout would read
+// every value 16 times over, 16 / n_tok times for nothing.
+template <bool I8, int MATS, int GP, int ROWS>
+__global__ void __launch_bounds__(64 * few_waves(MATS, ROWS)) k_w4_few(W4Args a) {
+  constexpr int kPer = 4 / GP, kGroups = kBatch * GP;
+  constexpr int kPitch = few_pitch(I8), kEsz = I8 ? 1 : 2;
   typedef typename std::conditional<I8, i4, f4>::type acc_t;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  float* part = reinterpret_cast<float*>(lds);  // [wave][MATS][NT][4][64], at the end
+  float* part = reinterpret_cast<float*>(lds);  // [wave][MATS][4][64], at the end
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int b = lane >> 4, i = lane & 15;
-  const int64_t n0 = int64_t(blockIdx.x) * 16, t0 = int64_t(blockIdx.y) * kW4Tokens;
+  const int b = lane >> 4, i = lane & 15, tokens = int(a.n_tok);
+  const int64_t n0 = int64_t(blockIdx.x) * 16;
   const int64_t n = std::min(n0 + i, a.d_out - 1);
-  const int tokens = int(std::min<int64_t>(a.n_tok - t0, 16 * NT));
-  const char* x = static_cast<const char*>(a.x) + t0 * a.ldx * kEsz;
-  const char* rows[NT];
-  const float* xs[NT];  // of token 4 b + i % 4
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    rows[t] = x + std::min(16 * t + i, tokens - 1) * a.ldx * kEsz;
-    xs[t] = a.xs + (t0 + std::min(16 * t + 4 * b + (i & 3), tokens - 1)) * a.x_groups;
-  }
+  const char* x = static_cast<const char*>(a.x);
+  const float* xs = a.xs + std::min(4 * b + (i & 3), tokens - 1) * a.x_groups;
   char* mine = lds + wave * tokens * kPitch;
-  f4 sum[MATS][NT];
+  f4 sum[MATS];
 #pragma unroll
-  for (int m = 0; m < MATS; ++m)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) sum[m][t] = f4{0.f, 0.f, 0.f, 0.f};
+  for (int m = 0; m < MATS; ++m) sum[m] = f4{0.f, 0.f, 0.f, 0.f};
   for (int c0 = kBatch * wave; c0 < a.chunks; c0 += kBatch * waves) {
     u32x4 w[kBatch][MATS];
-    uint32_t s[MATS][(kGroups + 1) / 2];
-    float sx[NT][kGroups];
-    // Lane l takes values 8 l .. of a token's batch, eight tokens at a time.
-    XFrag<I8> row[kStaged ? 8 : 1];
+    uint32_t s[MATS][kGroups / 2];
+    float sx[kGroups];
+    // Lane l takes values 8 l .. of a token's batch, ROWS tokens at a time.
+    XFrag<I8> row[ROWS];
     const int xk = c0 * kChunk + 8 * lane;
-    if constexpr (kStaged)
 #pragma unroll
-      for (int r = 0; r < 8; ++r)
-        if (r < tokens) row[r].load(x + r * a.ldx * kEsz, xk, a.d - xk);
+    for (int r = 0; r < ROWS; ++r)
+      if (r < tokens) row[r].load(x + r * a.ldx * kEsz, xk, a.d - xk);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       // Past the last chunk: its codes again, with scales and tokens of zeros.
@@ -225,148 +300,288 @@ __global__ void __launch_bounds__(64 * w4_waves(MATS, NT)) k_w4(W4Args a) {
     }
 #pragma unroll
     for (int m = 0; m < MATS; ++m)
-      load_scales<(kGroups + 1) / 2 * 2>(s[m], a.s[m] + n * a.groups, c0 * GP, a.groups);
-    if constexpr (I8)
+      load_scales<kGroups>(s[m], a.s[m] + n * a.groups, c0 * GP, a.groups);
+    if constexpr (I8) {
+      if (a.x_groups > 1)
+        load_scales<kGroups>(sx, xs, c0 * GP, a.groups);
+      else
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if (a.x_groups > 1)
-          load_scales<kGroups>(sx[t], xs[t], c0 * GP, a.groups);
-        else
-#pragma unroll
-          for (int g = 0; g < kGroups; ++g) sx[t][g] = 1.f;
-      }
-    if constexpr (kStaged) {
-      for (int r0 = 0;; r0 += 8) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (r0 + r < tokens)
-            *reinterpret_cast<decltype(row[r].v)*>(mine + (r0 + r) * kPitch + lane * 8 * kEsz) = row[r].v;
-        if (r0 + 8 >= tokens) break;
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (r0 + 8 + r < tokens) row[r].load(x + (r0 + 8 + r) * a.ldx * kEsz, xk, a.d - xk);
-      }
-      // The wave's own rows: its LDS accesses are served in order.
-      __builtin_amdgcn_wave_barrier();
+        for (int g = 0; g < kGroups; ++g) sx[g] = 1.f;
     }
+    for (int r0 = 0;; r0 += ROWS) {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+        if (r0 + r < tokens) put_x<I8>(mine + (r0 + r) * kPitch + lane * 8 * kEsz, row[r]);
+      if (r0 + ROWS >= tokens) break;
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+        if (r0 + ROWS + r < tokens) row[r].load(x + (r0 + ROWS + r) * a.ldx * kEsz, xk, a.d - xk);
+    }
+    // The wave's own rows: its LDS accesses are served in order.
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      XFrag<I8> f[NT][4];
+      XFrag<I8> f[4];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int j = 0; j < 4; ++j)
+        get_x<I8>(f[j], mine + std::min(i, tokens - 1) * kPitch + (u * kChunk + 32 * j + 8 * b) * kEsz);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (kStaged) {
-            f[t][j].v = *reinterpret_cast<const decltype(f[t][j].v)*>(
-                mine + std::min(i, tokens - 1) * kPitch + (u * kChunk + 32 * j + 8 * b) * kEsz);
-          } else {
-            const int k = (c0 + u) * kChunk + 32 * j + 8 * b;
-            f[t][j].load(rows[t], k, a.d - k);
-          }
+      for (int g = 0; g < GP; ++g) {
+        acc_t acc[MATS];
+        group_sums<I8, MATS, kPer>(acc, f, w[u], g * kPer);
+        const int gi = u * GP + g;
+        float r[4] = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (I8) {
+          r[0] = quad_lane<0>(sx[gi]);
+          r[1] = quad_lane<1>(sx[gi]);
+          r[2] = quad_lane<2>(sx[gi]);
+          r[3] = quad_lane<3>(sx[gi]);
         }
 #pragma unroll
-      for (int g = 0; g < GP; ++g)
+        for (int m = 0; m < MATS; ++m) {
+          const float sc = scale_of(s[m][gi >> 1], gi & 1);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          acc_t acc[MATS], base = {};
-#pragma unroll
-          for (int j = g * kPer; j < (g + 1) * kPer; ++j) {
-            if constexpr (I8) {
-              base = __builtin_amdgcn_mfma_i32_16x16x32_i8(
-                  f[t][j].v, long(0xF8F8F8F8F8F8F8F8ull), base, 0, 0, 0);
-            } else {
-              const bf16x8 k24 = __builtin_bit_cast(
-                  bf16x8, u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u});
-              base = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t][j].v, k24, base, 0, 0, 0);
-            }
-          }
-#pragma unroll
-          for (int m = 0; m < MATS; ++m) {
-            acc[m] = base;
-#pragma unroll
-            for (int j = g * kPer; j < (g + 1) * kPer; ++j) {
-              if constexpr (I8)
-                acc[m] = __builtin_amdgcn_mfma_i32_16x16x32_i8(f[t][j].v, codes_i8(w[u][m][j]),
-                                                               acc[m], 0, 0, 0);
-              else
-                acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    f[t][j].v, codes_bf16(w[u][m][j]), acc[m], 0, 0, 0);
-            }
-          }
-          const int gi = u * GP + g;
-          float sc[MATS];
-#pragma unroll
-          for (int m = 0; m < MATS; ++m) sc[m] = scale_of(s[m][gi >> 1], gi & 1);
-          float r[4] = {1.f, 1.f, 1.f, 1.f};
-          if constexpr (I8) {
-            r[0] = quad_lane<0>(sx[t][gi]);
-            r[1] = quad_lane<1>(sx[t][gi]);
-            r[2] = quad_lane<2>(sx[t][gi]);
-            r[3] = quad_lane<3>(sx[t][gi]);
-          }
-#pragma unroll
-          for (int m = 0; m < MATS; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              sum[m][t][e] += float(acc[m][e]) * (I8 ? sc[m] * r[e] : sc[m]);
+          for (int e = 0; e < 4; ++e) sum[m][e] += float(acc[m][e]) * (I8 ? sc * r[e] : sc);
         }
+      }
     }
-    if constexpr (kStaged) __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_wave_barrier();
   }
-  constexpr int kPart = MATS * NT * 256;
+  constexpr int kPart = MATS * 256;
   __syncthreads();  // the staged values' place
 #pragma unroll
   for (int m = 0; m < MATS; ++m)
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        part[wave * kPart + ((m * NT + t) * 4 + e) * 64 + lane] = sum[m][t][e];
+    for (int e = 0; e < 4; ++e) part[wave * kPart + (m * 4 + e) * 64 + lane] = sum[m][e];
   __syncthreads();
-  for (int o = threadIdx.x; o < 256 * NT; o += blockDim.x) {
-    const int nn = o & 15, m16 = (o >> 4) & 15, t = o >> 8;
-    const int64_t tok = t0 + 16 * t + m16;
-    if (tok >= a.n_tok || n0 + nn >= a.d_out) continue;
+  for (int o = threadIdx.x; o < 256; o += blockDim.x) {
+    const int nn = o & 15, tok = o >> 4;
+    if (tok >= tokens || n0 + nn >= a.d_out) continue;
     float v[MATS];
 #pragma unroll
     for (int m = 0; m < MATS; ++m) {
-      const float* p = part + ((m * NT + t) * 4 + (m16 & 3)) * 64 + (m16 >> 2) * 16 + nn;
+      const float* p = part + (m * 4 + (tok & 3)) * 64 + (tok >> 2) * 16 + nn;
       v[m] = 0.f;
       for (int w = 0; w < waves; ++w) v[m] += p[w * kPart];
-      if (I8 && a.x_groups == 1) v[m] *= a.xs[tok];
     }
-    const float y = MATS == 2 ? w4_act(a.act, v[0]) * v[MATS - 1] : v[0];
-    const int64_t at = tok * a.ldy + n0 + nn;
-    if (a.y_f32)
-      static_cast<float*>(a.y)[at] = y;
-    else
-      store1(static_cast<bf16_t*>(a.y) + at, y);
+    w4_store<I8, MATS>(a, tok, n0 + nn, v);
   }
 }
 
+// ---------------------------------------------------------------------------
+// More tokens, 64 at a time
+// ---------------------------------------------------------------------------
+
+constexpr int kSlabTokens = 64;
+constexpr int kSlabWaves = 8;
+constexpr int kSlabBatch = 2;                    // chunks
+constexpr int kSlabK = kSlabBatch * kChunk;
+constexpr int slab_pitch(bool i8) { return kSlabK * (i8 ? 1 : 2) + 16; }
+constexpr int slab_rows(int mats) { return kSlabWaves * 16 * (2 / mats); }  // a workgroup's
+
+// The tokens' values of a batch go through LDS, two batches in turn, for all waves of the
+// workgroup; a wave takes two operands of 16 rows (of both matrices, or two blocks of
+// one), whose codes it loads a batch ahead. With few rows the chunks are split over
+// blockIdx.y, and k_w4_join adds the parts: 16 rows' own read of the tokens, as above,
+// would bring every token N / 16 times out of the L2.
+// Bound by the MFMAs, of which the offset takes a third, and the LDS reads.
 template <bool I8, int MATS, int NT, int GP>
-void launch_w4(const W4Args& a, hipStream_t s) {
-  // Few enough waves that each has a batch of chunks to load together.
-  const int64_t batches = ceil_div(a.chunks, w4_batch(NT));
-  const size_t stage = NT == 1 ? size_t(std::min<int64_t>(a.n_tok, 16)) * w4_x_pitch(I8) : 0;
-  const size_t each = std::max(stage, size_t(MATS) * NT * 1024);
-  constexpr size_t kLds = 136 << 10;
-  const int most = int(std::min<size_t>(w4_waves(MATS, NT), kLds / each));
-  const int waves = int(std::min<int64_t>(std::max<int64_t>(batches, 1), most));
-  const dim3 grid(unsigned(ceil_div(a.d_out, 16)), unsigned(ceil_div(a.n_tok, kW4Tokens)));
-  hipLaunchKernelGGL((k_w4<I8, MATS, NT, GP>), grid, dim3(64 * waves), waves * each, s, a);
+__global__ void __launch_bounds__(64 * kSlabWaves) k_w4_slab(W4Args a) {
+  constexpr int kPer = 4 / GP, kGroups = kSlabBatch * GP, OPS = 2;
+  constexpr int kPitch = slab_pitch(I8), kEsz = I8 ? 1 : 2, kTok = 16 * NT;
+  typedef typename std::conditional<I8, i4, f4>::type acc_t;
+  __shared__ __attribute__((aligned(16))) char xl[2][kTok * kPitch];
+  __shared__ __attribute__((aligned(16))) float xsl[2][I8 ? kGroups * kTok : 1];  // [group][token]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int b = lane >> 4, i = lane & 15;
+  const int64_t t0 = int64_t(blockIdx.z) * kSlabTokens;
+  const int tokens = int(std::min<int64_t>(a.n_tok - t0, kTok));
+  const char* x = static_cast<const char*>(a.x) + t0 * a.ldx * kEsz;
+  const float* xs = a.xs + t0 * a.x_groups;
+  int64_t n[OPS];
+#pragma unroll
+  for (int m = 0; m < OPS; ++m)
+    n[m] = std::min(int64_t(blockIdx.x) * slab_rows(MATS) + wave * 16 * (2 / MATS) +
+                        (MATS == 1 ? 16 * m : 0) + i, a.d_out - 1);
+  const int batches = (a.chunks + kSlabBatch - 1) / kSlabBatch;
+  const int b0 = int(int64_t(batches) * blockIdx.y / gridDim.y);
+  const int b1 = int(int64_t(batches) * (blockIdx.y + 1) / gridDim.y);
+
+  // This thread's share of a batch's tokens: values 8 (thread % 32) .. of every 16th.
+  const int xt = threadIdx.x >> 5, xk = 8 * (threadIdx.x & 31);
+  XFrag<I8> row[NT];
+  float rs[I8 ? (kGroups * kTok + 511) / 512 : 1];
+  auto fetch_x = [&](int batch) {
+    const int k = batch * kSlabK + xk;
+#pragma unroll
+    for (int r = 0; r < NT; ++r)
+      row[r].load(x + std::min(xt + 16 * r, tokens - 1) * a.ldx * kEsz, k, a.d - k);
+    if constexpr (I8)
+      if (a.x_groups > 1)
+#pragma unroll
+        for (int v = 0; v < int(sizeof(rs) / 4); ++v) {
+          const int at = threadIdx.x + 512 * v, g = batch * kGroups + at / kTok;
+          rs[v] = g < a.groups && at < kGroups * kTok
+                      ? xs[std::min(at % kTok, tokens - 1) * a.x_groups + g] : 0.f;
+        }
+  };
+  auto put_batch = [&](int to) {
+#pragma unroll
+    for (int r = 0; r < NT; ++r) put_x<I8>(xl[to] + (xt + 16 * r) * kPitch + xk * kEsz, row[r]);
+    if constexpr (I8)
+      if (a.x_groups > 1)
+#pragma unroll
+        for (int v = 0; v < int(sizeof(rs) / 4); ++v) {
+          const int at = threadIdx.x + 512 * v;
+          if (at < kGroups * kTok) xsl[to][at] = rs[v];
+        }
+  };
+  u32x4 w[kSlabBatch][OPS];
+  uint32_t s[OPS][(kGroups / 2)];
+  auto fetch_w = [&](int batch) {
+#pragma unroll
+    for (int u = 0; u < kSlabBatch; ++u) {
+      const int c = std::min(batch * kSlabBatch + u, a.chunks - 1);
+#pragma unroll
+      for (int m = 0; m < OPS; ++m)
+        w[u][m] = *reinterpret_cast<const u32x4*>(a.q[m % MATS] + (n[m] * a.chunks + c) * kChunkBytes +
+                                                  b * 16);
+    }
+#pragma unroll
+    for (int m = 0; m < OPS; ++m)
+      load_scales<kGroups>(s[m], a.s[m % MATS] + n[m] * a.groups, batch * kGroups, a.groups);
+  };
+
+  f4 sum[OPS][NT];
+#pragma unroll
+  for (int m = 0; m < OPS; ++m)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum[m][t] = f4{0.f, 0.f, 0.f, 0.f};
+  if (b0 < b1) {
+    fetch_x(b0);
+    fetch_w(b0);
+    put_batch(0);
+  }
+  __syncthreads();
+  for (int batch = b0; batch < b1; ++batch) {
+    const int cur = (batch - b0) & 1;
+    u32x4 wc[kSlabBatch][OPS];
+    uint32_t sc[OPS][(kGroups / 2)];
+#pragma unroll
+    for (int u = 0; u < kSlabBatch; ++u)
+#pragma unroll
+      for (int m = 0; m < OPS; ++m) wc[u][m] = w[u][m];
+#pragma unroll
+    for (int m = 0; m < OPS; ++m)
+#pragma unroll
+      for (int g = 0; g < (kGroups / 2); ++g) sc[m][g] = s[m][g];
+    if (batch + 1 < b1) {
+      fetch_x(batch + 1);
+      fetch_w(batch + 1);
+    }
+#pragma unroll
+    for (int u = 0; u < kSlabBatch; ++u)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        XFrag<I8> f[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          get_x<I8>(f[j], xl[cur] + (16 * t + i) * kPitch + (u * kChunk + 32 * j + 8 * b) * kEsz);
+#pragma unroll
+        for (int g = 0; g < GP; ++g) {
+          acc_t acc[OPS];
+          group_sums<I8, OPS, kPer>(acc, f, wc[u], g * kPer);
+          const int gi = u * GP + g;
+          f4 r = {1.f, 1.f, 1.f, 1.f};
+          if constexpr (I8)
+            if (a.x_groups > 1) r = *reinterpret_cast<const f4*>(&xsl[cur][gi * kTok + 16 * t + 4 * b]);
+#pragma unroll
+          for (int m = 0; m < OPS; ++m) {
+            const float q = scale_of(sc[m][gi >> 1], gi & 1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[m][t][e] += float(acc[m][e]) * (I8 ? q * r[e] : q);
+          }
+        }
+        // Looking further ahead than this the compiler runs out of registers.
+#pragma unroll
+        for (int m = 0; m < OPS; ++m) asm volatile("" : "+v"(sum[m][t]));
+      }
+    if (batch + 1 < b1) put_batch(cur ^ 1);
+    __syncthreads();
+  }
+  if (gridDim.y > 1) {  // [split][workgroup][wave][operand][token block][lane]
+    f4* part = a.part + ((size_t(blockIdx.y) * gridDim.x + blockIdx.x) * kSlabWaves + wave) * OPS * NT * 64;
+#pragma unroll
+    for (int m = 0; m < OPS; ++m)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) part[(m * NT + t) * 64 + lane] = sum[m][t];
+    return;
+  }
+  slab_store<I8, MATS, NT>(a, sum, int64_t(blockIdx.x) * slab_rows(MATS) + wave * 16 * (2 / MATS), t0);
 }
+
+// The parts of the outputs, added in their order: one of the slab kernel's waves' outputs
+// for 16 tokens a wave.
 template <bool I8, int MATS, int NT>
+__global__ void __launch_bounds__(kThreads) k_w4_join(W4Args a, int splits, int waves) {
+  const int lane = threadIdx.x & 63, at = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int wave = at / NT, t = at - wave * NT;
+  if (wave >= waves) return;
+  const f4* part = a.part + (size_t(wave) * 2 * NT + t) * 64 + lane;
+  const size_t step = size_t(waves) * 2 * NT * 64;
+  f4 sum[2][1] = {{{0.f, 0.f, 0.f, 0.f}}, {{0.f, 0.f, 0.f, 0.f}}};
+#pragma unroll 8
+  for (int sp = 0; sp < splits; ++sp)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) sum[m][0] += part[sp * step + m * NT * 64];
+  slab_store<I8, MATS, 1>(a, sum, int64_t(wave) * 16 * (2 / MATS), 16 * t);
+}
+
+// Ranges that the chunks of a product of more than kFew tokens are split into: as many
+// as give every CU a workgroup, for one tile of tokens. Beyond eight they have two
+// batches at least: 4096 -> 4096, 64 tokens, 17.7 us in 8 ranges, 20.5 in 16.
+int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out, int mats) {
+  if (n_tok > kSlabTokens) return 1;
+  const int64_t wgs = ceil_div(d_out, slab_rows(mats));
+  const int64_t batches = ceil_div(d, kSlabK);
+  return std::max<int64_t>(1, std::min(256 / wgs, std::max(batches / 2, std::min<int64_t>(batches, 8))));
+}
+
+template <bool I8, int MATS, int NT, int GP>
+void launch_slab(const W4Args& a, hipStream_t s) {
+  const unsigned wgs = unsigned(ceil_div(a.d_out, slab_rows(MATS)));
+  const int splits = int(slab_splits(a.n_tok, a.d, a.d_out, MATS));
+  hipLaunchKernelGGL((k_w4_slab<I8, MATS, NT, GP>),
+                     dim3(wgs, unsigned(splits), unsigned(ceil_div(a.n_tok, kSlabTokens))),
+                     dim3(64 * kSlabWaves), 0, s, a);
+  if (splits > 1)
+    hipLaunchKernelGGL((k_w4_join<I8, MATS, NT>), dim3(wgs * kSlabWaves * NT / (kThreads / 64)),
+                       dim3(kThreads), 0, s, a, splits, int(wgs) * kSlabWaves);
+}
+
+template <bool I8, int MATS, int GP, int ROWS>
+void launch_few(const W4Args& a, hipStream_t s) {
+  // Few enough waves that each has a batch of chunks to load together.
+  const size_t each = std::max(size_t(a.n_tok) * few_pitch(I8), size_t(MATS) * 1024);
+  constexpr size_t kLds = 136 << 10;
+  const int most = int(std::min<size_t>(few_waves(MATS, ROWS), kLds / each));
+  const int waves = int(std::min<int64_t>(ceil_div(a.chunks, kBatch), most));
+  hipLaunchKernelGGL((k_w4_few<I8, MATS, GP, ROWS>), dim3(unsigned(ceil_div(a.d_out, 16))),
+                     dim3(64 * waves), waves * each, s, a);
+}
+
+template <bool I8, int MATS, int GP>
 void launch_w4(const W4Args& a, hipStream_t s) {
-  if (a.group == 32) launch_w4<I8, MATS, NT, 4>(a, s);
-  else if (a.group == 64) launch_w4<I8, MATS, NT, 2>(a, s);
-  else launch_w4<I8, MATS, NT, 1>(a, s);
+  if (a.n_tok > 32) launch_slab<I8, MATS, 4, GP>(a, s);
+  else if (a.n_tok > kFew) launch_slab<I8, MATS, 2, GP>(a, s);
+  else if (a.n_tok > 4) launch_few<I8, MATS, GP, 8>(a, s);
+  else launch_few<I8, MATS, GP, 4>(a, s);
 }
 template <bool I8, int MATS>
 void launch_w4(const W4Args& a, hipStream_t s) {
-  if (a.n_tok <= 16) launch_w4<I8, MATS, 1>(a, s);
-  else if (a.n_tok <= 32) launch_w4<I8, MATS, 2>(a, s);
-  else launch_w4<I8, MATS, 4>(a, s);
+  if (a.group == 32) launch_w4<I8, MATS, 4>(a, s);
+  else if (a.group == 64) launch_w4<I8, MATS, 2>(a, s);
+  else launch_w4<I8, MATS, 1>(a, s);
 }
 
 }  // namespace
@@ -388,12 +603,23 @@ optima_status w4_pack(const void* W, int dtype, int64_t n, int64_t d, int64_t gr
   return OPTIMA_OK;
 }
 
+size_t w4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out, int mats) {
+  if (n_tok <= kFew) return 0;
+  n_tok = std::min<int64_t>(n_tok, kSlabTokens);  // more are not split
+  const int64_t splits = slab_splits(n_tok, d, d_out, mats);
+  if (splits == 1) return 0;
+  // Sized for 64 tokens, so that it does not shrink with more.
+  return size_t(splits) * size_t(ceil_div(d_out, slab_rows(mats))) * kSlabWaves * 2 * 4 * 64 *
+         sizeof(f4);
+}
+
 // With Q2 and s2, act(X deq(Q)^T) o (X deq(Q2)^T).
 optima_status w4_linear(const void* X, int64_t ldx, const float* x_scales, int64_t x_group,
                         int64_t n_tok, int64_t d, const void* Q, const void* sc, const void* Q2,
                         const void* sc2, int64_t group, int64_t d_out, int act, void* Y,
-                        int64_t ldy, int y_dtype, hipStream_t s) {
+                        int64_t ldy, int y_dtype, void* ws, hipStream_t s) {
   W4Args a{};
+  a.part = static_cast<f4*>(ws);
   a.x = X;
   a.xs = x_scales;
   a.q[0] = static_cast<const uint8_t*>(Q);

@@ -160,16 +160,17 @@ def test_pack_refusals(lib, change, status):
 
 def _w4(lib, gated, **kw):
     a = dict(X=1 * MB, ldx=100, xdt=BF16, xs=None, xg=0, n=4, d=100, Q=2 * MB, sc=3 * MB, Q2=4 * MB,
-             sc2=5 * MB, group=64, n_out=10, act=1, Y=6 * MB, ldy=10, ydt=BF16)
+             sc2=5 * MB, group=64, n_out=10, act=1, Y=6 * MB, ldy=10, ydt=BF16, ws=None, bytes=0)
     a.update(kw)
     if gated:
         f = lib.optima_w4_gated
-        f.argtypes = [vp, i64, i32, vp, i64, i64, i64, vp, vp, vp, vp, i64, i64, i32, vp, i64, i32, vp]
+        f.argtypes = [vp, i64, i32, vp, i64, i64, i64, vp, vp, vp, vp, i64, i64, i32, vp, i64, i32,
+                      vp, sz, vp]
         return f(*a.values(), None)
     for k in ("Q2", "sc2", "act"):
         del a[k]
     f = lib.optima_w4_linear
-    f.argtypes = [vp, i64, i32, vp, i64, i64, i64, vp, vp, i64, i64, vp, i64, i32, vp]
+    f.argtypes = [vp, i64, i32, vp, i64, i64, i64, vp, vp, i64, i64, vp, i64, i32, vp, sz, vp]
     return f(*a.values(), None)
 
 
@@ -192,6 +193,20 @@ def test_w4_gated_refusals(lib):
     assert _w4(lib, True, act=9) == INVAL
     assert _w4(lib, True, Y=4 * MB) == INVAL
     assert _w4(lib, True, Q2=4 * MB + 8) == INVAL
+
+
+@pytest.mark.parametrize("mats", [1, 2])
+def test_w4_workspace(lib, mats):
+    import paper_2512_13886_amd as L
+    q = L.optima_w4_workspace_bytes
+    assert q(16, 4096, 4096, mats) == 0
+    need = [q(n, 4096, 4096, mats) for n in range(200)]
+    assert need[17] >= 2 * 4096 * 17 * 4 and all(a <= b for a, b in zip(need, need[1:]))
+    assert q(17, 4096, 4096, 3) == 0 and q(-1, 4096, 4096, mats) == 0
+    big = dict(n=20, d=4096, ldx=4096, n_out=512, ldy=512, X=16 * MB, Y=32 * MB)
+    assert _w4(lib, mats == 2, **big) == WORKSPACE
+    assert _w4(lib, mats == 2, **big, ws=64 * MB, bytes=1024) == WORKSPACE
+    assert _w4(lib, mats == 2, **big, ws=64 * MB + 8, bytes=64 * MB) == WORKSPACE
 
 
 def test_row_bytes():
