@@ -427,8 +427,7 @@ __global__ void __launch_bounds__(kThreads) k_gated_prep(ForwardPrep a) {
 // 114 for the transposed weights without; dW 767 us with TB, 670 and 14 for X^T without,
 // and 840 us with both operands read through LDS that way (46 us less to write before).
 // Both run in one launch, the longer sums first, so that the tiles of one fill the CUs
-// that the other leaves. A long sum over few tiles is split, and joined by
-// k_grad_join.
+// that the other leaves. Long sums over few tiles are split, and joined by k_grad_join.
 // ---------------------------------------------------------------------------
 
 // Rows of the product below `part` go to y[0], those from `split` to split + part to
@@ -533,20 +532,51 @@ __device__ inline const char* grad_b(const GradArgs& a, int64_t c0, int i) {
 }
 
 struct GradPair {
-  GradArgs x, w;         // dX, dW; of a product that is not wanted, no tiles
-  int64_t x_blocks;      // of dX: tiles, times `splits` ranges of its sum
-  int splits;
-  float* part;           // [split][tile][128][128] where there are several
+  GradArgs a[2];         // dX, dW; of a product that is not wanted, no tiles
+  int first;             // the product whose blocks come first, ..
+  int64_t first_blocks;  // .. and how many: tiles, times the ranges of its sum
+  int splits[2];
+  float* part[2];        // [split][tile][side][side] where there are several
 };
 
 #define GRAD_LDS(name, bytes) __shared__ __attribute__((aligned(1024))) char name[bytes]
 
+// What a block does: a product, its tile and stages [s0, s1) of the sum; to `part` where
+// that is not NULL.
+struct GradBlock {
+  int which, tile, s0, s1;
+  float* part;
+};
+__device__ inline GradBlock grad_block(const GradPair& p, int side) {
+  GradBlock g;
+  const bool head = blockIdx.x < p.first_blocks;
+  g.which = head ? p.first : 1 - p.first;
+  const int b = head ? int(blockIdx.x) : int(blockIdx.x - p.first_blocks);
+  const GradArgs& a = p.a[g.which];
+  const int tiles = cdiv(a.rows, side) * cdiv(a.out.cols, side), splits = p.splits[g.which];
+  const int sp = b / tiles;
+  g.tile = b - sp * tiles;
+  g.s0 = int(a.stages * sp / splits);
+  g.s1 = int(a.stages * (sp + 1) / splits);
+  g.part = splits > 1 ? p.part[g.which] + size_t(b) * side * side : nullptr;
+  return g;
+}
+
+// The two blocks of a wave's 32 columns of one row of a tile's partial sums.
 template <bool TB>
-__device__ inline void grad256_tile(const GradArgs& a, int block, char* l0, char* l1, char* l2,
-                                    char* l3, char* l4, char* l5, char* l6, char* l7) {
+__device__ inline void grad_part_blocks(float* row, const f4 (&c)[2]) {
+  const int q = (threadIdx.x >> 4) & 3;
+#pragma unroll
+  for (int ni = 0; ni < 2; ++ni)
+    *reinterpret_cast<f4*>(row + (TB ? 16 * ni + 4 * q : 8 * q + 4 * ni)) = c[ni];
+}
+
+template <bool TB>
+__device__ inline void grad256_tile(const GradArgs& a, const GradBlock& g, char* l0, char* l1,
+                                    char* l2, char* l3, char* l4, char* l5, char* l6, char* l7) {
   const int tiles_m = cdiv(a.rows, 256), tiles_n = cdiv(a.out.cols, 256);
   int tm, tn;
-  tile_of_block(block, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  tile_of_block(g.tile, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 256;
   Operands256 src;
 #pragma unroll
@@ -557,17 +587,21 @@ __device__ inline void grad256_tile(const GradArgs& a, int block, char* l0, char
       src.b[h][i] = grad_b<TB>(a, n0 + 128 * h, i);
     }
   Acc256 acc;
-  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), 0};
-  gemm256_mainloop<Bf16Rows<TB>>(acc, src, int(a.stages), l0, l1, l2, l3, l4, l5, l6, l7, [] {},
-                                 steps);
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), g.s0};
+  gemm256_mainloop<Bf16Rows<TB>>(acc, src, g.s1 - g.s0, l0, l1, l2, l3, l4, l5, l6, l7, [] {}, steps);
+  const int wn = (threadIdx.x >> 6) & 3;
 #pragma unroll
   for (int qa = 0; qa < 2; ++qa)
 #pragma unroll
     for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
-      for (int qb = 0; qb < 2; ++qb)
-        grad_store_blocks<TB>(a.out, m0 + t256_rows_row(qa, mi),
-                              n0 + 128 * qb + 32 * ((threadIdx.x >> 6) & 3), acc.q[qa][qb][mi]);
+      for (int qb = 0; qb < 2; ++qb) {
+        const int row = t256_rows_row(qa, mi), col = 128 * qb + 32 * wn;
+        if (g.part)
+          grad_part_blocks<TB>(g.part + row * 256 + col, acc.q[qa][qb][mi]);
+        else
+          grad_store_blocks<TB>(a.out, m0 + row, n0 + col, acc.q[qa][qb][mi]);
+      }
 }
 
 __global__ void __launch_bounds__(Tile256::kThreads) k_grad256(GradPair p) {
@@ -579,19 +613,19 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_grad256(GradPair p) {
   GRAD_LDS(l5, Tile256::kHalfBytes);
   GRAD_LDS(l6, Tile256::kHalfBytes);
   GRAD_LDS(l7, Tile256::kHalfBytes);
-  if (blockIdx.x < p.x_blocks)
-    grad256_tile<true>(p.x, blockIdx.x, l0, l1, l2, l3, l4, l5, l6, l7);
+  const GradBlock g = grad_block(p, 256);
+  if (g.which == 0)
+    grad256_tile<true>(p.a[0], g, l0, l1, l2, l3, l4, l5, l6, l7);
   else
-    grad256_tile<false>(p.w, blockIdx.x - int(p.x_blocks), l0, l1, l2, l3, l4, l5, l6, l7);
+    grad256_tile<false>(p.a[1], g, l0, l1, l2, l3, l4, l5, l6, l7);
 }
 
-// Stages [s0, s1) of the sum of a 128 x 128 tile; to `part` where that is not NULL.
 template <bool TB>
-__device__ inline void grad_ring_tile(const GradArgs& a, int tile, int s0, int s1, float* part,
-                                      char* b0, char* b1, char* b2, char* b3) {
+__device__ inline void grad_ring_tile(const GradArgs& a, const GradBlock& g, char* b0, char* b1,
+                                      char* b2, char* b3) {
   const int tiles_m = cdiv(a.rows, 128), tiles_n = cdiv(a.out.cols, 128);
   int tm, tn;
-  tile_of_block(tile, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  tile_of_block(g.tile, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = int64_t(tm) * 128, n0 = int64_t(tn) * 128;
   OperandsR128 src;
 #pragma unroll
@@ -600,21 +634,17 @@ __device__ inline void grad_ring_tile(const GradArgs& a, int tile, int s0, int s
     src.b[i] = grad_b<TB>(a, n0, i);
   }
   AccR128<false> acc;
-  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), s0};
-  r128_mainloop<Bf16Rows<TB>>(acc, src, SumShape{0, 0, 0}, s1 - s0, b0, b1, b2, b3, [] {}, steps);
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), g.s0};
+  r128_mainloop<Bf16Rows<TB>>(acc, src, SumShape{0, 0, 0}, g.s1 - g.s0, b0, b1, b2, b3, [] {}, steps);
   const int wn = (threadIdx.x >> 6) & 3;
-  if (part) {
-    float* q = part + 32 * wn + 4 * ((threadIdx.x >> 4) & 3);
 #pragma unroll
-    for (int mi = 0; mi < 4; ++mi)
-#pragma unroll
-      for (int ni = 0; ni < 2; ++ni)
-        *reinterpret_cast<f4*>(q + t256_rows_row(0, mi) * 128 + 16 * ni) = acc.q[mi][ni];
-    return;
+  for (int mi = 0; mi < 4; ++mi) {
+    const int row = t256_rows_row(0, mi), col = 32 * wn;
+    if (g.part)
+      grad_part_blocks<TB>(g.part + row * 128 + col, acc.q[mi]);
+    else
+      grad_store_blocks<TB>(a.out, m0 + row, n0 + col, acc.q[mi]);
   }
-#pragma unroll
-  for (int mi = 0; mi < 4; ++mi)
-    grad_store_blocks<TB>(a.out, m0 + t256_rows_row(0, mi), n0 + 32 * wn, acc.q[mi]);
 }
 
 __global__ void __launch_bounds__(Ring128::kThreads) k_grad_ring(GradPair p) {
@@ -622,35 +652,33 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_grad_ring(GradPair p) {
   GRAD_LDS(b1, Ring128::kBufBytes);
   GRAD_LDS(b2, Ring128::kBufBytes);
   GRAD_LDS(b3, Ring128::kBufBytes);
-  if (blockIdx.x < p.x_blocks) {
-    const int tiles = int(p.x_blocks) / p.splits, sp = blockIdx.x / tiles;
-    const int s0 = int(p.x.stages * sp / p.splits), s1 = int(p.x.stages * (sp + 1) / p.splits);
-    grad_ring_tile<true>(p.x, blockIdx.x - sp * tiles, s0, s1,
-                         p.splits > 1 ? p.part + size_t(blockIdx.x) * 16384 : nullptr, b0, b1, b2,
-                         b3);
-  } else {
-    grad_ring_tile<false>(p.w, blockIdx.x - int(p.x_blocks), 0, int(p.w.stages), nullptr, b0, b1,
-                          b2, b3);
-  }
+  const GradBlock g = grad_block(p, 128);
+  if (g.which == 0)
+    grad_ring_tile<true>(p.a[0], g, b0, b1, b2, b3);
+  else
+    grad_ring_tile<false>(p.a[1], g, b0, b1, b2, b3);
 }
 #undef GRAD_LDS
 
-// dX from the ranges' partial sums, in their order: four values a thread, a sixteenth
-// of a tile a workgroup.
-__global__ void __launch_bounds__(kThreads) k_grad_join(GradPair p) {
-  const int tiles_m = cdiv(p.x.rows, 128), tiles_n = cdiv(p.x.out.cols, 128);
-  const int tiles = tiles_m * tiles_n, tile = blockIdx.x >> 4;
+// The outputs of split sums from the ranges' parts, in their order: four values a
+// thread, 1024 of a tile a workgroup. blocks0 of them are dX's.
+__global__ void __launch_bounds__(kThreads) k_grad_join(GradPair p, int side, int64_t blocks0) {
+  const int which = blockIdx.x >= blocks0, per = side * side / 1024;
+  const GradArgs& a = p.a[which];
+  const int64_t b = which ? blockIdx.x - blocks0 : blockIdx.x;
+  const int tiles_m = cdiv(a.rows, side), tiles_n = cdiv(a.out.cols, side);
+  const int tiles = tiles_m * tiles_n, tile = int(b / per);
   int tm, tn;
   tile_of_block(tile, tiles, tiles_m, tiles_n, &tm, &tn);
-  const int at = (blockIdx.x & 15) * 1024 + 4 * threadIdx.x;
-  const int64_t row = int64_t(tm) * 128 + (at >> 7), col = int64_t(tn) * 128 + (at & 127);
-  if (row >= p.x.rows) return;
+  const int at = int(b % per) * 1024 + 4 * threadIdx.x;
+  const int64_t row = int64_t(tm) * side + at / side, col = int64_t(tn) * side + at % side;
+  if (row >= a.rows) return;
   f4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int sp = 0; sp < p.splits; ++sp)
-    sum += *reinterpret_cast<const f4*>(p.part + (size_t(sp) * tiles + tile) * 16384 + at);
+#pragma unroll 8
+  for (int sp = 0; sp < p.splits[which]; ++sp)
+    sum += *reinterpret_cast<const f4*>(p.part[which] + (size_t(sp) * tiles + tile) * side * side + at);
   float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-  grad_store<4>(p.x.out, row, col, v);
+  grad_store<4>(a.out, row, col, v);
 }
 
 // A round of 256 x 256 tiles over the CUs against one of 128 x 128 tiles, a
@@ -659,42 +687,78 @@ bool wide_tiles(int64_t wide, int64_t small) {
   return 5 * ceil_div(wide, kCus) <= 2 * ceil_div(small, kCus);
 }
 
-// Partial sums of at most kPartTiles tiles.
+// Partial sums of at most kPartTiles 128 x 128 tiles.
 constexpr int64_t kPartTiles = 512;
 
-// The tiles of both products over the CUs, by the time the plan should take: a stage
-// takes 1.4 us of a 256 x 256 tile and 0.56 of a 128 x 128 one, of which dX may be
-// split so that it takes no longer than the rest (5 us for the join).
-optima_status grad_products(GradPair& p, hipStream_t s) {
-  const int64_t xs = p.x.stages, wst = p.w.stages;
-  auto tiles = [](const GradArgs& a, int64_t side) {
-    return ceil_div(a.rows, side) * ceil_div(a.out.cols, side);
-  };
-  const int64_t x256 = tiles(p.x, 256), w256 = tiles(p.w, 256);
-  const int64_t x128 = tiles(p.x, 128), w128 = tiles(p.w, 128);
-  const int64_t even256 = ceil_div(x256 * xs + w256 * wst, kCus);
-  const int64_t even128 = ceil_div(x128 * xs + w128 * wst, kCus);
-  const int64_t wide = 140 * std::max({even256, x256 ? xs : 0, w256 ? wst : 0});
-  int64_t splits = 1;
-  if (x128 && xs > even128)
-    splits = std::min({ceil_div(xs, std::max<int64_t>(even128, 8)), kPartTiles / x128, xs});
-  splits = std::max<int64_t>(splits, 1);
-  const int64_t small = 56 * std::max({even128, x128 ? ceil_div(xs, splits) : 0, w128 ? wst : 0}) +
-                        (splits > 1 ? 500 : 0);
-  if (wide <= small) {
-    p.x_blocks = x256;
-    p.splits = 1;
-    hipLaunchKernelGGL(k_grad256, dim3(unsigned(x256 + w256)), dim3(Tile256::kThreads), 0, s, p);
-    OPTIMA_LAUNCH_CHECK();
-    return OPTIMA_OK;
+// Microseconds that n[0] blocks of c[0] and then n[1] of c[1] each take over the CUs,
+// the longer ones first.
+double grad_makespan(const int64_t (&n)[2], const double (&c)[2], int first) {
+  const int64_t n1 = n[first], n2 = n[1 - first];
+  const double c1 = c[first], c2 = c[1 - first];
+  const int64_t q = n1 / kCus, r = n1 % kCus;
+  if (r == 0) return double(q) * c1 + double(ceil_div(n2, kCus)) * c2;
+  const int64_t light = kCus - r, room = light * int64_t(c1 / c2);
+  if (n2 <= room)
+    return std::max(double(q + 1) * c1, double(q) * c1 + double(ceil_div(n2, light)) * c2);
+  return double(q + 1) * c1 + double(ceil_div(n2 - room, kCus)) * c2;
+}
+
+// The tiles of both products over the CUs, and how often their sums are split, by the
+// time the plan should take: 1.4 us a stage and 6 around them for a 256 x 256 tile, 0.56
+// and 3.5 for a 128 x 128 one, 3 us and 5 TB/s for the join.
+struct GradPlan {
+  int side, splits[2], first;
+};
+GradPlan plan_grad(const GradArgs (&a)[2]) {
+  GradPlan best{256, {1, 1}, 0};
+  double best_us = 1e30;
+  for (const int side : {256, 128}) {
+    const double stage = side == 256 ? 1.4 : 0.56, around = side == 256 ? 6 : 3.5;
+    const int64_t most = kPartTiles * 16384 / (side * side);
+    int64_t tiles[2];
+    for (int k = 0; k < 2; ++k) tiles[k] = ceil_div(a[k].rows, side) * ceil_div(a[k].out.cols, side);
+    for (const int sx : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32})
+      for (const int sw : {1, 2, 3, 4}) {
+        const int64_t parts = (sx > 1 ? sx * tiles[0] : 0) + (sw > 1 ? sw * tiles[1] : 0);
+        if (parts > most || (sx > 1 && sx > a[0].stages) || (sw > 1 && sw > a[1].stages)) continue;
+        const int64_t n[2] = {tiles[0] * sx, tiles[1] * sw};
+        const double c[2] = {stage * double(ceil_div(a[0].stages, sx)) + around,
+                             stage * double(ceil_div(a[1].stages, sw)) + around};
+        const int first = c[0] >= c[1] ? 0 : 1;
+        const double join = parts ? 3 + double(parts) * side * side * 8 / 5e6 : 0;
+        const double us = grad_makespan(n, c, first) + join;
+        if (us < best_us) {
+          best_us = us;
+          best = GradPlan{side, {sx, sw}, first};
+        }
+      }
   }
-  p.splits = int(splits);
-  p.x_blocks = x128 * splits;
-  hipLaunchKernelGGL(k_grad_ring, dim3(unsigned(p.x_blocks + w128)), dim3(Ring128::kThreads), 0, s,
-                     p);
+  return best;
+}
+
+optima_status grad_products(GradPair& p, float* part, hipStream_t s) {
+  const GradPlan plan = plan_grad(p.a);
+  const int64_t area = int64_t(plan.side) * plan.side;
+  int64_t tiles[2], joined[2];
+  for (int k = 0; k < 2; ++k) {
+    tiles[k] = ceil_div(p.a[k].rows, plan.side) * ceil_div(p.a[k].out.cols, plan.side);
+    p.splits[k] = plan.splits[k];
+    p.part[k] = part;
+    const bool split = plan.splits[k] > 1;
+    if (split) part += tiles[k] * plan.splits[k] * area;
+    joined[k] = split ? tiles[k] * (area / 1024) : 0;
+  }
+  p.first = plan.first;
+  p.first_blocks = tiles[p.first] * p.splits[p.first];
+  const dim3 grid(unsigned(tiles[0] * p.splits[0] + tiles[1] * p.splits[1]));
+  if (plan.side == 256)
+    hipLaunchKernelGGL(k_grad256, grid, dim3(Tile256::kThreads), 0, s, p);
+  else
+    hipLaunchKernelGGL(k_grad_ring, grid, dim3(Ring128::kThreads), 0, s, p);
   OPTIMA_LAUNCH_CHECK();
-  if (splits > 1) {
-    hipLaunchKernelGGL(k_grad_join, dim3(unsigned(16 * x128)), dim3(kThreads), 0, s, p);
+  if (joined[0] + joined[1]) {
+    hipLaunchKernelGGL(k_grad_join, dim3(unsigned(joined[0] + joined[1])), dim3(kThreads), 0, s, p,
+                       plan.side, joined[0]);
     OPTIMA_LAUNCH_CHECK();
   }
   return OPTIMA_OK;
@@ -754,9 +818,11 @@ GradLayout carve_grad(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* by
     l.wg = c.take<bf16_t>(ffp * dp);
     l.wu = c.take<bf16_t>(ffp * dp);
   }
-  // At most a range for every stage of dX's sum.
-  const int64_t x_tiles = ceil_div(n_tok, 128) * ceil_div(d, 128);
-  l.part = c.take<float>(16384 * size_t(std::min(kPartTiles, x_tiles * int64_t(2 * ffp / 64))));
+  // Split sums: no more parts than stages, of tiles of up to 256 x 256.
+  const int64_t cols = 4 * ceil_div(d, 256);
+  const int64_t parts = cols * (ceil_div(n_tok, 256) * int64_t(2 * ffp / 64) +
+                                ceil_div(2 * ff, 256) * int64_t(tp / 64));
+  l.part = c.take<float>(16384 * size_t(std::min(kPartTiles, parts)));
   if (bytes) *bytes = c.bytes();
   return l;
 }
@@ -839,7 +905,6 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
   const int64_t ffp = round_up(ff, 64), tp = round_up(n_tok, 64), dp = round_up(d, 8);
   GradPrep prep{};
   GradPair pair{};
-  pair.part = l.part;
   const void *wg = Wg, *wu = Wu;
   if (dX && n_tok > 0) {
     if (!weights_suit(d, ff)) {
@@ -851,7 +916,7 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
     // P [dG dU] times Wg, then Wu.
     const int64_t s1 = ffp / 64;
     const int64_t jump = static_cast<const char*>(wu) - static_cast<const char*>(wg) - 2 * ffp * dp;
-    pair.x = GradArgs{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg), 4 * ffp,
+    pair.a[0] = GradArgs{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg), 4 * ffp,
                       2 * dp, n_tok, dp, 2 * s1, s1, jump,
                       GradOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, n_tok, lddx, d,
                               dx_dtype == OPTIMA_DTYPE_F32, 0}};
@@ -859,7 +924,7 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
   if (dWg) {
     // No tokens: no stages, and the products are zero.
     if (n_tok > 0) prep.x = Transpose{static_cast<const bf16_t*>(X), ldx, n_tok, d, tp, l.xt};
-    pair.w = GradArgs{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt),
+    pair.a[1] = GradArgs{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt),
                       2 * tp, 2 * tp, 2 * ff, dp, tp / 64, 0, 0,
                       GradOut{{dWg, dWu}, {mask_g, mask_u}, ff, ff, d, d,
                               dw_dtype == OPTIMA_DTYPE_F32, accumulate}};
@@ -876,7 +941,7 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
     OPTIMA_LAUNCH_CHECK();
   }
   if (n_tok == 0 && !dWg) return OPTIMA_OK;
-  return grad_products(pair, s);
+  return grad_products(pair, l.part, s);
 }
 
 }  // namespace optima
