@@ -443,11 +443,11 @@ optima_status optima_qp_solve_batched(const float* H, int64_t d,
  * X, R and S are of `dtype` (F32 or BF16), weight of w_dtype. S (nullable)
  * receives s rounded to dtype; the norm is taken of the fp32 s. S may be X or R
  * themselves (same pointer and pitch), and so may Y if it has their type.
- * Y: y_dtype F32, BF16, or I8: codes q = rne(y / scale) within +-127 with
- *   scale = max |y| / 127 over each group of `group` consecutive values (32, 64 or
+ * Y: y_dtype F32, BF16, or I8: codes q = rne(y * (1 / scale)) within +-127 with
+ *   scale = max |y| / 127 (0 below the smallest normal number) over each group of `group` consecutive values (32, 64 or
  *   128; the last group of a row may be shorter) or over the row (group = 0).
  *   scales[n_tok][ceil(d / group)] (one a row for group = 0) is required then. A
- *   group of zeros has scale 0; one with a NaN or infinity has codes 0 and a NaN
+ *   group with scale 0 has codes 0; one with a NaN or infinity has codes 0 and a NaN
  *   or infinite scale. For other types scales is NULL and group 0.
  * eps > 0. */
 #define OPTIMA_NORM_MAX_DIM 16384

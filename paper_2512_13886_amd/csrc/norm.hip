@@ -5,9 +5,10 @@
 // dx = dS + rstd (p - c xh) and dw = sum over tokens of dy xh.
 //
 // Both read each row once and keep it in registers between the sum over the row
-// and the outputs, so that they are bound by HBM. A row belongs to one wave (up
-// to 1024 values), to 256 threads (up to 4096) or to 1024 (up to 16384); thread
-// t of them holds chunks t, t + THREADS, .. of 8 values. All sums are fp32.
+// and the outputs, so that they are bound by HBM. A row belongs to a group of threads
+// as large as it needs (by_width): part of a wave (up to 256 values), a wave, or a whole
+// workgroup; thread t of them holds pieces t, t + THREADS, .. of 8 values. All sums are
+// fp32.
 #include <type_traits>
 
 #include "common.h"
@@ -16,12 +17,12 @@
 namespace optima {
 namespace {
 
-// Sum of v[0 .. N-1] over the THREADS threads of a row (64: a wave; else the
+// Sum of v[0 .. N-1] over the THREADS threads of a row (up to 64: of a wave; else the
 // whole workgroup). red: N * THREADS / 64 floats that no earlier call still reads.
 template <int THREADS, int N>
 __device__ inline void row_sums(float (&v)[N], float* red) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1)
+  for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o >>= 1)
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, 64);
   if constexpr (THREADS > 64) {
@@ -49,7 +50,7 @@ __device__ inline uint32_t lanes_max(uint32_t m, int lanes) {
 
 template <int THREADS>
 __device__ inline uint32_t row_max(uint32_t m, uint32_t* red) {
-  m = lanes_max(m, 64);
+  m = lanes_max(m, THREADS < 64 ? THREADS : 64);
   if constexpr (THREADS > 64) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 0) red[wave] = m;
@@ -69,42 +70,51 @@ struct NormArgs {
   float eps;
 };
 
-__device__ inline void load_weights(const void* w, int w_bf16, int at, int left, float (&v)[8]) {
+__device__ inline void load_weights(const void* w, int w_bf16, int at, int d, float (&v)[8]) {
   if (w_bf16) {
     Raw8<bf16_t> raw;
-    load_upto8(raw, static_cast<const bf16_t*>(w) + at, left);
+    load_piece(raw, static_cast<const bf16_t*>(w), at, d);
     values8(raw, v);
   } else {
     Raw8<float> raw;
-    load_upto8(raw, static_cast<const float*>(w) + at, left);
+    load_piece(raw, static_cast<const float*>(w), at, d);
     values8(raw, v);
   }
 }
 
+// Rows of a workgroup, and this thread's of them and place in it.
+template <int THREADS>
+struct RowGroup {
+  static constexpr int kRows = THREADS <= 64 ? 256 / THREADS : 1;
+  static constexpr int kWg = THREADS <= 64 ? 256 : THREADS;
+  static constexpr int kWaves = (THREADS + 63) / 64;  // of a row
+  __device__ static inline int row() { return THREADS <= 64 ? threadIdx.x / THREADS : 0; }
+  __device__ static inline int at() { return THREADS <= 64 ? threadIdx.x % THREADS : threadIdx.x; }
+};
+
 // One row a group of THREADS threads, CH chunks a thread. T: type of x, r and s;
 // O: type of y (int8_t: with scales).
 template <typename T, typename O, int THREADS, int CH>
-__global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm(NormArgs a) {
-  constexpr int kRows = THREADS == 64 ? 4 : 1;
-  constexpr int kWaves = THREADS / 64;
-  __shared__ float red[kWaves];
-  __shared__ uint32_t red_max[kWaves];
-  const int t = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
-  int64_t row = int64_t(blockIdx.x) * kRows + (THREADS == 64 ? threadIdx.x >> 6 : 0);
-  if (row >= a.n) return;  // a whole wave
+__global__ void __launch_bounds__(RowGroup<THREADS>::kWg) k_rms_norm(NormArgs a) {
+  using Rows = RowGroup<THREADS>;
+  __shared__ float red[Rows::kWaves];
+  __shared__ uint32_t red_max[Rows::kWaves];
+  const int t = Rows::at();
+  const int64_t row = int64_t(blockIdx.x) * Rows::kRows + Rows::row();
+  if (row >= a.n) return;  // all threads of the row
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   const T* r = a.r ? static_cast<const T*>(a.r) + row * a.ldr : nullptr;
   Raw8<T> raw[CH], res[CH];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int at = 8 * (t + c * THREADS);
-    load_upto8(raw[c], x + at, a.d - at);
+    load_piece(raw[c], x, at, a.d);
   }
   if (r)
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int at = 8 * (t + c * THREADS);
-      load_upto8(res[c], r + at, a.d - at);
+      load_piece(res[c], r, at, a.d);
     }
   float v[CH][8];
   float sq[1] = {0.f};
@@ -135,7 +145,7 @@ __global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm(Norm
   for (int c = 0; c < CH; ++c) {
     const int at = 8 * (t + c * THREADS);
     float w[8];
-    load_weights(a.w, a.w_bf16, at, a.d - at, w);
+    load_weights(a.w, a.w_bf16, at, a.d, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * w[i];
   }
@@ -153,10 +163,11 @@ __global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm(Norm
     if (!a.group) all = row_max<THREADS>(all, red_max);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      // Groups are 4, 8 or 16 aligned lanes of one chunk.
+      // Groups are 4, 8 or 16 aligned lanes, or what a narrow row has.
       const int at = 8 * (t + c * THREADS);
-      const float top = __uint_as_float(a.group ? lanes_max(m[c], a.group / 8) : all);
-      const float scale = top / 127.f;
+      const float top = __uint_as_float(a.group ? lanes_max(m[c], min(a.group / 8, THREADS)) : all);
+      float scale = top / 127.f;
+      if (scale < 0x1p-126f) scale = 0.f;
       if (a.group) {
         if ((at & (a.group - 1)) == 0 && at < a.d) scales[at / a.group] = scale;
       } else if (c == 0 && t == 0) {
@@ -164,9 +175,9 @@ __global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm(Norm
       }
       // A group with an infinity or NaN has codes 0 and that scale: NaN as values.
       const bool fine = scale > 0.f && scale < __builtin_inff();
+      const float inv = 1.f / scale;  // |y| inv stays below 127.5
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        v[c][i] = fine ? fminf(fmaxf(rintf(v[c][i] / scale), -127.f), 127.f) : 0.f;
+      for (int i = 0; i < 8; ++i) v[c][i] = fine ? rintf(v[c][i] * inv) : 0.f;
       store_upto8(y + at, v[c], a.d - at);
     }
   } else {
@@ -190,20 +201,28 @@ struct NormGradArgs {
 // Rows blockIdx, blockIdx + gridDim, .. in groups of kRows; each thread keeps the
 // sums of its columns of dw over them.
 template <typename T, int THREADS, int CH>
-__global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm_grad(NormGradArgs a) {
-  constexpr int kRows = THREADS == 64 ? 4 : 1;
-  constexpr int kWaves = THREADS / 64;
+__global__ void __launch_bounds__(RowGroup<THREADS>::kWg) k_rms_norm_grad(NormGradArgs a) {
+  using Rows = RowGroup<THREADS>;
+  constexpr int kRows = Rows::kRows, kWaves = Rows::kWaves;
   // Two sets, taken in turn: a row's sums are not written before every wave has
   // read those of the row before the last.
   __shared__ float red[2][2 * kWaves];
-  __shared__ float cross[kRows == 1 ? 1 : 3 * 512 * CH];
-  const int t = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
-  const int sub = THREADS == 64 ? threadIdx.x >> 6 : 0;
-  float w[CH][8], dw[CH][8];
+  __shared__ float cross[kRows == 1 ? 1 : 256 * 8 * CH];
+  const int t = Rows::at(), sub = Rows::row();
+  // 1024 threads have no registers to keep the weights in: they load them again.
+  constexpr bool kKeep = THREADS < 1024;
+  float kept[kKeep ? CH : 1][8], dw[CH][8];
+  auto weights = [&](int c, float (&w)[8]) {
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = kept[c][i];
+    } else {
+      load_weights(a.w, a.w_bf16, 8 * (t + c * THREADS), a.d, w);
+    }
+  };
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int at = 8 * (t + c * THREADS);
-    load_weights(a.w, a.w_bf16, at, a.d - at, w[c]);
+    if constexpr (kKeep) load_weights(a.w, a.w_bf16, 8 * (t + c * THREADS), a.d, kept[c]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
   }
@@ -214,20 +233,21 @@ __global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm_grad
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int at = 8 * (t + c * THREADS);
-      load_upto8(rs[c], static_cast<const T*>(a.s) + row * a.lds + at, a.d - at);
-      load_upto8(rd[c], static_cast<const T*>(a.dy) + row * a.lddy + at, a.d - at);
-      if (a.ds) load_upto8(rr[c], static_cast<const T*>(a.ds) + row * a.ldds + at, a.d - at);
+      load_piece(rs[c], static_cast<const T*>(a.s) + row * a.lds, at, a.d);
+      load_piece(rd[c], static_cast<const T*>(a.dy) + row * a.lddy, at, a.d);
+      if (a.ds) load_piece(rr[c], static_cast<const T*>(a.ds) + row * a.ldds, at, a.d);
     }
     float sums[2] = {0.f, 0.f};  // s^2, p s
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float s[8], dy[8];
+      float s[8], dy[8], w[8];
       values8(rs[c], s);
       values8(rd[c], dy);
+      weights(c, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sums[0] += s[i] * s[i];
-        sums[1] += w[c][i] * dy[i] * s[i];
+        sums[1] += w[i] * dy[i] * s[i];
       }
     }
     row_sums<THREADS>(sums, red[turn]);
@@ -236,9 +256,10 @@ __global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm_grad
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int at = 8 * (t + c * THREADS);
-      float s[8], dy[8], dx[8];
+      float s[8], dy[8], dx[8], w[8];
       values8(rs[c], s);
       values8(rd[c], dy);
+      weights(c, w);
       if (a.ds)
         values8(rr[c], dx);
       else
@@ -246,7 +267,7 @@ __global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm_grad
         for (int i = 0; i < 8; ++i) dx[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        dx[i] += rstd * (w[c][i] * dy[i] - k * s[i]);
+        dx[i] += rstd * (w[i] * dy[i] - k * s[i]);
         dw[c][i] += dy[i] * (s[i] * rstd);
       }
       store_upto8(static_cast<T*>(a.dx) + row * a.lddx + at, dx, a.d - at);
@@ -254,19 +275,19 @@ __global__ void __launch_bounds__(THREADS > 256 ? THREADS : 256) k_rms_norm_grad
   }
   if (!a.part) return;
   if constexpr (kRows > 1) {
-    if (sub > 0)
+    // The rows' sums, in their order: [value][row][thread of the row].
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) cross[((sub - 1) * CH + c) * 512 + 64 * i + t] = dw[c][i];
+      for (int i = 0; i < 8; ++i) cross[(c * 8 + i) * 256 + threadIdx.x] = dw[c][i];
     __syncthreads();
     if (sub > 0) return;
-#pragma unroll
-    for (int u = 0; u < kRows - 1; ++u)
+#pragma unroll 1
+    for (int u = 1; u < kRows; ++u)
 #pragma unroll
       for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[c][i] += cross[(u * CH + c) * 512 + 64 * i + t];
+        for (int i = 0; i < 8; ++i) dw[c][i] += cross[(c * 8 + i) * 256 + u * THREADS + t];
   }
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -293,33 +314,61 @@ __global__ void __launch_bounds__(1024) k_norm_dw(const float* part, int blocks,
   dw[col] = accumulate ? dw[col] + s : s;
 }
 
-// Threads and chunks of a row of d values.
-template <typename F>
+// Threads, and pieces of 8 values a thread, of a row of d values. Few threads with
+// several pieces spare a row the barriers of its sums, which the 8-bit output has two
+// of, and a third piece spares rows of 5000 to 6144 values the idle fourth. 128 million
+// bf16 values to 8 bits: d = 2048 113 us in 256 threads, 93 in 64 (to bf16 174 and 181, so
+// that only the former take them); d = 8192 145 in 1024, 93 in 256; d = 5000 207 in 1024,
+// 135 and 103 in 256 with four and three pieces.
+template <int N>
+using Int = std::integral_constant<int, N>;
+template <bool TO_8_BITS, typename F>
 void by_width(int64_t d, F f) {
-  using std::integral_constant;
-  if (d <= 512) f(integral_constant<int, 64>(), integral_constant<int, 1>());
-  else if (d <= 1024) f(integral_constant<int, 64>(), integral_constant<int, 2>());
-  else if (d <= 2048) f(integral_constant<int, 256>(), integral_constant<int, 1>());
-  else if (d <= 4096) f(integral_constant<int, 256>(), integral_constant<int, 2>());
-  else if (d <= 8192) f(integral_constant<int, 1024>(), integral_constant<int, 1>());
-  else f(integral_constant<int, 1024>(), integral_constant<int, 2>());
+  if (d <= 64) f(Int<8>(), Int<1>());
+  else if (d <= 128) f(Int<16>(), Int<1>());
+  else if (d <= 256) f(Int<32>(), Int<1>());
+  else if (d <= 512) f(Int<64>(), Int<1>());
+  else if (d <= 1024) f(Int<64>(), Int<2>());
+  else if (d <= 2048) f(Int<TO_8_BITS ? 64 : 256>(), Int<TO_8_BITS ? 4 : 1>());
+  else if (d <= 4096) f(Int<256>(), Int<2>());
+  else if (d <= 6144) f(Int<256>(), Int<3>());
+  else if (d <= 8192) f(Int<256>(), Int<4>());
+  else if (d <= 12288) f(Int<512>(), Int<3>());
+  else f(Int<512>(), Int<4>());
 }
-static_assert(OPTIMA_NORM_MAX_DIM == 1024 * 2 * 8, "the widest row that by_width covers");
+static_assert(OPTIMA_NORM_MAX_DIM == 512 * 4 * 8, "the widest row that by_width covers");
+
+// The same for the gradient, which keeps more of each value.
+template <typename F>
+void grad_by_width(int64_t d, F f) {
+  if (d <= 64) f(Int<8>(), Int<1>());
+  else if (d <= 128) f(Int<16>(), Int<1>());
+  else if (d <= 256) f(Int<32>(), Int<1>());
+  else if (d <= 512) f(Int<64>(), Int<1>());
+  else if (d <= 1024) f(Int<64>(), Int<2>());
+  else if (d <= 2048) f(Int<256>(), Int<1>());
+  else if (d <= 4096) f(Int<256>(), Int<2>());
+  else if (d <= 8192) f(Int<512>(), Int<2>());
+  else f(Int<1024>(), Int<2>());
+}
 
 template <typename T, typename O>
 void launch_norm(const NormArgs& a, hipStream_t s) {
-  by_width(a.d, [&](auto threads, auto ch) {
+  by_width<sizeof(T) == 2 && sizeof(O) == 1>(a.d, [&](auto threads, auto ch) {
     constexpr int kT = decltype(threads)::value, kCh = decltype(ch)::value;
-    constexpr int rows = kT == 64 ? 4 : 1;
-    hipLaunchKernelGGL((k_rms_norm<T, O, kT, kCh>), dim3(unsigned(ceil_div(a.n, rows))),
-                       dim3(kT == 64 ? 256 : kT), 0, s, a);
+    hipLaunchKernelGGL((k_rms_norm<T, O, kT, kCh>),
+                       dim3(unsigned(ceil_div(a.n, RowGroup<kT>::kRows))), dim3(RowGroup<kT>::kWg), 0,
+                       s, a);
   });
 }
 
-// Workgroups of the gradient. Constant, so that the order of dw's sums is too.
+// Workgroups of the gradient, by the sizes alone, so that the order of dw's sums is too.
+// 128 million bf16 values, with 256, 512, 1024 and 2048 of them: d = 1024 218, 196, 205 and
+// 209 us, d = 4096 230, 193, 212 and 220.
 int grad_blocks(int64_t n, int64_t d) {
-  const int64_t rows = d <= 1024 ? 4 : 1;
-  return int(std::min<int64_t>(ceil_div(n, rows), d <= 4096 ? 1024 : 512));
+  int64_t rows = 0;
+  grad_by_width(d, [&](auto threads, auto) { rows = RowGroup<decltype(threads)::value>::kRows; });
+  return int(std::min<int64_t>(ceil_div(n, rows), d <= 2048 ? 1024 : d <= 8192 ? 512 : 256));
 }
 
 }  // namespace
@@ -355,9 +404,9 @@ optima_status rms_norm_backward(const void* S, int64_t lds, const void* w, int w
   if (n > 0) {
     NormGradArgs a{S, w, dY, dS, dX, dweight ? static_cast<float*>(ws) : nullptr, n, lds, lddy,
                    ldds, lddx, int(d), w_dtype == OPTIMA_DTYPE_BF16, eps};
-    by_width(d, [&](auto threads, auto ch) {
+    grad_by_width(d, [&](auto threads, auto ch) {
       constexpr int kT = decltype(threads)::value, kCh = decltype(ch)::value;
-      const dim3 wg(kT == 64 ? 256 : kT);
+      const dim3 wg(RowGroup<kT>::kWg);
       if (dtype == OPTIMA_DTYPE_BF16)
         hipLaunchKernelGGL((k_rms_norm_grad<bf16_t, kT, kCh>), dim3(blocks), wg, 0, s, a);
       else

@@ -76,6 +76,44 @@ __device__ inline void load_upto8(Raw8<T>& r, const T* p, int n) {
     load_some(r, p, n);
 }
 
+// Eight values moved down by s (0 .. 7) places, zeros from above.
+__device__ inline void shift_down(Raw8<bf16_t>& r, int s) {
+  if (s & 4) r.w = u32x4{r.w[2], r.w[3], 0, 0};
+  if (s & 2) r.w = u32x4{r.w[1], r.w[2], r.w[3], 0};
+  if (s & 1)
+    r.w = u32x4{__builtin_amdgcn_alignbit(r.w[1], r.w[0], 16),
+                __builtin_amdgcn_alignbit(r.w[2], r.w[1], 16),
+                __builtin_amdgcn_alignbit(r.w[3], r.w[2], 16), r.w[3] >> 16};
+}
+__device__ inline void shift_down(Raw8<float>& r, int s) {
+  if (s & 4) r.w[0] = r.w[1], r.w[1] = u32x4{0, 0, 0, 0};
+  if (s & 2) {
+    r.w[0] = u32x4{r.w[0][2], r.w[0][3], r.w[1][0], r.w[1][1]};
+    r.w[1] = u32x4{r.w[1][2], r.w[1][3], 0, 0};
+  }
+  if (s & 1) {
+    r.w[0] = u32x4{r.w[0][1], r.w[0][2], r.w[0][3], r.w[1][0]};
+    r.w[1] = u32x4{r.w[1][1], r.w[1][2], r.w[1][3], 0};
+  }
+}
+// Values at .. at + 7 of a row of d; zeros past its end. A row's last piece is loaded
+// from eight values before its end, and moved: one wide load like the others.
+template <typename T>
+__device__ inline void load_piece(Raw8<T>& r, const T* row, int at, int d) {
+  if (at + 8 <= d) {
+    load8(r, row + at);
+    return;
+  }
+  r = Raw8<T>{};
+  if (at >= d) return;
+  if (d < 8) {
+    load_some(r, row + at, d - at);
+  } else {
+    load8(r, row + d - 8);
+    shift_down(r, at + 8 - d);
+  }
+}
+
 __device__ inline void store8(bf16_t* p, const float (&v)[8]) {
   *reinterpret_cast<u32x4_2*>(p) =
       u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
@@ -116,11 +154,16 @@ __device__ inline void store_upto4(float* p, const float (&v)[4], int n) {
   for (int i = 0; i < 4; ++i)
     if (i < n) store1(p + i, v[i]);
 }
-// Whole numbers within int8.
+// Whole numbers within +-2^22: the low bytes of their bit patterns once 1.5 2^23 is added.
+__device__ inline uint32_t int_bits(float v) { return __float_as_uint(v + 12582912.f); }
 __device__ inline void store8(int8_t* p, const float (&v)[8]) {
-  uint32_t w[2] = {0, 0};
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t(int(v[i])) & 255u) << (8 * (i & 3));
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t lo = __builtin_amdgcn_perm(int_bits(v[4 * h + 1]), int_bits(v[4 * h]), 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(int_bits(v[4 * h + 3]), int_bits(v[4 * h + 2]), 0x04000C0Cu);
+    w[h] = lo | hi;
+  }
   *reinterpret_cast<u32x2_1*>(p) = u32x2{w[0], w[1]};
 }
 __device__ inline void store1(int8_t* p, float v) { *p = int8_t(int(v)); }

@@ -47,8 +47,8 @@ def _np(t):
 
 
 # Every width of by_width, its edges, and rows that end inside a chunk of 8.
-WIDTHS = [1, 7, 8, 64, 511, 512, 513, 1000, 1024, 1025, 2048, 2049, 4095, 4096, 4100, 8192, 8199,
-          16384]
+WIDTHS = [1, 7, 8, 9, 64, 65, 128, 129, 200, 256, 257, 511, 512, 513, 1000, 1024, 1025, 2048, 2049, 4095, 4096, 4100,
+          6144, 6145, 8192, 8199, 12288, 12290, 16384]
 
 
 @pytest.mark.parametrize("d", WIDTHS)
@@ -73,7 +73,8 @@ def test_forward(L, d, dt, out, residual):
         assert _untouched(sbuf, n, d)
 
 
-@pytest.mark.parametrize("d", [1, 31, 32, 100, 512, 1000, 4096, 5001, 16384])
+@pytest.mark.parametrize("d", [1, 31, 32, 64, 100, 130, 512, 1000, 1500, 4096, 5001, 7000, 12000,
+                               16384])
 @pytest.mark.parametrize("group", [0, 32, 64, 128])
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_eight_bits(L, d, group, dt):
@@ -98,9 +99,10 @@ def test_eight_bits(L, d, group, dt):
     assert _untouched(ybuf, n, d)
 
 
-def test_many_rows(L):
-    # More rows than a grid of one wave per row has workgroups' worth, odd count.
-    n, d = 10007, 96
+@pytest.mark.parametrize("d", [5, 33, 96, 200, 777])
+def test_many_rows(L, d):
+    # Rows that share a wave, and a last workgroup that is not full.
+    n = 10007
     g = torch.Generator(device=dev()).manual_seed(1)
     X, w = _rows(g, n, d, torch.bfloat16), torch.ones(d, device=dev())
     Y = torch.empty(n, d, device=dev())
@@ -149,7 +151,7 @@ def test_nonfinite_stays_in_its_row_and_group(L):
     assert bool(sc1[0].isnan().all()) and bool((q[0] == 0).all()) and bool(sc1[1:].isfinite().all())
 
 
-@pytest.mark.parametrize("d", [1, 8, 100, 512, 1000, 2048, 4096, 4100, 8192, 16384])
+@pytest.mark.parametrize("d", [1, 8, 60, 100, 250, 512, 1000, 2048, 4096, 4100, 8192, 16384])
 @pytest.mark.parametrize("dt, n, residual", [("bf16", 1, True), ("f32", 7, False),
                                              ("bf16", 2500, True)])
 def test_backward(L, d, dt, n, residual):
