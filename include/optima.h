@@ -477,8 +477,9 @@ optima_status optima_rms_norm_backward(const void* S, int64_t lds, const void* w
  * where d_in % 8 == 0). H: h_dtype BF16 or F32. G and U (nullable): bf16
  * [n_tok][d_ff], what the gradient takes; H is formed of the unrounded sums.
  * act: OPTIMA_ACT_SILU or OPTIMA_ACT_NONE.
- * ws: optima_gated_forward_workspace_bytes(n_tok, d_in, d_ff) bytes (0 for few
- * tokens): copies of operands whose rows do not suit wide loads. */
+ * ws: optima_gated_forward_workspace_bytes(n_tok, d_in, d_ff) bytes (0 for few tokens,
+ * never less for more): copies of operands whose rows do not suit wide loads, and parts
+ * of split sums. */
 size_t optima_gated_forward_workspace_bytes(int64_t n_tok, int64_t d_in, int64_t d_ff);
 optima_status optima_gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d_in,
                                    const void* Wg, const void* Wu, int64_t d_ff, int act, void* H,

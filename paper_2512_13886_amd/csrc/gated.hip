@@ -44,7 +44,31 @@ struct GatedArgs {
   int64_t n_tok, d, ff;
   int64_t ldx, ldw, ldh, ldg, ldu;  // in elements
   int h_f32, act;
+  int splits;   // ranges of the sum over d (k_gated_ring) ..
+  float* part;  // .. whose parts go here: [split][tile][128][g: 64, u: 64]
 };
+
+// Four or eight consecutive outputs of a token from their sums g and u.
+template <int N>
+__device__ inline void gated_store(const GatedArgs& a, int64_t tok, int64_t n, const float (&g)[N],
+                                   const float (&u)[N]) {
+  const int left = int(std::max<int64_t>(std::min<int64_t>(a.ff - n, N), 0));
+  float h[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) h[e] = gate_act(a.act, g[e]) * u[e];
+  auto put = [left](auto* p, const float (&v)[N]) {
+    if constexpr (N == 8)
+      store_upto8(p, v, left);
+    else
+      store_upto4(p, v, left);
+  };
+  if (a.g) put(a.g + tok * a.ldg + n, g);
+  if (a.u) put(a.u + tok * a.ldu + n, u);
+  if (a.h_f32)
+    put(static_cast<float*>(a.h) + tok * a.ldh + n, h);
+  else
+    put(static_cast<bf16_t*>(a.h) + tok * a.ldh + n, h);
+}
 
 // ---------------------------------------------------------------------------
 // Few tokens: the waves of a workgroup take the 64-value pieces of its weight rows in
@@ -193,39 +217,43 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_gated256(GatedArgs a) {
   gemm256_mainloop<Bf16Rows<false>>(acc, src, int(a.d / 64), l0, l1, l2, l3, l4, l5, l6, l7, [] {});
 
   const int64_t n = n0 + t256_rows_col(0);
-  const int left = int(std::max<int64_t>(std::min<int64_t>(a.ff - n, 8), 0));
 #pragma unroll
   for (int qa = 0; qa < 2; ++qa)
 #pragma unroll
     for (int mi = 0; mi < 4; ++mi) {
       const int64_t tok = m0 + t256_rows_row(qa, mi);
       if (tok >= a.n_tok) continue;
-      float g[8], u[8], h[8];
+      float g[8], u[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         g[e] = acc.q[qa][0][mi][e >> 2][e & 3];
         u[e] = acc.q[qa][1][mi][e >> 2][e & 3];
-        h[e] = gate_act(a.act, g[e]) * u[e];
       }
-      if (a.g) store_upto8(a.g + tok * a.ldg + n, g, left);
-      if (a.u) store_upto8(a.u + tok * a.ldu + n, u, left);
-      if (a.h_f32)
-        store_upto8(static_cast<float*>(a.h) + tok * a.ldh + n, h, left);
-      else
-        store_upto8(static_cast<bf16_t*>(a.h) + tok * a.ldh + n, h, left);
+      gated_store<8>(a, tok, n, g, u);
     }
 }
 
+struct SplitSteps {
+  int s0;  // the workgroup's first stage
+  __device__ inline int64_t a(int s) const { return int64_t(s0 + s) * 128; }
+  __device__ inline int64_t b(int s) const { return int64_t(s0 + s) * 128; }
+};
+
 // 128 tokens x 64 outputs on the 128 x 128 ring tile: 16-row blocks of B are rows
-// of Wg and Wu in turn, so that blocks 0 and 1 of a wave are g and u.
+// of Wg and Wu in turn, so that blocks 0 and 1 of a wave are g and u. With few tiles the
+// sum is split, and k_gated_join adds its parts: 256 tokens, 4032 -> 83, 32 us in one piece
+// and 12 split.
 __global__ void __launch_bounds__(Ring128::kThreads) k_gated_ring(GatedArgs a) {
   __shared__ __attribute__((aligned(1024))) char b0[Ring128::kBufBytes];
   __shared__ __attribute__((aligned(1024))) char b1[Ring128::kBufBytes];
   __shared__ __attribute__((aligned(1024))) char b2[Ring128::kBufBytes];
   __shared__ __attribute__((aligned(1024))) char b3[Ring128::kBufBytes];
-  const int tiles_m = cdiv(a.n_tok, 128), tiles_n = cdiv(a.ff, 64);
+  const int tiles_m = cdiv(a.n_tok, 128), tiles_n = cdiv(a.ff, 64), tiles = tiles_m * tiles_n;
+  const int sp = blockIdx.x / tiles, stages = int(a.d / 64);
+  const int s0 = int(int64_t(stages) * sp / a.splits);
+  const int s1 = int(int64_t(stages) * (sp + 1) / a.splits);
   int tm, tn;
-  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  tile_of_block(blockIdx.x - sp * tiles, tiles, tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = int64_t(tm) * 128, n0 = int64_t(tn) * 64;
   OperandsR128 src;
 #pragma unroll
@@ -236,28 +264,46 @@ __global__ void __launch_bounds__(Ring128::kThreads) k_gated_ring(GatedArgs a) {
     src.b[i] = ((r & 16) ? a.wu : a.wg) + std::min(n, a.ff - 1) * (2 * a.ldw) + seg;
   }
   AccR128<false> acc;
-  r128_mainloop<Bf16Rows<false>>(acc, src, SumShape{0, 0, 0}, int(a.d / 64), b0, b1, b2, b3, [] {});
+  r128_mainloop<Bf16Rows<false>>(acc, src, SumShape{0, 0, 0}, s1 - s0, b0, b1, b2, b3, [] {},
+                                 SplitSteps{s0});
 
-  const int64_t n = n0 + 16 * ((threadIdx.x >> 6) & 3) + 4 * ((threadIdx.x >> 4) & 3);
-  const int left = int(std::max<int64_t>(std::min<int64_t>(a.ff - n, 4), 0));
+  const int col = 16 * ((threadIdx.x >> 6) & 3) + 4 * ((threadIdx.x >> 4) & 3);
 #pragma unroll
   for (int mi = 0; mi < 4; ++mi) {
-    const int64_t tok = m0 + t256_rows_row(0, mi);
-    if (tok >= a.n_tok) continue;
-    float g[4], u[4], h[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      g[e] = acc.q[mi][0][e];
-      u[e] = acc.q[mi][1][e];
-      h[e] = gate_act(a.act, g[e]) * u[e];
+    const int row = t256_rows_row(0, mi);
+    if (a.splits > 1) {
+      float* p = a.part + size_t(blockIdx.x) * 16384 + row * 128 + col;
+      *reinterpret_cast<f4*>(p) = acc.q[mi][0];
+      *reinterpret_cast<f4*>(p + 64) = acc.q[mi][1];
+      continue;
     }
-    if (a.g) store_upto4(a.g + tok * a.ldg + n, g, left);
-    if (a.u) store_upto4(a.u + tok * a.ldu + n, u, left);
-    if (a.h_f32)
-      store_upto4(static_cast<float*>(a.h) + tok * a.ldh + n, h, left);
-    else
-      store_upto4(static_cast<bf16_t*>(a.h) + tok * a.ldh + n, h, left);
+    if (m0 + row >= a.n_tok) continue;
+    float g[4], u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g[e] = acc.q[mi][0][e], u[e] = acc.q[mi][1][e];
+    gated_store<4>(a, m0 + row, n0 + col, g, u);
   }
+}
+
+// The outputs from the parts of their sums, in their order: 16 tokens of a tile a
+// workgroup, four outputs a thread.
+__global__ void __launch_bounds__(kThreads) k_gated_join(GatedArgs a) {
+  const int tiles_m = cdiv(a.n_tok, 128), tiles_n = cdiv(a.ff, 64), tiles = tiles_m * tiles_n;
+  const int tile = blockIdx.x >> 3;
+  int tm, tn;
+  tile_of_block(tile, tiles, tiles_m, tiles_n, &tm, &tn);
+  const int row = (blockIdx.x & 7) * 16 + (threadIdx.x >> 4), col = 4 * (threadIdx.x & 15);
+  const int64_t tok = int64_t(tm) * 128 + row;
+  if (tok >= a.n_tok) return;
+  const float* p = a.part + size_t(tile) * 16384 + row * 128 + col;
+  f4 sg = {0.f, 0.f, 0.f, 0.f}, su = sg;
+#pragma unroll 4
+  for (int sp = 0; sp < a.splits; ++sp) {
+    sg += *reinterpret_cast<const f4*>(p + size_t(sp) * tiles * 16384);
+    su += *reinterpret_cast<const f4*>(p + size_t(sp) * tiles * 16384 + 64);
+  }
+  const float g[4] = {sg[0], sg[1], sg[2], sg[3]}, u[4] = {su[0], su[1], su[2], su[3]};
+  gated_store<4>(a, tok, int64_t(tn) * 64 + col, g, u);
 }
 
 // ---------------------------------------------------------------------------
@@ -681,12 +727,6 @@ __global__ void __launch_bounds__(kThreads) k_grad_join(GradPair p, int side, in
   grad_store<4>(a.out, row, col, v);
 }
 
-// A round of 256 x 256 tiles over the CUs against one of 128 x 128 tiles, a
-// quarter of the outputs: 1.4 against 0.56 us a stage of 64.
-bool wide_tiles(int64_t wide, int64_t small) {
-  return 5 * ceil_div(wide, kCus) <= 2 * ceil_div(small, kCus);
-}
-
 // Partial sums of at most kPartTiles 128 x 128 tiles.
 constexpr int64_t kPartTiles = 512;
 
@@ -764,24 +804,47 @@ optima_status grad_products(GradPair& p, float* part, hipStream_t s) {
   return OPTIMA_OK;
 }
 
+// The tile of the forward product and how often its sum is split, by what the rounds
+// over the CUs should take: 1.4 us a stage and 6 around them for 256 tokens x 128 outputs,
+// 0.56 and 3.5 for 128 x 64, 3 us and 5 TB/s for the join.
+struct GatedPlan {
+  bool wide;
+  int splits;
+  double us;
+};
+GatedPlan plan_gated(int64_t n_tok, int64_t d, int64_t ff) {
+  const int64_t stages = ceil_div(d, 64);
+  const int64_t wide = ceil_div(n_tok, 256) * ceil_div(ff, 128);
+  const int64_t small = ceil_div(n_tok, 128) * ceil_div(ff, 64);
+  GatedPlan best{true, 1, double(ceil_div(wide, kCus)) * (1.4 * double(stages) + 6)};
+  for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+    if (splits > stages || (splits > 1 && splits * small > kPartTiles)) break;
+    const double us = double(ceil_div(small * splits, kCus)) * (0.56 * double(ceil_div(stages, splits)) + 3.5) +
+                      (splits > 1 ? 3 + double(small) * splits * 131072 / 5e6 : 0);
+    if (us < best.us) best = GatedPlan{false, splits, us};
+  }
+  return best;
+}
+
 // Whether the weights are streamed once for all tokens, or tiles take them. Streamed
 // they come at 6 TB/s, and every 16 outputs read all tokens again, at 10 TB/s out of
-// the caches. A round of 64-output tiles takes 0.56 us for 64 values of d and 3.5 us
-// around them, at most 5.5 TB/s, and rows that do not suit them are copied first.
-// Measured, streamed against tiles: 4096 -> 14336, 4 tokens 39 to 42 us, 16 tokens 49 to
-// 43, 64 tokens 91 to 45; 1024 -> 8192, 32 tokens 10.7 to 12.2, 64 tokens 15.1 to 13.1;
-// 4096 -> 2048, 64 tokens 27 to 34; 1001 -> 2731, 64 tokens 17 to 21.
+// the caches; with few outputs a workgroup's own way through d is what counts. To tiles
+// they come at 5.5 TB/s at most, and rows that do not suit them are copied first. Measured,
+// streamed against tiles: 4096 -> 14336, 4 tokens 39 to 42 us, 16 tokens 49 to 43, 64 tokens
+// 91 to 45; 1024 -> 8192, 32 tokens 10.7 to 12.2, 64 tokens 15.1 to 13.1; 4096 -> 2048, 16
+// tokens 11 to 17, 64 tokens 26 to 17; 1001 -> 2731, 64 tokens 17 to 21.
 bool few_tokens(int64_t n_tok, int64_t d, int64_t ff) {
   if (n_tok > kFewTokens) return false;
   const double weights = 4e-6 * double(d) * double(ff);  // MB
-  const double streamed = weights / 6 + double(n_tok) * weights / 320;
-  const double rounds = double(ceil_div(ceil_div(ff, 64), kCus));
-  const double tiles = std::max(rounds * (0.56 * double(ceil_div(d, 64)) + 3.5), weights / 5.5 + 1);
+  const double streamed = std::max(weights / 6 + double(n_tok) * weights / 320,
+                                   4 + double(n_tok) * double(d) / 13000);
+  const double tiles = std::max(plan_gated(kFewTokens, d, ff).us, weights / 5.5 + 1);
   return streamed <= tiles + (d % 64 ? 2 * weights / 5 + 4 : 0);
 }
 
 struct GatedLayout {
   bf16_t *x, *wg, *wu;
+  float* part;
 };
 GatedLayout carve_gated(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* bytes) {
   Carver c(ws);
@@ -794,6 +857,9 @@ GatedLayout carve_gated(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* 
       l.wg = c.take<bf16_t>(size_t(ff) * size_t(dp));
       l.wu = c.take<bf16_t>(size_t(ff) * size_t(dp));
     }
+    // Split sums: no more parts than stages.
+    const int64_t parts = ceil_div(n_tok, 128) * ceil_div(ff, 64) * (dp / 64);
+    l.part = c.take<float>(16384 * size_t(std::min(kPartTiles, parts)));
   }
   if (bytes) *bytes = c.bytes();
   return l;
@@ -840,7 +906,7 @@ optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d
                             void* G, int64_t ldg, void* U, int64_t ldu, void* ws, hipStream_t s) {
   GatedArgs a{static_cast<const char*>(X), static_cast<const char*>(Wg),
               static_cast<const char*>(Wu), H, static_cast<bf16_t*>(G), static_cast<bf16_t*>(U),
-              n_tok, d, ff, ldx, d, ldh, ldg, ldu, h_dtype == OPTIMA_DTYPE_F32, act};
+              n_tok, d, ff, ldx, d, ldh, ldg, ldu, h_dtype == OPTIMA_DTYPE_F32, act, 1, nullptr};
   if (few_tokens(n_tok, d, ff)) {
     // Half the outputs a workgroup where that makes the launch, or its reads of the
     // tokens are few: 4096 -> 2048, 16 tokens, 10.3 against 13.9 us, 4096 -> 14336, 4
@@ -879,12 +945,19 @@ optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d
   }
   a.d = dp;
   OPTIMA_LAUNCH_CHECK();
-  const int64_t wide = ceil_div(n_tok, 256) * ceil_div(ff, 128);
-  const int64_t small = ceil_div(n_tok, 128) * ceil_div(ff, 64);
-  if (wide_tiles(wide, small))
-    hipLaunchKernelGGL(k_gated256, dim3(unsigned(wide)), dim3(Tile256::kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL(k_gated_ring, dim3(unsigned(small)), dim3(Ring128::kThreads), 0, s, a);
+  const GatedPlan plan = plan_gated(n_tok, d, ff);
+  a.splits = plan.splits;
+  a.part = l.part;
+  if (plan.wide) {
+    const int64_t tiles = ceil_div(n_tok, 256) * ceil_div(ff, 128);
+    hipLaunchKernelGGL(k_gated256, dim3(unsigned(tiles)), dim3(Tile256::kThreads), 0, s, a);
+  } else {
+    const int64_t tiles = ceil_div(n_tok, 128) * ceil_div(ff, 64);
+    hipLaunchKernelGGL(k_gated_ring, dim3(unsigned(tiles * plan.splits)), dim3(Ring128::kThreads), 0,
+                       s, a);
+    if (plan.splits > 1)
+      hipLaunchKernelGGL(k_gated_join, dim3(unsigned(tiles * 8)), dim3(kThreads), 0, s, a);
+  }
   OPTIMA_LAUNCH_CHECK();
   return OPTIMA_OK;
 }

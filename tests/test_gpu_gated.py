@@ -94,6 +94,14 @@ def test_small_tiles(L, n, d, ff):
     _forward(L, n, d, ff, name="none", out="f32", xpitch=d + 5, xoff=3)
 
 
+# Few tiles and long rows: the sum is split, evenly and not, and joined.
+@pytest.mark.parametrize("n, d, ff", [(64, 4032, 83), (66, 1025, 1), (130, 2048, 65),
+                                      (300, 1000, 33), (1000, 4100, 130)])
+@pytest.mark.parametrize("out, saved", [("bf16", True), ("f32", False)])
+def test_split_sums(L, n, d, ff, out, saved):
+    _forward(L, n, d, ff, out=out, saved=saved)
+
+
 @pytest.mark.parametrize("n, d, ff", [(2049, 64, 4100), (4096, 128, 2048), (4300, 65, 2300)])
 def test_large_tiles(L, n, d, ff):
     _forward(L, n, d, ff, saved=True)
