@@ -85,6 +85,39 @@ def skip_layer(converged: torch.Tensor, f_initial: torch.Tensor, f_final: torch.
     return bool(n and ((n - int(conv.sum())) * 2 > n or f1 > f0))
 
 
+@dataclass
+class SolvedLayer:
+    kept: torch.Tensor    # the solve's weights, or wanda's if the layer is skipped
+    wanda: torch.Tensor   # the mask-only weights
+    skipped: bool
+    stats: dict           # per-column device statistics of the solve
+    info: dict
+
+
+def solve_layer(H: torch.Tensor, lambda_max: torch.Tensor, W0: torch.Tensor, M: torch.Tensor,
+                opts: L.SolverOpts | None = None,
+                solved: Callable[[], None] | None = None) -> SolvedLayer:
+    """One layer's column QPs on its damped Hessian H, and the skip rule on their
+    statistics. `solved` is called between the two."""
+    d_out, d_in = W0.shape
+    dev = W0.device
+    W = torch.empty_like(W0)
+    stats = {"iters": torch.zeros(d_out, dtype=torch.int32, device=dev),
+             "converged": torch.zeros(d_out, dtype=torch.uint8, device=dev),
+             "f_initial": torch.zeros(d_out, dtype=torch.float32, device=dev),
+             "f_final": torch.zeros(d_out, dtype=torch.float32, device=dev)}
+    ws = torch.empty(L.optima_qp_workspace_bytes(d_in, d_out), dtype=torch.uint8, device=dev)
+    info = L.optima_qp_solve_batched(H, lambda_max, W0, M, W, opts=opts, ws=ws, stats=stats)
+    if solved is not None:
+        solved()
+    skipped = skip_layer(stats["converged"], stats["f_initial"], stats["f_final"])
+    # The mask-only weights sel(M, W0, +0): the solve's start point.
+    W_wanda = torch.empty_like(W0)
+    L.optima_qp_solve_batched(H, lambda_max, W0, M, W_wanda, opts=L.SolverOpts.default(max_iters=0),
+                              ws=ws)
+    return SolvedLayer(W_wanda if skipped else W, W_wanda, skipped, stats, info)
+
+
 def prune_chain(X0: torch.Tensor, weights: list, start: Callable[[int], torch.Tensor],
                 sparsity: float = 0.5, rel_damp: float = 0.01, act: int = L.ACT_SILU,
                 opts: L.SolverOpts | None = None, timed: bool = False):
@@ -117,22 +150,10 @@ def prune_chain(X0: torch.Tensor, weights: list, start: Callable[[int], torch.Te
         spectral_step_size(H, start(d_in), lmax)
         if timed:
             ev[1].record()
-        W = torch.empty_like(W0)
-        stats = {"iters": torch.zeros(d_out, dtype=torch.int32, device=dev),
-                 "converged": torch.zeros(d_out, dtype=torch.uint8, device=dev),
-                 "f_initial": torch.zeros(d_out, dtype=torch.float32, device=dev),
-                 "f_final": torch.zeros(d_out, dtype=torch.float32, device=dev)}
-        ws = torch.empty(L.optima_qp_workspace_bytes(d_in, d_out), dtype=torch.uint8, device=dev)
-        info = L.optima_qp_solve_batched(H, lmax, W0, M, W, opts=opts, ws=ws, stats=stats)
-        if timed:
-            ev[2].record()
-        skipped = skip_layer(stats["converged"], stats["f_initial"], stats["f_final"])
-        # The mask-only weights sel(M, W0, +0): the solve's start point.
-        W_wanda = torch.empty_like(W0)
-        L.optima_qp_solve_batched(H, lmax, W0, M, W_wanda, opts=L.SolverOpts.default(max_iters=0),
-                                  ws=ws)
-        del ws, H
-        kept = W_wanda if skipped else W
+        solved = solve_layer(H, lmax, W0, M, opts, ev[2].record if timed else None)
+        del H
+        kept, W_wanda, skipped = solved.kept, solved.wanda, solved.skipped
+        stats, info = solved.stats, solved.info
         if timed:
             ev[3].record()
         fws = torch.empty(L.optima_linear_forward_workspace_bytes(n_tok, d_in, d_out),
