@@ -476,7 +476,8 @@ optima_status optima_rms_norm_backward(const void* S, int64_t lds, const void* w
  * X: [n_tok][d_in] bf16, any d_in >= 1; Wg, Wu: [d_ff][d_in] bf16 (16-byte aligned
  * where d_in % 8 == 0). H: h_dtype BF16 or F32. G and U (nullable): bf16
  * [n_tok][d_ff], what the gradient takes; H is formed of the unrounded sums.
- * act: OPTIMA_ACT_SILU or OPTIMA_ACT_NONE.
+ * act: OPTIMA_ACT_SILU or OPTIMA_ACT_NONE. The 64 x 64 tiles of [n_tok][max(d_in, d_ff)]
+ * and twice those of [d_ff][d_in] stay below 2^23 together, here and in the gradient.
  * ws: optima_gated_forward_workspace_bytes(n_tok, d_in, d_ff) bytes (0 for few tokens,
  * never less for more): copies of operands whose rows do not suit wide loads, and parts
  * of split sums. */
@@ -507,8 +508,9 @@ optima_status optima_gated_backward(const void* X, int64_t ldx, int64_t n_tok, i
 /* 4-bit weights with group scales.
  * W: [n][d] F32 or BF16. Groups of `group` (32, 64 or 128) consecutive values of a
  * row have scale = bf16(max |w| * (1 / 7)), the product and 1 / 7 in fp32, and codes
- * clamp(rne(w / scale), -7, 7): a zero weight, as every pruned one is, stays exactly zero. A group with a NaN or infinity
- * has codes 0 and a NaN or infinite scale.
+ * clamp(rne(w / scale), -7, 7): a zero weight, as every pruned one is, stays exactly
+ * zero. A group with a NaN or infinity has codes 0 and a NaN or infinite scale. n d
+ * stays below 2^35.
  * Q: [n][optima_w4_row_bytes(d)], 16-byte aligned. A chunk of 128 codes takes 64
  *   bytes: dword j of its 16-byte block b holds codes 32 j + 8 b .. + 7, the even ones
  *   in nibbles 0..3 and the odd ones in nibbles 4..7, each as code + 8; rows are

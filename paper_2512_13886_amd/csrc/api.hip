@@ -100,11 +100,13 @@ int64_t esize(int dtype) {
 bool f32_or_bf16(int dtype) { return dtype == OPTIMA_DTYPE_F32 || dtype == OPTIMA_DTYPE_BF16; }
 bool group_ok(int64_t group) { return group == 32 || group == 64 || group == 128; }
 
-// Sizes of the gated product: tiles of tokens by values stay below 2^31.
+// Sizes of the gated product: the largest launch, which copies rows in blocks of 256
+// threads, two for 64 x 64 values, stays below 2^32 threads.
 bool gated_sizes(int64_t n_tok, int64_t d_in, int64_t d_ff) {
+  auto tiles = [](int64_t a, int64_t b) { return (a / 64 + 1) * (b / 64 + 1); };
   return n_tok >= 0 && n_tok <= kMaxTok && d_in >= 1 && d_in <= kMaxDim && d_ff >= 1 &&
          d_ff <= kMaxDim &&
-         (n_tok / 64 + 1) * (std::max(d_in, d_ff) / 64 + 1) < (int64_t(1) << 28);
+         2 * tiles(n_tok, std::max(d_in, d_ff)) + 4 * tiles(d_in, d_ff) < (int64_t(1) << 24);
 }
 
 optima_status w4_call(const void* X, int64_t ldx, int x_dtype, const float* x_scales,
@@ -494,7 +496,7 @@ optima_status optima_w4_pack(const void* W, int dtype, int64_t n, int64_t d, int
   if (!f32_or_bf16(dtype)) return OPTIMA_E_UNSUPPORTED;
   if (n < 0 || n > kMaxCols || d < 1 || d > kMaxDim || !group_ok(group)) return OPTIMA_E_INVAL;
   const int64_t groups = (d + group - 1) / group, row = int64_t(optima_w4_row_bytes(d));
-  if (n * (row / 64) >= int64_t(1) << 34) return OPTIMA_E_INVAL;  // 16 chunks a workgroup
+  if (n * (row / 64) >= int64_t(1) << 28) return OPTIMA_E_INVAL;  // 16 threads a chunk
   const Span w{W, n, d, d, esize(dtype)}, q{Q, n, row, row, 1}, sc{scales, n, groups, groups, 2};
   if (!w.good() || !q.good() || !sc.good() || !optima::aligned16(Q)) return OPTIMA_E_INVAL;
   if (q.meets(w) || sc.meets(w) || q.meets(sc)) return OPTIMA_E_INVAL;

@@ -65,7 +65,7 @@ struct NormArgs {
   const void *x, *r, *w;
   void *s, *y;
   float* scales;
-  int64_t n, ldx, ldr, lds, ldy;
+  int64_t n, row0, ldx, ldr, lds, ldy;  // row0: the launch's first row
   int d, group, groups, w_bf16;
   float eps;
 };
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(RowGroup<THREADS>::kWg) k_rms_norm(NormArgs a)
   __shared__ float red[Rows::kWaves];
   __shared__ uint32_t red_max[Rows::kWaves];
   const int t = Rows::at();
-  const int64_t row = int64_t(blockIdx.x) * Rows::kRows + Rows::row();
+  const int64_t row = a.row0 + int64_t(blockIdx.x) * Rows::kRows + Rows::row();
   if (row >= a.n) return;  // all threads of the row
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   const T* r = a.r ? static_cast<const T*>(a.r) + row * a.ldr : nullptr;
@@ -353,12 +353,16 @@ void grad_by_width(int64_t d, F f) {
 }
 
 template <typename T, typename O>
-void launch_norm(const NormArgs& a, hipStream_t s) {
+void launch_norm(NormArgs a, hipStream_t s) {
   by_width<sizeof(T) == 2 && sizeof(O) == 1>(a.d, [&](auto threads, auto ch) {
     constexpr int kT = decltype(threads)::value, kCh = decltype(ch)::value;
-    hipLaunchKernelGGL((k_rms_norm<T, O, kT, kCh>),
-                       dim3(unsigned(ceil_div(a.n, RowGroup<kT>::kRows))), dim3(RowGroup<kT>::kWg), 0,
-                       s, a);
+    using Rows = RowGroup<kT>;
+    // A launch has fewer than 2^32 threads.
+    constexpr int64_t kMost = (int64_t(1) << 22) * Rows::kRows;
+    for (; a.row0 < a.n; a.row0 += kMost)
+      hipLaunchKernelGGL((k_rms_norm<T, O, kT, kCh>),
+                         dim3(unsigned(ceil_div(std::min(a.n - a.row0, kMost), Rows::kRows))),
+                         dim3(Rows::kWg), 0, s, a);
   });
 }
 
@@ -377,7 +381,7 @@ optima_status rms_norm(const void* X, int64_t ldx, const void* R, int64_t ldr, i
                        int64_t d, const void* w, int w_dtype, float eps, void* S, int64_t lds,
                        void* Y, int64_t ldy, int y_dtype, float* scales, int64_t group,
                        hipStream_t s) {
-  NormArgs a{X, R, w, S, Y, scales, n, ldx, ldr, lds, ldy, int(d), int(group),
+  NormArgs a{X, R, w, S, Y, scales, n, 0, ldx, ldr, lds, ldy, int(d), int(group),
              int(group ? ceil_div(d, group) : 1), w_dtype == OPTIMA_DTYPE_BF16, eps};
   if (dtype == OPTIMA_DTYPE_BF16) {
     if (y_dtype == OPTIMA_DTYPE_BF16) launch_norm<bf16_t, bf16_t>(a, s);

@@ -253,3 +253,18 @@ def test_graph_replays_equal_eager_calls(L):
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (Y, S, dX, dw))), k
+
+
+def test_more_threads_than_a_launch_has(L):
+    # 256 threads a row: rows past 2^32 / 256 need another launch (and pass 2^31 elements).
+    n, d = (1 << 24) + 5, 1025
+    X = torch.empty((n, d), dtype=torch.bfloat16, device=dev())
+    Y = torch.empty_like(X)
+    g = torch.Generator(device=dev()).manual_seed(1)
+    w = torch.randn(d, generator=g, device=dev())
+    at = [0, 1 << 22, (1 << 22) + 1, (1 << 24) - 1, 1 << 24, n - 1]
+    X[at] = torch.randn((len(at), d), generator=g, device=dev()).bfloat16()
+    L.optima_rms_norm(X, w, Y)
+    want = torch.empty((len(at), d), dtype=torch.bfloat16, device=dev())
+    L.optima_rms_norm(X[at], w, want)
+    assert torch.equal(Y[at], want)
