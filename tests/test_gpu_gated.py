@@ -286,6 +286,40 @@ def test_side_stream_graph_and_repeats(L, n):
         assert all(torch.equal(a, b) for a, b in zip(got, outs())), k
 
 
+def test_offsets_past_32_bits(L):
+    # n d_ff past 2^31 values; the tokens are independent, so that a few of them alone
+    # give the same h and dX up to the order of the sums (and dG, dU rounded alike).
+    n, d, ff = 40001, 64, 60000
+    g = torch.Generator(device=dev()).manual_seed(5)
+
+    def rows(*shape, scale=1.0):
+        return torch.randn(shape, generator=g, device=dev(), dtype=torch.bfloat16).mul_(scale)
+
+    X, Wg, Wu = rows(n, d), rows(ff, d, scale=d ** -0.5), rows(ff, d, scale=d ** -0.5)
+    H, G, V, dH = (torch.empty((n, ff), dtype=torch.bfloat16, device=dev()) for _ in range(4))
+    L.optima_gated_forward(X, Wg, Wu, H, G=G, U=V)
+    dH.normal_(generator=g)
+    dX = torch.empty((n, d), dtype=torch.float32, device=dev())
+    dWg, dWu = (torch.empty((ff, d), dtype=torch.float32, device=dev()) for _ in range(2))
+    L.optima_gated_backward(X, Wg, Wu, G, V, dH, dX, dWg, dWu)
+    at = torch.tensor([0, 1, 20000, 35791, 35792, 39999, 40000], device=dev())
+    few = torch.empty((len(at), ff), dtype=torch.bfloat16, device=dev())
+    L.optima_gated_forward(X[at], Wg, Wu, few)
+    assert rel_fro(_np(H[at]), _np(few)) <= B
+    few_dx = torch.empty((len(at), d), dtype=torch.float32, device=dev())
+    L.optima_gated_backward(X[at], Wg, Wu, G[at], V[at], dH[at], dX=few_dx)
+    # Sums of 2 ff products in another order, in fp32.
+    _, _, _, dg, du = F.gated_backward(_np(X[at]), _np(Wg), _np(Wu), _np(G[at]), _np(V[at]),
+                                       _np(dH[at]), "silu")
+    bound = 2 * 2 * ff * U * (np.abs(dg) @ np.abs(_np(Wg)) + np.abs(du) @ np.abs(_np(Wu)))
+    assert np.all(np.abs(_np(dX[at]) - _np(few_dx)) <= 1.01 * bound)
+    # dW of the first and last outputs, against the oracle's on the same G and U.
+    cols = slice(ff - 8, ff)
+    _, wg, wu, _, _ = F.gated_backward(_np(X), _np(Wg[cols]), _np(Wu[cols]), _np(G[:, cols]),
+                                       _np(V[:, cols]), _np(dH[:, cols]), "silu")
+    assert rel_fro(_np(dWg[cols]), wg) <= B and rel_fro(_np(dWu[cols]), wu) <= B
+
+
 def test_no_tokens(L):
     e = torch.empty(0, 64, dtype=torch.bfloat16, device=dev())
     f = torch.empty(0, 32, dtype=torch.bfloat16, device=dev())

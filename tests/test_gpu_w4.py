@@ -216,6 +216,29 @@ def test_graph_and_side_stream(L):
         assert torch.equal(got, Y)
 
 
+def test_offsets_past_32_bits(L):
+    # Packed weights of more than 2^32 bytes, from 2^33 values.
+    n, d, group = (1 << 20) + 3, 8192, 128
+    g = torch.Generator(device=dev()).manual_seed(3)
+    W = torch.zeros((n, d), dtype=torch.bfloat16, device=dev())
+    at = torch.tensor([0, 5, 262143, 262144, 524287, 524288, n - 4, n - 1], device=dev())
+    W[at] = torch.randn((len(at), d), generator=g, device=dev()).bfloat16()
+    Q, sc = _pack(L, W, group)
+    q, s = _pack(L, W[at], group)
+    assert torch.equal(Q[at], q) and torch.equal(sc[at], s)
+    for tokens in (1, 40):
+        X = torch.randn((tokens, d), generator=g, device=dev()).bfloat16()
+        Y = torch.empty((tokens, n), dtype=torch.float32, device=dev())
+        y = torch.empty((tokens, len(at)), dtype=torch.float32, device=dev())
+        L.optima_w4_linear(X, Q, sc, Y, group)
+        L.optima_w4_linear(X, q, s, y, group)
+        # The same groups' sums, added in another order where the few rows' sums are split.
+        assert torch.allclose(Y[:, at], y, rtol=0, atol=float(d * 2.0 ** -24 * y.abs().max() * 8))
+        rest = torch.ones(n, dtype=torch.bool, device=dev())
+        rest[at] = False
+        assert bool((Y[:, rest] == 0).all())
+
+
 def test_no_tokens(L):
     g = torch.Generator(device=dev()).manual_seed(6)
     Q, sc = _pack(L, _weights(g, 20, 64), 64)
