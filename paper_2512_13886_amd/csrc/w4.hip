@@ -19,7 +19,10 @@
 //
 // Bound by the codes' way from HBM, once per call for up to 64 tokens. Up to 16 tokens
 // a workgroup takes 16 rows, its waves batches of their chunks, and the waves' sums are
-// joined in LDS in their order; more tokens share what is read of them.
+// joined in LDS in their order; more tokens share what is read of them. One 8-bit token,
+// 4096 -> 2 x 14336: 14.3 us, 4.2 TB/s; eight 16-bit ones, 14336 -> 4096 in groups of 64:
+// 9.5 us, 3.3 TB/s. Each wave has one or two batches, so that the launch's start and end
+// are what is left.
 #include <type_traits>
 
 #include "common.h"
@@ -33,7 +36,8 @@ constexpr int kChunkBytes = 64;
 
 typedef int i4 __attribute__((ext_vector_type(4)));
 
-// Sixteen lanes a chunk, one dword (eight codes) each.
+// Sixteen lanes a chunk, one dword (eight codes) each. Bound by HBM: 14336 x 4096 fp32
+// 48.6 us, 5.5 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_w4_pack(const T* W, int64_t total, int chunks, int d,
                                                       int group, int groups, uint8_t* Q,
