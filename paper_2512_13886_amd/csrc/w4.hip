@@ -513,8 +513,9 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_w4_slab(W4Args a) {
     if (batch + 1 < b1) put_batch(cur ^ 1);
     __syncthreads();
   }
-  if (gridDim.y > 1) {  // [split][workgroup][wave][operand][token block][lane]
-    f4* part = a.part + ((size_t(blockIdx.y) * gridDim.x + blockIdx.x) * kSlabWaves + wave) * OPS * NT * 64;
+  if (gridDim.y > 1) {  // [split][64 tokens][workgroup][wave][operand][token block][lane]
+    const size_t wg = (size_t(blockIdx.y) * gridDim.z + blockIdx.z) * gridDim.x + blockIdx.x;
+    f4* part = a.part + (wg * kSlabWaves + wave) * OPS * NT * 64;
 #pragma unroll
     for (int m = 0; m < OPS; ++m)
 #pragma unroll
@@ -525,12 +526,13 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_w4_slab(W4Args a) {
 }
 
 // The parts of the outputs, added in their order: one of the slab kernel's waves' outputs
-// for 16 tokens a wave.
+// for 16 tokens a wave. waves: of all tokens; per: of 64 of them.
 template <bool I8, int MATS, int NT>
-__global__ void __launch_bounds__(kThreads) k_w4_join(W4Args a, int splits, int waves) {
+__global__ void __launch_bounds__(kThreads) k_w4_join(W4Args a, int splits, int waves, int per) {
   const int lane = threadIdx.x & 63, at = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
   const int wave = at / NT, t = at - wave * NT;
   if (wave >= waves) return;
+  const int z = wave / per;
   const f4* part = a.part + (size_t(wave) * 2 * NT + t) * 64 + lane;
   const size_t step = size_t(waves) * 2 * NT * 64;
   f4 sum[2][1] = {{{0.f, 0.f, 0.f, 0.f}}, {{0.f, 0.f, 0.f, 0.f}}};
@@ -538,15 +540,16 @@ __global__ void __launch_bounds__(kThreads) k_w4_join(W4Args a, int splits, int 
   for (int sp = 0; sp < splits; ++sp)
 #pragma unroll
     for (int m = 0; m < 2; ++m) sum[m][0] += part[sp * step + m * NT * 64];
-  slab_store<I8, MATS, 1>(a, sum, int64_t(wave) * 16 * (2 / MATS), 16 * t);
+  slab_store<I8, MATS, 1>(a, sum, int64_t(wave - z * per) * 16 * (2 / MATS),
+                          int64_t(z) * kSlabTokens + 16 * t);
 }
 
 // Ranges that the chunks of a product of more than kFew tokens are split into: as many
-// as give every CU a workgroup, for one tile of tokens. Beyond eight they have two
-// batches at least: 4096 -> 4096, 64 tokens, 17.7 us in 8 ranges, 20.5 in 16.
+// as give every CU a workgroup (14336 -> 2 x 4096, 128 tokens: 181 us in one, 60 in
+// four). Beyond eight they have two batches at least: 4096 -> 4096, 64 tokens, 17.7 us in
+// 8 ranges, 20.5 in 16.
 int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out, int mats) {
-  if (n_tok > kSlabTokens) return 1;
-  const int64_t wgs = ceil_div(d_out, slab_rows(mats));
+  const int64_t wgs = ceil_div(d_out, slab_rows(mats)) * ceil_div(n_tok, kSlabTokens);
   const int64_t batches = ceil_div(d, kSlabK);
   return std::max<int64_t>(1, std::min(256 / wgs, std::max(batches / 2, std::min<int64_t>(batches, 8))));
 }
@@ -554,13 +557,15 @@ int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out, int mats) {
 template <bool I8, int MATS, int NT, int GP>
 void launch_slab(const W4Args& a, hipStream_t s) {
   const unsigned wgs = unsigned(ceil_div(a.d_out, slab_rows(MATS)));
+  const unsigned tiles = unsigned(ceil_div(a.n_tok, kSlabTokens));
   const int splits = int(slab_splits(a.n_tok, a.d, a.d_out, MATS));
-  hipLaunchKernelGGL((k_w4_slab<I8, MATS, NT, GP>),
-                     dim3(wgs, unsigned(splits), unsigned(ceil_div(a.n_tok, kSlabTokens))),
+  hipLaunchKernelGGL((k_w4_slab<I8, MATS, NT, GP>), dim3(wgs, unsigned(splits), tiles),
                      dim3(64 * kSlabWaves), 0, s, a);
-  if (splits > 1)
-    hipLaunchKernelGGL((k_w4_join<I8, MATS, NT>), dim3(wgs * kSlabWaves * NT / (kThreads / 64)),
-                       dim3(kThreads), 0, s, a, splits, int(wgs) * kSlabWaves);
+  if (splits > 1) {
+    const unsigned per = wgs * kSlabWaves, waves = per * tiles;
+    hipLaunchKernelGGL((k_w4_join<I8, MATS, NT>), dim3(waves * NT / (kThreads / 64)),
+                       dim3(kThreads), 0, s, a, splits, int(waves), int(per));
+  }
 }
 
 template <bool I8, int MATS, int GP, int ROWS>
@@ -609,12 +614,14 @@ optima_status w4_pack(const void* W, int dtype, int64_t n, int64_t d, int64_t gr
 
 size_t w4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out, int mats) {
   if (n_tok <= kFew) return 0;
-  n_tok = std::min<int64_t>(n_tok, kSlabTokens);  // more are not split
-  const int64_t splits = slab_splits(n_tok, d, d_out, mats);
-  if (splits == 1) return 0;
-  // Sized for 64 tokens, so that it does not shrink with more.
-  return size_t(splits) * size_t(ceil_div(d_out, slab_rows(mats))) * kSlabWaves * 2 * 4 * 64 *
-         sizeof(f4);
+  // The most of any number of tokens up to these, so that more need no less.
+  const int64_t wgs = ceil_div(d_out, slab_rows(mats)), tiles = ceil_div(n_tok, kSlabTokens);
+  int64_t parts = 0;
+  for (int64_t t = 1; t <= std::min(tiles, 128 / wgs); ++t) {
+    const int64_t splits = slab_splits(t * kSlabTokens, d, d_out, mats);
+    if (splits > 1) parts = std::max(parts, splits * t);
+  }
+  return size_t(parts) * size_t(wgs) * kSlabWaves * 2 * (kSlabTokens / 16) * 64 * sizeof(f4);
 }
 
 // With Q2 and s2, act(X deq(Q)^T) o (X deq(Q2)^T).

@@ -145,6 +145,14 @@ def test_gated(L, n, d, n_out, group, x, x_group, gated):
     _run(L, n, d, n_out, group, x, x_group, y="f32", pad=1, gated=gated)
 
 
+# Several workgroups of outputs, several 64 tokens and a split sum at once.
+@pytest.mark.parametrize("n, d, n_out", [(300, 2100, 300), (129, 4096, 520)])
+@pytest.mark.parametrize("group, x, x_group", [(64, "bf16", 0), (64, "i8", 64)])
+@pytest.mark.parametrize("gated", [None, "silu"])
+def test_many_tokens(L, n, d, n_out, group, x, x_group, gated):
+    _run(L, n, d, n_out, group, x, x_group, y="f32", pad=1, gated=gated)
+
+
 def test_wide(L):
     _run(L, 1, 14336, 512, 128, "i8", 128, y="bf16")
     _run(L, 5, 14336, 512, 64, "bf16", 0, y="f32")
