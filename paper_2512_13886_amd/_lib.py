@@ -481,6 +481,15 @@ def _rows(name, t, shape, dtypes):
     return (t.data_ptr() if n else None), ld, _ROW_DTYPES[t.dtype]
 
 
+def _take(name, t, shape, dtypes):
+    """_rows, for a contiguous tensor with fewer questions: a third of its time, of which a
+    call of a decoding step takes several."""
+    dtype = t.dtype
+    if t.is_contiguous() and dtype in dtypes and t.is_cuda and t.shape == shape:
+        return (t.data_ptr() if shape[0] else None), shape[1], _ROW_DTYPES[dtype]
+    return _rows(name, t, shape, dtypes)
+
+
 def _launch_stream(stream):
     """The stream's address, as _stream's. The decoding calls take a few microseconds, of
     which making a Stream object would be two or three."""
@@ -500,10 +509,13 @@ def _addr(t):
 
 
 def _opt_rows(name, t, shape, dtypes):
-    return (None, shape[1], 0) if t is None else _rows(name, t, shape, dtypes)
+    return (None, shape[1], 0) if t is None else _take(name, t, shape, dtypes)
 
 
 def _need_shape(name, t, shape, dtypes):
+    if t is not None and t.is_contiguous() and t.dtype in dtypes and t.is_cuda and \
+            t.shape == shape:
+        return
     _need_cuda(name, t)
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must be one of {dtypes}, got {t.dtype}")
@@ -527,10 +539,10 @@ def optima_rms_norm(X: torch.Tensor, weight: torch.Tensor, Y: torch.Tensor, eps:
     if X.dim() != 2:
         raise ValueError("X must be [n_tok, d]")
     n, d = X.shape
-    x, ldx, dt = _rows("X", X, (n, d), _F)
+    x, ldx, dt = _take("X", X, (n, d), _F)
     r, ldr, _ = _opt_rows("R", R, (n, d), (X.dtype,))
     s, lds, _ = _opt_rows("S", S, (n, d), (X.dtype,))
-    y, ldy, y_dt = _rows("Y", Y, (n, d), (*_F, torch.int8))
+    y, ldy, y_dt = _take("Y", Y, (n, d), (*_F, torch.int8))
     _need_shape("weight", weight, (d,), _F)
     if (Y.dtype == torch.int8) != (scales is not None):
         raise ValueError("scales go with an int8 Y")
@@ -555,10 +567,10 @@ def optima_rms_norm_backward(S: torch.Tensor, weight: torch.Tensor, dY: torch.Te
     if S.dim() != 2:
         raise ValueError("S must be [n_tok, d]")
     n, d = S.shape
-    s, lds, dt = _rows("S", S, (n, d), _F)
-    dy, lddy, _ = _rows("dY", dY, (n, d), (S.dtype,))
+    s, lds, dt = _take("S", S, (n, d), _F)
+    dy, lddy, _ = _take("dY", dY, (n, d), (S.dtype,))
     ds, ldds, _ = _opt_rows("dS", dS, (n, d), (S.dtype,))
-    dx, lddx, _ = _rows("dX", dX, (n, d), (S.dtype,))
+    dx, lddx, _ = _take("dX", dX, (n, d), (S.dtype,))
     _need_shape("weight", weight, (d,), _F)
     nbytes = 0
     if dweight is not None:
@@ -592,8 +604,8 @@ def optima_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, H:
     bfloat16 or float32 [n_tok, d_ff]. G and U (bfloat16) receive the two products, which
     optima_gated_backward takes."""
     n, d, ff = _gated_weights(X, Wg, Wu)
-    x, ldx, _ = _rows("X", X, (n, d), _B)
-    h, ldh, h_dt = _rows("H", H, (n, ff), _F)
+    x, ldx, _ = _take("X", X, (n, d), _B)
+    h, ldh, h_dt = _take("H", H, (n, ff), _F)
     g, ldg, _ = _opt_rows("G", G, (n, ff), _B)
     u, ldu, _ = _opt_rows("U", U, (n, ff), _B)
     need = optima_gated_forward_workspace_bytes(n, d, ff)
@@ -618,10 +630,10 @@ def optima_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G
     bfloat16 or float32 (dWg and dWu of one type, + what they hold with accumulate). Where
     mask_g or mask_u (uint8 [d_ff, d_in]) is 0 the weight's gradient is exactly 0."""
     n, d, ff = _gated_weights(X, Wg, Wu)
-    x, ldx, _ = _rows("X", X, (n, d), _B)
-    g, ldg, _ = _rows("G", G, (n, ff), _B)
-    u, ldu, _ = _rows("U", U, (n, ff), _B)
-    dh, lddh, _ = _rows("dH", dH, (n, ff), _B)
+    x, ldx, _ = _take("X", X, (n, d), _B)
+    g, ldg, _ = _take("G", G, (n, ff), _B)
+    u, ldu, _ = _take("U", U, (n, ff), _B)
+    dh, lddh, _ = _take("dH", dH, (n, ff), _B)
     dx, lddx, dx_dt = _opt_rows("dX", dX, (n, d), _F)
     if (dWg is None) != (dWu is None):
         raise ValueError("dWg and dWu go together")
@@ -668,7 +680,7 @@ def _w4_tokens(X, x_scales, x_group, group):
     if X.dim() != 2:
         raise ValueError("X must be [n_tok, d]")
     n, d = X.shape
-    x, ldx, x_dt = _rows("X", X, (n, d), (torch.bfloat16, torch.int8))
+    x, ldx, x_dt = _take("X", X, (n, d), (torch.bfloat16, torch.int8))
     if (X.dtype == torch.int8) != (x_scales is not None):
         raise ValueError("x_scales go with an int8 X")
     if x_scales is not None:
@@ -702,7 +714,7 @@ def optima_w4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y: 
     n, d, x, ldx, x_dt = _w4_tokens(X, x_scales, x_group, group)
     n_out = Q.shape[0]
     _w4_weights("Q", Q, "scales", scales, n_out, d, group)
-    y, ldy, y_dt = _rows("Y", Y, (n, n_out), _F)
+    y, ldy, y_dt = _take("Y", Y, (n, n_out), _F)
     ws, nbytes = _w4_space(n, d, n_out, 1, ws, X.device, stream)
     _check(_w4_linear(x, ldx, x_dt, _addr(x_scales), int(x_group), n, d, _addr(Q), _addr(scales),
                       int(group), n_out, y, ldy, y_dt, ws, nbytes, _launch_stream(stream)))
@@ -718,7 +730,7 @@ def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Q
     ff = Qg.shape[0]
     _w4_weights("Qg", Qg, "scales_g", scales_g, ff, d, group)
     _w4_weights("Qu", Qu, "scales_u", scales_u, ff, d, group)
-    h, ldh, h_dt = _rows("H", H, (n, ff), _F)
+    h, ldh, h_dt = _take("H", H, (n, ff), _F)
     ws, nbytes = _w4_space(n, d, ff, 2, ws, X.device, stream)
     _check(_w4_gated(x, ldx, x_dt, _addr(x_scales), int(x_group), n, d, _addr(Qg), _addr(scales_g),
                      _addr(Qu), _addr(scales_u), int(group), ff, int(act), h, ldh, h_dt, ws,
