@@ -183,6 +183,33 @@ def test_backward(L, n, d, ff, masked):
     _backward(L, n, d, ff, name="none", dx="f32", dw="f32", masked=masked)
 
 
+@pytest.mark.parametrize("n", [3, 200, 2000])
+def test_backward_nonfinite_under_masks(L, n):
+    # NaN and infinity where the masks are 0 leave no trace in the weights' gradients.
+    gen = torch.Generator(device=dev()).manual_seed(n)
+    X, Wg, Wu = (_rows(gen, r, 100) for r in (n, 150, 150))
+    G, V, dH = (_rows(gen, n, 150) for _ in range(3))
+    masks = [(torch.rand(150, 100, generator=gen, device=dev()) < 0.5).to(torch.uint8)
+             for _ in range(2)]
+    for m in masks:
+        m[10] = 0  # a row with nothing left
+        m[:, 5] = 0
+    outs = []
+    for bad in (False, True):
+        x, dh = X.clone(), dH.clone()
+        if bad:
+            x[n - 1, 5] = float("inf")
+            dh[0, 10] = float("nan")
+        dX = torch.empty(n, 100, device=dev())
+        dWg, dWu = (torch.full((150, 100), float("nan"), device=dev()) for _ in range(2))
+        L.optima_gated_backward(x, Wg, Wu, G, V, dh, dX=dX, dWg=dWg, dWu=dWu, mask_g=masks[0],
+                                mask_u=masks[1])
+        outs.append((dX, dWg, dWu))
+    for ref, got in zip(outs[0][1:], outs[1][1:]):
+        assert torch.equal(ref, got) and not bool(got[10].any()) and not bool(got[:, 5].any())
+    assert bool(outs[1][0][0].isnan().all()) and torch.equal(outs[0][0][1:], outs[1][0][1:])
+
+
 # Products that take the large tile, one of the two or both, and long sums over few
 # outputs.
 @pytest.mark.parametrize("n, d, ff", [(2300, 2100, 300), (4096, 64, 2048), (600, 128, 5000)])
