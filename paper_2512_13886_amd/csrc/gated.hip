@@ -135,15 +135,15 @@ __global__ void __launch_bounds__(64 * few_waves(MATS)) k_gated_few(GatedArgs a)
     }
   }
   if (a.d % 64 && wave == pieces % waves) {  // the rest, by the wave whose turn it is
-    const int k = 64 * pieces + 16 * q, left = int(a.d) - k;
+    const int k = 64 * pieces + 16 * q, d = int(a.d);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       Raw8<bf16_t> rw[MATS], rx;
 #pragma unroll
-      for (int m = 0; m < MATS; ++m) load_upto8(rw[m], w[m] + k + 8 * e, left - 8 * e);
+      for (int m = 0; m < MATS; ++m) load_piece(rw[m], w[m], k + 8 * e, d);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        load_upto8(rx, x[t] + k + 8 * e, left - 8 * e);
+        load_piece(rx, x[t], k + 8 * e, d);
 #pragma unroll
         for (int m = 0; m < MATS; ++m) acc[m][t] = few_mfma(rx, rw[m], acc[m][t]);
       }
@@ -324,8 +324,7 @@ __device__ inline void pad_rows(const PadRows& a, int64_t block) {
   const int64_t per = a.pitch / 8, r = i / per, c = 8 * (i - r * per);
   if (r >= a.rows_out) return;
   Raw8<bf16_t> v;
-  const int64_t left = r < a.rows ? a.cols - c : 0;
-  load_upto8(v, a.src + r * a.ld + c, int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
+  load_piece(v, a.src + r * a.ld, int(c), r < a.rows ? int(a.cols) : 0);
   *reinterpret_cast<u32x4*>(a.dst + r * a.pitch + c) = v.w;
 }
 
@@ -361,9 +360,7 @@ __device__ inline void transpose_tile(const Transpose& a, int block, uint16_t* t
   for (int k = 0; k < 2; ++k) {
     const int p = threadIdx.x + k * kThreads, r = p >> 3, c = 8 * (p & 7);
     Raw8<bf16_t> v;
-    const int64_t left = r0 + r < a.rows ? a.cols - c0 - c : 0;
-    load_upto8(v, a.src + (r0 + r) * a.ld + c0 + c,
-               int(std::max<int64_t>(std::min<int64_t>(left, 8), 0)));
+    load_piece(v, a.src + (r0 + r) * a.ld, int(c0) + c, r0 + r < a.rows ? int(a.cols) : 0);
     tr_put(tile, r, c, v.w);
   }
   __syncthreads();
@@ -395,11 +392,11 @@ __device__ inline void gate_grad_tile(const GateGradArgs& a, int block,
   for (int k = 0; k < 2; ++k) {
     const int i = threadIdx.x + k * kThreads, r = i >> 3, c = 8 * (i & 7);
     const int64_t t = t0 + r, f = f0 + c;
-    const int left = int(std::max<int64_t>(std::min<int64_t>(t < a.n_tok ? a.ff - f : 0, 8), 0));
+    const int ff = t < a.n_tok ? int(a.ff) : 0;
     Raw8<bf16_t> rg, ru, rh;
-    load_upto8(rg, a.g + t * a.ldg + f, left);
-    load_upto8(ru, a.u + t * a.ldu + f, left);
-    load_upto8(rh, a.dh + t * a.lddh + f, left);
+    load_piece(rg, a.g + t * a.ldg, int(f), ff);
+    load_piece(ru, a.u + t * a.ldu, int(f), ff);
+    load_piece(rh, a.dh + t * a.lddh, int(f), ff);
     float g[8], u[8], dh[8], dg[8], du[8];
     values8(rg, g);
     values8(ru, u);

@@ -68,13 +68,6 @@ __device__ inline void load_some(Raw8<float>& r, const float* p, int n) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.w[i >> 2][i & 3] = i < n ? __float_as_uint(p[i]) : 0u;
 }
-template <typename T>
-__device__ inline void load_upto8(Raw8<T>& r, const T* p, int n) {
-  if (n >= 8)
-    load8(r, p);
-  else
-    load_some(r, p, n);
-}
 
 // Eight values moved down by s (0 .. 7) places, zeros from above.
 __device__ inline void shift_down(Raw8<bf16_t>& r, int s) {
@@ -97,7 +90,9 @@ __device__ inline void shift_down(Raw8<float>& r, int s) {
   }
 }
 // Values at .. at + 7 of a row of d; zeros past its end. A row's last piece is loaded
-// from eight values before its end, and moved: one wide load like the others.
+// from eight values before its end, and moved: one wide load like the others (value by
+// value, each load waits for the one before: 8.4 us in place of 6.3 for the preparation of
+// the gated gradient at 192 tokens, 64 -> 335).
 template <typename T>
 __device__ inline void load_piece(Raw8<T>& r, const T* row, int at, int d) {
   if (at + 8 <= d) {

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kThreads) k_w4_pack(const T* W, int64_t total,
   const int i = threadIdx.x & 15;
   const int k = c * kChunk + 8 * i;
   Raw8<T> raw;
-  load_upto8(raw, W + n * d + k, live ? d - k : 0);
+  load_piece(raw, W + n * d, k, live ? d : 0);
   float w[8];
   values8(raw, w);
   uint32_t m = 0;
@@ -144,8 +144,12 @@ template <>
 struct XFrag<false> {
   bf16x8 v;
   __device__ inline void load(const void* row, int k, int left) {
+    const bf16_t* p = static_cast<const bf16_t*>(row) + k;
     Raw8<bf16_t> r;
-    load_upto8(r, static_cast<const bf16_t*>(row) + k, left);
+    if (left >= 8)
+      load8(r, p);
+    else
+      load_some(r, p, left);
     v = __builtin_bit_cast(bf16x8, r.w);
   }
 };
@@ -155,12 +159,16 @@ struct XFrag<true> {
   __device__ inline void load(const void* row, int k, int left) {
     const uint8_t* p = static_cast<const uint8_t*>(row) + k;
     u32x2 r = {0, 0};
-    if (left >= 8)
+    if (left >= 8) {
       r = *reinterpret_cast<const u32x2_1*>(p);
-    else
+    } else if (left > 0 && k + left >= 8) {  // the row's last eight, moved down
+      r = *reinterpret_cast<const u32x2_1*>(p + left - 8);
+      r = __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, r) >> (8 * (8 - left)));
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (i < left) r[i >> 2] |= uint32_t(p[i]) << (8 * (i & 3));
+    }
     v = order_i8(r);
   }
 };
