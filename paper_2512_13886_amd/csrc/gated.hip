@@ -828,16 +828,18 @@ GatedPlan plan_gated(int64_t n_tok, int64_t d, int64_t ff) {
 
 // Whether the weights are streamed once for all tokens, or tiles take them. Streamed
 // they come at 6 TB/s, and every 16 outputs read all tokens again, at 10 TB/s out of
-// the caches; with few outputs a workgroup's own way through d is what counts. To tiles
+// the caches; with few outputs a CU's workgroups' own way through d is what counts. To tiles
 // they come at 5.5 TB/s at most, and rows that do not suit them are copied first. Measured,
 // streamed against tiles: 4096 -> 14336, 4 tokens 39 to 42 us, 16 tokens 49 to 43, 64 tokens
-// 91 to 45; 1024 -> 8192, 32 tokens 10.7 to 12.2, 64 tokens 15.1 to 13.1; 4096 -> 2048, 16
-// tokens 11 to 17, 64 tokens 26 to 17; 1001 -> 2731, 64 tokens 17 to 21.
+// 91 to 45; 1024 -> 8192, 32 tokens 10.7 to 12.2, 64 tokens 15.1 to 13.1; 2048 -> 5632, 32
+// tokens 18 to 20, 64 tokens 25 to 20; 4096 -> 2048, 16 tokens 11 to 17, 64 tokens 26 to 17;
+// 1001 -> 2731, 64 tokens 17 to 21.
 bool few_tokens(int64_t n_tok, int64_t d, int64_t ff) {
   if (n_tok > kFewTokens) return false;
   const double weights = 4e-6 * double(d) * double(ff);  // MB
+  const int64_t rounds = ceil_div(ff, 16 * kCus);
   const double streamed = std::max(weights / 6 + double(n_tok) * weights / 320,
-                                   4 + double(n_tok) * double(d) / 13000);
+                                   4 + double(rounds * n_tok * d) / 13000);
   const double tiles = std::max(plan_gated(kFewTokens, d, ff).us, weights / 5.5 + 1);
   return streamed <= tiles + (d % 64 ? 2 * weights / 5 + 4 : 0);
 }

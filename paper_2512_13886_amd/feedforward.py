@@ -125,16 +125,19 @@ def prune_feedforward(block: FeedForward, X: torch.Tensor, R: torch.Tensor | Non
 
 
 def gradients(block: FeedForward, masks: dict, Y_dense: torch.Tensor, X: torch.Tensor,
-              R: torch.Tensor | None = None):
+              R: torch.Tensor | None = None, down_t: torch.Tensor | None = None):
     """(loss, gradients by name) of loss = mean over tokens of |y - y_dense|^2 / 2 in the
-    norm's weight and the kept entries of gate and up; float32, exactly 0 elsewhere."""
+    norm's weight and the kept entries of gate and up; float32, exactly 0 elsewhere.
+    down_t: block.down transposed, for callers that have it."""
     n, d = X.shape
     dev = X.device
     t = hidden(block, X, R)
     Y, err = _down(t.H, block.down, Y_dense)
     dY = Y.sub_(Y_dense).div_(n).bfloat16()
     dH = torch.empty_like(t.H)
-    L.optima_linear_forward(dY, block.down.t().contiguous(), Y=dH)
+    if down_t is None:
+        down_t = block.down.t().contiguous()
+    L.optima_linear_forward(dY, down_t, Y=dH)
     g = {"gate": torch.empty_like(block.gate), "up": torch.empty_like(block.up),
          "norm": torch.empty_like(block.norm)}
     dA = torch.empty((n, d), dtype=torch.bfloat16, device=dev)
@@ -156,9 +159,10 @@ def recover(block: FeedForward, masks: dict, Y_dense: torch.Tensor, X: torch.Ten
     params = {name: getattr(out, name) for name in ("norm", "gate", "up")}
     first = {k: torch.zeros_like(p) for k, p in params.items()}
     second = {k: torch.zeros_like(p) for k, p in params.items()}
+    down_t = block.down.t().contiguous()
     losses = []
     for step in range(1, steps + 1):
-        loss, g = gradients(out, masks, Y_dense, X, R)
+        loss, g = gradients(out, masks, Y_dense, X, R, down_t)
         losses.append(loss)
         for k, p in params.items():
             first[k].lerp_(g[k], 1 - betas[0])

@@ -262,3 +262,13 @@ def test_rows_takes_any_pitch_and_refuses_what_is_no_rows():
         _lib._rows("t", Fake((3, 4), (9, 1)), (3, 5), b)
     with pytest.raises(ValueError):
         _lib._rows("t", Fake((3, 5), (9, 1)), (3, 5), (torch.float32,))
+
+
+@pytest.mark.parametrize("d, ff", [(4032, 83), (300, 9000), (1001, 2731), (4096, 14336), (1, 1)])
+def test_more_tokens_need_no_less_workspace(d, ff):
+    import paper_2512_13886_amd as L
+    for query in (L.optima_gated_forward_workspace_bytes,
+                  lambda *a: L.optima_w4_workspace_bytes(*a, 1),
+                  lambda *a: L.optima_w4_workspace_bytes(*a, 2)):
+        need = [query(n, d, ff) for n in [*range(600), 1000, 4096, 4097, 100000]]
+        assert all(a <= b for a, b in zip(need, need[1:]))
