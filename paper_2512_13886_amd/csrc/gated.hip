@@ -47,6 +47,15 @@ struct GatedArgs {
   int h_f32, act;
   int splits;   // ranges of the sum over d (k_gated_ring) ..
   float* part;  // .. whose parts go here: [split][tile][128][g: 64, u: 64]
+  // The outputs from n on.
+  void skip(int64_t n) {
+    wg += 2 * n * ldw;
+    wu += 2 * n * ldw;
+    h = static_cast<char*>(h) + (h_f32 ? 4 : 2) * n;
+    if (g) g += n;
+    if (u) u += n;
+    ff -= n;
+  }
 };
 
 // Four or eight consecutive outputs of a token from their sums g and u.
@@ -804,24 +813,37 @@ optima_status grad_products(GradPair& p, float* part, hipStream_t s) {
   return OPTIMA_OK;
 }
 
-// The tile of the forward product and how often its sum is split, by what the rounds
-// over the CUs should take: 1.4 us a stage and 6 around them for 256 tokens x 128 outputs,
-// 0.56 and 3.5 for 128 x 64, 3 us and 5 TB/s for the join.
+// The tiles of the forward product: the first `wide` outputs take 256 tokens x 128
+// outputs, the others 128 x 64, with the sum in `splits` ranges where they are all. By what
+// the rounds over the CUs should take: 1.4 us a stage and 6 around them for the large tile,
+// 0.56 and 3.5 for the small one, 3 us and 5 TB/s for the join. Small tiles after whole
+// rounds of large ones take 4 us and 1.3 times that, since one launch ends before the other
+// begins, and are worth it from 7 % on: 2048 -> 5632, 1500 tokens 104 us in two rounds, 83
+// in one and small tiles; 1984 -> 12529, 700 tokens 115 and 93; but 4096 -> 14336, 2500
+// tokens 532 and 547.
 struct GatedPlan {
-  bool wide;
+  int64_t wide;
   int splits;
   double us;
 };
 GatedPlan plan_gated(int64_t n_tok, int64_t d, int64_t ff) {
   const int64_t stages = ceil_div(d, 64);
-  const int64_t wide = ceil_div(n_tok, 256) * ceil_div(ff, 128);
+  const double large_us = 1.4 * double(stages) + 6, small_us = 0.56 * double(stages) + 3.5;
+  const int64_t rows = ceil_div(n_tok, 256), cols = ceil_div(ff, 128);
+  GatedPlan best{ff, 1, double(ceil_div(rows * cols, kCus)) * large_us};
+  const int64_t rounds = rows * cols / kCus, whole = rounds * kCus / rows;
+  if (rounds && whole < cols) {
+    const int64_t rest = ceil_div(n_tok, 128) * ceil_div(ff - 128 * whole, 64);
+    const double us = double(rounds) * large_us + 1.3 * double(ceil_div(rest, kCus)) * small_us + 4;
+    if (us < 0.93 * best.us) best = GatedPlan{128 * whole, 1, us};
+  }
   const int64_t small = ceil_div(n_tok, 128) * ceil_div(ff, 64);
-  GatedPlan best{true, 1, double(ceil_div(wide, kCus)) * (1.4 * double(stages) + 6)};
   for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
     if (splits > stages || (splits > 1 && splits * small > kPartTiles)) break;
-    const double us = double(ceil_div(small * splits, kCus)) * (0.56 * double(ceil_div(stages, splits)) + 3.5) +
+    const double range = 0.56 * double(ceil_div(stages, splits)) + 3.5;
+    const double us = double(ceil_div(small * splits, kCus)) * range +
                       (splits > 1 ? 3 + double(small) * splits * 131072 / 5e6 : 0);
-    if (us < best.us) best = GatedPlan{false, splits, us};
+    if (us < best.us) best = GatedPlan{0, splits, us};
   }
   return best;
 }
@@ -951,10 +973,14 @@ optima_status gated_forward(const void* X, int64_t ldx, int64_t n_tok, int64_t d
   a.splits = plan.splits;
   a.part = l.part;
   if (plan.wide) {
-    const int64_t tiles = ceil_div(n_tok, 256) * ceil_div(ff, 128);
-    hipLaunchKernelGGL(k_gated256, dim3(unsigned(tiles)), dim3(Tile256::kThreads), 0, s, a);
-  } else {
-    const int64_t tiles = ceil_div(n_tok, 128) * ceil_div(ff, 64);
+    GatedArgs w = a;
+    w.ff = plan.wide;
+    const int64_t tiles = ceil_div(n_tok, 256) * ceil_div(w.ff, 128);
+    hipLaunchKernelGGL(k_gated256, dim3(unsigned(tiles)), dim3(Tile256::kThreads), 0, s, w);
+  }
+  if (plan.wide < ff) {
+    a.skip(plan.wide);
+    const int64_t tiles = ceil_div(n_tok, 128) * ceil_div(a.ff, 64);
     hipLaunchKernelGGL(k_gated_ring, dim3(unsigned(tiles * plan.splits)), dim3(Ring128::kThreads), 0,
                        s, a);
     if (plan.splits > 1)

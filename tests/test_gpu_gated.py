@@ -108,6 +108,13 @@ def test_large_tiles(L, n, d, ff):
     _forward(L, n, d, ff, out="f32", saved=False)
 
 
+# Whole rounds of large tiles and small ones for the outputs that are left.
+@pytest.mark.parametrize("n, d, ff", [(1500, 1000, 5632), (700, 960, 12529)])
+def test_both_tiles(L, n, d, ff):
+    _forward(L, n, d, ff, saved=True)
+    _forward(L, n, d, ff, out="f32", saved=False)
+
+
 def test_aligned_pitch_is_read_in_place(L):
     # A row pitch that suits wide loads, and one that does not, give the same bits.
     g = torch.Generator(device=dev()).manual_seed(1)
