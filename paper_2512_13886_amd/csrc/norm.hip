@@ -194,7 +194,8 @@ __global__ void __launch_bounds__(RowGroup<THREADS>::kWg) k_rms_norm(NormArgs a)
 struct NormGradArgs {
   const void *s, *w, *dy, *ds;
   void* dx;
-  float* part;  // [blocks][d] sums of dy xh, or NULL
+  float* part;  // [blocks][d] sums of dy xh, or NULL; of one block, dw itself
+  int add;      // .. to which they are added
   int64_t n, lds, lddy, ldds, lddx;
   int d, w_bf16;
   float eps;
@@ -294,7 +295,16 @@ __global__ void __launch_bounds__(RowGroup<THREADS>::kWg) k_rms_norm_grad(NormGr
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int at = 8 * (t + c * THREADS);
-    store_upto8(a.part + size_t(blockIdx.x) * size_t(a.d) + at, dw[c], a.d - at);
+    float* part = a.part + size_t(blockIdx.x) * size_t(a.d);
+    if (a.add) {
+      Raw8<float> was;
+      load_piece(was, part, at, a.d);
+      float old[8];
+      values8(was, old);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dw[c][i] += old[i];
+    }
+    store_upto8(part + at, dw[c], a.d - at);
   }
 }
 
@@ -368,12 +378,17 @@ void launch_norm(NormArgs a, hipStream_t s) {
   });
 }
 
+// Rows that one workgroup takes one after the other, so that it has dw by itself and
+// nothing has to be joined: d = 2048, one row 4.7 to 2.6 us, two rows 4.7 to 3.5, but four
+// 4.7 to 5.1.
+constexpr int64_t kOneBlock = 2;
 // Workgroups of the gradient, by the sizes alone, so that the order of dw's sums is too.
 // 128 million bf16 values, with 256, 512, 1024 and 2048 of them: d = 1024 218, 196, 205 and
 // 209 us, d = 4096 230, 193, 212 and 220.
 int grad_blocks(int64_t n, int64_t d) {
   int64_t rows = 0;
   grad_by_width(d, [&](auto threads, auto) { rows = RowGroup<decltype(threads)::value>::kRows; });
+  if (n > 0 && n <= kOneBlock * rows) return 1;
   return int(std::min<int64_t>(ceil_div(n, rows), d <= 2048 ? 1024 : d <= 8192 ? 512 : 256));
 }
 
@@ -408,8 +423,9 @@ optima_status rms_norm_backward(const void* S, int64_t lds, const void* w, int w
                                 float* dweight, int accumulate, void* ws, hipStream_t s) {
   const int blocks = grad_blocks(n, d);
   if (n > 0) {
-    NormGradArgs a{S, w, dY, dS, dX, dweight ? static_cast<float*>(ws) : nullptr, n, lds, lddy,
-                   ldds, lddx, int(d), w_dtype == OPTIMA_DTYPE_BF16, eps};
+    float* part = blocks == 1 ? dweight : static_cast<float*>(ws);
+    NormGradArgs a{S, w, dY, dS, dX, dweight ? part : nullptr, blocks == 1 && accumulate, n, lds,
+                   lddy, ldds, lddx, int(d), w_dtype == OPTIMA_DTYPE_BF16, eps};
     grad_by_width(d, [&](auto threads, auto ch) {
       constexpr int kT = decltype(threads)::value, kCh = decltype(ch)::value;
       const dim3 wg(RowGroup<kT>::kWg);
@@ -420,7 +436,7 @@ optima_status rms_norm_backward(const void* S, int64_t lds, const void* w, int w
     });
     OPTIMA_LAUNCH_CHECK();
   }
-  if (dweight) {
+  if (dweight && blocks != 1) {
     hipLaunchKernelGGL(k_norm_dw, dim3(unsigned(ceil_div(d, 64))), dim3(1024), 0, s,
                        static_cast<const float*>(ws), blocks, int(d), dweight, accumulate);
     OPTIMA_LAUNCH_CHECK();

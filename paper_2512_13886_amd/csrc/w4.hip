@@ -555,10 +555,12 @@ __global__ void __launch_bounds__(kThreads) k_w4_join(W4Args a, int splits, int 
 // Ranges that the chunks of a product of more than kFew tokens are split into: as many
 // as give every CU a workgroup (14336 -> 2 x 4096, 128 tokens: 181 us in one, 60 in
 // four). Beyond eight they have two batches at least: 4096 -> 4096, 64 tokens, 17.7 us in
-// 8 ranges, 20.5 in 16.
+// 8 ranges, 20.5 in 16. Two batches of up to 32 tokens stay whole: 512 -> 2048, 17 tokens,
+// 6.8 us and 7.4.
 int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out, int mats) {
   const int64_t wgs = ceil_div(d_out, slab_rows(mats)) * ceil_div(n_tok, kSlabTokens);
   const int64_t batches = ceil_div(d, kSlabK);
+  if (batches <= 2 && n_tok <= 32) return 1;
   return std::max<int64_t>(1, std::min(256 / wgs, std::max(batches / 2, std::min<int64_t>(batches, 8))));
 }
 
