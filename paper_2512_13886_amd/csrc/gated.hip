@@ -96,7 +96,38 @@ __device__ inline f4 few_mfma(const Raw8<bf16_t>& x, const Raw8<bf16_t>& w, cons
                                                  __builtin_bit_cast(bf16x8, w.w), acc, 0, 0, 0);
 }
 
-template <int MATS, int NT>
+// 16 values of a row. Where ODD, rows may lie at odd elements: a 16-byte load whose address
+// is no multiple of 4 is slow, so that these are loaded from one element earlier, and moved
+// (4097 -> 14336: one token 95 us as they lie, 51 moved, 64 tokens 295 and 139; 1001 ->
+// 2731, 13 tokens 10.4 and 7.5). Kernels with more waves to wait for gained nothing.
+template <bool ODD>
+struct FewRaw {
+  Raw8<bf16_t> half[2];
+  uint32_t last;
+  __device__ inline void load(const bf16_t* p, int shift) {
+    if (ODD) {
+      last = p[15].bits;
+      p -= shift / 16;
+    }
+    load8(half[0], p);
+    load8(half[1], p + 8);
+  }
+  __device__ inline Raw8<bf16_t> get(int e, int shift) const {
+    if (!ODD) return half[e];
+    const u32x4 w = half[e].w;
+    const uint32_t next = e == 0 ? half[1].w[0] : last;
+    return Raw8<bf16_t>{u32x4{__builtin_amdgcn_alignbit(w[1], w[0], shift),
+                              __builtin_amdgcn_alignbit(w[2], w[1], shift),
+                              __builtin_amdgcn_alignbit(w[3], w[2], shift),
+                              __builtin_amdgcn_alignbit(next, w[3], shift)}};
+  }
+};
+// Bits by which a row's values are moved. The element before the first row is not there.
+__device__ inline int row_shift(const bf16_t* row, int64_t index) {
+  return index > 0 && (reinterpret_cast<uintptr_t>(row) & 2) ? 16 : 0;
+}
+
+template <int MATS, int NT, bool ODD>
 __global__ void __launch_bounds__(64 * few_waves(MATS)) k_gated_few(GatedArgs a) {
   constexpr int kBatch = few_batch(NT), kOut = 8 * MATS;
   __shared__ float part[few_waves(MATS)][MATS][NT][4][64];
@@ -109,9 +140,15 @@ __global__ void __launch_bounds__(64 * few_waves(MATS)) k_gated_few(GatedArgs a)
   for (int m = 0; m < MATS; ++m)
     w[m] = reinterpret_cast<const bf16_t*>((MATS == 1 ? i >= 8 : m) ? a.wu : a.wg) + n * a.ldw;
   const bf16_t* x[NT];
+  int shift_w[MATS], shift_x[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-    x[t] = reinterpret_cast<const bf16_t*>(a.x) + std::min<int64_t>(16 * t + i, a.n_tok - 1) * a.ldx;
+  for (int m = 0; m < MATS; ++m) shift_w[m] = row_shift(w[m], n);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int64_t tok = std::min<int64_t>(16 * t + i, a.n_tok - 1);
+    x[t] = reinterpret_cast<const bf16_t*>(a.x) + tok * a.ldx;
+    shift_x[t] = row_shift(x[t], tok);
+  }
   f4 acc[MATS][NT];
 #pragma unroll
   for (int m = 0; m < MATS; ++m)
@@ -119,18 +156,15 @@ __global__ void __launch_bounds__(64 * few_waves(MATS)) k_gated_few(GatedArgs a)
     for (int t = 0; t < NT; ++t) acc[m][t] = f4{0.f, 0.f, 0.f, 0.f};
   const int pieces = int(a.d / 64);  // whole ones
   for (int c0 = wave; c0 < pieces; c0 += waves * kBatch) {
-    Raw8<bf16_t> rw[kBatch][MATS][2], rx[kBatch][NT][2];
+    FewRaw<ODD> rw[kBatch][MATS], rx[kBatch][NT];
 #pragma unroll
     for (int v = 0; v < kBatch; ++v) {
       const int k = 64 * (c0 + v * waves) + 16 * q;
       if (c0 + v * waves >= pieces) break;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
+      for (int m = 0; m < MATS; ++m) rw[v][m].load(w[m] + k, shift_w[m]);
 #pragma unroll
-        for (int m = 0; m < MATS; ++m) load8(rw[v][m][e], w[m] + k + 8 * e);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) load8(rx[v][t][e], x[t] + k + 8 * e);
-      }
+      for (int t = 0; t < NT; ++t) rx[v][t].load(x[t] + k, shift_x[t]);
     }
 #pragma unroll
     for (int v = 0; v < kBatch; ++v) {
@@ -140,7 +174,8 @@ __global__ void __launch_bounds__(64 * few_waves(MATS)) k_gated_few(GatedArgs a)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int m = 0; m < MATS; ++m) acc[m][t] = few_mfma(rx[v][t][e], rw[v][m][e], acc[m][t]);
+          for (int m = 0; m < MATS; ++m)
+            acc[m][t] = few_mfma(rx[v][t].get(e, shift_x[t]), rw[v][m].get(e, shift_w[m]), acc[m][t]);
     }
   }
   if (a.d % 64 && wave == pieces % waves) {  // the rest, by the wave whose turn it is
@@ -188,8 +223,11 @@ template <int MATS, int NT>
 void launch_few(const GatedArgs& a, hipStream_t s) {
   // Enough pieces for sixteen waves to have a batch each.
   const int waves = MATS == 1 && a.d >= 2048 ? 16 : 8;
-  hipLaunchKernelGGL((k_gated_few<MATS, NT>), dim3(unsigned(ceil_div(a.ff, 8 * MATS))),
-                     dim3(64 * waves), 0, s, a);
+  const dim3 grid(unsigned(ceil_div(a.ff, 8 * MATS))), block(64 * waves);
+  if (a.ldw % 2 || (a.n_tok > 1 && a.ldx % 2))
+    hipLaunchKernelGGL((k_gated_few<MATS, NT, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((k_gated_few<MATS, NT, false>), grid, block, 0, s, a);
 }
 
 // ---------------------------------------------------------------------------
@@ -855,7 +893,7 @@ GatedPlan plan_gated(int64_t n_tok, int64_t d, int64_t ff) {
 // streamed against tiles: 4096 -> 14336, 4 tokens 39 to 42 us, 16 tokens 49 to 43, 64 tokens
 // 91 to 45; 1024 -> 8192, 32 tokens 10.7 to 12.2, 64 tokens 15.1 to 13.1; 2048 -> 5632, 32
 // tokens 18 to 20, 64 tokens 25 to 20; 4096 -> 2048, 16 tokens 11 to 17, 64 tokens 26 to 17;
-// 1001 -> 2731, 64 tokens 17 to 21.
+// 1001 -> 2731, 64 tokens 13 to 21.
 bool few_tokens(int64_t n_tok, int64_t d, int64_t ff) {
   if (n_tok > kFewTokens) return false;
   const double weights = 4e-6 * double(d) * double(ff);  // MB

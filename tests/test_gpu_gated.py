@@ -143,6 +143,28 @@ def test_nonfinite_stays_in_its_rows(L, n):
     assert bool(H[n - 1].isnan().all()) and not bool(H[:, 149].isfinite().any())
 
 
+@pytest.mark.parametrize("n, xpitch", [(2, 257), (20, 257), (40, 259), (64, 258)])
+def test_odd_rows_leave_their_neighbours_alone(L, n, xpitch):
+    # Rows at odd elements may be read from the element before: it belongs to another row.
+    g = torch.Generator(device=dev()).manual_seed(n)
+    d, ff = 257, 40
+    wide = torch.full((n, xpitch), float("nan"), dtype=torch.bfloat16, device=dev())
+    X = wide[:, :d]
+    X.copy_(_rows(g, n, d))
+    Wg, Wu = _rows(g, ff, d), _rows(g, ff, d)
+    ref, H = (torch.empty(n, ff, device=dev()) for _ in range(2))
+    L.optima_gated_forward(X, Wg, Wu, ref)
+    _check_forward(X, Wg, Wu, "silu", ref, None, None, "f32")
+    X[0, d - 1] = float("nan")
+    Wg[3, d - 1] = float("inf")
+    Wu[8, d - 1] = float("nan")
+    L.optima_gated_forward(X, Wg, Wu, H)
+    rest = [i for i in range(ff) if i not in (3, 8)]
+    assert torch.equal(H[1:, rest], ref[1:, rest])
+    assert bool(H[0].isnan().all()) and bool(H[:, 8].isnan().all())
+    assert not bool(H[:, 3].isfinite().any())
+
+
 def _backward(L, n, d, ff, name="silu", dx="bf16", dw="bf16", masked=False, pad=0, seed=0):
     gen = torch.Generator(device=dev()).manual_seed(seed + n * 7 + d * 3 + ff)
     X = _rows(gen, n, d, d + pad, off=pad)
