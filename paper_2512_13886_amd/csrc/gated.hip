@@ -236,8 +236,8 @@ void launch_few(const GatedArgs& a, hipStream_t s) {
 
 // 256 tokens x 128 outputs on the 256 x 256 tile: half B0 holds rows of Wg, half
 // B1 the same rows of Wu, so quadrants (qa, 0) and (qa, 1) of a lane are g and u of
-// the same outputs. Bound by MFMA: 8192 tokens, 4096 -> 14336, g and u kept, 1419 us,
-// 1.36 PFLOP/s.
+// the same outputs. Bound by MFMA: 8192 tokens, 4096 -> 14336, g and u kept, 1430 us,
+// 1.35 PFLOP/s.
 __global__ void __launch_bounds__(Tile256::kThreads) k_gated256(GatedArgs a) {
   __shared__ __attribute__((aligned(1024))) char l0[Tile256::kHalfBytes];
   __shared__ __attribute__((aligned(1024))) char l1[Tile256::kHalfBytes];
