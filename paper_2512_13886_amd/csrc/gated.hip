@@ -10,6 +10,7 @@
 //   dX = [dG dU] [Wg; Wu],  [dWg; dWu] = [dG dU]^T X  (o masks).
 // P = [dG dU] is rounded to bf16, the type that the matrix instructions take.
 #include "common.h"
+#include "gated_plan.h"
 #include "gemm128.h"
 #include "gemm256.h"
 #include "gemm_core.h"
@@ -17,9 +18,6 @@
 
 namespace optima {
 namespace {
-
-constexpr int kFewTokens = 64;
-constexpr int64_t kCus = 256;
 
 __device__ inline int cdiv(int64_t a, int b) { return int((a + b - 1) / b); }
 
@@ -774,57 +772,8 @@ __global__ void __launch_bounds__(kThreads) k_grad_join(GradPair p, int side, in
   grad_store<4>(a.out, row, col, v);
 }
 
-// Partial sums of at most kPartTiles 128 x 128 tiles.
-constexpr int64_t kPartTiles = 512;
-
-// Microseconds that n[0] blocks of c[0] and then n[1] of c[1] each take over the CUs,
-// the longer ones first.
-double grad_makespan(const int64_t (&n)[2], const double (&c)[2], int first) {
-  const int64_t n1 = n[first], n2 = n[1 - first];
-  const double c1 = c[first], c2 = c[1 - first];
-  const int64_t q = n1 / kCus, r = n1 % kCus;
-  if (r == 0) return double(q) * c1 + double(ceil_div(n2, kCus)) * c2;
-  const int64_t light = kCus - r, room = light * int64_t(c1 / c2);
-  if (n2 <= room)
-    return std::max(double(q + 1) * c1, double(q) * c1 + double(ceil_div(n2, light)) * c2);
-  return double(q + 1) * c1 + double(ceil_div(n2 - room, kCus)) * c2;
-}
-
-// The tiles of both products over the CUs, and how often their sums are split, by the
-// time the plan should take: 1.4 us a stage and 6 around them for a 256 x 256 tile, 0.56
-// and 3.5 for a 128 x 128 one, 3 us and 5 TB/s for the join.
-struct GradPlan {
-  int side, splits[2], first;
-};
-GradPlan plan_grad(const GradArgs (&a)[2]) {
-  GradPlan best{256, {1, 1}, 0};
-  double best_us = 1e30;
-  for (const int side : {256, 128}) {
-    const double stage = side == 256 ? 1.4 : 0.56, around = side == 256 ? 6 : 3.5;
-    const int64_t most = kPartTiles * 16384 / (side * side);
-    int64_t tiles[2];
-    for (int k = 0; k < 2; ++k) tiles[k] = ceil_div(a[k].rows, side) * ceil_div(a[k].out.cols, side);
-    for (const int sx : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32})
-      for (const int sw : {1, 2, 3, 4}) {
-        const int64_t parts = (sx > 1 ? sx * tiles[0] : 0) + (sw > 1 ? sw * tiles[1] : 0);
-        if (parts > most || (sx > 1 && sx > a[0].stages) || (sw > 1 && sw > a[1].stages)) continue;
-        const int64_t n[2] = {tiles[0] * sx, tiles[1] * sw};
-        const double c[2] = {stage * double(ceil_div(a[0].stages, sx)) + around,
-                             stage * double(ceil_div(a[1].stages, sw)) + around};
-        const int first = c[0] >= c[1] ? 0 : 1;
-        const double join = parts ? 3 + double(parts) * side * side * 8 / 5e6 : 0;
-        const double us = grad_makespan(n, c, first) + join;
-        if (us < best_us) {
-          best_us = us;
-          best = GradPlan{side, {sx, sw}, first};
-        }
-      }
-  }
-  return best;
-}
-
-optima_status grad_products(GradPair& p, float* part, hipStream_t s) {
-  const GradPlan plan = plan_grad(p.a);
+// A product that is not wanted has no rows.
+optima_status grad_products(GradPair& p, const GradPlan& plan, float* part, hipStream_t s) {
   const int64_t area = int64_t(plan.side) * plan.side;
   int64_t tiles[2], joined[2];
   for (int k = 0; k < 2; ++k) {
@@ -835,7 +784,7 @@ optima_status grad_products(GradPair& p, float* part, hipStream_t s) {
     if (split) part += tiles[k] * plan.splits[k] * area;
     joined[k] = split ? tiles[k] * (area / 1024) : 0;
   }
-  p.first = plan.first;
+  p.first = ceil_div(p.a[0].stages, p.splits[0]) >= ceil_div(p.a[1].stages, p.splits[1]) ? 0 : 1;
   p.first_blocks = tiles[p.first] * p.splits[p.first];
   const dim3 grid(unsigned(tiles[0] * p.splits[0] + tiles[1] * p.splits[1]));
   if (plan.side == 256)
@@ -849,59 +798,6 @@ optima_status grad_products(GradPair& p, float* part, hipStream_t s) {
     OPTIMA_LAUNCH_CHECK();
   }
   return OPTIMA_OK;
-}
-
-// The tiles of the forward product: the first `wide` outputs take 256 tokens x 128
-// outputs, the others 128 x 64, with the sum in `splits` ranges where they are all. By what
-// the rounds over the CUs should take: 1.4 us a stage and 6 around them for the large tile,
-// 0.56 and 3.5 for the small one, 3 us and 5 TB/s for the join. Small tiles after whole
-// rounds of large ones take 4 us and 1.3 times that, since one launch ends before the other
-// begins, and are worth it from 7 % on: 2048 -> 5632, 1500 tokens 104 us in two rounds, 83
-// in one and small tiles; 1984 -> 12529, 700 tokens 115 and 93; but 4096 -> 14336, 2500
-// tokens 532 and 547.
-struct GatedPlan {
-  int64_t wide;
-  int splits;
-  double us;
-};
-GatedPlan plan_gated(int64_t n_tok, int64_t d, int64_t ff) {
-  const int64_t stages = ceil_div(d, 64);
-  const double large_us = 1.4 * double(stages) + 6, small_us = 0.56 * double(stages) + 3.5;
-  const int64_t rows = ceil_div(n_tok, 256), cols = ceil_div(ff, 128);
-  GatedPlan best{ff, 1, double(ceil_div(rows * cols, kCus)) * large_us};
-  const int64_t rounds = rows * cols / kCus, whole = rounds * kCus / rows;
-  if (rounds && whole < cols) {
-    const int64_t rest = ceil_div(n_tok, 128) * ceil_div(ff - 128 * whole, 64);
-    const double us = double(rounds) * large_us + 1.3 * double(ceil_div(rest, kCus)) * small_us + 4;
-    if (us < 0.93 * best.us) best = GatedPlan{128 * whole, 1, us};
-  }
-  const int64_t small = ceil_div(n_tok, 128) * ceil_div(ff, 64);
-  for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
-    if (splits > stages || (splits > 1 && splits * small > kPartTiles)) break;
-    const double range = 0.56 * double(ceil_div(stages, splits)) + 3.5;
-    const double us = double(ceil_div(small * splits, kCus)) * range +
-                      (splits > 1 ? 3 + double(small) * splits * 131072 / 5e6 : 0);
-    if (us < best.us) best = GatedPlan{0, splits, us};
-  }
-  return best;
-}
-
-// Whether the weights are streamed once for all tokens, or tiles take them. Streamed
-// they come at 6 TB/s, and every 16 outputs read all tokens again, at 10 TB/s out of
-// the caches; with few outputs a CU's workgroups' own way through d is what counts. To tiles
-// they come at 5.5 TB/s at most, and rows that do not suit them are copied first. Measured,
-// streamed against tiles: 4096 -> 14336, 4 tokens 39 to 42 us, 16 tokens 49 to 43, 64 tokens
-// 91 to 45; 1024 -> 8192, 32 tokens 10.7 to 12.2, 64 tokens 15.1 to 13.1; 2048 -> 5632, 32
-// tokens 18 to 20, 64 tokens 25 to 20; 4096 -> 2048, 16 tokens 11 to 17, 64 tokens 26 to 17;
-// 1001 -> 2731, 64 tokens 13 to 21.
-bool few_tokens(int64_t n_tok, int64_t d, int64_t ff) {
-  if (n_tok > kFewTokens) return false;
-  const double weights = 4e-6 * double(d) * double(ff);  // MB
-  const int64_t rounds = ceil_div(ff, 16 * kCus);
-  const double streamed = std::max(weights / 6 + double(n_tok) * weights / 320,
-                                   4 + double(rounds * n_tok * d) / 13000);
-  const double tiles = std::max(plan_gated(kFewTokens, d, ff).us, weights / 5.5 + 1);
-  return streamed <= tiles + (d % 64 ? 2 * weights / 5 + 4 : 0);
 }
 
 struct GatedLayout {
@@ -1080,7 +976,7 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
     OPTIMA_LAUNCH_CHECK();
   }
   if (n_tok == 0 && !dWg) return OPTIMA_OK;
-  return grad_products(pair, l.part, s);
+  return grad_products(pair, plan_grad(n_tok, d, ff), l.part, s);
 }
 
 }  // namespace optima
