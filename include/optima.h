@@ -432,7 +432,7 @@ optima_status optima_qp_solve_batched(const float* H, int64_t d,
  * weights are contiguous. All are asynchronous on `stream`, record no memset and
  * synchronise nothing, so that they can be captured in a HIP graph. NaN and
  * infinities go through the arithmetic. Every sum is fp32 or wider (whole numbers:
- * int32) and is taken in an order that depends on the sizes only. With no tokens
+ * int32) and is taken in an order that depends on the sizes and types only. With no tokens
  * nothing is read of token matrices. Outputs overlap neither inputs nor each other
  * except where stated.
  * ------------------------------------------------------------------------- */
@@ -488,8 +488,10 @@ optima_status optima_gated_forward(const void* X, int64_t ldx, int64_t n_tok, in
                                    int64_t ldu, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Gradient of the gated product.
- *   dU = dH * act(G), dG = dH * U * act'(G), each rounded to bf16 for the products
+ *   dU = dH * act(G), dG = dH * U * act'(G)
  *   dX = dG Wg + dU Wu,  dWg = mask_g * (dG^T X),  dWu = mask_u * (dU^T X)
+ * The products whose output is F32 take dG and dU in two bf16 parts, within 2^-16 of each value;
+ * those whose output is BF16 take them rounded to bf16, within 2^-9, in half the time.
  * X, Wg, Wu, act as in the forward call, G and U what it stored, dH bf16. dX
  * (nullable): dx_dtype BF16 or F32. dWg and dWu (both or neither): [d_ff][d_in] of
  * dw_dtype, added to what they hold with accumulate = 1. mask_g, mask_u (each

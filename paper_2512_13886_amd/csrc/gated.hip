@@ -8,7 +8,10 @@
 //
 // Backward: dU = dH o act(g), dG = dH o u o act'(g), then
 //   dX = [dG dU] [Wg; Wu],  [dWg; dWu] = [dG dU]^T X  (o masks).
-// P = [dG dU] is rounded to bf16, the type that the matrix instructions take.
+// The matrix instructions take P = [dG dU] in bf16. A product whose output is fp32 takes it in
+// two bf16 parts, 16 bits of mantissa, with twice the instructions: 4096 tokens, 4096 -> 14336,
+// off by 5e-6 in 3.16 ms, and by 1.7e-3 in 1.72 from P rounded to bf16. One whose output is bf16
+// takes P rounded: 2.35e-3 in place of the 1.66e-3 that the output's own rounding makes.
 #include "common.h"
 #include "gated_plan.h"
 #include "gemm128.h"
@@ -420,12 +423,37 @@ __device__ inline void transpose_tile(const Transpose& a, int block, uint16_t* t
 struct GateGradArgs {
   const bf16_t *g, *u, *dh;
   int64_t ldg, ldu, lddh, n_tok, ff;
-  bf16_t* p;   // [n_tok][2 ffp]: dG, dU, each with zeros up to ffp, or NULL
-  bf16_t* pt;  // [2 ff][tp]: their transpose with zeros from n_tok to tp, or NULL
+  bf16_t* p;   // [n_tok][planes_p][2 ffp]: dG, dU, each with zeros up to ffp, or NULL
+  bf16_t* pt;  // [2 ff][planes_t][tp]: their transpose with zeros from n_tok to tp, or NULL
   int64_t ffp, tp;
+  int planes_p, planes_t;  // 1: rounded; 2: the upper part, the lower part
   int act;
   int64_t blocks() const { return ffp / 64 * (tp / 64); }
 };
+
+// Eight values rounded to bf16.
+__device__ inline u32x4 rounded(const float (&v)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+  return w;
+}
+// Eight values as sums of two bf16 parts: cut to bf16, and the rest rounded, off by at most 2^-16
+// of the value. The parts have one sign and neither is 0 beside the other (a rest of 0 becomes
+// 2^-20 of the value), so that products with an infinity are those of the value.
+__device__ inline void two_parts(const float (&v)[8], u32x4* upper, u32x4* lower) {
+  float hi[8], lo[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t bits = __float_as_uint(v[e]);
+    const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
+    hi[e] = finite ? __uint_as_float(bits & 0xFFFF0000u) : v[e];
+    lo[e] = finite ? v[e] - hi[e] : v[e];
+    if (lo[e] == 0.f) lo[e] = hi[e] * 0x1p-20f;
+  }
+  *upper = rounded(hi);
+  *lower = rounded(lo);
+}
 
 // 64 tokens x 64 values of dG and dU. Bound by HBM: 14 bytes a value, 150 us for 4096 x
 // 14336.
@@ -433,6 +461,7 @@ __device__ inline void gate_grad_tile(const GateGradArgs& a, int block,
                                       uint16_t (&tile)[2][64 * kTrPitch]) {
   const int tiles_f = int(a.ffp / 64), tt = block / tiles_f;
   const int64_t t0 = int64_t(tt) * 64, f0 = int64_t(block - tt * tiles_f) * 64;
+  u32x4 lg[2], lu[2];  // the lower parts
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int i = threadIdx.x + k * kThreads, r = i >> 3, c = 8 * (i & 7);
@@ -453,29 +482,50 @@ __device__ inline void gate_grad_tile(const GateGradArgs& a, int block,
       du[e] = dh[e] * act;
       dg[e] = dh[e] * u[e] * slope;
     }
-    u32x4 wg, wu;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      wg[e] = pack_bf16(dg[2 * e], dg[2 * e + 1]);
-      wu[e] = pack_bf16(du[2 * e], du[2 * e + 1]);
+    const bool once = (a.p && a.planes_p == 1) || (a.pt && a.planes_t == 1);
+    const bool twice = (a.p && a.planes_p == 2) || (a.pt && a.planes_t == 2);
+    u32x4 wg, wu, hg, hu;
+    if (once) wg = rounded(dg), wu = rounded(du);
+    if (twice) {
+      two_parts(dg, &hg, &lg[k]);
+      two_parts(du, &hu, &lu[k]);
     }
     if (a.p && t < a.n_tok) {
-      *reinterpret_cast<u32x4*>(a.p + t * (2 * a.ffp) + f) = wg;
-      *reinterpret_cast<u32x4*>(a.p + t * (2 * a.ffp) + a.ffp + f) = wu;
+      bf16_t* row = a.p + t * (2 * a.ffp * a.planes_p) + f;
+      if (a.planes_p == 2) {
+        *reinterpret_cast<u32x4*>(row) = hg;
+        *reinterpret_cast<u32x4*>(row + a.ffp) = hu;
+        *reinterpret_cast<u32x4*>(row + 2 * a.ffp) = lg[k];
+        *reinterpret_cast<u32x4*>(row + 3 * a.ffp) = lu[k];
+      } else {
+        *reinterpret_cast<u32x4*>(row) = wg;
+        *reinterpret_cast<u32x4*>(row + a.ffp) = wu;
+      }
     }
     if (a.pt) {
-      tr_put(tile[0], r, c, wg);
-      tr_put(tile[1], r, c, wu);
+      tr_put(tile[0], r, c, a.planes_t == 2 ? hg : wg);
+      tr_put(tile[1], r, c, a.planes_t == 2 ? hu : wu);
     }
   }
   if (!a.pt) return;
-  __syncthreads();
+  for (int plane = 0;; ++plane) {
+    __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int i = threadIdx.x + k * kThreads, c = i >> 3, r = 8 * (i & 7);
-    if (f0 + c >= a.ff) continue;
-    *reinterpret_cast<u32x4*>(a.pt + (f0 + c) * a.tp + t0 + r) = tr_get(tile[0], r, c);
-    *reinterpret_cast<u32x4*>(a.pt + (a.ff + f0 + c) * a.tp + t0 + r) = tr_get(tile[1], r, c);
+    for (int k = 0; k < 2; ++k) {
+      const int i = threadIdx.x + k * kThreads, c = i >> 3, r = 8 * (i & 7);
+      if (f0 + c >= a.ff) continue;
+      bf16_t* to = a.pt + ((f0 + c) * a.planes_t + plane) * a.tp + t0 + r;
+      *reinterpret_cast<u32x4*>(to) = tr_get(tile[0], r, c);
+      *reinterpret_cast<u32x4*>(to + a.ff * a.planes_t * a.tp) = tr_get(tile[1], r, c);
+    }
+    if (plane + 1 == a.planes_t) return;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = threadIdx.x + k * kThreads, r = i >> 3, c = 8 * (i & 7);
+      tr_put(tile[0], r, c, lg[k]);
+      tr_put(tile[1], r, c, lu[k]);
+    }
   }
 }
 
@@ -534,18 +584,20 @@ struct GradArgs {
   const char *a, *b;
   int64_t pitch_a, pitch_b;  // bytes, multiples of 16
   int64_t rows, cols8;       // of the product; its columns rounded up to 8
-  int64_t stages;            // of 64 values of the contraction
-  int64_t s1, jump;          // TB: from stage s1 on B continues `jump` bytes further
+  int64_t stages;            // of 64 values of the contraction, over both parts of A
+  int64_t period;            // stages of one part: B is the same for each
+  int64_t s1, jump;          // TB: from its stage s1 on B continues `jump` bytes further
   GradOut out;
 };
 
 template <bool TB>
 struct GradSteps {
   int64_t pitch_b, jump;
-  int s1, s0;  // the workgroup's first stage
+  int period, s1, s0;  // s0: the workgroup's first stage
   __device__ inline int64_t a(int s) const { return int64_t(s0 + s) * 128; }
   __device__ inline int64_t b(int s) const {
-    return TB ? int64_t(s0 + s) * 64 * pitch_b + (s0 + s >= s1 ? jump : 0) : int64_t(s0 + s) * 128;
+    const int t = s0 + s < period ? s0 + s : s0 + s - period;
+    return TB ? int64_t(t) * 64 * pitch_b + (t >= s1 ? jump : 0) : int64_t(t) * 128;
   }
 };
 
@@ -678,7 +730,7 @@ __device__ inline void grad256_tile(const GradArgs& a, const GradBlock& g, char*
       src.b[h][i] = grad_b<TB>(a, n0 + 128 * h, i);
     }
   Acc256 acc;
-  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), g.s0};
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.period), int(a.s1), g.s0};
   gemm256_mainloop<Bf16Rows<TB>>(acc, src, g.s1 - g.s0, l0, l1, l2, l3, l4, l5, l6, l7, [] {}, steps);
   const int wn = (threadIdx.x >> 6) & 3;
 #pragma unroll
@@ -725,7 +777,7 @@ __device__ inline void grad_ring_tile(const GradArgs& a, const GradBlock& g, cha
     src.b[i] = grad_b<TB>(a, n0, i);
   }
   AccR128<false> acc;
-  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.s1), g.s0};
+  const GradSteps<TB> steps{a.pitch_b, a.jump, int(a.period), int(a.s1), g.s0};
   r128_mainloop<Bf16Rows<TB>>(acc, src, SumShape{0, 0, 0}, g.s1 - g.s0, b0, b1, b2, b3, [] {}, steps);
   const int wn = (threadIdx.x >> 6) & 3;
 #pragma unroll
@@ -835,14 +887,15 @@ GradLayout carve_grad(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* by
   GradLayout l{};
   const size_t ffp = size_t(round_up(ff, 64)), tp = size_t(round_up(n_tok, 64));
   const size_t dp = size_t(round_up(d, 8));
-  l.p = c.take<bf16_t>(size_t(n_tok) * 2 * ffp);
-  l.pt = c.take<bf16_t>(2 * size_t(ff) * tp);
+  // Room for both parts, whatever the outputs' types.
+  l.p = c.take<bf16_t>(size_t(n_tok) * 4 * ffp);
+  l.pt = c.take<bf16_t>(4 * size_t(ff) * tp);
   l.xt = c.take<bf16_t>(size_t(d) * tp);
   if (!weights_suit(d, ff)) {
     l.wg = c.take<bf16_t>(ffp * dp);
     l.wu = c.take<bf16_t>(ffp * dp);
   }
-  // Split sums: no more parts than stages, of tiles of up to 256 x 256.
+  // Split sums: no more ranges than stages of one part, of tiles of up to 256 x 256.
   const int64_t cols = 4 * ceil_div(d, 256);
   const int64_t parts = cols * (ceil_div(n_tok, 256) * int64_t(2 * ffp / 64) +
                                 ceil_div(2 * ff, 256) * int64_t(tp / 64));
@@ -938,6 +991,7 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
                              hipStream_t s) {
   const GradLayout l = carve_grad(ws, n_tok, d, ff, nullptr);
   const int64_t ffp = round_up(ff, 64), tp = round_up(n_tok, 64), dp = round_up(d, 8);
+  const int planes_x = dx_dtype == OPTIMA_DTYPE_F32 ? 2 : 1, planes_w = dw_dtype == OPTIMA_DTYPE_F32 ? 2 : 1;
   GradPrep prep{};
   GradPair pair{};
   const void *wg = Wg, *wu = Wu;
@@ -951,8 +1005,8 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
     // P [dG dU] times Wg, then Wu.
     const int64_t s1 = ffp / 64;
     const int64_t jump = static_cast<const char*>(wu) - static_cast<const char*>(wg) - 2 * ffp * dp;
-    pair.a[0] = GradArgs{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg), 4 * ffp,
-                      2 * dp, n_tok, dp, 2 * s1, s1, jump,
+    pair.a[0] = GradArgs{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg),
+                      4 * ffp * planes_x, 2 * dp, n_tok, dp, 2 * s1 * planes_x, 2 * s1, s1, jump,
                       GradOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, n_tok, lddx, d,
                               dx_dtype == OPTIMA_DTYPE_F32, 0}};
   }
@@ -960,14 +1014,15 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
     // No tokens: no stages, and the products are zero.
     if (n_tok > 0) prep.x = Transpose{static_cast<const bf16_t*>(X), ldx, n_tok, d, tp, l.xt};
     pair.a[1] = GradArgs{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt),
-                      2 * tp, 2 * tp, 2 * ff, dp, tp / 64, 0, 0,
+                      2 * tp * planes_w, 2 * tp, 2 * ff, dp, tp / 64 * planes_w, tp / 64, 0, 0,
                       GradOut{{dWg, dWu}, {mask_g, mask_u}, ff, ff, d, d,
                               dw_dtype == OPTIMA_DTYPE_F32, accumulate}};
   }
   if (n_tok > 0) {
     prep.gate = GateGradArgs{static_cast<const bf16_t*>(G), static_cast<const bf16_t*>(U),
                              static_cast<const bf16_t*>(dH), ldg, ldu, lddh, n_tok, ff,
-                             dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, act};
+                             dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, planes_x, planes_w,
+                             act};
     prep.gate_blocks = prep.gate.blocks();
     prep.x_blocks = prep.x.blocks();
     prep.w_blocks = prep.w[0].blocks();
