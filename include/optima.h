@@ -527,7 +527,8 @@ optima_status optima_w4_pack(const void* W, int dtype, int64_t n, int64_t d, int
  * X: [n_tok][d] of x_dtype BF16, or I8 with x_scales: fp32 [n_tok][ceil(d / x_group)]
  * with x_group = group, or one a token with x_group = 0 (as optima_rms_norm writes
  * them). Y: [n_tok][d_out] BF16 or F32. 8-bit codes are multiplied exactly within a
- * group.
+ * group; products of 16-bit tokens with codes are exact and summed in fp32. A zero weight adds
+ * exactly nothing, except to an infinite or NaN token (NaN).
  * ws: optima_w4_workspace_bytes(n_tok, d, d_out, n_mats) bytes, with n_mats 1 here and 2
  * for the gated product: 0 up to 16 tokens, and never less for more tokens. */
 size_t optima_w4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out, int n_mats);

@@ -9,13 +9,14 @@
 // 32 j + 8 b .. + 7, the even ones in nibbles 0..3 and the odd ones in nibbles
 // 4..7. In the products lane (b, n) of a wave takes block b of row n, and dword j
 // of the four blocks is one 16x16x32 MFMA operand, of one group at every group
-// size. Masking the nibbles in place gives pairs of bf16 (16-bit activations) or
-// bytes (8-bit ones) without any further movement:
-//   bf16: a nibble m in the upper mantissa bits of 2^4 is 16 + m = code + 24;
-//   int8: m = code + 8.
-// The offset comes off through a second MFMA with a constant operand (-24, -8),
-// whose result starts the sum of the group. Sums over a group are fp32 (int8: exact
-// in int32), the sum over groups, each times its scales, is fp32.
+// size.
+//   8-bit activations: the nibbles masked in place are bytes code + 8. The offset comes off
+//     through a second MFMA with a constant operand (-8), whose result starts the sum of the
+//     group; all of it is exact in int32.
+//   16-bit ones: the nibbles are converted to bf16 values code / 16, and the outputs' sums
+//     take the 16. No offset here: it would add to the fp32 sums what it takes off again, with
+//     its rounding, and turn an infinite token into NaN.
+// Sums over a group are fp32 or int32, the sum over groups, each times its scales, is fp32.
 //
 // Bound by the codes' way from HBM, once per call for up to 64 tokens. Up to 16 tokens
 // a workgroup takes 16 rows, its waves batches of their chunks, and the waves' sums are
@@ -92,7 +93,10 @@ template <bool I8, int MATS>
 __device__ inline void w4_store(const W4Args& a, int64_t tok, int64_t n, float (&v)[MATS]) {
 #pragma unroll
   for (int m = 0; m < MATS; ++m)
-    if (I8 && a.x_groups == 1) v[m] *= a.xs[tok];
+    if (!I8)
+      v[m] *= 16.f;
+    else if (a.x_groups == 1)
+      v[m] *= a.xs[tok];
   const float y = MATS == 2 ? w4_act(a.act, v[0]) * v[MATS - 1] : v[0];
   const int64_t at = tok * a.ldy + n;
   if (a.y_f32)
@@ -122,11 +126,28 @@ __device__ inline void slab_store(const W4Args& a, const f4 (&sum)[2][NT], int64
     }
 }
 
-// Eight codes as bf16 values code + 24, in the order of their indices.
+// code / 16 of a signed 4-bit code in the low half of byte BYTE. (The compiler's own builtin
+// shifts the byte down first.)
+template <int BYTE>
+__device__ inline float code_of(uint32_t v) {
+  static_assert(BYTE >= 0 && BYTE < 4, "");
+  float r;
+  if constexpr (BYTE == 0)
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(r) : "v"(v));
+  else if constexpr (BYTE == 1)
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(r) : "v"(v));
+  else if constexpr (BYTE == 2)
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(r) : "v"(v));
+  else
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(r) : "v"(v));
+  return r;
+}
+// Eight codes as bf16 values code / 16, in the order of their indices.
 __device__ inline bf16x8 codes_bf16(uint32_t w) {
-  constexpr uint32_t kMask = 0x00780078u, kBase = 0x41804180u;
-  return __builtin_bit_cast(bf16x8, u32x4{((w << 3) & kMask) | kBase, ((w >> 1) & kMask) | kBase,
-                                          ((w >> 5) & kMask) | kBase, ((w >> 9) & kMask) | kBase});
+  const uint32_t lo = w ^ 0x88888888u, hi = lo >> 4;  // code + 8 as a signed code
+  return __builtin_bit_cast(
+      bf16x8, u32x4{pack_bf16(code_of<0>(lo), code_of<2>(lo)), pack_bf16(code_of<0>(hi), code_of<2>(hi)),
+                    pack_bf16(code_of<1>(lo), code_of<3>(lo)), pack_bf16(code_of<1>(hi), code_of<3>(hi))});
 }
 // Eight codes as bytes code + 8, in the order 0 4 1 5, 2 6 3 7.
 __device__ inline long codes_i8(uint32_t w) {
@@ -214,22 +235,16 @@ __device__ inline void load_scales(float (&v)[N], const float* row, int g, int g
 }
 
 // The sum of one group's products of 16 tokens with the 16 rows of each of OPS
-// operands. acc's layout: lane (b, i) holds tokens 4 b + e of row i.
+// operands, of 16-bit tokens 1/16 of it. acc's layout: lane (b, i) holds tokens 4 b + e of row i.
 template <bool I8, int OPS, int PER>
 __device__ inline void group_sums(typename std::conditional<I8, i4, f4>::type (&acc)[OPS],
                                   const XFrag<I8> (&f)[4], const u32x4 (&w)[OPS], int j0) {
   typename std::conditional<I8, i4, f4>::type base = {};
+  if constexpr (I8)
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    if constexpr (I8) {
+    for (int j = 0; j < PER; ++j)
       base = __builtin_amdgcn_mfma_i32_16x16x32_i8(f[j0 + j].v, long(0xF8F8F8F8F8F8F8F8ull), base,
                                                    0, 0, 0);
-    } else {
-      const bf16x8 k24 = __builtin_bit_cast(
-          bf16x8, u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u});
-      base = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j0 + j].v, k24, base, 0, 0, 0);
-    }
-  }
 #pragma unroll
   for (int m = 0; m < OPS; ++m) {
     acc[m] = base;
