@@ -511,8 +511,8 @@ optima_status optima_gated_backward(const void* X, int64_t ldx, int64_t n_tok, i
  * W: [n][d] F32 or BF16. Groups of `group` (32, 64 or 128) consecutive values of a
  * row have scale = bf16(max |w| * (1 / 7)), the product and 1 / 7 in fp32, and codes
  * clamp(rne(w / scale), -7, 7): a zero weight, as every pruned one is, stays exactly
- * zero. A group with a NaN or infinity has codes 0 and a NaN or infinite scale. n d
- * stays below 2^35.
+ * zero. A group with a NaN or infinity has codes 0 and a NaN or infinite scale. The chunks
+ * (below), n ceil(d / 128), are at most 2^28 - 16.
  * Q: [n][optima_w4_row_bytes(d)], 16-byte aligned. A chunk of 128 codes takes 64
  *   bytes: dword j of its 16-byte block b holds codes 32 j + 8 b .. + 7, the even ones
  *   in nibbles 0..3 and the odd ones in nibbles 4..7, each as code + 8; rows are

@@ -496,7 +496,8 @@ optima_status optima_w4_pack(const void* W, int dtype, int64_t n, int64_t d, int
   if (!f32_or_bf16(dtype)) return OPTIMA_E_UNSUPPORTED;
   if (n < 0 || n > kMaxCols || d < 1 || d > kMaxDim || !group_ok(group)) return OPTIMA_E_INVAL;
   const int64_t groups = (d + group - 1) / group, row = int64_t(optima_w4_row_bytes(d));
-  if (n * (row / 64) >= int64_t(1) << 28) return OPTIMA_E_INVAL;  // 16 threads a chunk
+  // 16 threads a chunk, in blocks of 256: a launch has fewer than 2^32 threads.
+  if ((n * (row / 64) + 15) / 16 >= int64_t(1) << 24) return OPTIMA_E_INVAL;
   const Span w{W, n, d, d, esize(dtype)}, q{Q, n, row, row, 1}, sc{scales, n, groups, groups, 2};
   if (!w.good() || !q.good() || !sc.good() || !optima::aligned16(Q)) return OPTIMA_E_INVAL;
   if (q.meets(w) || sc.meets(w) || q.meets(sc)) return OPTIMA_E_INVAL;
