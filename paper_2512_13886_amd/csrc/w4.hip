@@ -287,6 +287,14 @@ constexpr int few_waves(int mats, int rows) { return mats == 1 || rows == 4 ? 16
 // the reads of several tokens off each other's banks.
 constexpr int few_pitch(bool i8) { return kBatchK * (i8 ? 1 : 2) + 64; }
 
+// What lanes of a wave wrote to LDS before is there for its other lanes after. A wave's LDS
+// accesses are served in order, so that this only keeps the compiler from moving them.
+__device__ inline void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // 16 outputs of each of MATS matrices; GP groups a chunk. A wave takes every waves-th
 // batch and brings the tokens' values of it through LDS: the operand layout would read
 // every value 16 times over, 16 / n_tok times for nothing.
@@ -344,8 +352,7 @@ __global__ void __launch_bounds__(64 * few_waves(MATS, ROWS)) k_w4_few(W4Args a)
       for (int r = 0; r < ROWS; ++r)
         if (r0 + ROWS + r < tokens) row[r].load(x + (r0 + ROWS + r) * a.ldx * kEsz, xk, a.d - xk);
     }
-    // The wave's own rows: its LDS accesses are served in order.
-    __builtin_amdgcn_wave_barrier();
+    wave_exchange();
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       XFrag<I8> f[4];
@@ -372,7 +379,7 @@ __global__ void __launch_bounds__(64 * few_waves(MATS, ROWS)) k_w4_few(W4Args a)
         }
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_exchange();
   }
   constexpr int kPart = MATS * 256;
   __syncthreads();  // the staged values' place
