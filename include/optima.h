@@ -433,8 +433,9 @@ optima_status optima_qp_solve_batched(const float* H, int64_t d,
  * synchronise nothing, so that they can be captured in a HIP graph. NaN and
  * infinities go through the arithmetic. Every sum is fp32 or wider (whole numbers:
  * int32) and is taken in an order that depends on the sizes and types only. With no tokens
- * nothing is read of token matrices. Outputs overlap neither inputs nor each other
- * except where stated.
+ * nothing is read of token matrices. Outputs share elements with neither inputs nor each
+ * other except where stated; rows of one pitch may lie between each other's (halves of one
+ * buffer's columns), of different pitches the whole extents count.
  * ------------------------------------------------------------------------- */
 
 /* RMS norm with the residual's addition.

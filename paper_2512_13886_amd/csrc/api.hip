@@ -84,8 +84,19 @@ struct Span {
   bool good() const {
     return ld >= cols && ld < (int64_t(1) << 31) && (rows < 1 || p) && aligned();
   }
+  // Whether any element is in both. Rows of one pitch may lie between each other's, as the
+  // halves of one buffer's columns do; of different pitches the whole extents count.
   bool meets(const Span& o) const {
-    return bytes() && o.bytes() && overlaps(p, bytes(), o.p, o.bytes());
+    if (!bytes() || !o.bytes() || !overlaps(p, bytes(), o.p, o.bytes())) return false;
+    const int64_t pitch = (rows > 1 ? ld * esz : o.ld * o.esz), a = cols * esz, b = o.cols * o.esz;
+    if ((o.rows > 1 && o.ld * o.esz != pitch) || a > pitch || b > pitch) return true;
+    const int64_t apart = int64_t(reinterpret_cast<uintptr_t>(o.p) - reinterpret_cast<uintptr_t>(p));
+    const int64_t down = apart >= 0 ? apart / pitch : -((pitch - 1 - apart) / pitch);
+    // o's first row begins `rest` bytes into the pitch of row `down`. Its rows reach into
+    // those of row `down` from there and into row down + 1 from before it.
+    const int64_t rest = apart - down * pitch;
+    auto rows_apart = [&](int64_t k) { return k < rows && -k < o.rows; };
+    return (rest < a && rows_apart(down)) || (pitch - rest < b && rows_apart(down + 1));
   }
   // The same elements in the same places: a kernel that reads a row before it
   // writes it may work in place.
