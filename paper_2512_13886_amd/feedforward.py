@@ -20,6 +20,7 @@ from dataclasses import dataclass, replace
 from typing import Callable
 
 import torch
+from torch.nn.functional import pad
 
 from . import _lib as L
 from .pipeline import solve_layer, spectral_step_size
@@ -59,12 +60,27 @@ def hidden(block: FeedForward, X: torch.Tensor, R: torch.Tensor | None = None) -
     return t
 
 
+def _product(X: torch.Tensor, W: torch.Tensor, dtype: torch.dtype,
+             ref: torch.Tensor | None = None, err: torch.Tensor | None = None) -> torch.Tensor:
+    """X W^T. The forward product takes inputs in multiples of 64 and outputs in multiples of 4:
+    other widths are filled up with zeros."""
+    d_out, d_in = W.shape
+    more_in, more_out = -d_in % 64, -d_out % 4
+    if more_in:
+        X = pad(X, (0, more_in))
+    if more_in or more_out:
+        W = pad(W, (0, more_in, 0, more_out))
+    if more_out and ref is not None:
+        ref = pad(ref, (0, more_out))
+    Y = torch.empty((X.shape[0], d_out + more_out), dtype=dtype, device=X.device)
+    L.optima_linear_forward(X, W, Y=Y, Y_ref=ref, err_out=err)
+    return Y[:, :d_out].contiguous() if more_out else Y
+
+
 def _down(H: torch.Tensor, down: torch.Tensor, ref: torch.Tensor | None = None):
     """H down^T in float32, and with ref the sum of squared differences."""
-    Y = torch.empty((H.shape[0], down.shape[0]), dtype=torch.float32, device=H.device)
     err = None if ref is None else torch.zeros(1, dtype=torch.float64, device=H.device)
-    L.optima_linear_forward(H, down, Y=Y, Y_ref=ref, err_out=err)
-    return Y, err
+    return _product(H, down, torch.float32, ref, err), err
 
 
 def output(block: FeedForward, X: torch.Tensor, R: torch.Tensor | None = None) -> torch.Tensor:
@@ -134,10 +150,9 @@ def gradients(block: FeedForward, masks: dict, Y_dense: torch.Tensor, X: torch.T
     t = hidden(block, X, R)
     Y, err = _down(t.H, block.down, Y_dense)
     dY = Y.sub_(Y_dense).div_(n).bfloat16()
-    dH = torch.empty_like(t.H)
     if down_t is None:
         down_t = block.down.t().contiguous()
-    L.optima_linear_forward(dY, down_t, Y=dH)
+    dH = _product(dY, down_t, torch.bfloat16)
     g = {"gate": torch.empty_like(block.gate), "up": torch.empty_like(block.up),
          "norm": torch.empty_like(block.norm)}
     dA = torch.empty((n, d), dtype=torch.bfloat16, device=dev)
