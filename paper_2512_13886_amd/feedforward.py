@@ -6,8 +6,8 @@ with the root-mean-square norm and its weight. prune_feedforward runs the steps 
 Algorithm 1 (pipeline.py) on its three matrices: gate and up share their inputs a, and so
 their Hessian; down's inputs h are those of the pruned gate and up. recover then lowers
 the output error with gradient steps on the norm's weight and on the kept entries of gate
-and up; down stays at its own optimum, the solve's. PackedFeedForward holds the three
-matrices in 4 bits and runs a few tokens at a time.
+and up; down stays as its solve left it, for the inputs that it had then. PackedFeedForward
+holds the three matrices in 4 bits and runs a few tokens at a time.
 
 Run as a program it does all three on a synthetic block and prints what each costs.
 This module sequences library calls and allocates with torch; norms, products, their
