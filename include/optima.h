@@ -442,7 +442,8 @@ optima_status optima_qp_solve_batched(const float* H, int64_t d,
  *   s = x + r (r = 0 where R is NULL), y = s * weight / sqrt(mean(s^2) + eps)
  * over rows of d <= OPTIMA_NORM_MAX_DIM values (larger: OPTIMA_E_UNSUPPORTED).
  * X, R and S are of `dtype` (F32 or BF16), weight of w_dtype. S (nullable)
- * receives s rounded to dtype; the norm is taken of the fp32 s. S may be X or R
+ * receives s rounded to dtype; the norm is taken of the fp32 s, whose squares overflow (y = 0)
+ * where |s| passes about 1e19. S may be X or R
  * themselves (same pointer and pitch), and so may Y if it has their type.
  * Y: y_dtype F32, BF16, or I8: codes q = rne(y * (1 / scale)) within +-127 with
  *   scale = max |y| / 127 (0 below the smallest normal number) over each group of `group` consecutive values (32, 64 or

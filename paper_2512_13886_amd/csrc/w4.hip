@@ -18,12 +18,12 @@
 //     its rounding, and turn an infinite token into NaN.
 // Sums over a group are fp32 or int32, the sum over groups, each times its scales, is fp32.
 //
-// Bound by the codes' way from HBM, once per call for up to 64 tokens. Up to 16 tokens
-// a workgroup takes 16 rows, its waves batches of their chunks, and the waves' sums are
-// joined in LDS in their order; more tokens share what is read of them. One 8-bit token,
-// 4096 -> 2 x 14336: 14.3 us, 4.2 TB/s; eight 16-bit ones, 14336 -> 4096 in groups of 64:
-// 9.5 us, 3.3 TB/s. Each wave has one or two batches, so that the launch's start and end
-// are what is left.
+// The codes come from HBM once per call for up to 64 tokens. Up to 16 tokens a workgroup
+// takes 16 rows, its waves batches of their chunks, and the waves' sums are joined in LDS in
+// their order; more tokens share what is read of them. One 8-bit token, 4096 -> 2 x 14336:
+// 14.5 us, 4.2 TB/s; eight 16-bit ones, 14336 -> 4096 in groups of 64: 10.2 us, 3.1 TB/s (16.9
+// and 12.9 from weights that no cache holds). Bound by the latency of the one or two batches of
+// loads that each wave has, and with more tokens by their reads out of the L2.
 #include <type_traits>
 
 #include "common.h"
@@ -280,8 +280,9 @@ constexpr int kBatchK = kBatch * kChunk;  // 512 values
 constexpr int kFew = 16;
 // Waves of a workgroup at most, where a wave loads `rows` tokens at once: four for up to
 // four tokens, which leaves the gated kernels registers for more waves a SIMD (one token,
-// 4096 -> 14336, 16-bit: 23.4 us with eight, 18.4 with four), eight for more (eight
-// tokens: 24.5 and 26.7).
+// 4096 -> 2 x 14336, 16-bit: 24.5 us with eight, 19.3 with four), eight for more (8 tokens,
+// 2048 -> 2 x 5632, 8.9 against 9.4; 16 tokens, 14336 -> 4096, 18.6 against 19.7; though 8
+// tokens at 4096 -> 2 x 14336 25.8 against 22.4).
 constexpr int few_waves(int mats, int rows) { return mats == 1 || rows == 4 ? 16 : 8; }
 // Bytes of one token's values of a batch in LDS, with 64 bytes between rows that keep
 // the reads of several tokens off each other's banks.
@@ -418,7 +419,8 @@ constexpr int slab_rows(int mats) { return kSlabWaves * 16 * (2 / mats); }  // a
 // one), whose codes it loads a batch ahead. With few rows the chunks are split over
 // blockIdx.y, and k_w4_join adds the parts: 16 rows' own read of the tokens, as above,
 // would bring every token N / 16 times out of the L2.
-// Bound by the MFMAs, of which the offset takes a third, and the LDS reads.
+// Bound by latency: at 64 tokens, 4096 -> 2 x 14336, the MFMAs are busy for 16 % of 38 us
+// (8-bit: 21 % of 42), and the two waves a SIMD wait for loads and barriers for 41 and 50 %.
 template <bool I8, int MATS, int NT, int GP>
 __global__ void __launch_bounds__(64 * kSlabWaves) k_w4_slab(W4Args a) {
   constexpr int kPer = 4 / GP, kGroups = kSlabBatch * GP, OPS = 2;
@@ -575,10 +577,10 @@ __global__ void __launch_bounds__(kThreads) k_w4_join(W4Args a, int splits, int 
 }
 
 // Ranges that the chunks of a product of more than kFew tokens are split into: as many
-// as give every CU a workgroup (14336 -> 2 x 4096, 128 tokens: 181 us in one, 60 in
-// four). Beyond eight they have two batches at least: 4096 -> 4096, 64 tokens, 17.7 us in
-// 8 ranges, 20.5 in 16. Two batches of up to 32 tokens stay whole: 512 -> 2048, 17 tokens,
-// 6.8 us and 7.4.
+// as give every CU a workgroup (14336 -> 2 x 4096, 128 tokens: 186 us in one, 62 in
+// four). Beyond eight they have two batches at least: 4096 -> 4096, 64 tokens, 16.6 us in
+// 8 ranges, 19.7 in 16. Two batches of up to 32 tokens stay whole: 512 -> 2048, 17 tokens,
+// 6.9 us and 7.4.
 int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out, int mats) {
   const int64_t wgs = ceil_div(d_out, slab_rows(mats)) * ceil_div(n_tok, kSlabTokens);
   const int64_t batches = ceil_div(d, kSlabK);
