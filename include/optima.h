@@ -492,8 +492,8 @@ optima_status optima_gated_forward(const void* X, int64_t ldx, int64_t n_tok, in
 /* Gradient of the gated product.
  *   dU = dH * act(G), dG = dH * U * act'(G)
  *   dX = dG Wg + dU Wu,  dWg = mask_g * (dG^T X),  dWu = mask_u * (dU^T X)
- * The products whose output is F32 take dG and dU in two bf16 parts, within 2^-16 of each value;
- * those whose output is BF16 take them rounded to bf16, within 2^-9, in half the time.
+ * The products take dG and dU in two bf16 parts, within 2^-16 of each value, and round once, to
+ * the type of the output.
  * X, Wg, Wu, act as in the forward call, G and U what it stored, dH bf16. dX
  * (nullable): dx_dtype BF16 or F32. dWg and dWu (both or neither): [d_ff][d_in] of
  * dw_dtype, added to what they hold with accumulate = 1. mask_g, mask_u (each

@@ -628,8 +628,7 @@ def optima_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G
                           ws: torch.Tensor | None = None, stream=None) -> None:
     """Gradients of optima_gated_forward: dX [n_tok, d_in] and dWg, dWu [d_ff, d_in], each
     bfloat16 or float32 (dWg and dWu of one type, + what they hold with accumulate). Where
-    mask_g or mask_u (uint8 [d_ff, d_in]) is 0 the weight's gradient is exactly 0. A float32
-    output has the precision of its type and takes twice a bfloat16 one's time."""
+    mask_g or mask_u (uint8 [d_ff, d_in]) is 0 the weight's gradient is exactly 0."""
     n, d, ff = _gated_weights(X, Wg, Wu)
     x, ldx, _ = _take("X", X, (n, d), _B)
     g, ldg, _ = _take("G", G, (n, ff), _B)

@@ -8,10 +8,10 @@
 //
 // Backward: dU = dH o act(g), dG = dH o u o act'(g), then
 //   dX = [dG dU] [Wg; Wu],  [dWg; dWu] = [dG dU]^T X  (o masks).
-// The matrix instructions take P = [dG dU] in bf16. A product whose output is fp32 takes it in
-// two bf16 parts, 16 bits of mantissa, with twice the instructions: 4096 tokens, 4096 -> 14336,
-// off by 5e-6 in 3.16 ms, and by 1.7e-3 in 1.72 from P rounded to bf16. One whose output is bf16
-// takes P rounded: 2.35e-3 in place of the 1.66e-3 that the output's own rounding makes.
+// The matrix instructions take P = [dG dU] in bf16: it comes in two bf16 parts, 16 bits of
+// mantissa, with twice the instructions. Rounded to one, 4096 tokens, 4096 -> 14336: fp32
+// gradients 1.7e-3 off in place of 5e-6, bf16 ones 2.35e-3 in place of the 1.66e-3 that their own
+// rounding makes; 1.58 ms in place of 3.07.
 #include "common.h"
 #include "gated_plan.h"
 #include "gemm128.h"
@@ -423,10 +423,10 @@ __device__ inline void transpose_tile(const Transpose& a, int block, uint16_t* t
 struct GateGradArgs {
   const bf16_t *g, *u, *dh;
   int64_t ldg, ldu, lddh, n_tok, ff;
-  bf16_t* p;   // [n_tok][planes_p][2 ffp]: dG, dU, each with zeros up to ffp, or NULL
-  bf16_t* pt;  // [2 ff][planes_t][tp]: their transpose with zeros from n_tok to tp, or NULL
+  // Upper parts, then lower ones:
+  bf16_t* p;   // [n_tok][2][2 ffp]: dG, dU, each with zeros up to ffp, or NULL
+  bf16_t* pt;  // [2 ff][2][tp]: their transpose with zeros from n_tok to tp, or NULL
   int64_t ffp, tp;
-  int planes_p, planes_t;  // 1: rounded; 2: the upper part, the lower part
   int act;
   int64_t blocks() const { return ffp / 64 * (tp / 64); }
 };
@@ -455,7 +455,7 @@ __device__ inline void two_parts(const float (&v)[8], u32x4* upper, u32x4* lower
   *lower = rounded(lo);
 }
 
-// 64 tokens x 64 values of dG and dU. Bound by HBM: 14 bytes a value, 150 us for 4096 x
+// 64 tokens x 64 values of dG and dU. Bound by HBM: 22 bytes a value, 270 us for 4096 x
 // 14336.
 __device__ inline void gate_grad_tile(const GateGradArgs& a, int block,
                                       uint16_t (&tile)[2][64 * kTrPitch]) {
@@ -482,43 +482,34 @@ __device__ inline void gate_grad_tile(const GateGradArgs& a, int block,
       du[e] = dh[e] * act;
       dg[e] = dh[e] * u[e] * slope;
     }
-    const bool once = (a.p && a.planes_p == 1) || (a.pt && a.planes_t == 1);
-    const bool twice = (a.p && a.planes_p == 2) || (a.pt && a.planes_t == 2);
-    u32x4 wg, wu, hg, hu;
-    if (once) wg = rounded(dg), wu = rounded(du);
-    if (twice) {
-      two_parts(dg, &hg, &lg[k]);
-      two_parts(du, &hu, &lu[k]);
-    }
+    u32x4 hg, hu;
+    two_parts(dg, &hg, &lg[k]);
+    two_parts(du, &hu, &lu[k]);
     if (a.p && t < a.n_tok) {
-      bf16_t* row = a.p + t * (2 * a.ffp * a.planes_p) + f;
-      if (a.planes_p == 2) {
-        *reinterpret_cast<u32x4*>(row) = hg;
-        *reinterpret_cast<u32x4*>(row + a.ffp) = hu;
-        *reinterpret_cast<u32x4*>(row + 2 * a.ffp) = lg[k];
-        *reinterpret_cast<u32x4*>(row + 3 * a.ffp) = lu[k];
-      } else {
-        *reinterpret_cast<u32x4*>(row) = wg;
-        *reinterpret_cast<u32x4*>(row + a.ffp) = wu;
-      }
+      bf16_t* row = a.p + t * (4 * a.ffp) + f;
+      *reinterpret_cast<u32x4*>(row) = hg;
+      *reinterpret_cast<u32x4*>(row + a.ffp) = hu;
+      *reinterpret_cast<u32x4*>(row + 2 * a.ffp) = lg[k];
+      *reinterpret_cast<u32x4*>(row + 3 * a.ffp) = lu[k];
     }
     if (a.pt) {
-      tr_put(tile[0], r, c, a.planes_t == 2 ? hg : wg);
-      tr_put(tile[1], r, c, a.planes_t == 2 ? hu : wu);
+      tr_put(tile[0], r, c, hg);
+      tr_put(tile[1], r, c, hu);
     }
   }
   if (!a.pt) return;
-  for (int plane = 0;; ++plane) {
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int i = threadIdx.x + k * kThreads, c = i >> 3, r = 8 * (i & 7);
       if (f0 + c >= a.ff) continue;
-      bf16_t* to = a.pt + ((f0 + c) * a.planes_t + plane) * a.tp + t0 + r;
+      bf16_t* to = a.pt + (2 * (f0 + c) + part) * a.tp + t0 + r;
       *reinterpret_cast<u32x4*>(to) = tr_get(tile[0], r, c);
-      *reinterpret_cast<u32x4*>(to + a.ff * a.planes_t * a.tp) = tr_get(tile[1], r, c);
+      *reinterpret_cast<u32x4*>(to + 2 * a.ff * a.tp) = tr_get(tile[1], r, c);
     }
-    if (plane + 1 == a.planes_t) return;
+    if (part == 1) return;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -564,7 +555,7 @@ __global__ void __launch_bounds__(kThreads) k_gated_prep(ForwardPrep a) {
 // written by k_gated_grad_prep, with the contraction contiguous in its rows. dX takes the
 // weights as they are, with the contraction along their rows, through the transposing
 // LDS reads of gemm256.h (TB); dW takes X^T, transposed in memory.
-// Measured at 4096 tokens, 4096 -> 14336, of 962 GFLOP each: dX 701 us with TB, 670 and
+// Measured at 4096 tokens, 4096 -> 14336, with one part of P, 962 GFLOP each: dX 701 us with TB, 670 and
 // 114 for the transposed weights without; dW 767 us with TB, 670 and 14 for X^T without,
 // and 840 us with both operands read through LDS that way (46 us less to write before).
 // Both run in one launch, the longer sums first, so that the tiles of one fill the CUs
@@ -887,7 +878,6 @@ GradLayout carve_grad(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* by
   GradLayout l{};
   const size_t ffp = size_t(round_up(ff, 64)), tp = size_t(round_up(n_tok, 64));
   const size_t dp = size_t(round_up(d, 8));
-  // Room for both parts, whatever the outputs' types.
   l.p = c.take<bf16_t>(size_t(n_tok) * 4 * ffp);
   l.pt = c.take<bf16_t>(4 * size_t(ff) * tp);
   l.xt = c.take<bf16_t>(size_t(d) * tp);
@@ -895,10 +885,10 @@ GradLayout carve_grad(void* ws, int64_t n_tok, int64_t d, int64_t ff, size_t* by
     l.wg = c.take<bf16_t>(ffp * dp);
     l.wu = c.take<bf16_t>(ffp * dp);
   }
-  // Split sums: no more ranges than stages of one part, of tiles of up to 256 x 256.
+  // Split sums: no more ranges than stages, of tiles of up to 256 x 256.
   const int64_t cols = 4 * ceil_div(d, 256);
-  const int64_t parts = cols * (ceil_div(n_tok, 256) * int64_t(2 * ffp / 64) +
-                                ceil_div(2 * ff, 256) * int64_t(tp / 64));
+  const int64_t parts = cols * (ceil_div(n_tok, 256) * int64_t(4 * ffp / 64) +
+                                ceil_div(2 * ff, 256) * int64_t(2 * tp / 64));
   l.part = c.take<float>(16384 * size_t(std::min(kPartTiles, parts)));
   if (bytes) *bytes = c.bytes();
   return l;
@@ -991,7 +981,6 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
                              hipStream_t s) {
   const GradLayout l = carve_grad(ws, n_tok, d, ff, nullptr);
   const int64_t ffp = round_up(ff, 64), tp = round_up(n_tok, 64), dp = round_up(d, 8);
-  const int planes_x = dx_dtype == OPTIMA_DTYPE_F32 ? 2 : 1, planes_w = dw_dtype == OPTIMA_DTYPE_F32 ? 2 : 1;
   GradPrep prep{};
   GradPair pair{};
   const void *wg = Wg, *wu = Wu;
@@ -1006,7 +995,7 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
     const int64_t s1 = ffp / 64;
     const int64_t jump = static_cast<const char*>(wu) - static_cast<const char*>(wg) - 2 * ffp * dp;
     pair.a[0] = GradArgs{reinterpret_cast<const char*>(l.p), static_cast<const char*>(wg),
-                      4 * ffp * planes_x, 2 * dp, n_tok, dp, 2 * s1 * planes_x, 2 * s1, s1, jump,
+                      8 * ffp, 2 * dp, n_tok, dp, 4 * s1, 2 * s1, s1, jump,
                       GradOut{{dX, nullptr}, {nullptr, nullptr}, INT64_MAX, n_tok, lddx, d,
                               dx_dtype == OPTIMA_DTYPE_F32, 0}};
   }
@@ -1014,15 +1003,14 @@ optima_status gated_backward(const void* X, int64_t ldx, int64_t n_tok, int64_t 
     // No tokens: no stages, and the products are zero.
     if (n_tok > 0) prep.x = Transpose{static_cast<const bf16_t*>(X), ldx, n_tok, d, tp, l.xt};
     pair.a[1] = GradArgs{reinterpret_cast<const char*>(l.pt), reinterpret_cast<const char*>(l.xt),
-                      2 * tp * planes_w, 2 * tp, 2 * ff, dp, tp / 64 * planes_w, tp / 64, 0, 0,
+                      4 * tp, 2 * tp, 2 * ff, dp, tp / 32, tp / 64, 0, 0,
                       GradOut{{dWg, dWu}, {mask_g, mask_u}, ff, ff, d, d,
                               dw_dtype == OPTIMA_DTYPE_F32, accumulate}};
   }
   if (n_tok > 0) {
     prep.gate = GateGradArgs{static_cast<const bf16_t*>(G), static_cast<const bf16_t*>(U),
                              static_cast<const bf16_t*>(dH), ldg, ldu, lddh, n_tok, ff,
-                             dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, planes_x, planes_w,
-                             act};
+                             dX ? l.p : nullptr, dWg ? l.pt : nullptr, ffp, tp, act};
     prep.gate_blocks = prep.gate.blocks();
     prep.x_blocks = prep.x.blocks();
     prep.w_blocks = prep.w[0].blocks();

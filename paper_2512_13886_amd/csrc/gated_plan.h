@@ -33,7 +33,8 @@ struct GradPlan {
   int side, splits[2];
 };
 inline GradPlan plan_grad(int64_t n_tok, int64_t d, int64_t ff) {
-  const int64_t rows[2] = {n_tok, 2 * ff}, stages[2] = {2 * ceil_div(ff, 64), ceil_div(n_tok, 64)};
+  // Stages of 64 values of the contraction, of both parts of the operand that has two.
+  const int64_t rows[2] = {n_tok, 2 * ff}, stages[2] = {4 * ceil_div(ff, 64), 2 * ceil_div(n_tok, 64)};
   GradPlan best{256, {1, 1}};
   double best_us = 1e30;
   for (const int side : {256, 128}) {

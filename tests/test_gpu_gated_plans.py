@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 # n, d, ff -> tile side, ranges of dX's and dW's sums.
 GRADIENTS = {(1999, 1001, 2731): (256, 3, 1), (1024, 1024, 4096): (256, 8, 1),
              (8192, 768, 3000): (256, 1, 1), (8000, 1000, 700): (256, 1, 4),
-             (300, 200, 129): (128, 1, 1), (600, 128, 5000): (128, 16, 1)}
+             (190, 100, 70): (128, 1, 1), (300, 200, 129): (128, 4, 4), (600, 128, 5000): (128, 16, 1)}
 # All taken by the few-token kernel: sixteen waves (d >= 2048, up to 8 tokens, or up to 16 and
 # few outputs), both widths of its operands, one to four blocks of tokens.
 FEW = [(1, 2048, 700), (8, 2048, 700), (1, 4096, 300), (8, 4096, 700), (1, 4097, 400), (8, 4097, 400),

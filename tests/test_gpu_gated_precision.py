@@ -1,11 +1,12 @@
-"""The gated gradient's fp32 outputs against the fp64 oracle.
+"""The gated gradient against the fp64 oracle: fp32 inside, rounded once at the end.
 
-Tolerances. U = 2^-24. dG and dU come in two bf16 parts: cut to bf16 (the rest is below 2^-7
-of the value) and the rest rounded (2^-9 of it), so that each is within 2^-16 of its value.
-Both parts' products are summed in fp32: 2 K U of the sum of magnitudes over K. The
-activation's slope may cancel: 16 U of its two parts. Over many entries the parts' roundings
-are independent, so that the Frobenius norm is off by less than 2^-16 of itself, and by less
-than 2^-14 with the fp32 sums."""
+Tolerances. U = 2^-24, B = 2^-8 (half a bf16 step). dG and dU come in two bf16 parts: cut to
+bf16, and the rest, below 2^-7 of the value, rounded to its own upper eight bits, so that each is
+within 2^-16 of its value. Both parts' products are summed in fp32: 2 K U of the sum of
+magnitudes over K. The activation's slope may cancel: 16 U of its two parts. Over many entries the
+parts' roundings are independent, so that the Frobenius norm is off by less than 2^-16 of itself, by
+less than 2^-14 with the fp32 sums, and by the output's rounding: B / sqrt(3) at most, that of
+values just above powers of two."""
 import numpy as np
 import pytest
 import torch
@@ -15,7 +16,7 @@ from oracle import feedforward_oracle as F
 
 pytestmark = pytest.mark.gpu
 
-U, PARTS = 2.0 ** -24, 2.0 ** -16
+U, B, PARTS = 2.0 ** -24, 2.0 ** -8, 2.0 ** -16
 T = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
@@ -39,13 +40,12 @@ def _inputs(n, d, ff, seed):
             rows(n, ff)), g
 
 
-# Small tiles and large ones, split sums, ragged sizes, one token; the other output in bf16
-# or in fp32 too, so that one call forms both kinds of operands.
+# Small tiles and large ones, split sums, ragged sizes, one token.
 @pytest.mark.parametrize("n, d, ff", [(1, 1, 1), (5, 100, 33), (65, 64, 63), (300, 200, 129),
                                       (1999, 1001, 2731)])
-@pytest.mark.parametrize("dx, dw", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("dx, dw", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
 @pytest.mark.parametrize("name", ["silu", "none"])
-def test_fp32_outputs(L, n, d, ff, dx, dw, name):
+def test_outputs_are_rounded_once(L, n, d, ff, dx, dw, name):
     (X, Wg, Wu, G, V, dH), g = _inputs(n, d, ff, n + d + ff)
     mask = (torch.rand(ff, d, generator=g, device=dev()) < 0.5).to(torch.uint8)
     dX = torch.empty(n, d, dtype=T[dx], device=dev())
@@ -54,21 +54,18 @@ def test_fp32_outputs(L, n, d, ff, dx, dw, name):
                             act=1 if name == "silu" else 0, mask_g=mask)
     x, wg, wu, gg, u, dh = (_np(t) for t in (X, Wg, Wu, G, V, dH))
     rx, rg, ru, dg, du = F.gated_backward(x, wg, wu, gg, u, dh, name)
-    rg = rg * _np(mask)
     slope = np.abs(dh * u) * 16 * U * (1 + np.abs(gg))
     act = np.abs(dh * gg) * 16 * U * (1 + np.abs(gg))
-    if dx == "f32":
-        size = np.abs(dg) @ np.abs(wg) + np.abs(du) @ np.abs(wu)
-        assert np.all(np.abs(_np(dX) - rx) <= (PARTS + (4 * ff + 64) * U) * size +
-                      2 * (slope @ np.abs(wg) + act @ np.abs(wu)) + U * np.abs(rx) + 1e-36)
-        assert rel_fro(_np(dX), rx) <= 2.0 ** -14
-    if dw == "f32":
-        for got, ref, p, ex, m in ((dWg, rg, dg, slope, _np(mask)), (dWu, ru, du, act, 1.0)):
-            bound = (PARTS + (2 * n + 64) * U) * (np.abs(p).T @ np.abs(x)) + \
-                2 * ex.T @ np.abs(x) + U * np.abs(ref) + 1e-36
-            assert np.all(np.abs(_np(got) - ref) <= bound * m)
-            if np.any(ref):
-                assert rel_fro(_np(got), ref) <= 2.0 ** -14
+    checks = [(dX, rx, np.abs(dg) @ np.abs(wg) + np.abs(du) @ np.abs(wu),
+               slope @ np.abs(wg) + act @ np.abs(wu), 4 * ff, dx, 1.0)]
+    for got, ref, p, ex, m in ((dWg, rg, dg, slope, _np(mask)), (dWu, ru, du, act, 1.0)):
+        checks.append((got, ref * m, np.abs(p).T @ np.abs(x), ex.T @ np.abs(x), 2 * n, dw, m))
+    for got, ref, size, extra, k, out, m in checks:
+        half = {"f32": U, "bf16": 1.01 * B}[out]
+        bound = (1 + half) * ((PARTS + (k + 64) * U) * size + 2 * extra) + half * np.abs(ref) + 1e-36
+        assert np.all(np.abs(_np(got) - ref) <= bound * m)
+        if np.count_nonzero(ref) > 1000:
+            assert rel_fro(_np(got), ref) <= 2.0 ** -14 + (B / 3 ** 0.5 if out == "bf16" else 0.0)
 
 
 def test_infinities_are_those_of_the_values(L):
