@@ -49,6 +49,7 @@ typedef int optima_status;
 #define OPTIMA_DTYPE_BF16 1
 #define OPTIMA_DTYPE_F64 2
 #define OPTIMA_DTYPE_I8 3 /* 8-bit codes with scales (optima_rms_norm, optima_w4_*) */
+#define OPTIMA_DTYPE_MX4 4 /* microscaled 4-bit codes with scales (optima_mx4_linear) */
 
 /* Arithmetic of the solver's per-iteration H-products (optima_solver_opts).
  * FP32: v_mfma_f32_16x16x4_f32, fp32 products and sums.
@@ -546,6 +547,78 @@ optima_status optima_w4_gated(const void* X, int64_t ldx, int x_dtype, const flo
                               const void* scales_g, const void* Qu, const void* scales_u,
                               int64_t group, int64_t d_ff, int act, void* H, int64_t ldh,
                               int h_dtype, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * From packed weights to a model's answers. The conventions are those of the
+ * calls above.
+ * ------------------------------------------------------------------------- */
+
+/* Microscaled 4-bit floating point: rows of n x d values in blocks of 32.
+ * A block has the scale 2^(e - 2), e = floor(log2(max |v|)), not below 2^-127, and the code of a
+ * value is v / scale rounded to nearest even among 0, 0.5, 1, 1.5, 2, 3, 4 and 6 (codes 0 .. 7;
+ * + 8 for negative ones), at most 6: a zero weight, as every pruned one is, stays exactly zero. A
+ * block with a NaN or infinity has scale byte 255 and codes 0: all its values are NaN.
+ * X: [n][ldx] of `dtype` F32 or BF16; weights or tokens.
+ * Q: [n][optima_mx4_row_bytes(d)], 16-byte aligned. Code k is in byte k / 2 of its row, an even
+ *   one in the low half; rows are padded to whole 256 values with zero codes.
+ * scales: [n][optima_mx4_scale_bytes(d)], 4-byte aligned: the exponent plus 127, that of block b
+ *   (0 .. 3) of the 128 values c at byte 16 (c / 4) + 4 b + c % 4; rows are padded with zeros.
+ * The 256-value pieces, n ceil(d / 256), are below 2^27, here and in unpack. */
+size_t optima_mx4_row_bytes(int64_t d);
+size_t optima_mx4_scale_bytes(int64_t d);
+optima_status optima_mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t d, void* Q,
+                              void* scales, hipStream_t stream);
+
+/* The values that codes and scales stand for, Y: [n][ldy] of `dtype` F32 or BF16. Both hold every
+ * value of pack exactly. */
+optima_status optima_mx4_unpack(const void* Q, const void* scales, int64_t n, int64_t d, void* Y,
+                                int64_t ldy, int dtype, hipStream_t stream);
+
+/* Y = X W^T for packed weights W [d_out][d], as optima_mx4_pack lays them out.
+ * X: [n_tok][d] of x_dtype BF16 with pitch ldx and x_scales NULL, or of MX4: packed tokens with
+ * x_scales (ldx is not used). n_tok <= 2^21, d <= 2^20, d_out <= 2^24. Y: [n_tok][d_out] BF16 or F32. Products of
+ * values are exact, their sums fp32. A zero weight adds exactly nothing, except to an infinite or
+ * NaN token (NaN).
+ * ws: optima_mx4_workspace_bytes(n_tok, d, d_out) bytes: 0 up to 16 tokens, never less for more. */
+size_t optima_mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out);
+optima_status optima_mx4_linear(const void* X, int64_t ldx, int x_dtype, const void* x_scales,
+                                int64_t n_tok, int64_t d, const void* Q, const void* scales,
+                                int64_t d_out, void* Y, int64_t ldy, int y_dtype, void* ws,
+                                size_t ws_bytes, hipStream_t stream);
+
+/* Log probabilities of given tokens under rows of logits, z = scale * X (scale > 0, as one over a
+ * temperature):
+ *   lse = log sum exp z,  logp = z[token] - lse,  entropy = - sum p log p,  p = exp(z - lse)
+ * and the k most probable alternatives, top_index and top_logp: [n][k], by falling logit, equal
+ * ones by rising index (-0 is 0; in a row with NaN they are k different places, no more is said).
+ * X: [n][ldx] of `dtype` F32 or BF16, vocab <= 2^20 of them a row. tokens: [n], needed for logp; a
+ * negative one is none (logp 0), one of vocab or more gives NaN. logp, lse, entropy: fp32 [n],
+ * each nullable; k <= OPTIMA_TOP_MAX and vocab, top_index and top_logp each nullable, one at
+ * least with k > 0.
+ * Logits of -inf have probability 0 and add nothing to the entropy. A row with nothing else has lse,
+ * logp and top_logp -inf and entropy 0; one with NaN or +inf has NaN in all four.
+ * ws: optima_token_logprobs_workspace_bytes(n, vocab, k) bytes, 8-byte aligned: never less for
+ * more rows. */
+#define OPTIMA_TOP_MAX 32
+size_t optima_token_logprobs_workspace_bytes(int64_t n, int64_t vocab, int64_t k);
+optima_status optima_token_logprobs(const void* X, int64_t ldx, int dtype, int64_t n, int64_t vocab,
+                                    const int64_t* tokens, float scale, float* logp, float* lse,
+                                    float* entropy, int64_t k, int64_t* top_index, float* top_logp,
+                                    void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradient of the log probabilities, the entropy and lse, from what the forward call stored:
+ *   dX = scale * (dlogp (onehot(token) - p) - dentropy p (log p + entropy) + dlse p)
+ * with p = exp(z - lse). dlogp (with tokens), dentropy (with entropy) and dlse: fp32 [n], each
+ * nullable, one at least. A row without a token has no part of dlogp; one whose token is vocab or
+ * more is NaN; one whose lse is below -1e30 (nothing but masks) has gradient 0. p is as exact as
+ * lse, within |lse| 2^-24 of itself. dX: [n][lddx] of X's dtype, and may be X
+ * itself (same pointer and pitch). */
+optima_status optima_token_logprobs_backward(const void* X, int64_t ldx, int dtype, int64_t n,
+                                             int64_t vocab, const int64_t* tokens, float scale,
+                                             const float* lse, const float* entropy,
+                                             const float* dlogp, const float* dentropy,
+                                             const float* dlse, void* dX, int64_t lddx,
+                                             hipStream_t stream);
 
 #ifdef __cplusplus
 }

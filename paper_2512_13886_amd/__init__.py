@@ -22,7 +22,11 @@ from ._lib import (OptimaError, SolverOpts, DTYPE_F32, DTYPE_BF16, DTYPE_F64, PR
                    optima_rms_norm_backward, optima_gated_forward_workspace_bytes,
                    optima_gated_forward, optima_gated_backward_workspace_bytes,
                    optima_gated_backward, optima_w4_row_bytes, optima_w4_pack,
-                   optima_w4_workspace_bytes, optima_w4_linear, optima_w4_gated)
+                   optima_w4_workspace_bytes, optima_w4_linear, optima_w4_gated,
+                   DTYPE_MX4, optima_mx4_row_bytes, optima_mx4_scale_bytes, optima_mx4_pack,
+                   optima_mx4_unpack, optima_mx4_workspace_bytes, optima_mx4_linear, TOP_MAX,
+                   optima_token_logprobs_workspace_bytes, optima_token_logprobs,
+                   optima_token_logprobs_backward)
 
 __all__ = [
     "OptimaError", "SolverOpts", "DTYPE_F32", "DTYPE_BF16", "DTYPE_F64", "PREC_FP32",
@@ -39,4 +43,8 @@ __all__ = [
     "optima_rms_norm_backward", "optima_gated_forward_workspace_bytes", "optima_gated_forward",
     "optima_gated_backward_workspace_bytes", "optima_gated_backward", "optima_w4_row_bytes",
     "optima_w4_pack", "optima_w4_workspace_bytes", "optima_w4_linear", "optima_w4_gated",
+    "DTYPE_MX4", "optima_mx4_row_bytes", "optima_mx4_scale_bytes", "optima_mx4_pack",
+    "optima_mx4_unpack", "optima_mx4_workspace_bytes", "optima_mx4_linear", "TOP_MAX",
+    "optima_token_logprobs_workspace_bytes", "optima_token_logprobs",
+    "optima_token_logprobs_backward",
 ]

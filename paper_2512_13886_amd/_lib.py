@@ -28,6 +28,7 @@ DTYPE_F32 = 0
 DTYPE_BF16 = 1
 DTYPE_F64 = 2
 DTYPE_I8 = 3
+DTYPE_MX4 = 4
 METHOD_RAPDHG = 0
 METHOD_CG = 1
 PREC_FP32 = 0
@@ -83,7 +84,7 @@ def _sig(name, res, args):
 _status_string = _sig("optima_status_string", ctypes.c_char_p, [_i32])
 _abi_version = _sig("optima_abi_version", _i32, [])
 # The structs above mirror include/optima.h at this ABI version.
-ABI_VERSION = 12
+ABI_VERSION = 13
 if _abi_version() != ABI_VERSION:
     raise ImportError(f"{_LIB_PATH} has ABI version {_abi_version()}, the binding expects "
                       f"{ABI_VERSION}: rebuild the library")
@@ -134,6 +135,22 @@ _w4_ws = _sig("optima_w4_workspace_bytes", _sz, [_i64, _i64, _i64, _i32])
 _w4_gated = _sig("optima_w4_gated", _i32,
                  [_vp, _i64, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _i64, _i32,
                   _vp, _i64, _i32, _vp, _sz, _vp])
+
+_mx4_row = _sig("optima_mx4_row_bytes", _sz, [_i64])
+_mx4_scale_row = _sig("optima_mx4_scale_bytes", _sz, [_i64])
+_mx4_pack = _sig("optima_mx4_pack", _i32, [_vp, _i64, _i32, _i64, _i64, _vp, _vp, _vp])
+_mx4_unpack = _sig("optima_mx4_unpack", _i32, [_vp, _vp, _i64, _i64, _vp, _i64, _i32, _vp])
+_mx4_ws = _sig("optima_mx4_workspace_bytes", _sz, [_i64, _i64, _i64])
+_mx4_linear = _sig("optima_mx4_linear", _i32,
+                   [_vp, _i64, _i32, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _i32, _vp, _sz,
+                    _vp])
+_logprobs_ws = _sig("optima_token_logprobs_workspace_bytes", _sz, [_i64, _i64, _i64])
+_logprobs = _sig("optima_token_logprobs", _i32,
+                 [_vp, _i64, _i32, _i64, _i64, _vp, _f32, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz,
+                  _vp])
+_logprobs_bwd = _sig("optima_token_logprobs_backward", _i32,
+                     [_vp, _i64, _i32, _i64, _i64, _vp, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _i64,
+                      _vp])
 
 
 def library_path() -> str:
@@ -735,3 +752,178 @@ def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Q
     _check(_w4_gated(x, ldx, x_dt, _addr(x_scales), int(x_group), n, d, _addr(Qg), _addr(scales_g),
                      _addr(Qu), _addr(scales_u), int(group), ff, int(act), h, ldh, h_dt, ws,
                      nbytes, _launch_stream(stream)))
+
+
+def _need_one_device(stream, *tensors):
+    """A call launches on the current device, or its stream's: all its tensors are there."""
+    at = _current_device() if stream is None else stream.device.index
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != at:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the call runs on {at}")
+
+
+def optima_mx4_row_bytes(d: int) -> int:
+    return int(_mx4_row(d))
+
+
+def optima_mx4_scale_bytes(d: int) -> int:
+    return int(_mx4_scale_row(d))
+
+
+def _mx4_codes(q_name, Q, s_name, scales, n, d):
+    _need_shape(q_name, Q, (n, -(-d // 256) * 128), (torch.uint8,))
+    _need_shape(s_name, scales, (n, -(-d // 512) * 16), (torch.uint8,))
+
+
+def _mx4_addr(t):
+    return t.data_ptr() if t.shape[0] else None
+
+
+def optima_mx4_pack(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """Microscaled 4-bit floating point codes and scales of X [n, d] (float32 or bfloat16, weights
+    or tokens; rows may have any pitch): Q uint8 [n, optima_mx4_row_bytes(d)], scales uint8
+    [n, optima_mx4_scale_bytes(d)]. Zeros stay exactly zero."""
+    if X.dim() != 2:
+        raise ValueError("X must be [n, d]")
+    n, d = X.shape
+    x, ldx, dt = _take("X", X, (n, d), _F)
+    _mx4_codes("Q", Q, "scales", scales, n, d)
+    _need_one_device(stream, X, Q, scales)
+    _check(_mx4_pack(x, ldx, dt, n, d, _mx4_addr(Q), _mx4_addr(scales), _launch_stream(stream)))
+
+
+def optima_mx4_unpack(Q: torch.Tensor, scales: torch.Tensor, Y: torch.Tensor,
+                      stream=None) -> None:
+    """Y [n, d] (float32 or bfloat16), the values that Q and scales stand for (optima_mx4_pack)."""
+    if Y.dim() != 2:
+        raise ValueError("Y must be [n, d]")
+    n, d = Y.shape
+    y, ldy, dt = _take("Y", Y, (n, d), _F)
+    _mx4_codes("Q", Q, "scales", scales, n, d)
+    _need_one_device(stream, Q, scales, Y)
+    _check(_mx4_unpack(_mx4_addr(Q), _mx4_addr(scales), n, d, y, ldy, dt, _launch_stream(stream)))
+
+
+def optima_mx4_workspace_bytes(n_tok: int, d: int, d_out: int) -> int:
+    return int(_mx4_ws(n_tok, d, d_out))
+
+
+def optima_mx4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y: torch.Tensor,
+                      x_scales: torch.Tensor | None = None, ws: torch.Tensor | None = None,
+                      stream=None) -> None:
+    """Y = X W^T for the weights W [d_out, d] that Q and scales stand for (optima_mx4_pack). X
+    [n_tok, d] bfloat16, or the codes of packed tokens with x_scales; Y [n_tok, d_out] bfloat16
+    or float32."""
+    if X.dim() != 2 or Q.dim() != 2:
+        raise ValueError("X must be [n_tok, d], or codes, and Q codes")
+    n, n_out = X.shape[0], Q.shape[0]
+    if (X.dtype == torch.uint8) != (x_scales is not None):
+        raise ValueError("x_scales go with the codes of packed tokens")
+    if x_scales is None:
+        d = X.shape[1]
+        x, ldx, x_dt = _take("X", X, (n, d), _B)
+        _mx4_codes("Q", Q, "scales", scales, n_out, d)
+    else:
+        # The padding's codes are 0: the width up to it does as well as the tokens' own.
+        d = 2 * X.shape[1]
+        _mx4_codes("X", X, "x_scales", x_scales, n, d)
+        _mx4_codes("Q", Q, "scales", scales, n_out, d)
+        x, ldx, x_dt, xs = _mx4_addr(X), 0, DTYPE_MX4, _mx4_addr(x_scales)
+    y, ldy, y_dt = _take("Y", Y, (n, n_out), _F)
+    _need_one_device(stream, X, x_scales, Q, scales, Y, ws)
+    need = optima_mx4_workspace_bytes(n, d, n_out) if n > 16 else 0
+    nbytes = 0
+    if need or ws is not None:
+        ws, nbytes = _workspace(need, ws, X.device, stream)
+    _check(_mx4_linear(x, ldx, x_dt, None if x_scales is None else xs, n, d, _addr(Q),
+                       _addr(scales), n_out, y, ldy, y_dt, _addr(ws), nbytes,
+                       _launch_stream(stream)))
+
+
+TOP_MAX = 32
+_I = (torch.int64,)
+_F32 = (torch.float32,)
+
+
+def optima_token_logprobs_workspace_bytes(n: int, vocab: int, top: int = 0) -> int:
+    return int(_logprobs_ws(n, vocab, top))
+
+
+def _logits(logits):
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n, vocab]")
+    n, vocab = logits.shape
+    return (n, vocab, *_take("logits", logits, (n, vocab), _F))
+
+
+def _opt_shape(name, t, shape, dtypes):
+    if t is not None:
+        _need_shape(name, t, shape, dtypes)
+        return t.data_ptr() if t.numel() else None
+    return None
+
+
+def optima_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None,
+                          logp: torch.Tensor | None, lse: torch.Tensor | None = None,
+                          entropy: torch.Tensor | None = None,
+                          top_index: torch.Tensor | None = None,
+                          top_logp: torch.Tensor | None = None, scale: float = 1.0,
+                          ws: torch.Tensor | None = None, stream=None) -> None:
+    """Log probabilities of the given tokens (int64 [n]; a negative one is none: 0) under the
+    logits [n, vocab] (float32 or bfloat16; rows may have any pitch) times scale, with the
+    logarithm of the sum of exponentials lse and the entropy, float32 [n]; and the k most probable
+    alternatives, top_index int64 and top_logp float32 [n, k], equal ones by rising index."""
+    n, vocab, x, ldx, dt = _logits(logits)
+    t = _opt_shape("tokens", tokens, (n,), _I)
+    if logp is not None and tokens is None:
+        raise ValueError("logp goes with tokens")
+    k = 0
+    for name, o in (("top_index", top_index), ("top_logp", top_logp)):
+        if o is not None:
+            if o.dim() != 2 or (k and o.shape[1] != k):
+                raise ValueError("top_index and top_logp must be [n, k] of one k")
+            k = o.shape[1]
+            if not 0 < k <= min(vocab, TOP_MAX):
+                raise ValueError(f"k must be 1 to {min(vocab, TOP_MAX)}, got {k}")
+    outs = [_opt_shape(name, o, (n,), _F32)
+            for name, o in (("logp", logp), ("lse", lse), ("entropy", entropy))]
+    top = [_opt_shape("top_index", top_index, (n, k), _I),
+           _opt_shape("top_logp", top_logp, (n, k), _F32)]
+    if all(o is None for o in (logp, lse, entropy, top_index, top_logp)):
+        raise ValueError("one output is needed")
+    _need_one_device(stream, logits, tokens, logp, lse, entropy, top_index, top_logp, ws)
+    need = optima_token_logprobs_workspace_bytes(n, vocab, k)
+    nbytes = 0
+    if need or ws is not None:
+        ws, nbytes = _workspace(need, ws, logits.device, stream)
+    _check(_logprobs(x, ldx, dt, n, vocab, t, float(scale), *outs, k, *top, _addr(ws), nbytes,
+                     _launch_stream(stream)))
+
+
+def optima_token_logprobs_backward(logits: torch.Tensor, lse: torch.Tensor,
+                                   dlogits: torch.Tensor, tokens: torch.Tensor | None = None,
+                                   dlogp: torch.Tensor | None = None,
+                                   entropy: torch.Tensor | None = None,
+                                   dentropy: torch.Tensor | None = None,
+                                   dlse: torch.Tensor | None = None, scale: float = 1.0,
+                                   stream=None) -> None:
+    """dlogits [n, vocab], of the logits' type, from the gradients that reach logp (with tokens),
+    the entropy (with the entropy) and lse, float32 [n] each, and the lse that
+    optima_token_logprobs stored. dlogits may be the logits themselves."""
+    n, vocab, x, ldx, dt = _logits(logits)
+    dx, lddx, _ = _take("dlogits", dlogits, (n, vocab), (logits.dtype,))
+    t = _opt_shape("tokens", tokens, (n,), _I)
+    if lse is None:
+        raise ValueError("lse is required")
+    if dlogp is None and dentropy is None and dlse is None:
+        raise ValueError("one of dlogp, dentropy and dlse is needed")
+    if dlogp is not None and tokens is None:
+        raise ValueError("dlogp goes with tokens")
+    if dentropy is not None and entropy is None:
+        raise ValueError("dentropy goes with the entropy")
+    rows = [_opt_shape(name, o, (n,), _F32)
+            for name, o in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp),
+                            ("dentropy", dentropy), ("dlse", dlse))]
+    _need_one_device(stream, logits, lse, dlogits, tokens, dlogp, entropy, dentropy, dlse)
+    _check(_logprobs_bwd(x, ldx, dt, n, vocab, t, float(scale), *rows, dx, lddx,
+                         _launch_stream(stream)))

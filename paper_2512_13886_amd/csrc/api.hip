@@ -58,6 +58,26 @@ optima_status w4_linear(const void* X, int64_t ldx, const float* x_scales, int64
                         const void* sc2, int64_t group, int64_t d_out, int act, void* Y,
                         int64_t ldy, int y_dtype, void* ws, hipStream_t s);
 size_t w4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out, int mats);
+size_t mx4_row_bytes(int64_t d);
+size_t mx4_scale_bytes(int64_t d);
+optima_status mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t d, void* Q,
+                       void* scales, hipStream_t s);
+optima_status mx4_unpack(const void* Q, const void* scales, int64_t n, int64_t d, void* Y,
+                         int64_t ldy, int dtype, hipStream_t s);
+size_t mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out);
+optima_status mx4_linear(const void* X, int64_t ldx, const void* x_scales, int64_t n_tok, int64_t d,
+                         const void* Q, const void* scales, int64_t d_out, void* Y, int64_t ldy,
+                         int y_dtype, void* ws, hipStream_t s);
+size_t token_logprobs_workspace_bytes(int64_t n, int64_t vocab, int64_t k);
+optima_status token_logprobs(const void* X, int64_t ldx, int dtype, int64_t n, int64_t vocab,
+                             const int64_t* tokens, float scale, float* logp, float* lse,
+                             float* entropy, int64_t k, int64_t* top_index, float* top_logp,
+                             void* ws, hipStream_t s);
+optima_status token_logprobs_backward(const void* X, int64_t ldx, int dtype, int64_t n,
+                                      int64_t vocab, const int64_t* tokens, float scale,
+                                      const float* lse, const float* entropy, const float* dlogp,
+                                      const float* dentropy, const float* dlse, void* dX,
+                                      int64_t lddx, hipStream_t s);
 }  // namespace optima
 
 namespace {
@@ -150,6 +170,29 @@ optima_status w4_call(const void* X, int64_t ldx, int x_dtype, const float* x_sc
   return optima::w4_linear(X, ldx, i8 ? x_scales : nullptr, x_group, n_tok, d, Q, scales, Q2,
                            scales2, group, d_out, act, Y, ldy, y_dtype, ws, stream);
 }
+
+// Rows in pieces of 256 values, 32 threads each: a launch has fewer than 2^32 threads.
+bool mx4_rows(int64_t n, int64_t d) {
+  return n >= 0 && n < (int64_t(1) << 27) && d >= 1 && d <= kMaxDim &&
+         n * ((d + 255) / 256) < (int64_t(1) << 27);
+}
+bool mx4_sizes(int64_t n_tok, int64_t d, int64_t d_out) {
+  return n_tok >= 0 && n_tok <= (int64_t(1) << 21) && d >= 1 && d <= kMaxDim && d_out >= 1 &&
+         d_out <= kMaxCols;
+}
+// Codes and scales of n rows.
+Span mx4_codes(const void* Q, int64_t n, int64_t d) {
+  const int64_t row = int64_t(optima::mx4_row_bytes(d));
+  return {Q, n, row, row, 1};
+}
+Span mx4_scales(const void* scales, int64_t n, int64_t d) {
+  const int64_t row = int64_t(optima::mx4_scale_bytes(d)) / 4;
+  return {scales, n, row, row, 4};
+}
+bool logprob_sizes(int64_t n, int64_t vocab) {
+  return n >= 0 && n <= kMaxTok && vocab >= 1 && vocab <= kMaxDim;
+}
+bool positive(float v) { return v > 0.f && v < __builtin_inff(); }
 }  // namespace
 
 extern "C" {
@@ -166,7 +209,7 @@ const char* optima_status_string(optima_status status) {
   }
 }
 
-int optima_abi_version(void) { return 12; }
+int optima_abi_version(void) { return 13; }
 
 size_t optima_hessian_workspace_bytes(int64_t n_tok, int64_t d, int dtype) {
   if (n_tok < 0 || d < 1 || d > kMaxDim) return 0;
@@ -540,6 +583,119 @@ optima_status optima_w4_gated(const void* X, int64_t ldx, int x_dtype, const flo
   if (!Qu || !scales_u || (act != OPTIMA_ACT_NONE && act != OPTIMA_ACT_SILU)) return OPTIMA_E_INVAL;
   return w4_call(X, ldx, x_dtype, x_scales, x_group, n_tok, d, Qg, scales_g, Qu, scales_u, group,
                  d_ff, act, H, ldh, h_dtype, ws, ws_bytes, stream);
+}
+
+size_t optima_mx4_row_bytes(int64_t d) {
+  return d < 1 || d > kMaxDim ? 0 : optima::mx4_row_bytes(d);
+}
+size_t optima_mx4_scale_bytes(int64_t d) {
+  return d < 1 || d > kMaxDim ? 0 : optima::mx4_scale_bytes(d);
+}
+
+optima_status optima_mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t d, void* Q,
+                              void* scales, hipStream_t stream) {
+  if (!f32_or_bf16(dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (!mx4_rows(n, d)) return OPTIMA_E_INVAL;
+  const Span x{X, n, d, ldx, esize(dtype)}, q = mx4_codes(Q, n, d), sc = mx4_scales(scales, n, d);
+  if (!x.good() || !q.good() || !sc.good() || !optima::aligned16(Q)) return OPTIMA_E_INVAL;
+  if (q.meets(x) || sc.meets(x) || q.meets(sc)) return OPTIMA_E_INVAL;
+  if (n == 0) return OPTIMA_OK;
+  return optima::mx4_pack(X, ldx, dtype, n, d, Q, scales, stream);
+}
+
+optima_status optima_mx4_unpack(const void* Q, const void* scales, int64_t n, int64_t d, void* Y,
+                                int64_t ldy, int dtype, hipStream_t stream) {
+  if (!f32_or_bf16(dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (!mx4_rows(n, d)) return OPTIMA_E_INVAL;
+  const Span y{Y, n, d, ldy, esize(dtype)}, q = mx4_codes(Q, n, d), sc = mx4_scales(scales, n, d);
+  if (!y.good() || !q.good() || !sc.good() || !optima::aligned16(Q)) return OPTIMA_E_INVAL;
+  if (y.meets(q) || y.meets(sc)) return OPTIMA_E_INVAL;
+  if (n == 0) return OPTIMA_OK;
+  return optima::mx4_unpack(Q, scales, n, d, Y, ldy, dtype, stream);
+}
+
+size_t optima_mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
+  return mx4_sizes(n_tok, d, d_out) ? optima::mx4_workspace_bytes(n_tok, d, d_out) : 0;
+}
+
+optima_status optima_mx4_linear(const void* X, int64_t ldx, int x_dtype, const void* x_scales,
+                                int64_t n_tok, int64_t d, const void* Q, const void* scales,
+                                int64_t d_out, void* Y, int64_t ldy, int y_dtype, void* ws,
+                                size_t ws_bytes, hipStream_t stream) {
+  const bool packed = x_dtype == OPTIMA_DTYPE_MX4;
+  if ((!packed && x_dtype != OPTIMA_DTYPE_BF16) || !f32_or_bf16(y_dtype))
+    return OPTIMA_E_UNSUPPORTED;
+  if (!mx4_sizes(n_tok, d, d_out) || (!packed && x_scales)) return OPTIMA_E_INVAL;
+  const Span x = packed ? mx4_codes(X, n_tok, d) : Span{X, n_tok, d, ldx, 2};
+  const Span xs = mx4_scales(packed ? x_scales : nullptr, n_tok, d);
+  const Span q = mx4_codes(Q, d_out, d), sc = mx4_scales(scales, d_out, d);
+  const Span y{Y, n_tok, d_out, ldy, esize(y_dtype)};
+  if (!x.good() || (packed && (!xs.good() || !optima::aligned16(X))) || !q.good() || !sc.good() ||
+      !optima::aligned16(Q) || !y.good())
+    return OPTIMA_E_INVAL;
+  for (const Span& i : {x, xs, q, sc})
+    if (y.meets(i)) return OPTIMA_E_INVAL;
+  const size_t need = optima::mx4_workspace_bytes(n_tok, d, d_out);
+  if (need && (!ws || !optima::aligned16(ws) || ws_bytes < need)) return OPTIMA_E_WORKSPACE;
+  if (n_tok == 0) return OPTIMA_OK;
+  return optima::mx4_linear(X, ldx, packed ? x_scales : nullptr, n_tok, d, Q, scales, d_out, Y, ldy,
+                            y_dtype, ws, stream);
+}
+
+size_t optima_token_logprobs_workspace_bytes(int64_t n, int64_t vocab, int64_t k) {
+  if (!logprob_sizes(n, vocab) || k < 0 || k > std::min<int64_t>(vocab, OPTIMA_TOP_MAX)) return 0;
+  return optima::token_logprobs_workspace_bytes(n, vocab, k);
+}
+
+optima_status optima_token_logprobs(const void* X, int64_t ldx, int dtype, int64_t n, int64_t vocab,
+                                    const int64_t* tokens, float scale, float* logp, float* lse,
+                                    float* entropy, int64_t k, int64_t* top_index, float* top_logp,
+                                    void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!f32_or_bf16(dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (!logprob_sizes(n, vocab) || !positive(scale) || k < 0 || k > vocab) return OPTIMA_E_INVAL;
+  if (k > OPTIMA_TOP_MAX) return OPTIMA_E_UNSUPPORTED;
+  const bool top = top_index || top_logp;
+  if (n > 0 && (top != (k > 0) || (!logp && !lse && !entropy && !top) || (logp && !tokens)))
+    return OPTIMA_E_INVAL;
+  const Span x{X, n, vocab, ldx, esize(dtype)}, t{tokens, 1, n, n, 8};
+  const Span out[5] = {{logp, 1, n, n, 4}, {lse, 1, n, n, 4}, {entropy, 1, n, n, 4},
+                       {top_index, 1, n * k, n * k, 8}, {top_logp, 1, n * k, n * k, 4}};
+  if (!x.good() || !t.aligned()) return OPTIMA_E_INVAL;
+  for (const Span& o : out) {
+    if (!o.aligned() || o.meets(x) || o.meets(t)) return OPTIMA_E_INVAL;
+    for (const Span& p : out)
+      if (&p != &o && o.meets(p)) return OPTIMA_E_INVAL;
+  }
+  const size_t need = optima::token_logprobs_workspace_bytes(n, vocab, k);
+  if (need && (!ws || (reinterpret_cast<uintptr_t>(ws) & 7) || ws_bytes < need))
+    return OPTIMA_E_WORKSPACE;
+  if (n == 0) return OPTIMA_OK;
+  return optima::token_logprobs(X, ldx, dtype, n, vocab, tokens, scale, logp, lse, entropy, k,
+                                top_index, top_logp, ws, stream);
+}
+
+optima_status optima_token_logprobs_backward(const void* X, int64_t ldx, int dtype, int64_t n,
+                                             int64_t vocab, const int64_t* tokens, float scale,
+                                             const float* lse, const float* entropy,
+                                             const float* dlogp, const float* dentropy,
+                                             const float* dlse, void* dX, int64_t lddx,
+                                             hipStream_t stream) {
+  if (!f32_or_bf16(dtype)) return OPTIMA_E_UNSUPPORTED;
+  if (!logprob_sizes(n, vocab) || !positive(scale)) return OPTIMA_E_INVAL;
+  if (n > 0 && (!lse || (!dlogp && !dentropy && !dlse) || (dlogp && !tokens) ||
+                (dentropy && !entropy)))
+    return OPTIMA_E_INVAL;
+  const Span x{X, n, vocab, ldx, esize(dtype)}, dx{dX, n, vocab, lddx, esize(dtype)};
+  if (!x.good() || !dx.good() || (dx.meets(x) && !dx.same(x))) return OPTIMA_E_INVAL;
+  const Span t{tokens, 1, n, n, 8};
+  if (!t.aligned() || dx.meets(t)) return OPTIMA_E_INVAL;
+  for (const float* p : {lse, entropy, dlogp, dentropy, dlse}) {
+    const Span i{p, 1, n, n, 4};
+    if (!i.aligned() || dx.meets(i)) return OPTIMA_E_INVAL;
+  }
+  if (n == 0) return OPTIMA_OK;
+  return optima::token_logprobs_backward(X, ldx, dtype, n, vocab, tokens, scale, lse, entropy, dlogp,
+                                         dentropy, dlse, dX, lddx, stream);
 }
 
 }  // extern "C"

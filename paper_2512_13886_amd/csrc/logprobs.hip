@@ -1,0 +1,508 @@
+// Log probabilities of given tokens, with the entropy and the most probable alternatives, and
+// their gradient.
+//
+// With z = scale x over a row of the vocabulary, m = max x, y = scale (x - m), S = sum exp(y) and
+// T = sum exp(y) y: lse = scale m + ln S, logp = scale (x_t - m) - ln S, H = ln S - T / S. S and T
+// are kept for a running m, so that a row is read once; parts of a row (m, S, T) join to the
+// whole's.
+//
+// The k largest come out of the same pass. Each thread keeps the largest of its values and the
+// first group of eight that holds it; groups compare by value and then by their place. The k
+// largest of a row lie in the k best threads' values (a value elsewhere has k larger ones before
+// it), which are read again, and those not below the k-th best thread's are ranked.
+#include <type_traits>
+
+#include "common.h"
+#include "vec8.h"
+
+namespace optima {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct LogprobArgs {
+  const void* x;
+  const int64_t* tokens;
+  float *logp, *lse, *entropy, *top_logp;
+  int64_t* top_index;
+  float* stat;     // of parts: [row][part][m, S, T]
+  uint64_t* keys;  // of parts: [row][part][k], largest first, 0 for none
+  int64_t ldx, n, row0;  // row0: the launch's first row
+  int vocab, k, parts, part_len;
+  float scale;
+};
+
+// ---------------------------------------------------------------------------
+// Values in their order: larger values, and of equal ones earlier places, have larger keys. -0 is
+// 0, and NaN is -inf.
+// ---------------------------------------------------------------------------
+
+__device__ inline uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x == x ? x + 0.f : -__builtin_inff());
+  return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
+}
+__device__ inline float value_of(uint32_t o) {
+  return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ inline uint64_t key_of(float x, uint32_t place) {
+  return uint64_t(order_of(x)) << 32 | uint32_t(~place);
+}
+
+template <int CTRL>
+__device__ inline uint32_t dpp_max(uint32_t v) {
+  return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false)));
+}
+// Largest over a wave: within rows of 16 lanes, then rows and halves into the last lane.
+__device__ inline uint32_t wave_max(uint32_t v) {
+  v = dpp_max<0x111>(v);  // from 1, 2, 4 and 8 lanes before
+  v = dpp_max<0x112>(v);
+  v = dpp_max<0x114>(v);
+  v = dpp_max<0x118>(v);
+  v = dpp_max<0x142>(v);  // a row's last lane to the next row
+  v = dpp_max<0x143>(v);  // lane 31 to the second half
+  return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+}
+__device__ inline uint64_t wave_max64(uint64_t v) {
+  const uint32_t hi = wave_max(uint32_t(v >> 32));
+  return uint64_t(hi) << 32 | wave_max(uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
+}
+
+__device__ inline float max3(float a, float b, float c) {
+  // NaN loses. (The builtin maximum makes every operand canonical first, at an instruction each.)
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+// S and T for a running m
+// ---------------------------------------------------------------------------
+
+struct Sums {
+  float m, s, t;  // t in units of log 2: sum of 2^y y
+};
+// The reference of the exponents: any finite one for a row that has only -inf yet.
+__device__ inline float finite_max(float m) { return m > -__builtin_inff() ? m : 0.f; }
+// to the maximum m (not smaller). c: scale log2 e.
+__device__ inline void rebase(Sums& a, float m, float c) {
+  // Above 0 only from -inf, with sums of 0.
+  const float d = fminf(fmaxf((finite_max(a.m) - finite_max(m)) * c, -1e30f), 0.f);
+  const float r = __builtin_amdgcn_exp2f(d);
+  a.t = r * (a.t + d * a.s);
+  a.s *= r;
+  a.m = m;
+}
+__device__ inline Sums wave_sums(Sums a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  rebase(a, m, c);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    a.s += __shfl_xor(a.s, o, 64);
+    a.t += __shfl_xor(a.t, o, 64);
+  }
+  return a;
+}
+
+// The row's outputs of its sums, by one thread.
+__device__ inline float logp_of(float x, const Sums& a, float scale) {
+  return a.m == -__builtin_inff() && a.s == 0.f ? -__builtin_inff() : scale * (x - a.m) - logf(a.s);
+}
+template <typename T>
+__device__ inline float value1(const T* p);
+template <>
+__device__ inline float value1(const float* p) { return *p; }
+template <>
+__device__ inline float value1(const bf16_t* p) { return bf16_low(p->bits); }
+
+template <typename T>
+__device__ inline void write_row(const LogprobArgs& a, int64_t row, const Sums& s) {
+  // Nothing left of the row: lse and its log probabilities are -inf, its entropy 0.
+  const bool none = s.m == -__builtin_inff() && s.s == 0.f;
+  if (a.lse) a.lse[row] = none ? -__builtin_inff() : a.scale * s.m + logf(s.s);
+  if (a.entropy) a.entropy[row] = none ? 0.f : logf(s.s) - s.t / s.s * kLn2;
+  if (a.logp) {
+    const int64_t t = a.tokens[row];
+    float v = 0.f;
+    if (t >= a.vocab)
+      v = __builtin_nanf("");
+    else if (t >= 0)
+      v = logp_of(value1(static_cast<const T*>(a.x) + row * a.ldx + t), s, a.scale);
+    a.logp[row] = v;
+  }
+}
+__device__ inline void write_top(const LogprobArgs& a, int64_t row, int j, uint64_t key,
+                                 const Sums& s) {
+  const int64_t at = row * a.k + j;
+  if (a.top_index) a.top_index[at] = int64_t(uint32_t(~uint32_t(key)));
+  if (a.top_logp) a.top_logp[at] = logp_of(value_of(uint32_t(key >> 32)), s, a.scale);
+}
+
+// What lanes of a wave wrote to LDS before is there for its other lanes after.
+__device__ inline void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+template <int WAVES>
+__device__ inline void group_sync() {
+  if constexpr (WAVES > 1)
+    __syncthreads();
+  else
+    wave_exchange();
+}
+
+constexpr int kGroups = 4;         // of eight values that a thread loads together
+constexpr int kTopSteps = 16;      // groups of a thread, at most, where alternatives are wanted
+constexpr int kPartLen = kTopSteps * 256 * 8;
+
+// A part of a row by WAVES waves (4: a workgroup; 1: four rows a workgroup).
+template <typename T, int WAVES, bool TOP>
+__global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
+  constexpr int kThr = 64 * WAVES, kStep = 8 * kThr, kSub = 4 / WAVES;
+  __shared__ float red[WAVES][3];
+  __shared__ uint64_t best_of[TOP ? 256 : 1];
+  __shared__ int chosen[TOP ? kSub : 1][OPTIMA_TOP_MAX];
+  __shared__ uint64_t border[kSub];
+  __shared__ int found[kSub], picked[kSub];
+  extern __shared__ uint64_t lists[];
+  const int sub = WAVES > 1 ? 0 : threadIdx.x >> 6, t = threadIdx.x & (kThr - 1);
+  const int64_t task = int64_t(blockIdx.x) * kSub + sub;
+  const int64_t row = a.row0 + task / a.parts;
+  if (row >= a.n) return;  // all threads of the row
+  const int part = int(task % a.parts), p0 = part * a.part_len;
+  const int len = std::min(a.part_len, a.vocab - p0);
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx + p0;
+  const float c = a.scale * kLog2e;
+
+  Sums s = {-__builtin_inff(), 0.f, 0.f};
+  float best = -__builtin_inff();
+  int base = 8 * t;
+  auto groups = [&](int at0, auto whole) {
+    Raw8<T> raw[kGroups];
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      if (whole)
+        load8(raw[u], x + at0 + u * kStep);
+      else
+        load_piece(raw[u], x, at0 + u * kStep, len);
+    }
+    float v[kGroups][8], m = s.m;
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      values8(raw[u], v[u]);
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (at0 + u * kStep + e >= len) v[u][e] = -__builtin_inff();
+      }
+      float g = max3(max3(v[u][0], v[u][1], v[u][2]), v[u][3], v[u][4]);
+      g = max3(max3(g, v[u][5], v[u][6]), v[u][7], v[u][7]);
+      if (TOP && g > best) {
+        best = g;
+        base = at0 + u * kStep;
+      }
+      m = max3(m, g, g);
+    }
+    if (m > s.m) rebase(s, m, c);
+    const float ref = finite_max(m);
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = (v[u][e] - ref) * c;
+        const float p = __builtin_amdgcn_exp2f(y);
+        s.s += p;
+        s.t += p * max3(y, -1e4f, -1e4f);  // 0 for p = 0; NaN comes in by p
+      }
+  };
+  int at = 8 * t, left = len;
+  for (; left >= kGroups * kStep; left -= kGroups * kStep, at += kGroups * kStep)
+    groups(at, std::true_type());
+  if (left > 0) groups(at, std::false_type());
+
+  s = wave_sums(s, c);
+  if constexpr (WAVES > 1) {
+    const int wave = threadIdx.x >> 6;
+    if ((t & 63) == 0) red[wave][0] = s.m, red[wave][1] = s.s, red[wave][2] = s.t;
+    __syncthreads();
+    float m = red[0][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, red[w][0]);
+    Sums all = {m, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      Sums one = {red[w][0], red[w][1], red[w][2]};
+      rebase(one, m, c);
+      all.s += one.s;
+      all.t += one.t;
+    }
+    s = all;
+  }
+  if (t == 0) {
+    if (a.parts == 1) {
+      write_row<T>(a, row, s);
+    } else {
+      float* to = a.stat + (row * a.parts + part) * 3;
+      to[0] = s.m, to[1] = s.s, to[2] = s.t;
+    }
+  }
+  if constexpr (TOP) {
+    // The best threads, one after the other, by one wave.
+    const uint64_t mine = 8 * t < len ? key_of(best, uint32_t(p0 + base)) : 0u;
+    if constexpr (WAVES > 1) {
+      best_of[t] = mine;
+      __syncthreads();
+    }
+    if (t < 64) {
+      uint64_t own[WAVES];
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) own[w] = WAVES > 1 ? best_of[t + 64 * w] : mine;
+      uint64_t last = 0;
+      int j = 0;
+      for (; j < a.k; ++j) {
+        uint64_t top = own[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = max(top, own[w]);
+        top = wave_max64(top);
+        if (!top) break;
+        last = top;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+          if (own[w] == top) {
+            chosen[sub][j] = t + 64 * w;
+            own[w] = 0;
+          }
+      }
+      if (t == 0) {
+        found[sub] = 0;
+        picked[sub] = j;
+        border[sub] = j < a.k ? 0 : last;  // fewer threads than k: all their values
+      }
+    }
+    group_sync<WAVES>();
+    const uint64_t limit = border[sub];
+    const uint32_t limit_value = uint32_t(limit >> 32), limit_place = ~uint32_t(limit);
+    const int steps = (len + kStep - 1) / kStep;
+    uint64_t* list = lists + sub * list_len;
+    const int tasks = picked[sub] * steps;
+    for (int q = t; q < tasks; q += kThr) {
+      const int j = q / steps, g = 8 * chosen[sub][j] + (q - j * steps) * kStep;
+      if (g >= len) continue;
+      Raw8<T> raw;
+      load_piece(raw, x, g, len);
+      float v[8];
+      values8(raw, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t o = order_of(v[e]);
+        if (g + e < len && (o > limit_value || (o == limit_value && uint32_t(p0 + g) <= limit_place)))
+          list[atomicAdd(&found[sub], 1)] = uint64_t(o) << 32 | uint32_t(~uint32_t(p0 + g + e));
+      }
+    }
+    group_sync<WAVES>();
+    const int count = found[sub];
+    uint64_t* to = a.keys + (row * a.parts + part) * a.k;
+    for (int q = t; q < count; q += kThr) {
+      const uint64_t key = list[q];
+      int rank = 0;
+      for (int r = 0; r < count; ++r) rank += list[r] > key;
+      if (rank >= a.k) continue;
+      if (a.parts == 1)
+        write_top(a, row, rank, key, s);
+      else
+        to[rank] = key;
+    }
+    if (a.parts > 1)
+      for (int q = count + t; q < a.k; q += kThr) to[q] = 0;
+  }
+}
+
+// The parts of a row, by one wave: lane p has part p.
+template <typename T>
+__global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = a.row0 + int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= a.n) return;
+  const float c = a.scale * kLog2e;
+  Sums s = {-__builtin_inff(), 0.f, 0.f};
+  if (lane < a.parts) {
+    const float* p = a.stat + (row * a.parts + lane) * 3;
+    s = Sums{p[0], p[1], p[2]};
+  }
+  s = wave_sums(s, c);
+  if (lane == 0) write_row<T>(a, row, s);
+  if (!a.k) return;
+  const uint64_t* mine = a.keys + (row * a.parts + lane) * a.k;
+  int at = 0;
+  uint64_t head = lane < a.parts ? mine[0] : 0, next = lane < a.parts && a.k > 1 ? mine[1] : 0;
+  uint64_t out = 0;
+  for (int j = 0; j < a.k; ++j) {
+    const uint64_t top = wave_max64(head);
+    if (lane == j) out = top;
+    if (head == top && top) {
+      head = next;
+      ++at;
+      next = at + 1 < a.k ? mine[at + 1] : 0;
+    }
+  }
+  if (lane < a.k) write_top(a, row, lane, out, s);
+}
+
+struct LogprobGradArgs {
+  const void* x;
+  const int64_t* tokens;
+  const float *lse, *entropy, *dlogp, *dentropy, *dlse;
+  void* dx;
+  int64_t ldx, lddx, n, row0;
+  int vocab, parts;
+  float scale;
+};
+
+// dx = scale (g at the token + p (dlse - g - dH (ln p + H))), p = exp(z - lse). Bound by HBM.
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
+  constexpr int kThr = 64 * WAVES, kStep = 8 * kThr, kSub = 4 / WAVES;
+  const int sub = WAVES > 1 ? 0 : threadIdx.x >> 6, t = threadIdx.x & (kThr - 1);
+  const int64_t task = int64_t(blockIdx.x) * kSub + sub;
+  const int64_t row = a.row0 + task / a.parts;
+  if (row >= a.n) return;
+  const int at0 = int(task % a.parts) * kGroups * kStep + 8 * t;
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  T* dx = static_cast<T*>(a.dx) + row * a.lddx;
+  const float lse = a.lse[row];
+  const int64_t token = a.tokens ? a.tokens[row] : -1;
+  float g = a.dlogp && token >= 0 ? a.dlogp[row] : 0.f;
+  if (token >= a.vocab) g = __builtin_nanf("");
+  const float gh = a.dentropy ? a.dentropy[row] : 0.f, h = a.dentropy ? a.entropy[row] : 0.f;
+  const float gl = (a.dlse ? a.dlse[row] : 0.f) - g;
+  // Nothing left of the row: no gradient. A row of the lowest finite value counts as such: beside
+  // it lse cannot hold the logarithm of the vocabulary, and p would be 1 everywhere.
+  const bool none = lse < -1e30f;
+  Raw8<T> raw[kGroups];
+#pragma unroll
+  for (int u = 0; u < kGroups; ++u) load_piece(raw[u], x, at0 + u * kStep, a.vocab);
+#pragma unroll
+  for (int u = 0; u < kGroups; ++u) {
+    const int at = at0 + u * kStep;
+    if (at >= a.vocab) break;
+    float v[8];
+    values8(raw[u], v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float lp = v[e] * a.scale - lse;
+      const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+      float d = p * (gl - gh * (max3(lp, -1e4f, -1e4f) + h));
+      if (at + e == token) d += g;
+      v[e] = none ? 0.f : d * a.scale;
+    }
+    store_upto8(dx + at, v, a.vocab - at);
+  }
+}
+
+constexpr int64_t kMostTasks = int64_t(1) << 22;  // of a launch, in workgroups
+
+// Waves of a row: one for up to 2048 values.
+bool narrow(int64_t vocab) { return vocab <= 2048; }
+
+// Parts of a row: enough workgroups for the chip, of 2048 values at least, and with alternatives
+// of kPartLen at most.
+struct LogprobPlan {
+  int parts, len;
+};
+LogprobPlan plan(int64_t n, int64_t vocab, int k) {
+  if (narrow(vocab)) return {1, int(vocab)};
+  int64_t parts = std::min<int64_t>({ceil_div(2048, std::max<int64_t>(n, 1)), ceil_div(vocab, 2048), 64});
+  if (k) parts = std::max(parts, ceil_div(vocab, kPartLen));
+  const int64_t len = round_up(ceil_div(vocab, parts), 8);
+  return {int(ceil_div(vocab, len)), int(len)};
+}
+
+template <typename T, int WAVES>
+void launch_logprobs(LogprobArgs a, hipStream_t s) {
+  constexpr int kSub = 4 / WAVES;
+  const int64_t rows = kMostTasks * kSub / a.parts;
+  const int list = a.k * int(ceil_div(a.part_len, 512 * WAVES)) * 8;
+  for (; a.row0 < a.n; a.row0 += rows) {
+    const int64_t now = std::min(a.n - a.row0, rows);
+    LogprobArgs b = a;
+    b.n = a.row0 + now;
+    const dim3 grid(unsigned(ceil_div(now * a.parts, kSub)));
+    if (a.k)
+      hipLaunchKernelGGL((k_logprobs<T, WAVES, true>), grid, dim3(256), size_t(list) * kSub * 8, s, b,
+                         list);
+    else
+      hipLaunchKernelGGL((k_logprobs<T, WAVES, false>), grid, dim3(256), 0, s, b, 0);
+    if (a.parts > 1)
+      hipLaunchKernelGGL(k_logprobs_join<T>, dim3(unsigned(ceil_div(now, 4))), dim3(256), 0, s, b);
+  }
+}
+
+template <typename T, int WAVES>
+void launch_grad(LogprobGradArgs a, hipStream_t s) {
+  constexpr int kSub = 4 / WAVES;
+  a.parts = int(ceil_div(a.vocab, kGroups * 512 * WAVES));
+  const int64_t rows = std::max<int64_t>(1, kMostTasks * kSub / a.parts);
+  for (; a.row0 < a.n; a.row0 += rows) {
+    LogprobGradArgs b = a;
+    b.n = std::min(a.n, a.row0 + rows);
+    hipLaunchKernelGGL((k_logprobs_grad<T, WAVES>),
+                       dim3(unsigned(ceil_div((b.n - a.row0) * a.parts, kSub))), dim3(256), 0, s, b);
+  }
+}
+
+}  // namespace
+
+size_t token_logprobs_workspace_bytes(int64_t n, int64_t vocab, int64_t k) {
+  // The most of any number of rows up to these, so that more need no less.
+  size_t most = 0;
+  auto of = [&](int64_t rows) {
+    const LogprobPlan p = plan(rows, vocab, int(k));
+    if (p.parts > 1) most = std::max(most, size_t(rows) * p.parts * size_t(12 + 8 * k));
+  };
+  for (int64_t parts = 2; parts <= 64; ++parts)  // the last rows of each number of parts
+    of(std::min<int64_t>(n, (2048 - 1) / (parts - 1)));
+  of(n);
+  return most;
+}
+
+optima_status token_logprobs(const void* X, int64_t ldx, int dtype, int64_t n, int64_t vocab,
+                             const int64_t* tokens, float scale, float* logp, float* lse,
+                             float* entropy, int64_t k, int64_t* top_index, float* top_logp,
+                             void* ws, hipStream_t s) {
+  const LogprobPlan p = plan(n, vocab, int(k));
+  uint64_t* keys = static_cast<uint64_t*>(ws);
+  float* stat = keys ? reinterpret_cast<float*>(keys + size_t(n) * p.parts * size_t(k)) : nullptr;
+  LogprobArgs a{X, tokens, logp, lse, entropy, top_logp, top_index, stat, keys, ldx, n, 0,
+                int(vocab), int(k), p.parts, p.len, scale};
+  if (dtype == OPTIMA_DTYPE_BF16) {
+    if (narrow(vocab)) launch_logprobs<bf16_t, 1>(a, s);
+    else launch_logprobs<bf16_t, 4>(a, s);
+  } else {
+    if (narrow(vocab)) launch_logprobs<float, 1>(a, s);
+    else launch_logprobs<float, 4>(a, s);
+  }
+  OPTIMA_LAUNCH_CHECK();
+  return OPTIMA_OK;
+}
+
+optima_status token_logprobs_backward(const void* X, int64_t ldx, int dtype, int64_t n,
+                                      int64_t vocab, const int64_t* tokens, float scale,
+                                      const float* lse, const float* entropy, const float* dlogp,
+                                      const float* dentropy, const float* dlse, void* dX,
+                                      int64_t lddx, hipStream_t s) {
+  LogprobGradArgs a{X, tokens, lse, entropy, dlogp, dentropy, dlse, dX, ldx, lddx, n, 0,
+                    int(vocab), 0, scale};
+  if (dtype == OPTIMA_DTYPE_BF16) {
+    if (narrow(vocab)) launch_grad<bf16_t, 1>(a, s);
+    else launch_grad<bf16_t, 4>(a, s);
+  } else {
+    if (narrow(vocab)) launch_grad<float, 1>(a, s);
+    else launch_grad<float, 4>(a, s);
+  }
+  OPTIMA_LAUNCH_CHECK();
+  return OPTIMA_OK;
+}
+
+}  // namespace optima

@@ -1,0 +1,551 @@
+// Microscaled 4-bit floating point: packing rows, the values they stand for, and products
+// Y = X W^T with packed weights, of 16-bit tokens or packed ones.
+//
+// A block of 32 values v has the scale 2^(e - 2), e = floor(log2 max |v|), kept as a biased
+// exponent in a byte, and codes of v / scale: sign, two bits of exponent and one of mantissa
+// (0, 0.5, 1, 1.5, 2, 3, 4, 6), nearest even, at most 6. A zero has code 0, so that pruned
+// entries stay exactly zero.
+//
+// Rows of codes are padded to whole 256 values (128 bytes) and lie in the order of the values:
+// in the products lane (b, i) of a wave holds the 16 bytes of block b of 128 values of row i,
+// which is an operand of the 16x16x128 block-scaled MFMA as it lies, and four of the 16x16x32
+// bf16 one. The scales of four such 128s lie together for each b: a lane's four are one dword,
+// and the MFMA picks the byte, so that scales cost no instructions.
+//   packed tokens: products of codes and scales are exact, the sum is the MFMA's fp32.
+//   16-bit tokens: codes times scale are exact in bf16 (one instruction for two).
+#include "common.h"
+#include "vec8.h"
+
+namespace optima {
+namespace {
+
+constexpr int kChunk = 128;  // values of an operand
+constexpr int kChunkBytes = 64;
+
+typedef int i8x32 __attribute__((ext_vector_type(8)));
+
+int64_t row_bytes(int64_t d) { return ceil_div(d, 256) * 128; }
+int64_t scale_bytes(int64_t d) { return ceil_div(d, 512) * 16; }
+
+// ---------------------------------------------------------------------------
+// Packing, and back
+// ---------------------------------------------------------------------------
+
+// Largest of m over the four lanes of a block.
+__device__ inline uint32_t quad_max(uint32_t m) {
+  m = max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0xB1, 0xF, 0xF, true)));  // lanes 1 0 3 2
+  return max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0x4E, 0xF, 0xF, true)));  // 2 3 0 1
+}
+
+// Thirty-two lanes for 256 values, one dword (eight codes) each.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, int64_t total,
+                                                       int pieces, int d, uint8_t* Q,
+                                                       uint8_t* scales, int srow) {
+  const int64_t idx = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  const bool live = idx < total;  // of all 32 lanes
+  const int64_t n = live ? idx / pieces : 0;
+  const int h = live ? int(idx - n * pieces) : 0;
+  const int i = threadIdx.x & 31;
+  Raw8<T> raw;
+  load_piece(raw, X + n * ldx, 256 * h + 8 * i, live ? d : 0);
+  float v[8];
+  values8(raw, v);
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  m = quad_max(m);
+  // The exponent's field of the largest less 2, within 0 .. 252; 255 with infinity or NaN, whose
+  // block has codes 0: NaN as values.
+  const uint32_t top = m >> 23;
+  const bool fine = top < 255u;
+  const uint32_t s = fine ? max(top, 2u) - 2u : 255u;
+  const float inv = __uint_as_float((254u - s) << 23);  // 2^(127 - s): the quotients are exact
+  uint32_t q = 0;
+  if (fine) {
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[0] * inv, v[1] * inv, 1.f, 0);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[2] * inv, v[3] * inv, 1.f, 1);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4] * inv, v[5] * inv, 1.f, 2);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6] * inv, v[7] * inv, 1.f, 3);
+  }
+  // Lanes 0 .. 15 hold the first 128 values, 16 .. 31 the second, whose scales are neighbours.
+  const uint32_t both = s | uint32_t(__shfl_xor(int(s), 16, 64)) << 8;
+  if (!live) return;
+  *reinterpret_cast<uint32_t*>(Q + (n * pieces + h) * 128 + 4 * i) = q;
+  if (i < 16 && (i & 3) == 0) {
+    uint8_t* at = scales + n * srow + 16 * (h >> 1) + i + 2 * (h & 1);
+    if ((h & 1) == 0 && h + 1 == pieces)  // the row's padding
+      *reinterpret_cast<uint32_t*>(at) = both;
+    else
+      *reinterpret_cast<uint16_t*>(at) = uint16_t(both);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_mx4_unpack(const uint8_t* Q, const uint8_t* scales,
+                                                         int srow, int64_t total, int pieces,
+                                                         int d, T* Y, int64_t ldy) {
+  const int64_t idx = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  if (idx >= total) return;
+  const int64_t n = idx / pieces;
+  const int h = int(idx - n * pieces);
+  const int i = threadIdx.x & 31, k = 256 * h + 8 * i;
+  if (k >= d) return;
+  const uint32_t q = *reinterpret_cast<const uint32_t*>(Q + (n * pieces + h) * 128 + 4 * i);
+  const uint32_t s = scales[n * srow + 16 * (h >> 1) + (i & 12) + 2 * (h & 1) + (i >> 4)];
+  const float scale = __uint_as_float(s << 23);  // its exponent alone counts
+  const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 0);
+  const f2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 1);
+  const f2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 2);
+  const f2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 3);
+  const float v[8] = {a[0], a[1], b[0], b[1], c[0], c[1], e[0], e[1]};
+  store_upto8(Y + n * ldy + k, v, d - k);
+}
+
+// ---------------------------------------------------------------------------
+// Products
+// ---------------------------------------------------------------------------
+
+struct Mx4Args {
+  const void* x;      // bf16 [n_tok][ldx], or codes
+  const uint8_t* xs;  // scales of codes
+  const uint8_t *q, *s;
+  void* y;
+  f4* part;
+  int64_t n_tok, d_out, ldx, ldy;
+  int d, chunks, row, srow, y_f32;  // chunks of 128 values; bytes of a row of codes, of scales
+};
+
+// Eight codes of a block times its scale (a float of which the exponent counts).
+__device__ inline bf16x8 weights8(uint32_t w, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// Byte U of a lane's scales as such a float.
+template <int U>
+__device__ inline float scale_at(uint32_t s) {
+  return __uint_as_float(((s >> (8 * U)) & 255u) << 23);
+}
+// c += W X^T for 128 values of 16 rows and 16 packed tokens; byte U of the lanes' scales.
+template <int U>
+__device__ inline void mfma_mx4(f4& c, const u32x4& w, uint32_t sw, const u32x4& x, uint32_t sx) {
+  const i8x32 a = {int(w[0]), int(w[1]), int(w[2]), int(w[3]), 0, 0, 0, 0};
+  const i8x32 b = {int(x[0]), int(x[1]), int(x[2]), int(x[3]), 0, 0, 0, 0};
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, U, int(sw), U, int(sx));
+}
+// The same with 16-bit tokens: x[j] holds values 8 j .. of the lane's block.
+template <int U>
+__device__ inline void mfma_bf16(f4& c, const u32x4& w, uint32_t sw, const bf16x8 (&x)[4]) {
+  const float scale = scale_at<U>(sw);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(weights8(w[j], scale), x[j], c, 0, 0, 0);
+}
+
+// Values k .. k + 7 of a row of d 16-bit values; zeros past its end.
+__device__ inline u32x4 tokens8(const bf16_t* row, int k, int d) {
+  Raw8<bf16_t> r;
+  load_piece(r, row, k, d);
+  return r.w;
+}
+
+__device__ inline void store_y4(const Mx4Args& a, int64_t tok, int64_t n, const f4& v) {
+  if (tok >= a.n_tok || n >= a.d_out) return;
+  const float w[4] = {v[0], v[1], v[2], v[3]};
+  const int left = int(std::min<int64_t>(a.d_out - n, 4));
+  const int64_t at = tok * a.ldy + n;
+  if (a.y_f32)
+    store_upto4(static_cast<float*>(a.y) + at, w, left);
+  else
+    store_upto4(static_cast<bf16_t*>(a.y) + at, w, left);
+}
+
+constexpr int kBatch = 4;                 // chunks that a wave's loads go out together for
+constexpr int kBatchK = kBatch * kChunk;  // 512 values, whose scales are one dword a lane
+
+// What lanes of a wave wrote to LDS before is there for its other lanes after. A wave's LDS
+// accesses are served in order, so that this only keeps the compiler from moving them.
+__device__ inline void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Up to 16 tokens. A workgroup takes 16 outputs, its waves every waves-th batch of 512 values,
+// and the waves' sums are joined in LDS in their order.
+constexpr int kFew = 16;
+constexpr int kFewWaves = 16;
+// Bytes of a token's batch in LDS, with 64 between rows.
+constexpr int kFewPitch = kBatchK * 2 + 64;
+
+// A batch's codes and scales of row n: zeros for chunks past the row's end.
+__device__ inline void load_codes(u32x4 (&w)[kBatch], uint32_t& s, const uint8_t* q,
+                                  const uint8_t* sc, const Mx4Args& a, int64_t n, int batch, int b) {
+  const uint8_t* p = q + n * a.row + b * 16;
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    const int c = batch * kBatch + u;
+    w[u] = u32x4{0, 0, 0, 0};
+    if (c < a.chunks) w[u] = *reinterpret_cast<const u32x4*>(p + c * kChunkBytes);
+  }
+  s = *reinterpret_cast<const uint32_t*>(sc + n * a.srow + batch * 16 + 4 * b);
+}
+
+// ROWS: tokens that a lane loads values of together.
+template <bool PACKED, int ROWS>
+__global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  float* part = reinterpret_cast<float*>(lds);  // [wave][lane][4], at the end
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int b = lane >> 4, i = lane & 15, tokens = int(a.n_tok);
+  const int64_t n0 = int64_t(blockIdx.x) * 16, n = std::min(n0 + i, a.d_out - 1);
+  const int tok = std::min(i, tokens - 1), batches = (a.chunks + kBatch - 1) / kBatch;
+  const bf16_t* x = static_cast<const bf16_t*>(a.x);
+  char* mine = lds + wave * tokens * kFewPitch;
+  f4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int batch = wave; batch < batches; batch += waves) {
+    u32x4 w[kBatch];
+    uint32_t s;
+    load_codes(w, s, a.q, a.s, a, n, batch, b);
+    if constexpr (PACKED) {
+      u32x4 f[kBatch];
+      uint32_t sx;
+      load_codes(f, sx, static_cast<const uint8_t*>(a.x), a.xs, a, tok, batch, b);
+      mfma_mx4<0>(sum, w[0], s, f[0], sx);
+      mfma_mx4<1>(sum, w[1], s, f[1], sx);
+      mfma_mx4<2>(sum, w[2], s, f[2], sx);
+      mfma_mx4<3>(sum, w[3], s, f[3], sx);
+    } else {
+      // The tokens' values come through LDS: the operands would read each 16 times over.
+      const int k = batch * kBatchK + 8 * lane;
+      for (int r0 = 0; r0 < tokens; r0 += ROWS) {
+        u32x4 v[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+          if (r0 + r < tokens) v[r] = tokens8(x + (r0 + r) * a.ldx, k, a.d);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+          if (r0 + r < tokens)
+            *reinterpret_cast<u32x4*>(mine + (r0 + r) * kFewPitch + 16 * lane) = v[r];
+      }
+      wave_exchange();
+      auto chunk = [&](int u, bf16x8 (&f)[4]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          f[j] = *reinterpret_cast<const bf16x8*>(mine + tok * kFewPitch +
+                                                  (u * kChunk + 32 * b + 8 * j) * 2);
+      };
+      bf16x8 f[4];
+      chunk(0, f);
+      mfma_bf16<0>(sum, w[0], s, f);
+      chunk(1, f);
+      mfma_bf16<1>(sum, w[1], s, f);
+      chunk(2, f);
+      mfma_bf16<2>(sum, w[2], s, f);
+      chunk(3, f);
+      mfma_bf16<3>(sum, w[3], s, f);
+      wave_exchange();
+    }
+  }
+  __syncthreads();  // the staged values' place
+  *reinterpret_cast<f4*>(part + (wave * 64 + lane) * 4) = sum;
+  __syncthreads();
+  for (int o = threadIdx.x; o < 256; o += blockDim.x) {
+    const int nn = o & 15, t = o >> 4;
+    if (t >= tokens || n0 + nn >= a.d_out) continue;
+    const float* p = part + ((nn >> 2) * 16 + t) * 4 + (nn & 3);
+    float v = 0.f;
+    for (int w = 0; w < waves; ++w) v += p[w * 256];
+    const int64_t at = t * a.ldy + n0 + nn;
+    if (a.y_f32)
+      static_cast<float*>(a.y)[at] = v;
+    else
+      store1(static_cast<bf16_t*>(a.y) + at, v);
+  }
+}
+
+// More tokens, 64 at a time. The tokens' values of a batch of 256 go through LDS, two batches in
+// turn, for all waves of a workgroup; a wave takes 32 outputs, whose codes it loads a batch
+// ahead. With few outputs the batches are split over blockIdx.y, and k_mx4_join adds the parts.
+constexpr int kSlabTokens = 64;
+constexpr int kSlabWaves = 8;
+constexpr int kSlabRows = kSlabWaves * 32;
+constexpr int kSlabChunks = 2, kSlabK = kSlabChunks * kChunk;
+
+template <bool PACKED, int NT>
+__global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
+  constexpr int kTok = 16 * NT, kXBytes = PACKED ? kSlabK / 2 : kSlabK * 2, kPitch = kXBytes + 16;
+  constexpr int kPieces = kXBytes / 16;                      // of 16 bytes, of a token's batch
+  constexpr int kEach = (kTok * kPieces + 511) / 512;        // that a thread brings
+  __shared__ __attribute__((aligned(16))) char xl[2][kTok * kPitch];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = lane >> 4, i = lane & 15;
+  const int64_t t0 = int64_t(blockIdx.z) * kSlabTokens;
+  const int tokens = int(std::min<int64_t>(a.n_tok - t0, kTok));
+  const int64_t n0 = int64_t(blockIdx.x) * kSlabRows + wave * 32;
+  int64_t n[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) n[m] = std::min(n0 + 16 * m + i, a.d_out - 1);
+  const int batches = (a.chunks + kSlabChunks - 1) / kSlabChunks;
+  const int b0 = int(int64_t(batches) * blockIdx.y / gridDim.y);
+  const int b1 = int(int64_t(batches) * (blockIdx.y + 1) / gridDim.y);
+
+  u32x4 xv[kEach];
+  uint32_t sxn[NT];
+  auto fetch_x = [&](int batch) {
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) {
+      const int at = threadIdx.x + 512 * r;
+      const int64_t t = t0 + std::min(at / kPieces, tokens - 1);
+      const int p = at % kPieces;
+      if constexpr (PACKED)
+        xv[r] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.x) + t * a.row +
+                                                batch * kXBytes + 16 * p);
+      else
+        xv[r] = tokens8(static_cast<const bf16_t*>(a.x) + t * a.ldx, batch * kSlabK + 8 * p, a.d);
+    }
+    if constexpr (PACKED)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        sxn[t] = *reinterpret_cast<const uint32_t*>(
+                     a.xs + (t0 + std::min(16 * t + i, tokens - 1)) * a.srow + 16 * (batch >> 1) + 4 * b) >>
+                 (16 * (batch & 1));
+  };
+  auto put_x = [&](int to) {
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) {
+      const int at = threadIdx.x + 512 * r;
+      if (kTok * kPieces % 512 == 0 || at < kTok * kPieces)
+        *reinterpret_cast<u32x4*>(xl[to] + at / kPieces * kPitch + at % kPieces * 16) = xv[r];
+    }
+  };
+  u32x4 w[kSlabChunks][2];
+  uint32_t s[2];
+  auto fetch_w = [&](int batch) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      // Rows are padded to whole batches.
+#pragma unroll
+      for (int u = 0; u < kSlabChunks; ++u)
+        w[u][m] = *reinterpret_cast<const u32x4*>(a.q + n[m] * a.row + batch * 128 + u * kChunkBytes +
+                                                  16 * b);
+      s[m] = *reinterpret_cast<const uint32_t*>(a.s + n[m] * a.srow + 16 * (batch >> 1) + 4 * b) >>
+             (16 * (batch & 1));
+    }
+  };
+
+  f4 sum[2][NT];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum[m][t] = f4{0.f, 0.f, 0.f, 0.f};
+  if (b0 < b1) {
+    fetch_x(b0);
+    fetch_w(b0);
+    put_x(0);
+  }
+  __syncthreads();
+  for (int batch = b0; batch < b1; ++batch) {
+    const int cur = (batch - b0) & 1;
+    u32x4 wc[kSlabChunks][2];
+    uint32_t sc[2], sx[NT];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+      for (int u = 0; u < kSlabChunks; ++u) wc[u][m] = w[u][m];
+      sc[m] = s[m];
+    }
+    if constexpr (PACKED)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sx[t] = sxn[t];
+    if (batch + 1 < b1) {
+      fetch_x(batch + 1);
+      fetch_w(batch + 1);
+    }
+    const char* xc = xl[cur] + i * kPitch;
+    if constexpr (PACKED) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const u32x4 f0 = *reinterpret_cast<const u32x4*>(xc + 16 * t * kPitch + 16 * b);
+        const u32x4 f1 = *reinterpret_cast<const u32x4*>(xc + 16 * t * kPitch + 64 + 16 * b);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          mfma_mx4<0>(sum[m][t], wc[0][m], sc[m], f0, sx[t]);
+          mfma_mx4<1>(sum[m][t], wc[1][m], sc[m], f1, sx[t]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kSlabChunks; ++u) {
+        bf16x8 v[2][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const float scale = u ? scale_at<1>(sc[m]) : scale_at<0>(sc[m]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[m][j] = weights8(wc[u][m][j], scale);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bf16x8 f = *reinterpret_cast<const bf16x8*>(
+                xc + 16 * t * kPitch + (u * kChunk + 32 * b + 8 * j) * 2);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+              sum[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[m][j], f, sum[m][t], 0, 0, 0);
+          }
+      }
+    }
+    if (batch + 1 < b1) put_x(cur ^ 1);
+    __syncthreads();
+  }
+  if (gridDim.y > 1) {  // [split][64 tokens][workgroup][wave][row block][token block][lane]
+    const size_t wg = (size_t(blockIdx.y) * gridDim.z + blockIdx.z) * gridDim.x + blockIdx.x;
+    f4* part = a.part + (wg * kSlabWaves + wave) * 2 * NT * 64;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) part[(m * NT + t) * 64 + lane] = sum[m][t];
+    return;
+  }
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) store_y4(a, t0 + 16 * t + i, n0 + 16 * m + 4 * b, sum[m][t]);
+}
+
+// The parts of the outputs, added in their order. blocks: 16 x 16 outputs, of all splits' one.
+template <int NT>
+__global__ void __launch_bounds__(kThreads) k_mx4_join(Mx4Args a, int splits, int64_t blocks,
+                                                       int64_t per) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  if (at >= blocks) return;
+  const f4* part = a.part + at * 64 + lane;
+  f4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int sp = 0; sp < splits; ++sp) sum += part[sp * blocks * 64];
+  const int64_t z = at / per, in = at - z * per;  // of 64 tokens
+  const int64_t wave = in / (2 * NT);
+  const int m = int(in / NT) & 1, t = int(in % NT);
+  store_y4(a, z * kSlabTokens + 16 * t + (lane & 15), wave * 32 + 16 * m + 4 * (lane >> 4), sum);
+}
+
+// Ranges that the sums of more than kFew tokens are split into: as many as give every CU a
+// workgroup, of two batches at least beyond eight.
+int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out) {
+  const int64_t wgs = ceil_div(d_out, kSlabRows) * ceil_div(n_tok, kSlabTokens);
+  const int64_t batches = ceil_div(d, kSlabK);
+  if (batches <= 2) return 1;
+  return std::max<int64_t>(1, std::min(256 / wgs, std::max(batches / 2, std::min<int64_t>(batches, 8))));
+}
+
+template <bool PACKED, int NT>
+void launch_slab(const Mx4Args& a, hipStream_t s) {
+  const unsigned wgs = unsigned(ceil_div(a.d_out, kSlabRows));
+  const unsigned tiles = unsigned(ceil_div(a.n_tok, kSlabTokens));
+  const int splits = int(slab_splits(a.n_tok, a.d, a.d_out));
+  hipLaunchKernelGGL((k_mx4_slab<PACKED, NT>), dim3(wgs, unsigned(splits), tiles),
+                     dim3(64 * kSlabWaves), 0, s, a);
+  if (splits > 1) {
+    const int64_t per = int64_t(wgs) * kSlabWaves * 2 * NT, blocks = per * tiles;
+    hipLaunchKernelGGL((k_mx4_join<NT>), dim3(unsigned(ceil_div(blocks, kThreads / 64))),
+                       dim3(kThreads), 0, s, a, splits, blocks, per);
+  }
+}
+
+template <bool PACKED, int ROWS>
+void launch_few(const Mx4Args& a, hipStream_t s) {
+  // As many waves as there are batches, and as the CU's LDS holds tokens for.
+  const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kFewPitch, 1024);
+  const int most = int(std::min<size_t>(kFewWaves, (size_t(160) << 10) / each));
+  const int waves = int(std::min<int64_t>(ceil_div(a.chunks, kBatch), most));
+  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS>), dim3(unsigned(ceil_div(a.d_out, 16))),
+                     dim3(64 * waves), waves * each, s, a);
+}
+
+template <bool PACKED>
+void launch_mx4(const Mx4Args& a, hipStream_t s) {
+  if (a.n_tok > 32) launch_slab<PACKED, 4>(a, s);
+  else if (a.n_tok > kFew) launch_slab<PACKED, 2>(a, s);
+  else if (a.n_tok > 4 && !PACKED) launch_few<PACKED, 8>(a, s);
+  else launch_few<PACKED, 4>(a, s);
+}
+
+}  // namespace
+
+size_t mx4_row_bytes(int64_t d) { return size_t(row_bytes(d)); }
+size_t mx4_scale_bytes(int64_t d) { return size_t(scale_bytes(d)); }
+
+optima_status mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t d, void* Q,
+                       void* scales, hipStream_t s) {
+  const int pieces = int(ceil_div(d, 256)), srow = int(scale_bytes(d));
+  const int64_t total = n * pieces;
+  const dim3 grid(unsigned(ceil_div(total, kThreads / 32)));
+  uint8_t *q = static_cast<uint8_t*>(Q), *sc = static_cast<uint8_t*>(scales);
+  if (dtype == OPTIMA_DTYPE_BF16)
+    hipLaunchKernelGGL(k_mx4_pack<bf16_t>, grid, dim3(kThreads), 0, s,
+                       static_cast<const bf16_t*>(X), ldx, total, pieces, int(d), q, sc, srow);
+  else
+    hipLaunchKernelGGL(k_mx4_pack<float>, grid, dim3(kThreads), 0, s, static_cast<const float*>(X),
+                       ldx, total, pieces, int(d), q, sc, srow);
+  OPTIMA_LAUNCH_CHECK();
+  return OPTIMA_OK;
+}
+
+optima_status mx4_unpack(const void* Q, const void* scales, int64_t n, int64_t d, void* Y,
+                         int64_t ldy, int dtype, hipStream_t s) {
+  const int pieces = int(ceil_div(d, 256)), srow = int(scale_bytes(d));
+  const int64_t total = n * pieces;
+  const dim3 grid(unsigned(ceil_div(total, kThreads / 32)));
+  const uint8_t *q = static_cast<const uint8_t*>(Q), *sc = static_cast<const uint8_t*>(scales);
+  if (dtype == OPTIMA_DTYPE_BF16)
+    hipLaunchKernelGGL(k_mx4_unpack<bf16_t>, grid, dim3(kThreads), 0, s, q, sc, srow, total, pieces,
+                       int(d), static_cast<bf16_t*>(Y), ldy);
+  else
+    hipLaunchKernelGGL(k_mx4_unpack<float>, grid, dim3(kThreads), 0, s, q, sc, srow, total, pieces,
+                       int(d), static_cast<float*>(Y), ldy);
+  OPTIMA_LAUNCH_CHECK();
+  return OPTIMA_OK;
+}
+
+size_t mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
+  if (n_tok <= kFew) return 0;
+  // The most of any number of tokens up to these, so that more need no less.
+  const int64_t wgs = ceil_div(d_out, kSlabRows), tiles = ceil_div(n_tok, kSlabTokens);
+  int64_t parts = 0;
+  for (int64_t t = 1; t <= std::min(tiles, 128 / wgs); ++t) {
+    const int64_t splits = slab_splits(t * kSlabTokens, d, d_out);
+    if (splits > 1) parts = std::max(parts, splits * t);
+  }
+  return size_t(parts) * size_t(wgs) * kSlabWaves * 2 * (kSlabTokens / 16) * 64 * sizeof(f4);
+}
+
+optima_status mx4_linear(const void* X, int64_t ldx, const void* x_scales, int64_t n_tok, int64_t d,
+                         const void* Q, const void* scales, int64_t d_out, void* Y, int64_t ldy,
+                         int y_dtype, void* ws, hipStream_t s) {
+  Mx4Args a{};
+  a.x = X;
+  a.xs = static_cast<const uint8_t*>(x_scales);
+  a.q = static_cast<const uint8_t*>(Q);
+  a.s = static_cast<const uint8_t*>(scales);
+  a.y = Y;
+  a.part = static_cast<f4*>(ws);
+  a.n_tok = n_tok;
+  a.d_out = d_out;
+  a.ldx = ldx;
+  a.ldy = ldy;
+  a.d = int(d);
+  a.chunks = int(ceil_div(d, kChunk));
+  a.row = int(row_bytes(d));
+  a.srow = int(scale_bytes(d));
+  a.y_f32 = y_dtype == OPTIMA_DTYPE_F32;
+  if (x_scales) launch_mx4<true>(a, s);
+  else launch_mx4<false>(a, s);
+  OPTIMA_LAUNCH_CHECK();
+  return OPTIMA_OK;
+}
+
+}  // namespace optima
