@@ -13,8 +13,11 @@
 // and the MFMA picks the byte, so that scales cost no instructions.
 //   packed tokens: products of codes and scales are exact, the sum is the MFMA's fp32.
 //   16-bit tokens: codes times scale are exact in bf16 (one instruction for two).
+#include <type_traits>
+
 #include "common.h"
 #include "vec8.h"
+#include "mx4_tile.h"
 
 namespace optima {
 namespace {
@@ -22,7 +25,7 @@ namespace {
 constexpr int kChunk = 128;  // values of an operand
 constexpr int kChunkBytes = 64;
 
-typedef int i8x32 __attribute__((ext_vector_type(8)));
+using mx4::i8x32;
 
 int64_t row_bytes(int64_t d) { return ceil_div(d, 256) * 128; }
 int64_t scale_bytes(int64_t d) { return ceil_div(d, 512) * 16; }
@@ -161,6 +164,17 @@ __device__ inline void store_y4(const Mx4Args& a, int64_t tok, int64_t n, const 
     store_upto4(static_cast<float*>(a.y) + at, w, left);
   else
     store_upto4(static_cast<bf16_t*>(a.y) + at, w, left);
+}
+
+__device__ inline void store_y8(const Mx4Args& a, int64_t tok, int64_t n, const f4& v, const f4& w) {
+  if (tok >= a.n_tok || n >= a.d_out) return;
+  const float u[8] = {v[0], v[1], v[2], v[3], w[0], w[1], w[2], w[3]};
+  const int left = int(std::min<int64_t>(a.d_out - n, 8));
+  const int64_t at = tok * a.ldy + n;
+  if (a.y_f32)
+    store_upto8(static_cast<float*>(a.y) + at, u, left);
+  else
+    store_upto8(static_cast<bf16_t*>(a.y) + at, u, left);
 }
 
 constexpr int kBatch = 4;                 // chunks that a wave's loads go out together for
@@ -456,6 +470,108 @@ void launch_slab(const Mx4Args& a, hipStream_t s) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many packed tokens
+// ---------------------------------------------------------------------------
+
+// A 256 x 256 tile of outputs, or with gridDim.y > 1 a range of its sum's pairs of stages.
+__global__ void __launch_bounds__(Tile256::kThreads) k_mx4_tile(Mx4Args a) {
+  __shared__ __attribute__((aligned(1024))) char l0[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l1[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l2[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l3[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l4[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l5[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l6[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char l7[Tile256::kHalfBytes];
+  __shared__ __attribute__((aligned(1024))) char s0[mx4::kScaleBytes];
+  __shared__ __attribute__((aligned(1024))) char s1[mx4::kScaleBytes];
+  const int tiles_m = int((a.n_tok + 255) / 256), tiles_n = int((a.d_out + 255) / 256);
+  int tm, tn;
+  tile_of_block(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 256;
+  const int stages = a.row / Tile256::kSRB, pairs = (stages + 1) / 2;
+  const int p0 = int(int64_t(pairs) * blockIdx.y / gridDim.y);
+  const int p1 = int(int64_t(pairs) * (blockIdx.y + 1) / gridDim.y);
+  Operands256 src;
+#pragma unroll
+  for (int i = 0; i < Tile256::kHalfLoads; ++i) {
+    const int r = t256_load_row(i);
+    const int64_t at = int64_t(2 * p0) * Tile256::kSRB + t256_seg_bytes(i);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      src.a[h][i] = static_cast<const char*>(a.x) + std::min(m0 + 128 * h + r, a.n_tok - 1) * a.row + at;
+      src.b[h][i] = reinterpret_cast<const char*>(a.q) +
+                    std::min(n0 + 128 * h + t256_rows_source(r), a.d_out - 1) * a.row + at;
+    }
+  }
+  const int r = threadIdx.x & 255;
+  const char* scales = reinterpret_cast<const char*>(
+      threadIdx.x < 256 ? a.xs + std::min(m0 + r, a.n_tok - 1) * a.srow
+                        : a.s + std::min(n0 + (r & 128) + t256_rows_source(r & 127), a.d_out - 1) * a.srow);
+  Acc256 acc;
+  mx4::mainloop(acc, src, scales + 16 * p0, std::min(2 * p1, stages) - 2 * p0, l0, l1, l2, l3, l4, l5,
+                l6, l7, s0, s1);
+  f4* part = gridDim.y > 1
+                 ? a.part + ((size_t(blockIdx.y) * gridDim.x + blockIdx.x) * Tile256::kWaves +
+                             (threadIdx.x >> 6)) * 32 * 64 + (threadIdx.x & 63)
+                 : nullptr;
+#pragma unroll
+  for (int qa = 0; qa < 2; ++qa)
+#pragma unroll
+    for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+      for (int qb = 0; qb < 2; ++qb) {
+        const f4 *c = acc.q[qa][qb][mi];
+        if (part) {
+          part[((qa * 4 + mi) * 4 + 2 * qb) * 64] = c[0];
+          part[((qa * 4 + mi) * 4 + 2 * qb + 1) * 64] = c[1];
+        } else {
+          store_y8(a, m0 + t256_rows_row(qa, mi), n0 + t256_rows_col(qb), c[0], c[1]);
+        }
+      }
+}
+
+// The parts of the tiles' outputs, added in their order: 16 rows of a wave's a wave.
+__global__ void __launch_bounds__(kThreads) k_mx4_tile_join(Mx4Args a, int splits, int tiles) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  if (at >= int64_t(tiles) * 64) return;
+  const int tile = int(at >> 6), wave = int(at >> 3) & 7, qa = int(at >> 2) & 1, mi = int(at & 3);
+  const f4* part = a.part + at * 4 * 64 + lane;
+  const size_t step = size_t(tiles) * 64 * 4 * 64;
+  f4 c[4] = {};
+#pragma unroll 4
+  for (int sp = 0; sp < splits; ++sp)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) c[q] += part[sp * step + q * 64];
+  const int tiles_m = int((a.n_tok + 255) / 256);
+  int tm, tn;
+  tile_of_block(tile, tiles, tiles_m, tiles / tiles_m, &tm, &tn);
+  const int64_t tok = int64_t(tm) * 256 + qa * 128 + (wave >> 2) * 64 + mi * 16 + (lane & 15);
+  const int64_t n = int64_t(tn) * 256 + (wave & 3) * 32 + 8 * (lane >> 4);
+  store_y8(a, tok, n, c[0], c[1]);
+  store_y8(a, tok, n + 128, c[2], c[3]);
+}
+
+// Ranges of a tile's sum: as many as give every CU a workgroup, of two pairs of stages at least.
+int tile_splits(int64_t n_tok, int64_t d, int64_t d_out) {
+  const int64_t tiles = ceil_div(n_tok, 256) * ceil_div(d_out, 256);
+  return int(std::max<int64_t>(1, std::min(256 / tiles, ceil_div(d, 512) / 2)));
+}
+size_t tile_part_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
+  const int splits = tile_splits(n_tok, d, d_out);
+  return splits < 2 ? 0 : size_t(splits) * size_t(ceil_div(n_tok, 256) * ceil_div(d_out, 256)) << 18;
+}
+
+void launch_tile(const Mx4Args& a, hipStream_t s) {
+  const unsigned tiles = unsigned(ceil_div(a.n_tok, 256) * ceil_div(a.d_out, 256));
+  const int splits = tile_splits(a.n_tok, a.d, a.d_out);
+  hipLaunchKernelGGL(k_mx4_tile, dim3(tiles, unsigned(splits)), dim3(Tile256::kThreads), 0, s, a);
+  if (splits > 1)
+    hipLaunchKernelGGL(k_mx4_tile_join, dim3(tiles * 16), dim3(kThreads), 0, s, a, splits, int(tiles));
+}
+
 template <bool PACKED, int ROWS>
 void launch_few(const Mx4Args& a, hipStream_t s) {
   // As many waves as there are batches, and as the CU's LDS holds tokens for.
@@ -468,7 +584,8 @@ void launch_few(const Mx4Args& a, hipStream_t s) {
 
 template <bool PACKED>
 void launch_mx4(const Mx4Args& a, hipStream_t s) {
-  if (a.n_tok > 32) launch_slab<PACKED, 4>(a, s);
+  if (PACKED && a.n_tok > kSlabTokens) launch_tile(a, s);
+  else if (a.n_tok > 32) launch_slab<PACKED, 4>(a, s);
   else if (a.n_tok > kFew) launch_slab<PACKED, 2>(a, s);
   else if (a.n_tok > 4 && !PACKED) launch_few<PACKED, 8>(a, s);
   else launch_few<PACKED, 4>(a, s);
@@ -520,7 +637,12 @@ size_t mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
     const int64_t splits = slab_splits(t * kSlabTokens, d, d_out);
     if (splits > 1) parts = std::max(parts, splits * t);
   }
-  return size_t(parts) * size_t(wgs) * kSlabWaves * 2 * (kSlabTokens / 16) * 64 * sizeof(f4);
+  const size_t slab = size_t(parts) * size_t(wgs) * kSlabWaves * 2 * (kSlabTokens / 16) * 64 * sizeof(f4);
+  size_t tile = 0;
+  const int64_t tiles_n = ceil_div(d_out, 256);
+  for (int64_t t = 1; t <= std::min(ceil_div(n_tok, 256), 128 / tiles_n); ++t)
+    tile = std::max(tile, tile_part_bytes(256 * t, d, d_out));
+  return std::max(slab, n_tok > kSlabTokens ? tile : 0);
 }
 
 optima_status mx4_linear(const void* X, int64_t ldx, const void* x_scales, int64_t n_tok, int64_t d,

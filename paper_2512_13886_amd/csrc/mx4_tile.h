@@ -1,0 +1,145 @@
+// MFMA main loop of a 256 x 256 tile of outputs Y = X W^T of packed tokens and weights: the
+// pipeline of gemm256.h, whose stage of 128 bytes a row is 256 codes here and whose two K steps
+// are two block-scaled 16x16x128 MFMAs.
+//
+// The scales of two stages are 16 bytes a row: one direct load a thread brings those of the 256
+// rows of X and of W into LDS, in the first phase of every even stage for the two stages after
+// the present pair, and each lane keeps the twelve dwords of its rows for both stages (the MFMA
+// picks the byte). That load is older than the loads that the stage's last wait leaves in flight,
+// and its buffer was last read two stages before, in the first phase.
+#pragma once
+
+#include "gemm256.h"
+
+namespace optima {
+namespace mx4 {
+
+typedef int i8x32 __attribute__((ext_vector_type(8)));
+
+constexpr int kScaleBytes = 512 * 16;  // of a pair of stages: 256 rows of X, then 256 of W
+
+template <int U>
+__device__ inline void mfma(f4& c, const bf16x8& w, uint32_t sw, const bf16x8& x, uint32_t sx) {
+  typedef int i4x __attribute__((ext_vector_type(4)));
+  const i4x p = __builtin_bit_cast(i4x, w), q = __builtin_bit_cast(i4x, x);
+  const i8x32 a = {p[0], p[1], p[2], p[3], 0, 0, 0, 0}, b = {q[0], q[1], q[2], q[3], 0, 0, 0, 0};
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, U, int(sw), U, int(sx));
+}
+
+struct Scales {
+  uint32_t a[2][4], b[2][2];  // of this lane's rows: [half][16-row block]
+};
+
+__device__ inline void read_scales(Scales& s, const char* l) {
+  const int lane = threadIdx.x & 63, wm = threadIdx.x >> 8, wn = (threadIdx.x >> 6) & 3;
+  const char* p = l + (lane & 15) * 16 + (lane >> 4) * 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+      s.a[h][m] = *reinterpret_cast<const uint32_t*>(p + (h * 128 + wm * 64 + m * 16) * 16);
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+      s.b[h][m] = *reinterpret_cast<const uint32_t*>(p + (256 + h * 128 + wn * 32 + m * 16) * 16);
+  }
+}
+
+template <int U0>
+__device__ inline void quadrant(f4 (&c)[4][2], const bf16x8 (&a)[4][2], const uint32_t (&sa)[4],
+                                const bf16x8 (&b)[2][2], const uint32_t (&sb)[2]) {
+#pragma unroll
+  for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < 2; ++ni) mfma<U0>(c[mi][ni], b[ni][0], sb[ni], a[mi][0], sa[mi]);
+#pragma unroll
+  for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < 2; ++ni) mfma<U0 + 1>(c[mi][ni], b[ni][1], sb[ni], a[mi][1], sa[mi]);
+}
+
+__device__ inline void fetch_scales(const char* src, char* l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)(l + (threadIdx.x >> 6) * 1024),
+                                   16, 0, 0);
+}
+
+// As t256::stage. In an even one (U0 = 0) the scales `now` are read and those at `src_s` fetched
+// into `next`.
+template <int U0>
+__device__ inline void stage(Acc256& acc, Scales& sc, const Operands256& src, int64_t off1,
+                             int64_t off2, char* a0, char* a1, char* b0, char* b1, char* na1,
+                             const char* now, const char* src_s, char* next) {
+  const int wm = threadIdx.x >> 8, wn = (threadIdx.x >> 6) & 3;
+  bf16x8 fa[4][2], fb0[2][2], fb1[2][2];
+  if constexpr (U0 == 0) read_scales(sc, now);
+  t256::read<4>(fa, a0, wm * 64);
+  t256::read<2>(fb0, b0, wn * 32);
+  if constexpr (U0 == 0) fetch_scales(src_s, next);
+  t256::fetch(src.a[1], off1, na1);
+  t256::end_memory<-1>();
+  quadrant<U0>(acc.q[0][0], fa, sc.a[0], fb0, sc.b[0]);
+  t256::barrier();
+  t256::read<2>(fb1, b1, wn * 32);
+  t256::fetch(src.a[0], off2, a0);
+  t256::end_memory<-1>();
+  quadrant<U0>(acc.q[0][1], fa, sc.a[0], fb1, sc.b[1]);
+  t256::barrier();
+  t256::read<4>(fa, a1, wm * 64);
+  t256::fetch(src.b[0], off2, b0);
+  t256::end_memory<-1>();
+  quadrant<U0>(acc.q[1][1], fa, sc.a[1], fb1, sc.b[1]);
+  t256::barrier();
+  t256::fetch(src.b[1], off2, b1);
+  t256::end_memory<3 * Tile256::kHalfLoads>();
+  quadrant<U0>(acc.q[1][0], fa, sc.a[1], fb0, sc.b[0]);
+  t256::barrier();
+}
+
+// n stages (n >= 1) from an even one on. l: the eight half tiles; s: two buffers of kScaleBytes;
+// scales: this thread's row's at the first stage.
+__device__ inline void mainloop(Acc256& acc, const Operands256& src, const char* scales, int n,
+                                char* a00, char* a01, char* b00, char* b01, char* a10, char* a11,
+                                char* b10, char* b11, char* s0, char* s1) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) acc.q[i >> 4][(i >> 3) & 1][(i >> 1) & 3][i & 1] = f4{0.f, 0.f, 0.f, 0.f};
+  const int pairs = (n + 1) >> 1;
+  auto at = [n](int s) { return int64_t(s < n ? s : n - 1) * Tile256::kSRB; };
+  auto at_s = [pairs, scales](int p) { return scales + 16 * (p < pairs ? p : pairs - 1); };
+  fetch_scales(at_s(0), s0);
+  t256::fetch(src.a[0], at(0), a00);
+  t256::fetch(src.b[0], at(0), b00);
+  t256::fetch(src.b[1], at(0), b01);
+  t256::fetch(src.a[1], at(0), a01);
+  t256::fetch(src.a[0], at(1), a10);
+  t256::fetch(src.b[0], at(1), b10);
+  t256::fetch(src.b[1], at(1), b11);
+  t256::end_memory<3 * Tile256::kHalfLoads>();
+  const bool behind = threadIdx.x >= 256;  // waves 4-7
+  if (behind) t256::barrier();
+  Scales sc;
+  // The buffers by name: through a pointer the compiler loses track of the array and waits for
+  // the loads in flight into the others.
+  auto even = [&](int s, const char* now, char* next) {
+    stage<0>(acc, sc, src, at(s + 1), at(s + 2), a00, a01, b00, b01, a11, now, at_s(s / 2 + 1), next);
+  };
+  auto odd = [&](int s) {
+    stage<2>(acc, sc, src, at(s + 1), at(s + 2), a10, a11, b10, b11, a01, nullptr, nullptr, nullptr);
+  };
+  int s = 0;
+  for (; s + 3 < n; s += 4) {
+    even(s, s0, s1);
+    odd(s + 1);
+    even(s + 2, s1, s0);
+    odd(s + 3);
+  }
+  if (s < n) even(s, s0, s1);
+  if (s + 1 < n) odd(s + 1);
+  if (s + 2 < n) even(s + 2, s1, s0);
+  if (!behind) t256::barrier();
+  // No load may still be writing LDS when the workgroup moves on.
+  wait_vmcnt<0>();
+  __syncthreads();
+}
+
+}  // namespace mx4
+}  // namespace optima
