@@ -579,7 +579,7 @@ optima_status optima_mx4_unpack(const void* Q, const void* scales, int64_t n, in
  * x_scales (ldx is not used). n_tok <= 2^21, d <= 2^20, d_out <= 2^24. Y: [n_tok][d_out] BF16 or F32. Products of
  * values are exact, their sums fp32. A zero weight adds exactly nothing, except to an infinite or
  * NaN token (NaN).
- * ws: optima_mx4_workspace_bytes(n_tok, d, d_out) bytes: 0 up to 16 tokens, never less for more. */
+ * ws: optima_mx4_workspace_bytes(n_tok, d, d_out) bytes: 0 up to 8 tokens, never less for more. */
 size_t optima_mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out);
 optima_status optima_mx4_linear(const void* X, int64_t ldx, int x_dtype, const void* x_scales,
                                 int64_t n_tok, int64_t d, const void* Q, const void* scales,

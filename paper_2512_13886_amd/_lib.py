@@ -831,7 +831,7 @@ def optima_mx4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y:
         x, ldx, x_dt, xs = _mx4_addr(X), 0, DTYPE_MX4, _mx4_addr(x_scales)
     y, ldy, y_dt = _take("Y", Y, (n, n_out), _F)
     _need_one_device(stream, X, x_scales, Q, scales, Y, ws)
-    need = optima_mx4_workspace_bytes(n, d, n_out) if n > 16 else 0
+    need = optima_mx4_workspace_bytes(n, d, n_out) if n > 8 else 0
     nbytes = 0
     if need or ws is not None:
         ws, nbytes = _workspace(need, ws, X.device, stream)

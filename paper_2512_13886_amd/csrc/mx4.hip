@@ -17,6 +17,7 @@
 
 #include "common.h"
 #include "vec8.h"
+#include "mx4_plan.h"
 #include "mx4_tile.h"
 
 namespace optima {
@@ -191,6 +192,11 @@ __device__ inline void wave_exchange() {
 // Up to 16 tokens. A workgroup takes 16 outputs, its waves every waves-th batch of 512 values,
 // and the waves' sums are joined in LDS in their order.
 constexpr int kFew = 16;
+// 16-bit tokens above kFewest of larger weights share what is read of them: 16 tokens, 4096 -> 14336
+// 16.7 us here and 15.2 in slabs, 4096 -> 128000 120 and 71, 14336 -> 4096 17.2 and 15.4, but
+// 4096 -> 4096 7.0 and 10.8; 8 tokens, 4096 -> 14336 11.8 and 15.2.
+constexpr int kFewest = 8;
+constexpr int64_t kSlabWeights = 48 << 20;
 constexpr int kFewWaves = 16;
 // Bytes of a token's batch in LDS, with 64 between rows.
 constexpr int kFewPitch = kBatchK * 2 + 64;
@@ -208,30 +214,37 @@ __device__ inline void load_codes(u32x4 (&w)[kBatch], uint32_t& s, const uint8_t
   s = *reinterpret_cast<const uint32_t*>(sc + n * a.srow + batch * 16 + 4 * b);
 }
 
-// ROWS: tokens that a lane loads values of together.
-template <bool PACKED, int ROWS>
+// ROWS: tokens that a lane loads values of together; RB: blocks of 16 outputs.
+template <bool PACKED, int ROWS, int RB>
 __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   float* part = reinterpret_cast<float*>(lds);  // [wave][lane][4], at the end
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int b = lane >> 4, i = lane & 15, tokens = int(a.n_tok);
-  const int64_t n0 = int64_t(blockIdx.x) * 16, n = std::min(n0 + i, a.d_out - 1);
+  const int64_t n0 = int64_t(blockIdx.x) * 16 * RB;
   const int tok = std::min(i, tokens - 1), batches = (a.chunks + kBatch - 1) / kBatch;
   const bf16_t* x = static_cast<const bf16_t*>(a.x);
   char* mine = lds + wave * tokens * kFewPitch;
-  f4 sum = {0.f, 0.f, 0.f, 0.f};
+  f4 sum[RB];
+#pragma unroll
+  for (int m = 0; m < RB; ++m) sum[m] = f4{0.f, 0.f, 0.f, 0.f};
   for (int batch = wave; batch < batches; batch += waves) {
-    u32x4 w[kBatch];
-    uint32_t s;
-    load_codes(w, s, a.q, a.s, a, n, batch, b);
+    u32x4 w[RB][kBatch];
+    uint32_t s[RB];
+#pragma unroll
+    for (int m = 0; m < RB; ++m)
+      load_codes(w[m], s[m], a.q, a.s, a, std::min(n0 + 16 * m + i, a.d_out - 1), batch, b);
     if constexpr (PACKED) {
       u32x4 f[kBatch];
       uint32_t sx;
       load_codes(f, sx, static_cast<const uint8_t*>(a.x), a.xs, a, tok, batch, b);
-      mfma_mx4<0>(sum, w[0], s, f[0], sx);
-      mfma_mx4<1>(sum, w[1], s, f[1], sx);
-      mfma_mx4<2>(sum, w[2], s, f[2], sx);
-      mfma_mx4<3>(sum, w[3], s, f[3], sx);
+#pragma unroll
+      for (int m = 0; m < RB; ++m) {
+        mfma_mx4<0>(sum[m], w[m][0], s[m], f[0], sx);
+        mfma_mx4<1>(sum[m], w[m][1], s[m], f[1], sx);
+        mfma_mx4<2>(sum[m], w[m][2], s[m], f[2], sx);
+        mfma_mx4<3>(sum[m], w[m][3], s[m], f[3], sx);
+      }
     } else {
       // The tokens' values come through LDS: the operands would read each 16 times over.
       const int k = batch * kBatchK + 8 * lane;
@@ -246,33 +259,33 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
             *reinterpret_cast<u32x4*>(mine + (r0 + r) * kFewPitch + 16 * lane) = v[r];
       }
       wave_exchange();
-      auto chunk = [&](int u, bf16x8 (&f)[4]) {
+      auto chunk = [&](auto u) {
+        constexpr int U = decltype(u)::value;
+        bf16x8 f[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           f[j] = *reinterpret_cast<const bf16x8*>(mine + tok * kFewPitch +
-                                                  (u * kChunk + 32 * b + 8 * j) * 2);
+                                                  (U * kChunk + 32 * b + 8 * j) * 2);
+#pragma unroll
+        for (int m = 0; m < RB; ++m) mfma_bf16<U>(sum[m], w[m][U], s[m], f);
       };
-      bf16x8 f[4];
-      chunk(0, f);
-      mfma_bf16<0>(sum, w[0], s, f);
-      chunk(1, f);
-      mfma_bf16<1>(sum, w[1], s, f);
-      chunk(2, f);
-      mfma_bf16<2>(sum, w[2], s, f);
-      chunk(3, f);
-      mfma_bf16<3>(sum, w[3], s, f);
+      chunk(std::integral_constant<int, 0>());
+      chunk(std::integral_constant<int, 1>());
+      chunk(std::integral_constant<int, 2>());
+      chunk(std::integral_constant<int, 3>());
       wave_exchange();
     }
   }
   __syncthreads();  // the staged values' place
-  *reinterpret_cast<f4*>(part + (wave * 64 + lane) * 4) = sum;
+#pragma unroll
+  for (int m = 0; m < RB; ++m) *reinterpret_cast<f4*>(part + ((wave * RB + m) * 64 + lane) * 4) = sum[m];
   __syncthreads();
-  for (int o = threadIdx.x; o < 256; o += blockDim.x) {
-    const int nn = o & 15, t = o >> 4;
+  for (int o = threadIdx.x; o < 256 * RB; o += blockDim.x) {
+    const int nn = o % (16 * RB), t = o / (16 * RB);
     if (t >= tokens || n0 + nn >= a.d_out) continue;
-    const float* p = part + ((nn >> 2) * 16 + t) * 4 + (nn & 3);
+    const float* p = part + ((nn >> 4) * 64 + (nn >> 2 & 3) * 16 + t) * 4 + (nn & 3);
     float v = 0.f;
-    for (int w = 0; w < waves; ++w) v += p[w * 256];
+    for (int w = 0; w < waves; ++w) v += p[w * RB * 256];
     const int64_t at = t * a.ldy + n0 + nn;
     if (a.y_f32)
       static_cast<float*>(a.y)[at] = v;
@@ -281,17 +294,16 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
   }
 }
 
-// More tokens, 64 at a time. The tokens' values of a batch of 256 go through LDS, two batches in
+// More 16-bit tokens, 64 at a time. The tokens' values of a batch go through LDS, two batches in
 // turn, for all waves of a workgroup; a wave takes 32 outputs, whose codes it loads a batch
 // ahead. With few outputs the batches are split over blockIdx.y, and k_mx4_join adds the parts.
 constexpr int kSlabTokens = 64;
 constexpr int kSlabWaves = 8;
 constexpr int kSlabRows = kSlabWaves * 32;
-constexpr int kSlabChunks = 2, kSlabK = kSlabChunks * kChunk;
 
-template <bool PACKED, int NT>
+template <int NT>
 __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
-  constexpr int kTok = 16 * NT, kXBytes = PACKED ? kSlabK / 2 : kSlabK * 2, kPitch = kXBytes + 16;
+  constexpr int kTok = 16 * NT, kXBytes = kBatchK * 2, kPitch = kXBytes + 16;
   constexpr int kPieces = kXBytes / 16;                      // of 16 bytes, of a token's batch
   constexpr int kEach = (kTok * kPieces + 511) / 512;        // that a thread brings
   __shared__ __attribute__((aligned(16))) char xl[2][kTok * kPitch];
@@ -302,30 +314,19 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
   int64_t n[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) n[m] = std::min(n0 + 16 * m + i, a.d_out - 1);
-  const int batches = (a.chunks + kSlabChunks - 1) / kSlabChunks;
+  const int batches = (a.chunks + kBatch - 1) / kBatch;
   const int b0 = int(int64_t(batches) * blockIdx.y / gridDim.y);
   const int b1 = int(int64_t(batches) * (blockIdx.y + 1) / gridDim.y);
 
   u32x4 xv[kEach];
-  uint32_t sxn[NT];
   auto fetch_x = [&](int batch) {
 #pragma unroll
     for (int r = 0; r < kEach; ++r) {
       const int at = threadIdx.x + 512 * r;
       const int64_t t = t0 + std::min(at / kPieces, tokens - 1);
       const int p = at % kPieces;
-      if constexpr (PACKED)
-        xv[r] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.x) + t * a.row +
-                                                batch * kXBytes + 16 * p);
-      else
-        xv[r] = tokens8(static_cast<const bf16_t*>(a.x) + t * a.ldx, batch * kSlabK + 8 * p, a.d);
+      xv[r] = tokens8(static_cast<const bf16_t*>(a.x) + t * a.ldx, batch * kBatchK + 8 * p, a.d);
     }
-    if constexpr (PACKED)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        sxn[t] = *reinterpret_cast<const uint32_t*>(
-                     a.xs + (t0 + std::min(16 * t + i, tokens - 1)) * a.srow + 16 * (batch >> 1) + 4 * b) >>
-                 (16 * (batch & 1));
   };
   auto put_x = [&](int to) {
 #pragma unroll
@@ -335,19 +336,11 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
         *reinterpret_cast<u32x4*>(xl[to] + at / kPieces * kPitch + at % kPieces * 16) = xv[r];
     }
   };
-  u32x4 w[kSlabChunks][2];
+  u32x4 w[2][kBatch];
   uint32_t s[2];
   auto fetch_w = [&](int batch) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      // Rows are padded to whole batches.
-#pragma unroll
-      for (int u = 0; u < kSlabChunks; ++u)
-        w[u][m] = *reinterpret_cast<const u32x4*>(a.q + n[m] * a.row + batch * 128 + u * kChunkBytes +
-                                                  16 * b);
-      s[m] = *reinterpret_cast<const uint32_t*>(a.s + n[m] * a.srow + 16 * (batch >> 1) + 4 * b) >>
-             (16 * (batch & 1));
-    }
+    for (int m = 0; m < 2; ++m) load_codes(w[m], s[m], a.q, a.s, a, n[m], batch, b);
   };
 
   f4 sum[2][NT];
@@ -363,54 +356,39 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
   __syncthreads();
   for (int batch = b0; batch < b1; ++batch) {
     const int cur = (batch - b0) & 1;
-    u32x4 wc[kSlabChunks][2];
-    uint32_t sc[2], sx[NT];
+    u32x4 wc[2][kBatch];
+    uint32_t sc[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
 #pragma unroll
-      for (int u = 0; u < kSlabChunks; ++u) wc[u][m] = w[u][m];
+      for (int u = 0; u < kBatch; ++u) wc[m][u] = w[m][u];
       sc[m] = s[m];
     }
-    if constexpr (PACKED)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) sx[t] = sxn[t];
     if (batch + 1 < b1) {
       fetch_x(batch + 1);
       fetch_w(batch + 1);
     }
     const char* xc = xl[cur] + i * kPitch;
-    if constexpr (PACKED) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const u32x4 f0 = *reinterpret_cast<const u32x4*>(xc + 16 * t * kPitch + 16 * b);
-        const u32x4 f1 = *reinterpret_cast<const u32x4*>(xc + 16 * t * kPitch + 64 + 16 * b);
+    for (int u = 0; u < kBatch; ++u) {
+      if (batch * kBatch + u >= a.chunks) break;  // past the row's end
+      bf16x8 v[2][4];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          mfma_mx4<0>(sum[m][t], wc[0][m], sc[m], f0, sx[t]);
-          mfma_mx4<1>(sum[m][t], wc[1][m], sc[m], f1, sx[t]);
-        }
+      for (int m = 0; m < 2; ++m) {
+        const float scale = __uint_as_float(((sc[m] >> (8 * u)) & 255u) << 23);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[m][j] = weights8(wc[m][u][j], scale);
       }
-    } else {
 #pragma unroll
-      for (int u = 0; u < kSlabChunks; ++u) {
-        bf16x8 v[2][4];
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const float scale = u ? scale_at<1>(sc[m]) : scale_at<0>(sc[m]);
+        for (int j = 0; j < 4; ++j) {
+          const bf16x8 f =
+              *reinterpret_cast<const bf16x8*>(xc + 16 * t * kPitch + (u * kChunk + 32 * b + 8 * j) * 2);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[m][j] = weights8(wc[u][m][j], scale);
+          for (int m = 0; m < 2; ++m)
+            sum[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[m][j], f, sum[m][t], 0, 0, 0);
         }
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const bf16x8 f = *reinterpret_cast<const bf16x8*>(
-                xc + 16 * t * kPitch + (u * kChunk + 32 * b + 8 * j) * 2);
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-              sum[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[m][j], f, sum[m][t], 0, 0, 0);
-          }
-      }
     }
     if (batch + 1 < b1) put_x(cur ^ 1);
     __syncthreads();
@@ -451,17 +429,16 @@ __global__ void __launch_bounds__(kThreads) k_mx4_join(Mx4Args a, int splits, in
 // workgroup, of two batches at least beyond eight.
 int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out) {
   const int64_t wgs = ceil_div(d_out, kSlabRows) * ceil_div(n_tok, kSlabTokens);
-  const int64_t batches = ceil_div(d, kSlabK);
-  if (batches <= 2) return 1;
-  return std::max<int64_t>(1, std::min(256 / wgs, std::max(batches / 2, std::min<int64_t>(batches, 8))));
+  const int64_t batches = ceil_div(d, kBatchK);
+  return std::max<int64_t>(1, std::min(256 / wgs, batches));
 }
 
-template <bool PACKED, int NT>
+template <int NT>
 void launch_slab(const Mx4Args& a, hipStream_t s) {
   const unsigned wgs = unsigned(ceil_div(a.d_out, kSlabRows));
   const unsigned tiles = unsigned(ceil_div(a.n_tok, kSlabTokens));
   const int splits = int(slab_splits(a.n_tok, a.d, a.d_out));
-  hipLaunchKernelGGL((k_mx4_slab<PACKED, NT>), dim3(wgs, unsigned(splits), tiles),
+  hipLaunchKernelGGL((k_mx4_slab<NT>), dim3(wgs, unsigned(splits), tiles),
                      dim3(64 * kSlabWaves), 0, s, a);
   if (splits > 1) {
     const int64_t per = int64_t(wgs) * kSlabWaves * 2 * NT, blocks = per * tiles;
@@ -554,39 +531,129 @@ __global__ void __launch_bounds__(kThreads) k_mx4_tile_join(Mx4Args a, int split
   store_y8(a, tok, n + 128, c[2], c[3]);
 }
 
-// Ranges of a tile's sum: as many as give every CU a workgroup, of two pairs of stages at least.
-int tile_splits(int64_t n_tok, int64_t d, int64_t d_out) {
-  const int64_t tiles = ceil_div(n_tok, 256) * ceil_div(d_out, 256);
-  return int(std::max<int64_t>(1, std::min(256 / tiles, ceil_div(d, 512) / 2)));
+// Smaller tiles. Workgroups of one XCD (index modulo 8) take consecutive tiles, the tiles of one
+// column of outputs first, so that its L2 reads the weights once.
+template <typename R>
+__global__ void __launch_bounds__(R::kThreads) k_mx4_ring(Mx4Args a) {
+  __shared__ __attribute__((aligned(1024))) char b0[R::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b1[R::kBufBytes];
+  __shared__ __attribute__((aligned(1024))) char b2[R::NBUF == 4 ? R::kBufBytes : 16];
+  __shared__ __attribute__((aligned(1024))) char b3[R::NBUF == 4 ? R::kBufBytes : 16];
+  __shared__ __attribute__((aligned(1024))) char s0[R::kScaleBytes];
+  __shared__ __attribute__((aligned(1024))) char s1[R::kScaleBytes];
+  const int tiles_m = int((a.n_tok + R::TM - 1) / R::TM), tiles_n = int((a.d_out + R::TN - 1) / R::TN);
+  const int tile = int(blockIdx.x & 7) * int(gridDim.x >> 3) + int(blockIdx.x >> 3);
+  if (tile >= tiles_m * tiles_n) return;
+  const int tn = tile / tiles_m;
+  const int64_t m0 = int64_t(tile - tn * tiles_m) * R::TM, n0 = int64_t(tn) * R::TN;
+  const int stages = a.row / 128, pairs = (stages + 1) / 2;
+  const int p0 = int(int64_t(pairs) * blockIdx.y / gridDim.y);
+  const int p1 = int(int64_t(pairs) * (blockIdx.y + 1) / gridDim.y);
+  auto token = [&](int r) { return std::min(m0 + r, a.n_tok - 1); };
+  auto output = [&](int r) { return std::min(n0 + t256_rows_source(r), a.d_out - 1); };
+  mx4::RingSource<R> src;
+#pragma unroll
+  for (int i = 0; i < R::kLoads; ++i) {
+    const int r = mx4::ring_load_row(i);
+    src.row[i] = (r < R::TM ? static_cast<const char*>(a.x) + token(r) * a.row
+                            : reinterpret_cast<const char*>(a.q) + output(r - R::TM) * a.row) +
+                 int64_t(2 * p0) * 128 + ((int(threadIdx.x & 7) ^ (r & 7)) * 16);
+  }
+  const int r = std::min(int(threadIdx.x), R::TM + R::TN - 1);
+  src.scales = reinterpret_cast<const char*>(r < R::TM ? a.xs + token(r) * a.srow
+                                                       : a.s + output(r - R::TM) * a.srow) + 16 * p0;
+  f4 acc[R::MB][R::NB];
+  mx4::ring_mainloop<R>(acc, src, std::min(2 * p1, stages) - 2 * p0, b0, b1, b2, b3, s0, s1);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (gridDim.y > 1) {  // [split][tile][wave][block][lane]
+    f4* part = a.part + ((size_t(blockIdx.y) * (tiles_m * tiles_n) + tile) * 4 + wave) * R::MB * R::NB * 64 +
+               lane;
+#pragma unroll
+    for (int mi = 0; mi < R::MB; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < R::NB; ++ni) part[(mi * R::NB + ni) * 64] = acc[mi][ni];
+    return;
+  }
+#pragma unroll
+  for (int mi = 0; mi < R::MB; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < R::NB; ni += 2)
+      store_y8(a, m0 + ((wave / R::WN) * R::MB + mi) * 16 + (lane & 15),
+               n0 + (wave % R::WN) * R::NB * 16 + ni * 16 + 8 * (lane >> 4), acc[mi][ni], acc[mi][ni + 1]);
 }
-size_t tile_part_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
-  const int splits = tile_splits(n_tok, d, d_out);
-  return splits < 2 ? 0 : size_t(splits) * size_t(ceil_div(n_tok, 256) * ceil_div(d_out, 256)) << 18;
+
+template <typename R>
+__global__ void __launch_bounds__(kThreads) k_mx4_ring_join(Mx4Args a, int splits, int tiles, int tiles_m) {
+  constexpr int kPairs = R::MB * R::NB / 2;  // of blocks, of a wave
+  const int lane = threadIdx.x & 63;
+  const int64_t at = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  if (at >= int64_t(tiles) * 4 * kPairs) return;
+  const f4* part = a.part + at * 2 * 64 + lane;
+  const size_t step = size_t(tiles) * 4 * kPairs * 2 * 64;
+  f4 c[2] = {};
+#pragma unroll 4
+  for (int sp = 0; sp < splits; ++sp)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) c[q] += part[sp * step + q * 64];
+  const int tile = int(at / (4 * kPairs)), wave = int(at / kPairs) & 3, pair = int(at % kPairs);
+  const int tn = tile / tiles_m, mi = pair / (R::NB / 2), ni = pair % (R::NB / 2) * 2;
+  store_y8(a, int64_t(tile - tn * tiles_m) * R::TM + ((wave / R::WN) * R::MB + mi) * 16 + (lane & 15),
+           int64_t(tn) * R::TN + (wave % R::WN) * R::NB * 16 + ni * 16 + 8 * (lane >> 4), c[0], c[1]);
+}
+
+using Ring128x128 = mx4::Ring<128, 128, 2, 2, 2>;
+using Ring64x128 = mx4::Ring<64, 128, 1, 4, 2>;
+using Ring64x64 = mx4::Ring<64, 64, 2, 2, 4>;
+
+template <typename R>
+void launch_ring(const Mx4Args& a, const Mx4Plan& p, hipStream_t s) {
+  hipLaunchKernelGGL(k_mx4_ring<R>, dim3(unsigned(round_up(p.tiles, 8)), unsigned(p.splits)),
+                     dim3(R::kThreads), 0, s, a);
+  if (p.splits > 1)
+    hipLaunchKernelGGL(k_mx4_ring_join<R>,
+                       dim3(unsigned(ceil_div(p.tiles * 2 * R::MB * R::NB, kThreads / 64))),
+                       dim3(kThreads), 0, s, a, p.splits, int(p.tiles), int(ceil_div(a.n_tok, R::TM)));
 }
 
 void launch_tile(const Mx4Args& a, hipStream_t s) {
-  const unsigned tiles = unsigned(ceil_div(a.n_tok, 256) * ceil_div(a.d_out, 256));
-  const int splits = tile_splits(a.n_tok, a.d, a.d_out);
-  hipLaunchKernelGGL(k_mx4_tile, dim3(tiles, unsigned(splits)), dim3(Tile256::kThreads), 0, s, a);
-  if (splits > 1)
-    hipLaunchKernelGGL(k_mx4_tile_join, dim3(tiles * 16), dim3(kThreads), 0, s, a, splits, int(tiles));
+  const Mx4Plan p = mx4_plan(a.n_tok, a.d, a.d_out);
+  if (p.tile == kMx4Tile128) return launch_ring<Ring128x128>(a, p, s);
+  if (p.tile == kMx4Tile64x128) return launch_ring<Ring64x128>(a, p, s);
+  if (p.tile == kMx4Tile64) return launch_ring<Ring64x64>(a, p, s);
+  hipLaunchKernelGGL(k_mx4_tile, dim3(unsigned(p.tiles), unsigned(p.splits)), dim3(Tile256::kThreads), 0,
+                     s, a);
+  if (p.splits > 1)
+    hipLaunchKernelGGL(k_mx4_tile_join, dim3(unsigned(p.tiles) * 16), dim3(kThreads), 0, s, a, p.splits,
+                       int(p.tiles));
 }
 
-template <bool PACKED, int ROWS>
+template <bool PACKED, int ROWS, int RB>
 void launch_few(const Mx4Args& a, hipStream_t s) {
   // As many waves as there are batches, and as the CU's LDS holds tokens for.
-  const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kFewPitch, 1024);
+  const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kFewPitch, RB * 1024);
   const int most = int(std::min<size_t>(kFewWaves, (size_t(160) << 10) / each));
   const int waves = int(std::min<int64_t>(ceil_div(a.chunks, kBatch), most));
-  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS>), dim3(unsigned(ceil_div(a.d_out, 16))),
+  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB>), dim3(unsigned(ceil_div(a.d_out, 16 * RB))),
                      dim3(64 * waves), waves * each, s, a);
+}
+// Two blocks of outputs where every CU still has a workgroup: they halve what is read of the
+// tokens. 16 tokens, 4096 -> 8192 12.4 to 9.3 us, -> 14336 22.3 to 16.8, but -> 1000 with d = 1000 5.9
+// to 6.8; one token, 14336 -> 4096 9.4 to 12.8.
+template <bool PACKED, int ROWS>
+void launch_few(const Mx4Args& a, hipStream_t s) {
+  if (a.d_out > 32 * 255) launch_few<PACKED, ROWS, 2>(a, s);
+  else launch_few<PACKED, ROWS, 1>(a, s);
 }
 
 template <bool PACKED>
 void launch_mx4(const Mx4Args& a, hipStream_t s) {
-  if (PACKED && a.n_tok > kSlabTokens) launch_tile(a, s);
-  else if (a.n_tok > 32) launch_slab<PACKED, 4>(a, s);
-  else if (a.n_tok > kFew) launch_slab<PACKED, 2>(a, s);
+  // Every 16 outputs of the few-token kernel read all tokens again. Packed ones, us with it and in
+  // tiles: 16 tokens, 4096 -> 4096 5.6 and 9.6, -> 14336 12.6 and 11.5; 8 tokens, 4096 -> 14336
+  // 10.9 and 11.3, -> 128000 70 and 55; one token, -> 128000 55 and 57.
+  if (PACKED && (a.n_tok > kFew || a.n_tok * a.d_out > 131072)) launch_tile(a, s);
+  else if (a.n_tok > 32) launch_slab<4>(a, s);
+  else if (a.n_tok > kFew) launch_slab<2>(a, s);
+  else if (!PACKED && a.n_tok > kFewest && a.d * a.d_out > kSlabWeights) launch_slab<1>(a, s);
   else if (a.n_tok > 4 && !PACKED) launch_few<PACKED, 8>(a, s);
   else launch_few<PACKED, 4>(a, s);
 }
@@ -629,7 +696,7 @@ optima_status mx4_unpack(const void* Q, const void* scales, int64_t n, int64_t d
 }
 
 size_t mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
-  if (n_tok <= kFew) return 0;
+  if (n_tok <= kFewest) return 0;
   // The most of any number of tokens up to these, so that more need no less.
   const int64_t wgs = ceil_div(d_out, kSlabRows), tiles = ceil_div(n_tok, kSlabTokens);
   int64_t parts = 0;
@@ -638,11 +705,7 @@ size_t mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
     if (splits > 1) parts = std::max(parts, splits * t);
   }
   const size_t slab = size_t(parts) * size_t(wgs) * kSlabWaves * 2 * (kSlabTokens / 16) * 64 * sizeof(f4);
-  size_t tile = 0;
-  const int64_t tiles_n = ceil_div(d_out, 256);
-  for (int64_t t = 1; t <= std::min(ceil_div(n_tok, 256), 128 / tiles_n); ++t)
-    tile = std::max(tile, tile_part_bytes(256 * t, d, d_out));
-  return std::max(slab, n_tok > kSlabTokens ? tile : 0);
+  return std::max<size_t>(slab, mx4_tile_workspace(n_tok, d, d_out));
 }
 
 optima_status mx4_linear(const void* X, int64_t ldx, const void* x_scales, int64_t n_tok, int64_t d,

@@ -94,10 +94,10 @@ def test_linear_refusals(lib, change, status):
 def test_linear_workspace(lib):
     f = _sizes(lib).optima_mx4_workspace_bytes
     f.argtypes = [i64, i64, i64]
-    assert f(16, 4096, 4096) == 0 and f(17, 4096, 1000) > 0
+    assert f(8, 4096, 4096) == 0 and f(9, 4096, 1000) > 0
     for d, out in ((4096, 4096), (14336, 4096), (1001, 2731), (64, 64), (4096, 128000)):
         last = 0
-        for n in (1, 16, 17, 33, 64, 65, 100, 129, 255, 256, 257, 400, 777, 1025, 2049, 8192, 1 << 21):
+        for n in (1, 8, 9, 16, 17, 33, 64, 65, 100, 129, 255, 256, 257, 400, 777, 1025, 2049, 8192, 1 << 21):
             assert f(n, d, out) >= last
             last = f(n, d, out)
     need = f(20, 4096, 500)

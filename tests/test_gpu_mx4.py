@@ -149,7 +149,8 @@ def test_linear(L, d, ff, packed):
 
 
 @pytest.mark.parametrize("packed", (False, True))
-@pytest.mark.parametrize("n, d, ff", ((1, 14336, 4096), (16, 4096, 14336), (64, 4096, 1000),
+@pytest.mark.parametrize("n, d, ff", ((1, 14336, 4096), (16, 4096, 14336), (10, 4096, 14336),
+                                      (6, 1500, 9000), (12, 4096, 8200), (9, 14336, 9001), (64, 4096, 1000),
                                       (100, 14336, 768), (300, 1000, 2731), (777, 4097, 5001)))
 def test_linear_of_full_sizes(L, n, d, ff, packed):
     Q, s, w = _weights(L, ff, d, 3)
