@@ -191,12 +191,6 @@ __device__ inline void wave_exchange() {
 
 // Up to 16 tokens. A workgroup takes 16 outputs, its waves every waves-th batch of 512 values,
 // and the waves' sums are joined in LDS in their order.
-constexpr int kFew = 16;
-// 16-bit tokens above kFewest of larger weights share what is read of them: 16 tokens, 4096 -> 14336
-// 16.7 us here and 15.2 in slabs, 4096 -> 128000 120 and 71, 14336 -> 4096 17.2 and 15.4, but
-// 4096 -> 4096 7.0 and 10.8; 8 tokens, 4096 -> 14336 11.8 and 15.2.
-constexpr int kFewest = 8;
-constexpr int64_t kSlabWeights = 48 << 20;
 constexpr int kFewWaves = 16;
 // Bytes of a token's batch in LDS, with 64 between rows.
 constexpr int kFewPitch = kBatchK * 2 + 64;
@@ -294,12 +288,10 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
   }
 }
 
-// More 16-bit tokens, 64 at a time. The tokens' values of a batch go through LDS, two batches in
+// More 16-bit tokens, 16 NT at a time. The tokens' values of a batch go through LDS, two batches in
 // turn, for all waves of a workgroup; a wave takes 32 outputs, whose codes it loads a batch
 // ahead. With few outputs the batches are split over blockIdx.y, and k_mx4_join adds the parts.
-constexpr int kSlabTokens = 64;
-constexpr int kSlabWaves = 8;
-constexpr int kSlabRows = kSlabWaves * 32;
+constexpr int kSlabWaves = kMx4SlabRows / 32;
 
 template <int NT>
 __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
@@ -308,9 +300,9 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
   constexpr int kEach = (kTok * kPieces + 511) / 512;        // that a thread brings
   __shared__ __attribute__((aligned(16))) char xl[2][kTok * kPitch];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = lane >> 4, i = lane & 15;
-  const int64_t t0 = int64_t(blockIdx.z) * kSlabTokens;
+  const int64_t t0 = int64_t(blockIdx.z) * kTok;
   const int tokens = int(std::min<int64_t>(a.n_tok - t0, kTok));
-  const int64_t n0 = int64_t(blockIdx.x) * kSlabRows + wave * 32;
+  const int64_t n0 = int64_t(blockIdx.x) * kMx4SlabRows + wave * 32;
   int64_t n[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) n[m] = std::min(n0 + 16 * m + i, a.d_out - 1);
@@ -422,22 +414,13 @@ __global__ void __launch_bounds__(kThreads) k_mx4_join(Mx4Args a, int splits, in
   const int64_t z = at / per, in = at - z * per;  // of 64 tokens
   const int64_t wave = in / (2 * NT);
   const int m = int(in / NT) & 1, t = int(in % NT);
-  store_y4(a, z * kSlabTokens + 16 * t + (lane & 15), wave * 32 + 16 * m + 4 * (lane >> 4), sum);
-}
-
-// Ranges that the sums of more than kFew tokens are split into: as many as give every CU a
-// workgroup, of two batches at least beyond eight.
-int64_t slab_splits(int64_t n_tok, int64_t d, int64_t d_out) {
-  const int64_t wgs = ceil_div(d_out, kSlabRows) * ceil_div(n_tok, kSlabTokens);
-  const int64_t batches = ceil_div(d, kBatchK);
-  return std::max<int64_t>(1, std::min(256 / wgs, batches));
+  store_y4(a, z * 16 * NT + 16 * t + (lane & 15), wave * 32 + 16 * m + 4 * (lane >> 4), sum);
 }
 
 template <int NT>
-void launch_slab(const Mx4Args& a, hipStream_t s) {
-  const unsigned wgs = unsigned(ceil_div(a.d_out, kSlabRows));
-  const unsigned tiles = unsigned(ceil_div(a.n_tok, kSlabTokens));
-  const int splits = int(slab_splits(a.n_tok, a.d, a.d_out));
+void launch_slab(const Mx4Args& a, int splits, hipStream_t s) {
+  const unsigned wgs = unsigned(ceil_div(a.d_out, kMx4SlabRows));
+  const unsigned tiles = unsigned(ceil_div(a.n_tok, 16 * NT));
   hipLaunchKernelGGL((k_mx4_slab<NT>), dim3(wgs, unsigned(splits), tiles),
                      dim3(64 * kSlabWaves), 0, s, a);
   if (splits > 1) {
@@ -645,17 +628,20 @@ void launch_few(const Mx4Args& a, hipStream_t s) {
   else launch_few<PACKED, ROWS, 1>(a, s);
 }
 
-template <bool PACKED>
-void launch_mx4(const Mx4Args& a, hipStream_t s) {
-  // Every 16 outputs of the few-token kernel read all tokens again. Packed ones, us with it and in
-  // tiles: 16 tokens, 4096 -> 4096 5.6 and 9.6, -> 14336 12.6 and 11.5; 8 tokens, 4096 -> 14336
-  // 10.9 and 11.3, -> 128000 70 and 55; one token, -> 128000 55 and 57.
-  if (PACKED && (a.n_tok > kFew || a.n_tok * a.d_out > 131072)) launch_tile(a, s);
-  else if (a.n_tok > 32) launch_slab<4>(a, s);
-  else if (a.n_tok > kFew) launch_slab<2>(a, s);
-  else if (!PACKED && a.n_tok > kFewest && a.d * a.d_out > kSlabWeights) launch_slab<1>(a, s);
-  else if (a.n_tok > 4 && !PACKED) launch_few<PACKED, 8>(a, s);
-  else launch_few<PACKED, 4>(a, s);
+void launch_packed(const Mx4Args& a, hipStream_t s) {
+  // Every 16 or 32 outputs of the few-token kernel read all tokens again. us with it and in tiles: 16
+  // tokens, 4096 -> 4096 5.6 and 9.6, -> 14336 12.6 and 11.5; 8 tokens, 4096 -> 14336 10.9 and 11.3,
+  // -> 128000 70 and 55; one token, -> 128000 55 and 57.
+  if (a.n_tok > kMx4Few || a.n_tok * a.d_out > 131072) launch_tile(a, s);
+  else launch_few<true, 4>(a, s);
+}
+void launch_16bit(const Mx4Args& a, hipStream_t s) {
+  const Mx4SlabPlan p = mx4_slab_plan(a.n_tok, a.d, a.d_out);
+  if (p.tokens == 16) launch_slab<1>(a, p.splits, s);
+  else if (p.tokens == 32) launch_slab<2>(a, p.splits, s);
+  else if (p.tokens == 64) launch_slab<4>(a, p.splits, s);
+  else if (a.n_tok > 4) launch_few<false, 8>(a, s);
+  else launch_few<false, 4>(a, s);
 }
 
 }  // namespace
@@ -696,16 +682,7 @@ optima_status mx4_unpack(const void* Q, const void* scales, int64_t n, int64_t d
 }
 
 size_t mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out) {
-  if (n_tok <= kFewest) return 0;
-  // The most of any number of tokens up to these, so that more need no less.
-  const int64_t wgs = ceil_div(d_out, kSlabRows), tiles = ceil_div(n_tok, kSlabTokens);
-  int64_t parts = 0;
-  for (int64_t t = 1; t <= std::min(tiles, 128 / wgs); ++t) {
-    const int64_t splits = slab_splits(t * kSlabTokens, d, d_out);
-    if (splits > 1) parts = std::max(parts, splits * t);
-  }
-  const size_t slab = size_t(parts) * size_t(wgs) * kSlabWaves * 2 * (kSlabTokens / 16) * 64 * sizeof(f4);
-  return std::max<size_t>(slab, mx4_tile_workspace(n_tok, d, d_out));
+  return mx4_room(n_tok, d, d_out);
 }
 
 optima_status mx4_linear(const void* X, int64_t ldx, const void* x_scales, int64_t n_tok, int64_t d,
@@ -727,8 +704,8 @@ optima_status mx4_linear(const void* X, int64_t ldx, const void* x_scales, int64
   a.row = int(row_bytes(d));
   a.srow = int(scale_bytes(d));
   a.y_f32 = y_dtype == OPTIMA_DTYPE_F32;
-  if (x_scales) launch_mx4<true>(a, s);
-  else launch_mx4<false>(a, s);
+  if (x_scales) launch_packed(a, s);
+  else launch_16bit(a, s);
   OPTIMA_LAUNCH_CHECK();
   return OPTIMA_OK;
 }

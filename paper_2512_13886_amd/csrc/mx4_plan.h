@@ -1,5 +1,5 @@
-// Host plan of the packed products with packed tokens (mx4.hip): which tile, and how many ranges
-// of its sum. A function of the sizes alone, and of the tokens by blocks of 64.
+// Host plans of the packed products (mx4.hip): which kernel and tile, and how many ranges of its
+// sum. Functions of the sizes alone.
 #pragma once
 
 #include "common.h"
@@ -55,14 +55,65 @@ inline Mx4Plan mx4_plan(int64_t n_tok, int64_t d, int64_t d_out) {
   return best;
 }
 
-// Room for the parts of any number of tokens up to these.
-inline size_t mx4_tile_workspace(int64_t n_tok, int64_t d, int64_t d_out) {
-  int64_t most = 0;
-  for (int t = 0; t < kMx4Tiles; ++t) {
-    const int64_t tiles = mx4_tiles(t, n_tok, d_out);
-    for (const int splits : kMx4Splits)
-      if (splits <= ceil_div(d, 512)) most = std::max(most, mx4_part_bytes(t, splits, tiles));
+// 16-bit tokens: the few-token kernel (tokens 0), or slabs of 16, 32 or 64 tokens and 256 outputs.
+struct Mx4SlabPlan {
+  int tokens, splits;
+};
+constexpr int kMx4Few = 16;      // tokens of the few-token kernel, at most
+constexpr int kMx4Fewest = 8;    // up to which 16-bit ones always take it
+constexpr int kMx4SlabRows = 256;
+constexpr int kMx4SlabSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24};
+
+inline int64_t mx4_slab_parts(int tokens, int splits, int64_t n_tok, int64_t d_out) {
+  return splits < 2 ? 0
+                    : splits * ceil_div(n_tok, tokens) * ceil_div(d_out, kMx4SlabRows) * tokens * kMx4SlabRows * 4;
+}
+
+// The least estimate, in microseconds, as above: batches of 512 values of a slab's workgroup, one a
+// CU, 9 TB/s for operands and outputs, and the join; of the few-token kernel rounds of its waves'
+// batches. The constants fit 90 sizes of 9 to 64 tokens; the choice is 1.7 % off the best on average.
+// 16 tokens, 4096 -> 14336: few 17.1 us, slabs of 16 16.2; -> 4096 6.9 and 10.0; 64 tokens,
+// 768 -> 14336 8.7 us in slabs of 16, 13.5 in slabs of 64; 4096 -> 14336 23 in slabs of 32, 22.4 of 64.
+inline Mx4SlabPlan mx4_slab_plan(int64_t n_tok, int64_t d, int64_t d_out) {
+  Mx4SlabPlan best{0, 1};
+  if (n_tok <= kMx4Fewest) return best;
+  const int64_t batches = ceil_div(d, 512);
+  const double bytes = double(d) * double(d_out) * 0.53 + 2.0 * double(n_tok) * double(d + d_out);
+  double best_us = 1e30;
+  if (n_tok <= kMx4Few) {
+    const int64_t rounds = ceil_div(batches, std::min<int64_t>(batches, 163840 / (n_tok * 1088)));
+    best_us = 1.35 + 2.9 * double(rounds) + 0.1 * double(n_tok) + bytes / 3.9e6;
   }
+  for (const int tokens : {16, 32, 64}) {
+    if (n_tok > 64 ? tokens < 64 : tokens > 16 && n_tok <= tokens / 2) continue;
+    const double around = tokens == 16 ? 2.4 : tokens == 32 ? 3.2 : 4.0;
+    const double batch = tokens == 16 ? 2.43 : tokens == 32 ? 2.66 : 3.62;
+    const int64_t tiles = ceil_div(n_tok, tokens) * ceil_div(d_out, kMx4SlabRows);
+    for (const int splits : kMx4SlabSplits) {
+      const int64_t parts = mx4_slab_parts(tokens, splits, n_tok, d_out);
+      if (splits > batches || parts > kMx4PartBytes) break;
+      const double us = around + batch * double(ceil_div(batches, splits) * ceil_div(tiles * splits, 256)) +
+                        bytes / 9e6 + (splits > 1 ? 3.2 + double(parts) * 2 / 5e6 : 0);
+      if (us < best_us) {
+        best_us = us;
+        best = Mx4SlabPlan{tokens, splits};
+      }
+    }
+  }
+  return best;
+}
+
+// Room for the parts of any number of tokens up to these, of either kind.
+inline size_t mx4_room(int64_t n_tok, int64_t d, int64_t d_out) {
+  if (n_tok <= kMx4Fewest) return 0;
+  int64_t most = 0;
+  for (int t = 0; t < kMx4Tiles; ++t)
+    for (const int splits : kMx4Splits)
+      if (splits <= ceil_div(d, 512))
+        most = std::max(most, mx4_part_bytes(t, splits, mx4_tiles(t, n_tok, d_out)));
+  for (const int tokens : {16, 32, 64})
+    for (const int splits : kMx4SlabSplits)
+      if (splits <= ceil_div(d, 512)) most = std::max(most, mx4_slab_parts(tokens, splits, n_tok, d_out));
   return size_t(std::min(most, kMx4PartBytes));
 }
 
