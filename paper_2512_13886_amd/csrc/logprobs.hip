@@ -9,7 +9,7 @@
 // The k largest come out of the same pass. Each thread keeps the largest of its values and the
 // first group of eight that holds it; groups compare by value and then by their place. The k
 // largest of a row lie in the k best threads' values (a value elsewhere has k larger ones before
-// it), which are read again, and those not below the k-th best thread's are ranked.
+// it), which are read again, and those that reach the k-th best thread's are ranked.
 #include <type_traits>
 
 #include "common.h"
@@ -48,23 +48,27 @@ __device__ inline uint64_t key_of(float x, uint32_t place) {
   return uint64_t(order_of(x)) << 32 | uint32_t(~place);
 }
 
+// v of another lane of the same 16: rotated by 8, 4, 2 and 1 lanes in turn, every lane gets a sum or
+// maximum of all 16.
 template <int CTRL>
-__device__ inline uint32_t dpp_max(uint32_t v) {
-  return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false)));
+__device__ inline uint32_t rotated(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_mov_dpp(int(v), CTRL, 0xF, 0xF, true));
 }
-// Largest over a wave: within rows of 16 lanes, then rows and halves into the last lane.
+constexpr int kBy8 = 0x128, kBy4 = 0x124, kBy2 = 0x122, kBy1 = 0x121;
+template <int CTRL>
+__device__ inline float rotated(float v) {
+  return __uint_as_float(rotated<CTRL>(__float_as_uint(v)));
+}
+__device__ inline float lane_value(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
 __device__ inline uint32_t wave_max(uint32_t v) {
-  v = dpp_max<0x111>(v);  // from 1, 2, 4 and 8 lanes before
-  v = dpp_max<0x112>(v);
-  v = dpp_max<0x114>(v);
-  v = dpp_max<0x118>(v);
-  v = dpp_max<0x142>(v);  // a row's last lane to the next row
-  v = dpp_max<0x143>(v);  // lane 31 to the second half
-  return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
-}
-__device__ inline uint64_t wave_max64(uint64_t v) {
-  const uint32_t hi = wave_max(uint32_t(v >> 32));
-  return uint64_t(hi) << 32 | wave_max(uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
+  v = max(v, rotated<kBy8>(v));
+  v = max(v, rotated<kBy4>(v));
+  v = max(v, rotated<kBy2>(v));
+  v = max(v, rotated<kBy1>(v));
+  auto of = [v](int lane) { return uint32_t(__builtin_amdgcn_readlane(int(v), lane)); };
+  return max(max(of(0), of(16)), max(of(32), of(48)));
 }
 
 __device__ inline float max3(float a, float b, float c) {
@@ -92,16 +96,28 @@ __device__ inline void rebase(Sums& a, float m, float c) {
   a.s *= r;
   a.m = m;
 }
-__device__ inline Sums wave_sums(Sums a, float c) {
+// Of the LANES (16 or 64) lanes of a row: all of them have m, the first one s and t.
+template <int LANES>
+__device__ inline Sums lanes_sums(Sums a, float c) {
   float m = a.m;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  m = max3(m, rotated<kBy8>(m), m);
+  m = max3(m, rotated<kBy4>(m), m);
+  m = max3(m, rotated<kBy2>(m), m);
+  m = max3(m, rotated<kBy1>(m), m);
+  if constexpr (LANES == 64)
+    m = max3(max3(lane_value(m, 0), lane_value(m, 16), lane_value(m, 32)), lane_value(m, 48), m);
   rebase(a, m, c);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    a.s += __shfl_xor(a.s, o, 64);
-    a.t += __shfl_xor(a.t, o, 64);
-  }
+  auto sum = [](float v) {
+    v += rotated<kBy8>(v);
+    v += rotated<kBy4>(v);
+    v += rotated<kBy2>(v);
+    v += rotated<kBy1>(v);
+    if constexpr (LANES == 64)
+      v = (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+    return v;
+  };
+  a.s = sum(a.s);
+  a.t = sum(a.t);
   return a;
 }
 
@@ -145,9 +161,9 @@ __device__ inline void wave_exchange() {
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-template <int WAVES>
+template <int LANES>
 __device__ inline void group_sync() {
-  if constexpr (WAVES > 1)
+  if constexpr (LANES > 64)
     __syncthreads();
   else
     wave_exchange();
@@ -157,17 +173,71 @@ constexpr int kGroups = 4;         // of eight values that a thread loads togeth
 constexpr int kTopSteps = 16;      // groups of a thread, at most, where alternatives are wanted
 constexpr int kPartLen = kTopSteps * 256 * 8;
 
-// A part of a row by WAVES waves (4: a workgroup; 1: four rows a workgroup).
-template <typename T, int WAVES, bool TOP>
+// The k best of the values `order` with their places that a wave's lanes hold W of (0: none), or
+// all if there are fewer: numbers lane + 64 w in `chosen`, and what an element has to reach, a value
+// and with that value the place of its group. A value that k of them reach is searched bit by bit;
+// only where more than k are equal to the last one places decide.
+template <int W>
+struct Choice {
+  int picked;
+  uint32_t value, place;
+};
+template <int W>
+__device__ inline Choice<W> choose(const uint32_t (&order)[W], const uint32_t (&place)[W], int k,
+                                   int* chosen) {
+  auto count = [](auto of) {
+    int c = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) c += __popcll(__ballot(of(w)));
+    return c;
+  };
+  Choice<W> r{count([&](int w) { return order[w] > 0; }), 0u, ~0u};
+  if (r.picked > k) {
+    int reach = r.picked;
+    for (int bit = 31; bit >= 0 && reach != k; --bit) {
+      const uint32_t v = r.value | 1u << bit;
+      const int c = count([&](int w) { return order[w] >= v; });
+      if (c >= k) {
+        r.value = v;
+        reach = c;
+      }
+    }
+    if (reach > k) {
+      const int more = k - count([&](int w) { return order[w] > r.value; });
+      r.place = 0;
+      for (int bit = 20; bit >= 0; --bit) {  // places are below 2^20
+        const uint32_t below = r.place | ((1u << bit) - 1);
+        if (count([&](int w) { return order[w] == r.value && place[w] <= below; }) < more)
+          r.place |= 1u << bit;
+      }
+    }
+    r.picked = k;
+  }
+  int at = 0;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const bool in = order[w] > max(r.value, 1u) - 1u &&
+                    (order[w] != r.value || place[w] <= r.place);
+    const uint64_t mask = __ballot(in);
+    if (in) chosen[at + __popcll(mask & ((uint64_t(1) << lane) - 1))] = lane + 64 * w;
+    at += __popcll(mask);
+  }
+  return r;
+}
+
+// A part of a row by LANES lanes (256: a workgroup; 64 and 16: more rows a workgroup).
+template <typename T, int LANES, bool TOP>
 __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
-  constexpr int kThr = 64 * WAVES, kStep = 8 * kThr, kSub = 4 / WAVES;
-  __shared__ float red[WAVES][3];
-  __shared__ uint64_t best_of[TOP ? 256 : 1];
+  static_assert(!TOP || LANES >= 64, "alternatives are chosen by waves");
+  constexpr int kStep = 8 * LANES, kSub = 256 / LANES, kWaves = LANES > 64 ? LANES / 64 : 1;
+  __shared__ float red[kWaves][3];
+  __shared__ uint32_t best_of[TOP ? 256 : 1], base_of[TOP ? 256 : 1];
   __shared__ int chosen[TOP ? kSub : 1][OPTIMA_TOP_MAX];
-  __shared__ uint64_t border[kSub];
+  __shared__ uint32_t border[kSub][2];
   __shared__ int found[kSub], picked[kSub];
   extern __shared__ uint64_t lists[];
-  const int sub = WAVES > 1 ? 0 : threadIdx.x >> 6, t = threadIdx.x & (kThr - 1);
+  const int sub = threadIdx.x / LANES, t = threadIdx.x % LANES;
   const int64_t task = int64_t(blockIdx.x) * kSub + sub;
   const int64_t row = a.row0 + task / a.parts;
   if (row >= a.n) return;  // all threads of the row
@@ -179,20 +249,22 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
   Sums s = {-__builtin_inff(), 0.f, 0.f};
   float best = -__builtin_inff();
   int base = 8 * t;
-  auto groups = [&](int at0, auto whole) {
+  // Groups from at0 on, of the `left` values that the row's lanes have before them.
+  auto groups = [&](int at0, int left, auto whole) {
     Raw8<T> raw[kGroups];
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
       if (whole)
         load8(raw[u], x + at0 + u * kStep);
-      else
+      else if (u * kStep < left)
         load_piece(raw[u], x, at0 + u * kStep, len);
     }
     float v[kGroups][8], m = s.m;
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
+      if (!whole && u * kStep >= left) break;
       values8(raw[u], v[u]);
-      if (!whole) {
+      if (!whole && (u + 1) * kStep > left) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (at0 + u * kStep + e >= len) v[u][e] = -__builtin_inff();
@@ -208,7 +280,8 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
     if (m > s.m) rebase(s, m, c);
     const float ref = finite_max(m);
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u)
+    for (int u = 0; u < kGroups; ++u) {
+      if (!whole && u * kStep >= left) break;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float y = (v[u][e] - ref) * c;
@@ -216,23 +289,24 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
         s.s += p;
         s.t += p * max3(y, -1e4f, -1e4f);  // 0 for p = 0; NaN comes in by p
       }
+    }
   };
   int at = 8 * t, left = len;
   for (; left >= kGroups * kStep; left -= kGroups * kStep, at += kGroups * kStep)
-    groups(at, std::true_type());
-  if (left > 0) groups(at, std::false_type());
+    groups(at, left, std::true_type());
+  if (left > 0) groups(at, left, std::false_type());
 
-  s = wave_sums(s, c);
-  if constexpr (WAVES > 1) {
+  s = lanes_sums<(LANES < 64 ? LANES : 64)>(s, c);
+  if constexpr (LANES > 64) {
     const int wave = threadIdx.x >> 6;
     if ((t & 63) == 0) red[wave][0] = s.m, red[wave][1] = s.s, red[wave][2] = s.t;
     __syncthreads();
     float m = red[0][0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, red[w][0]);
+    for (int w = 1; w < kWaves; ++w) m = max3(m, red[w][0], m);
     Sums all = {m, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
       Sums one = {red[w][0], red[w][1], red[w][2]};
       rebase(one, m, c);
       all.s += one.s;
@@ -249,45 +323,33 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
     }
   }
   if constexpr (TOP) {
-    // The best threads, one after the other, by one wave.
-    const uint64_t mine = 8 * t < len ? key_of(best, uint32_t(p0 + base)) : 0u;
-    if constexpr (WAVES > 1) {
+    const uint32_t mine = 8 * t < len ? order_of(best) : 0u;
+    if constexpr (LANES > 64) {
       best_of[t] = mine;
+      base_of[t] = uint32_t(p0 + base);
       __syncthreads();
     }
     if (t < 64) {
-      uint64_t own[WAVES];
+      uint32_t order[kWaves], place[kWaves];
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) own[w] = WAVES > 1 ? best_of[t + 64 * w] : mine;
-      uint64_t last = 0;
-      int j = 0;
-      for (; j < a.k; ++j) {
-        uint64_t top = own[0];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) top = max(top, own[w]);
-        top = wave_max64(top);
-        if (!top) break;
-        last = top;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w)
-          if (own[w] == top) {
-            chosen[sub][j] = t + 64 * w;
-            own[w] = 0;
-          }
+      for (int w = 0; w < kWaves; ++w) {
+        order[w] = LANES > 64 ? best_of[t + 64 * w] : mine;
+        place[w] = LANES > 64 ? base_of[t + 64 * w] : uint32_t(p0 + base);
       }
+      const Choice<kWaves> r = choose(order, place, a.k, chosen[sub]);
       if (t == 0) {
         found[sub] = 0;
-        picked[sub] = j;
-        border[sub] = j < a.k ? 0 : last;  // fewer threads than k: all their values
+        picked[sub] = r.picked;
+        border[sub][0] = r.value;
+        border[sub][1] = r.place;
       }
     }
-    group_sync<WAVES>();
-    const uint64_t limit = border[sub];
-    const uint32_t limit_value = uint32_t(limit >> 32), limit_place = ~uint32_t(limit);
+    group_sync<LANES>();
+    const uint32_t limit_value = border[sub][0], limit_place = border[sub][1];
     const int steps = (len + kStep - 1) / kStep;
     uint64_t* list = lists + sub * list_len;
     const int tasks = picked[sub] * steps;
-    for (int q = t; q < tasks; q += kThr) {
+    for (int q = t; q < tasks; q += LANES) {
       const int j = q / steps, g = 8 * chosen[sub][j] + (q - j * steps) * kStep;
       if (g >= len) continue;
       Raw8<T> raw;
@@ -301,10 +363,10 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
           list[atomicAdd(&found[sub], 1)] = uint64_t(o) << 32 | uint32_t(~uint32_t(p0 + g + e));
       }
     }
-    group_sync<WAVES>();
+    group_sync<LANES>();
     const int count = found[sub];
     uint64_t* to = a.keys + (row * a.parts + part) * a.k;
-    for (int q = t; q < count; q += kThr) {
+    for (int q = t; q < count; q += LANES) {
       const uint64_t key = list[q];
       int rank = 0;
       for (int r = 0; r < count; ++r) rank += list[r] > key;
@@ -315,36 +377,48 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
         to[rank] = key;
     }
     if (a.parts > 1)
-      for (int q = count + t; q < a.k; q += kThr) to[q] = 0;
+      for (int q = count + t; q < a.k; q += LANES) to[q] = 0;
   }
 }
 
-// The parts of a row, by one wave: lane p has part p.
+// The parts of a row, by one wave: lane p has part p, whose keys lie in LDS.
 template <typename T>
 __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = a.row0 + int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  extern __shared__ uint64_t lists[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = a.row0 + int64_t(blockIdx.x) * 4 + wave;
   if (row >= a.n) return;
   const float c = a.scale * kLog2e;
+  const int keys = a.parts * a.k;
+  uint64_t* list = lists + wave * keys;
+  for (int q = lane; q < keys; q += 64) list[q] = a.keys[row * keys + q];
   Sums s = {-__builtin_inff(), 0.f, 0.f};
   if (lane < a.parts) {
     const float* p = a.stat + (row * a.parts + lane) * 3;
     s = Sums{p[0], p[1], p[2]};
   }
-  s = wave_sums(s, c);
+  s = lanes_sums<64>(s, c);
   if (lane == 0) write_row<T>(a, row, s);
   if (!a.k) return;
-  const uint64_t* mine = a.keys + (row * a.parts + lane) * a.k;
+  wave_exchange();
+  const uint64_t* mine = list + lane * a.k;
   int at = 0;
-  uint64_t head = lane < a.parts ? mine[0] : 0, next = lane < a.parts && a.k > 1 ? mine[1] : 0;
-  uint64_t out = 0;
+  uint64_t head = lane < a.parts ? mine[0] : 0, out = 0;
   for (int j = 0; j < a.k; ++j) {
-    const uint64_t top = wave_max64(head);
+    const uint32_t hi = uint32_t(head >> 32), most = wave_max(hi);
+    uint64_t first = __ballot(hi == most);
+    if (__popcll(first) > 1) {  // equal values: the earliest place
+      const uint32_t place = hi == most ? uint32_t(head) : 0u, earliest = wave_max(place);
+      first = __ballot(hi == most && place == earliest);
+    }
+    const int who = __builtin_ctzll(first);
+    const uint64_t top =
+        uint64_t(uint32_t(__builtin_amdgcn_readlane(int(hi), who))) << 32 |
+        uint32_t(__builtin_amdgcn_readlane(int(uint32_t(head)), who));
     if (lane == j) out = top;
-    if (head == top && top) {
-      head = next;
+    if (lane == who) {
       ++at;
-      next = at + 1 < a.k ? mine[at + 1] : 0;
+      head = at < a.k && lane < a.parts ? mine[at] : 0;
     }
   }
   if (lane < a.k) write_top(a, row, lane, out, s);
@@ -403,41 +477,48 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
 
 constexpr int64_t kMostTasks = int64_t(1) << 22;  // of a launch, in workgroups
 
-// Waves of a row: one for up to 2048 values.
-bool narrow(int64_t vocab) { return vocab <= 2048; }
-
-// Parts of a row: enough workgroups for the chip, of 2048 values at least, and with alternatives
-// of kPartLen at most.
+// Lanes of a row: 16 for up to 128 values without alternatives, a wave, or a workgroup. Parts of a row
+// of a workgroup's: enough workgroups for the chip, of 2048 values at least, and with alternatives of
+// kPartLen at most.
 struct LogprobPlan {
-  int parts, len;
+  int lanes, parts, len;
 };
 LogprobPlan plan(int64_t n, int64_t vocab, int k) {
-  if (narrow(vocab)) return {1, int(vocab)};
+  if (vocab <= 128 && !k) return {16, 1, int(vocab)};
+  if (vocab <= (n >= 4096 ? 8192 : 2048)) return {64, 1, int(vocab)};
   int64_t parts = std::min<int64_t>({ceil_div(2048, std::max<int64_t>(n, 1)), ceil_div(vocab, 2048), 64});
   if (k) parts = std::max(parts, ceil_div(vocab, kPartLen));
   const int64_t len = round_up(ceil_div(vocab, parts), 8);
-  return {int(ceil_div(vocab, len)), int(len)};
+  return {256, int(ceil_div(vocab, len)), int(len)};
 }
 
-template <typename T, int WAVES>
+template <typename T, int LANES, bool TOP>
 void launch_logprobs(LogprobArgs a, hipStream_t s) {
-  constexpr int kSub = 4 / WAVES;
+  constexpr int kSub = 256 / LANES;
   const int64_t rows = kMostTasks * kSub / a.parts;
-  const int list = a.k * int(ceil_div(a.part_len, 512 * WAVES)) * 8;
+  const int list = a.k * int(ceil_div(a.part_len, 8 * LANES)) * 8;
   for (; a.row0 < a.n; a.row0 += rows) {
     const int64_t now = std::min(a.n - a.row0, rows);
     LogprobArgs b = a;
     b.n = a.row0 + now;
-    const dim3 grid(unsigned(ceil_div(now * a.parts, kSub)));
-    if (a.k)
-      hipLaunchKernelGGL((k_logprobs<T, WAVES, true>), grid, dim3(256), size_t(list) * kSub * 8, s, b,
-                         list);
-    else
-      hipLaunchKernelGGL((k_logprobs<T, WAVES, false>), grid, dim3(256), 0, s, b, 0);
+    hipLaunchKernelGGL((k_logprobs<T, LANES, TOP>), dim3(unsigned(ceil_div(now * a.parts, kSub))),
+                       dim3(256), size_t(list) * kSub * 8, s, b, list);
     if (a.parts > 1)
-      hipLaunchKernelGGL(k_logprobs_join<T>, dim3(unsigned(ceil_div(now, 4))), dim3(256), 0, s, b);
+      hipLaunchKernelGGL(k_logprobs_join<T>, dim3(unsigned(ceil_div(now, 4))), dim3(256),
+                         size_t(a.parts) * size_t(a.k) * 32, s, b);
   }
 }
+template <typename T>
+void launch_logprobs(const LogprobArgs& a, int lanes, hipStream_t s) {
+  if (lanes == 16) launch_logprobs<T, 16, false>(a, s);
+  else if (lanes == 64 && a.k) launch_logprobs<T, 64, true>(a, s);
+  else if (lanes == 64) launch_logprobs<T, 64, false>(a, s);
+  else if (a.k) launch_logprobs<T, 256, true>(a, s);
+  else launch_logprobs<T, 256, false>(a, s);
+}
+
+// The gradient: a wave a row for up to 2048 values.
+bool narrow(int64_t vocab) { return vocab <= 2048; }
 
 template <typename T, int WAVES>
 void launch_grad(LogprobGradArgs a, hipStream_t s) {
@@ -476,13 +557,8 @@ optima_status token_logprobs(const void* X, int64_t ldx, int dtype, int64_t n, i
   float* stat = keys ? reinterpret_cast<float*>(keys + size_t(n) * p.parts * size_t(k)) : nullptr;
   LogprobArgs a{X, tokens, logp, lse, entropy, top_logp, top_index, stat, keys, ldx, n, 0,
                 int(vocab), int(k), p.parts, p.len, scale};
-  if (dtype == OPTIMA_DTYPE_BF16) {
-    if (narrow(vocab)) launch_logprobs<bf16_t, 1>(a, s);
-    else launch_logprobs<bf16_t, 4>(a, s);
-  } else {
-    if (narrow(vocab)) launch_logprobs<float, 1>(a, s);
-    else launch_logprobs<float, 4>(a, s);
-  }
+  if (dtype == OPTIMA_DTYPE_BF16) launch_logprobs<bf16_t>(a, p.lanes, s);
+  else launch_logprobs<float>(a, p.lanes, s);
   OPTIMA_LAUNCH_CHECK();
   return OPTIMA_OK;
 }
