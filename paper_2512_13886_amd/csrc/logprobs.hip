@@ -96,7 +96,7 @@ __device__ inline void rebase(Sums& a, float m, float c) {
   a.s *= r;
   a.m = m;
 }
-// Of the LANES (16 or 64) lanes of a row: all of them have m, the first one s and t.
+// Of the LANES (16 or 64) lanes of a row, in every lane (of 16, s and t in the first).
 template <int LANES>
 __device__ inline Sums lanes_sums(Sums a, float c) {
   float m = a.m;
@@ -173,57 +173,66 @@ constexpr int kGroups = 4;         // of eight values that a thread loads togeth
 constexpr int kTopSteps = 16;      // groups of a thread, at most, where alternatives are wanted
 constexpr int kPartLen = kTopSteps * 256 * 8;
 
-// The k best of the values `order` with their places that a wave's lanes hold W of (0: none), or
-// all if there are fewer: numbers lane + 64 w in `chosen`, and what an element has to reach, a value
-// and with that value the place of its group. A value that k of them reach is searched bit by bit;
-// only where more than k are equal to the last one places decide.
-template <int W>
-struct Choice {
-  int picked;
+// What reaches the k best of the values `order` with their places that a wave's lanes hold W of (0:
+// none): a value, and with that value a place that is not later. Searched from the highest bits on,
+// two at a time, until a value is reached by k of them; only where more than k reach the last one,
+// and so equal it, places decide. With no more than k of them 0 is reached by all.
+struct Border {
   uint32_t value, place;
-};
-template <int W>
-__device__ inline Choice<W> choose(const uint32_t (&order)[W], const uint32_t (&place)[W], int k,
-                                   int* chosen) {
-  auto count = [](auto of) {
-    int c = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) c += __popcll(__ballot(of(w)));
-    return c;
-  };
-  Choice<W> r{count([&](int w) { return order[w] > 0; }), 0u, ~0u};
-  if (r.picked > k) {
-    int reach = r.picked;
-    for (int bit = 31; bit >= 0 && reach != k; --bit) {
-      const uint32_t v = r.value | 1u << bit;
-      const int c = count([&](int w) { return order[w] >= v; });
-      if (c >= k) {
-        r.value = v;
-        reach = c;
-      }
-    }
-    if (reach > k) {
-      const int more = k - count([&](int w) { return order[w] > r.value; });
-      r.place = 0;
-      for (int bit = 20; bit >= 0; --bit) {  // places are below 2^20
-        const uint32_t below = r.place | ((1u << bit) - 1);
-        if (count([&](int w) { return order[w] == r.value && place[w] <= below; }) < more)
-          r.place |= 1u << bit;
-      }
-    }
-    r.picked = k;
+  __device__ inline bool reached(uint32_t order, uint32_t at) const {
+    return order > value || (order == value && at <= place);
   }
-  int at = 0;
-  const int lane = threadIdx.x & 63;
+};
+template <int W, typename F>
+__device__ inline int count_of(F of) {
+  int c = 0;
 #pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const bool in = order[w] > max(r.value, 1u) - 1u &&
-                    (order[w] != r.value || place[w] <= r.place);
-    const uint64_t mask = __ballot(in);
-    if (in) chosen[at + __popcll(mask & ((uint64_t(1) << lane) - 1))] = lane + 64 * w;
-    at += __popcll(mask);
+  for (int w = 0; w < W; ++w) c += __popcll(__ballot(of(w)));
+  return c;
+}
+template <int W>
+__device__ inline Border border_of(const uint32_t (&order)[W], const uint32_t (&place)[W], int k) {
+  Border r{0u, ~0u};
+  int reach = count_of<W>([&](int w) { return order[w] > 0; });
+  if (reach <= k) return r;
+  uint32_t most = 0, least = ~0u;
+#pragma unroll
+  for (int w = 0; w < W; ++w) most = max(most, order[w]), least = min(least, order[w] - 1);  // not of 0
+  most = wave_max(most);
+  least = ~wave_max(~least) + 1;
+  int bit = (31 - __builtin_clz((most ^ least) | 1)) & ~1;  // the highest that they differ in
+  r.value = most & ~((4u << bit) - 1);
+  for (; bit >= 0 && reach != k; bit -= 2) {
+    const uint32_t one = r.value | 1u << bit, two = r.value | 2u << bit, three = r.value | 3u << bit;
+    const int c1 = count_of<W>([&](int w) { return order[w] >= one; });
+    const int c2 = count_of<W>([&](int w) { return order[w] >= two; });
+    const int c3 = count_of<W>([&](int w) { return order[w] >= three; });
+    if (c3 >= k) r.value = three, reach = c3;
+    else if (c2 >= k) r.value = two, reach = c2;
+    else if (c1 >= k) r.value = one, reach = c1;
+  }
+  if (reach > k) {
+    const int more = k - count_of<W>([&](int w) { return order[w] > r.value; });
+    r.place = 0;
+    for (int bit = 20; bit >= 0; --bit) {  // places are at most 2^20
+      const uint32_t below = r.place | ((1u << bit) - 1);
+      if (count_of<W>([&](int w) { return order[w] == r.value && place[w] <= below; }) < more)
+        r.place |= 1u << bit;
+    }
   }
   return r;
+}
+
+// The first k of `count` different keys in LDS, by LANES threads: each counts what is larger.
+template <int LANES, typename F>
+__device__ inline void ranked(const uint64_t* list, int count, int k, int t, F out) {
+  for (int q = t; q < count; q += LANES) {
+    const uint64_t key = list[q];
+    int rank = 0;
+#pragma unroll 4
+    for (int r = 0; r < count; ++r) rank += list[r] > key;
+    if (rank < k) out(rank, key);
+  }
 }
 
 // A part of a row by LANES lanes (256: a workgroup; 64 and 16: more rows a workgroup).
@@ -232,9 +241,9 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
   static_assert(!TOP || LANES >= 64, "alternatives are chosen by waves");
   constexpr int kStep = 8 * LANES, kSub = 256 / LANES, kWaves = LANES > 64 ? LANES / 64 : 1;
   __shared__ float red[kWaves][3];
-  __shared__ uint32_t best_of[TOP ? 256 : 1], base_of[TOP ? 256 : 1];
-  __shared__ int chosen[TOP ? kSub : 1][OPTIMA_TOP_MAX];
-  __shared__ uint32_t border[kSub][2];
+  __shared__ uint32_t best_of[TOP && LANES > 64 ? 256 : 1], base_of[TOP && LANES > 64 ? 256 : 1];
+  __shared__ int chosen[kSub][OPTIMA_TOP_MAX];
+  __shared__ Border borders[kSub];
   __shared__ int found[kSub], picked[kSub];
   extern __shared__ uint64_t lists[];
   const int sub = threadIdx.x / LANES, t = threadIdx.x % LANES;
@@ -323,10 +332,10 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
     }
   }
   if constexpr (TOP) {
-    const uint32_t mine = 8 * t < len ? order_of(best) : 0u;
+    const uint32_t mine = 8 * t < len ? order_of(best) : 0u, from = uint32_t(p0 + base);
     if constexpr (LANES > 64) {
       best_of[t] = mine;
-      base_of[t] = uint32_t(p0 + base);
+      base_of[t] = from;
       __syncthreads();
     }
     if (t < 64) {
@@ -334,94 +343,101 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         order[w] = LANES > 64 ? best_of[t + 64 * w] : mine;
-        place[w] = LANES > 64 ? base_of[t + 64 * w] : uint32_t(p0 + base);
+        place[w] = LANES > 64 ? base_of[t + 64 * w] : from;
       }
-      const Choice<kWaves> r = choose(order, place, a.k, chosen[sub]);
+      const Border r = border_of(order, place, a.k);
+      int at = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const bool in = order[w] > 0 && r.reached(order[w], place[w]);
+        const uint64_t mask = __ballot(in);
+        if (in) chosen[sub][at + __popcll(mask & ((uint64_t(1) << t) - 1))] = t + 64 * w;
+        at += __popcll(mask);
+      }
       if (t == 0) {
         found[sub] = 0;
-        picked[sub] = r.picked;
-        border[sub][0] = r.value;
-        border[sub][1] = r.place;
+        picked[sub] = at;
+        borders[sub] = r;
       }
     }
     group_sync<LANES>();
-    const uint32_t limit_value = border[sub][0], limit_place = border[sub][1];
-    const int steps = (len + kStep - 1) / kStep;
+    const Border limit = borders[sub];
     uint64_t* list = lists + sub * list_len;
-    const int tasks = picked[sub] * steps;
+    const int steps = (len + kStep - 1) / kStep, tasks = picked[sub] * steps;
     for (int q = t; q < tasks; q += LANES) {
       const int j = q / steps, g = 8 * chosen[sub][j] + (q - j * steps) * kStep;
       if (g >= len) continue;
-      Raw8<T> raw;
-      load_piece(raw, x, g, len);
+      Raw8<T> r;
+      load_piece(r, x, g, len);
       float v[8];
-      values8(raw, v);
+      values8(r, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t o = order_of(v[e]);
-        if (g + e < len && (o > limit_value || (o == limit_value && uint32_t(p0 + g) <= limit_place)))
+        if (g + e < len && limit.reached(o, uint32_t(p0 + g)))
           list[atomicAdd(&found[sub], 1)] = uint64_t(o) << 32 | uint32_t(~uint32_t(p0 + g + e));
       }
     }
     group_sync<LANES>();
     const int count = found[sub];
     uint64_t* to = a.keys + (row * a.parts + part) * a.k;
-    for (int q = t; q < count; q += LANES) {
-      const uint64_t key = list[q];
-      int rank = 0;
-      for (int r = 0; r < count; ++r) rank += list[r] > key;
-      if (rank >= a.k) continue;
+    ranked<LANES>(list, count, a.k, t, [&](int rank, uint64_t key) {
       if (a.parts == 1)
         write_top(a, row, rank, key, s);
       else
         to[rank] = key;
-    }
+    });
     if (a.parts > 1)
       for (int q = count + t; q < a.k; q += LANES) to[q] = 0;
   }
 }
 
-// The parts of a row, by one wave: lane p has part p, whose keys lie in LDS.
-template <typename T>
+// The parts of a row, by LANES threads (64 or 256): lane p of each wave has the sums of part p and
+// the first of its keys. Of all keys those that reach the k best of the parts' first are ranked. The
+// keys come from other XCDs, so that all loads of a thread go out together.
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
+  constexpr int kSub = 256 / LANES, kEach = LANES > 64 ? 8 : 4;
   extern __shared__ uint64_t lists[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = a.row0 + int64_t(blockIdx.x) * 4 + wave;
+  __shared__ int found[kSub];
+  const int sub = threadIdx.x / LANES, t = threadIdx.x % LANES, lane = threadIdx.x & 63;
+  const int64_t row = a.row0 + int64_t(blockIdx.x) * kSub + sub;
   if (row >= a.n) return;
   const float c = a.scale * kLog2e;
   const int keys = a.parts * a.k;
-  uint64_t* list = lists + wave * keys;
-  for (int q = lane; q < keys; q += 64) list[q] = a.keys[row * keys + q];
+  const uint64_t* all = a.keys + row * keys;
+  uint64_t key[kEach] = {}, first = 0;
+  if (a.k)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (t + i * LANES < keys) key[i] = all[t + i * LANES];
   Sums s = {-__builtin_inff(), 0.f, 0.f};
   if (lane < a.parts) {
     const float* p = a.stat + (row * a.parts + lane) * 3;
     s = Sums{p[0], p[1], p[2]};
+    if (a.k) first = all[lane * a.k];
   }
+  if (t == 0) found[sub] = 0;
   s = lanes_sums<64>(s, c);
-  if (lane == 0) write_row<T>(a, row, s);
+  if (t == 0) write_row<T>(a, row, s);
   if (!a.k) return;
-  wave_exchange();
-  const uint64_t* mine = list + lane * a.k;
-  int at = 0;
-  uint64_t head = lane < a.parts ? mine[0] : 0, out = 0;
-  for (int j = 0; j < a.k; ++j) {
-    const uint32_t hi = uint32_t(head >> 32), most = wave_max(hi);
-    uint64_t first = __ballot(hi == most);
-    if (__popcll(first) > 1) {  // equal values: the earliest place
-      const uint32_t place = hi == most ? uint32_t(head) : 0u, earliest = wave_max(place);
-      first = __ballot(hi == most && place == earliest);
-    }
-    const int who = __builtin_ctzll(first);
-    const uint64_t top =
-        uint64_t(uint32_t(__builtin_amdgcn_readlane(int(hi), who))) << 32 |
-        uint32_t(__builtin_amdgcn_readlane(int(uint32_t(head)), who));
-    if (lane == j) out = top;
-    if (lane == who) {
-      ++at;
-      head = at < a.k && lane < a.parts ? mine[at] : 0;
-    }
+  const uint32_t order[1] = {uint32_t(first >> 32)}, place[1] = {~uint32_t(first)};
+  const Border limit = border_of(order, place, a.k);
+  group_sync<LANES>();
+  uint64_t* list = lists + sub * keys;
+  for (int q = 0;;) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (key[i] && limit.reached(uint32_t(key[i] >> 32), ~uint32_t(key[i])))
+        list[atomicAdd(&found[sub], 1)] = key[i];
+    q += kEach * LANES;
+    if (q >= keys) break;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) key[i] = q + t + i * LANES < keys ? all[q + t + i * LANES] : 0;
   }
-  if (lane < a.k) write_top(a, row, lane, out, s);
+  group_sync<LANES>();
+  ranked<LANES>(list, found[sub], a.k, t,
+                [&](int rank, uint64_t best) { write_top(a, row, rank, best, s); });
 }
 
 struct LogprobGradArgs {
@@ -503,9 +519,12 @@ void launch_logprobs(LogprobArgs a, hipStream_t s) {
     b.n = a.row0 + now;
     hipLaunchKernelGGL((k_logprobs<T, LANES, TOP>), dim3(unsigned(ceil_div(now * a.parts, kSub))),
                        dim3(256), size_t(list) * kSub * 8, s, b, list);
-    if (a.parts > 1)
-      hipLaunchKernelGGL(k_logprobs_join<T>, dim3(unsigned(ceil_div(now, 4))), dim3(256),
-                         size_t(a.parts) * size_t(a.k) * 32, s, b);
+    const size_t keys = size_t(a.parts) * size_t(a.k) * 8;
+    if (a.parts > 1 && keys > 2048)
+      hipLaunchKernelGGL((k_logprobs_join<T, 256>), dim3(unsigned(now)), dim3(256), keys, s, b);
+    else if (a.parts > 1)
+      hipLaunchKernelGGL((k_logprobs_join<T, 64>), dim3(unsigned(ceil_div(now, 4))), dim3(256), 4 * keys,
+                         s, b);
   }
 }
 template <typename T>
