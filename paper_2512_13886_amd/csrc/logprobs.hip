@@ -235,6 +235,14 @@ __device__ inline void ranked(const uint64_t* list, int count, int k, int t, F o
   }
 }
 
+// Which of a workgroup's rows a thread has: the same for a wave of 64 or more, and known to be.
+template <int LANES>
+__device__ inline int row_of_thread() {
+  if constexpr (LANES >= 256) return 0;
+  const int sub = threadIdx.x / LANES;
+  return LANES == 64 ? __builtin_amdgcn_readfirstlane(sub) : sub;
+}
+
 // A part of a row by LANES lanes (256: a workgroup; 64 and 16: more rows a workgroup).
 template <typename T, int LANES, bool TOP>
 __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
@@ -246,11 +254,11 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
   __shared__ Border borders[kSub];
   __shared__ int found[kSub], picked[kSub];
   extern __shared__ uint64_t lists[];
-  const int sub = threadIdx.x / LANES, t = threadIdx.x % LANES;
-  const int64_t task = int64_t(blockIdx.x) * kSub + sub;
-  const int64_t row = a.row0 + task / a.parts;
+  const int sub = row_of_thread<LANES>(), t = threadIdx.x % LANES;
+  const uint32_t task = blockIdx.x * kSub + sub, parts = a.parts;
+  const int64_t row = a.row0 + task / parts;
   if (row >= a.n) return;  // all threads of the row
-  const int part = int(task % a.parts), p0 = part * a.part_len;
+  const int part = int(task % parts), p0 = part * a.part_len;
   const int len = std::min(a.part_len, a.vocab - p0);
   const T* x = static_cast<const T*>(a.x) + row * a.ldx + p0;
   const float c = a.scale * kLog2e;
@@ -400,7 +408,7 @@ __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
   constexpr int kSub = 256 / LANES, kEach = LANES > 64 ? 8 : 4;
   extern __shared__ uint64_t lists[];
   __shared__ int found[kSub];
-  const int sub = threadIdx.x / LANES, t = threadIdx.x % LANES, lane = threadIdx.x & 63;
+  const int sub = row_of_thread<LANES>(), t = threadIdx.x % LANES, lane = threadIdx.x & 63;
   const int64_t row = a.row0 + int64_t(blockIdx.x) * kSub + sub;
   if (row >= a.n) return;
   const float c = a.scale * kLog2e;
@@ -451,14 +459,14 @@ struct LogprobGradArgs {
 };
 
 // dx = scale (g at the token + p (dlse - g - dH (ln p + H))), p = exp(z - lse). Bound by HBM.
-template <typename T, int WAVES>
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
-  constexpr int kThr = 64 * WAVES, kStep = 8 * kThr, kSub = 4 / WAVES;
-  const int sub = WAVES > 1 ? 0 : threadIdx.x >> 6, t = threadIdx.x & (kThr - 1);
-  const int64_t task = int64_t(blockIdx.x) * kSub + sub;
-  const int64_t row = a.row0 + task / a.parts;
+  constexpr int kStep = 8 * LANES, kSub = 256 / LANES;
+  const int sub = row_of_thread<LANES>(), t = threadIdx.x % LANES;
+  const uint32_t task = blockIdx.x * kSub + sub, parts = a.parts;
+  const int64_t row = a.row0 + task / parts;
   if (row >= a.n) return;
-  const int at0 = int(task % a.parts) * kGroups * kStep + 8 * t;
+  const int at0 = int(task % parts) * kGroups * kStep + 8 * t;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   T* dx = static_cast<T*>(a.dx) + row * a.lddx;
   const float lse = a.lse[row];
@@ -472,7 +480,8 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
   const bool none = lse < -1e30f;
   Raw8<T> raw[kGroups];
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u) load_piece(raw[u], x, at0 + u * kStep, a.vocab);
+  for (int u = 0; u < kGroups; ++u)
+    if (at0 - 8 * t + u * kStep < a.vocab) load_piece(raw[u], x, at0 + u * kStep, a.vocab);
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
     const int at = at0 + u * kStep;
@@ -536,20 +545,24 @@ void launch_logprobs(const LogprobArgs& a, int lanes, hipStream_t s) {
   else launch_logprobs<T, 256, false>(a, s);
 }
 
-// The gradient: a wave a row for up to 2048 values.
-bool narrow(int64_t vocab) { return vocab <= 2048; }
-
-template <typename T, int WAVES>
+template <typename T, int LANES>
 void launch_grad(LogprobGradArgs a, hipStream_t s) {
-  constexpr int kSub = 4 / WAVES;
-  a.parts = int(ceil_div(a.vocab, kGroups * 512 * WAVES));
+  constexpr int kSub = 256 / LANES;
+  a.parts = int(ceil_div(a.vocab, kGroups * 8 * LANES));
   const int64_t rows = std::max<int64_t>(1, kMostTasks * kSub / a.parts);
   for (; a.row0 < a.n; a.row0 += rows) {
     LogprobGradArgs b = a;
     b.n = std::min(a.n, a.row0 + rows);
-    hipLaunchKernelGGL((k_logprobs_grad<T, WAVES>),
+    hipLaunchKernelGGL((k_logprobs_grad<T, LANES>),
                        dim3(unsigned(ceil_div((b.n - a.row0) * a.parts, kSub))), dim3(256), 0, s, b);
   }
+}
+// The gradient's lanes of a row.
+template <typename T>
+void launch_grad(const LogprobGradArgs& a, hipStream_t s) {
+  if (a.vocab <= 256) launch_grad<T, 16>(a, s);
+  else if (a.vocab <= 2048) launch_grad<T, 64>(a, s);
+  else launch_grad<T, 256>(a, s);
 }
 
 }  // namespace
@@ -589,13 +602,8 @@ optima_status token_logprobs_backward(const void* X, int64_t ldx, int dtype, int
                                       int64_t lddx, hipStream_t s) {
   LogprobGradArgs a{X, tokens, lse, entropy, dlogp, dentropy, dlse, dX, ldx, lddx, n, 0,
                     int(vocab), 0, scale};
-  if (dtype == OPTIMA_DTYPE_BF16) {
-    if (narrow(vocab)) launch_grad<bf16_t, 1>(a, s);
-    else launch_grad<bf16_t, 4>(a, s);
-  } else {
-    if (narrow(vocab)) launch_grad<float, 1>(a, s);
-    else launch_grad<float, 4>(a, s);
-  }
+  if (dtype == OPTIMA_DTYPE_BF16) launch_grad<bf16_t>(a, s);
+  else launch_grad<float>(a, s);
   OPTIMA_LAUNCH_CHECK();
   return OPTIMA_OK;
 }

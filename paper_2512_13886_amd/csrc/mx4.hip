@@ -43,13 +43,13 @@ __device__ inline uint32_t quad_max(uint32_t m) {
 
 // Thirty-two lanes for 256 values, one dword (eight codes) each.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, int64_t total,
-                                                       int pieces, int d, uint8_t* Q,
+__global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, uint32_t total,
+                                                       uint32_t pieces, int d, uint8_t* Q,
                                                        uint8_t* scales, int srow) {
-  const int64_t idx = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t idx = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   const bool live = idx < total;  // of all 32 lanes
-  const int64_t n = live ? idx / pieces : 0;
-  const int h = live ? int(idx - n * pieces) : 0;
+  const int64_t n = live ? idx / pieces : 0u;
+  const int h = live ? int(idx % pieces) : 0;
   const int i = threadIdx.x & 31;
   Raw8<T> raw;
   load_piece(raw, X + n * ldx, 256 * h + 8 * i, live ? d : 0);
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, 
   *reinterpret_cast<uint32_t*>(Q + (n * pieces + h) * 128 + 4 * i) = q;
   if (i < 16 && (i & 3) == 0) {
     uint8_t* at = scales + n * srow + 16 * (h >> 1) + i + 2 * (h & 1);
-    if ((h & 1) == 0 && h + 1 == pieces)  // the row's padding
+    if ((h & 1) == 0 && h + 1 == int(pieces))  // the row's padding
       *reinterpret_cast<uint32_t*>(at) = both;
     else
       *reinterpret_cast<uint16_t*>(at) = uint16_t(both);
@@ -87,12 +87,12 @@ __global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, 
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_mx4_unpack(const uint8_t* Q, const uint8_t* scales,
-                                                         int srow, int64_t total, int pieces,
+                                                         int srow, uint32_t total, uint32_t pieces,
                                                          int d, T* Y, int64_t ldy) {
-  const int64_t idx = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t idx = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   if (idx >= total) return;
   const int64_t n = idx / pieces;
-  const int h = int(idx - n * pieces);
+  const int h = int(idx % pieces);
   const int i = threadIdx.x & 31, k = 256 * h + 8 * i;
   if (k >= d) return;
   const uint32_t q = *reinterpret_cast<const uint32_t*>(Q + (n * pieces + h) * 128 + 4 * i);
@@ -651,8 +651,8 @@ size_t mx4_scale_bytes(int64_t d) { return size_t(scale_bytes(d)); }
 
 optima_status mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t d, void* Q,
                        void* scales, hipStream_t s) {
-  const int pieces = int(ceil_div(d, 256)), srow = int(scale_bytes(d));
-  const int64_t total = n * pieces;
+  const uint32_t pieces = uint32_t(ceil_div(d, 256)), total = uint32_t(n * pieces);  // below 2^27
+  const int srow = int(scale_bytes(d));
   const dim3 grid(unsigned(ceil_div(total, kThreads / 32)));
   uint8_t *q = static_cast<uint8_t*>(Q), *sc = static_cast<uint8_t*>(scales);
   if (dtype == OPTIMA_DTYPE_BF16)
@@ -667,8 +667,8 @@ optima_status mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t
 
 optima_status mx4_unpack(const void* Q, const void* scales, int64_t n, int64_t d, void* Y,
                          int64_t ldy, int dtype, hipStream_t s) {
-  const int pieces = int(ceil_div(d, 256)), srow = int(scale_bytes(d));
-  const int64_t total = n * pieces;
+  const uint32_t pieces = uint32_t(ceil_div(d, 256)), total = uint32_t(n * pieces);  // below 2^27
+  const int srow = int(scale_bytes(d));
   const dim3 grid(unsigned(ceil_div(total, kThreads / 32)));
   const uint8_t *q = static_cast<const uint8_t*>(Q), *sc = static_cast<const uint8_t*>(scales);
   if (dtype == OPTIMA_DTYPE_BF16)
