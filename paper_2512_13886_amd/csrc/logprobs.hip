@@ -173,52 +173,64 @@ constexpr int kGroups = 4;         // of eight values that a thread loads togeth
 constexpr int kTopSteps = 16;      // groups of a thread, at most, where alternatives are wanted
 constexpr int kPartLen = kTopSteps * 256 * 8;
 
-// What reaches the k best of the values `order` with their places that a wave's lanes hold W of (0:
-// none): a value, and with that value a place that is not later. Searched from the highest bits on,
-// two at a time, until a value is reached by k of them; only where more than k reach the last one,
-// and so equal it, places decide. With no more than k of them 0 is reached by all.
+// How many of a wave's values, W a lane, are v or more.
+template <int W>
+__device__ inline int count_from(const uint32_t (&value)[W], uint32_t v) {
+  int c = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(value[w] >= v));
+  return c;
+}
+// A v that `need` of the values are or exceed, and no more unless they equal the last of them: its bits
+// from `bit` (even) down to LOW, two at a time; `from` has those above. reach: how many reach v.
+template <int LOW, int W>
+__device__ inline uint32_t reached_by(const uint32_t (&value)[W], int need, uint32_t from, int bit,
+                                      int& reach) {
+  for (; bit >= LOW && reach != need; bit -= 2) {
+    const int c1 = count_from(value, from | 1u << bit), c2 = count_from(value, from | 2u << bit);
+    const int c3 = count_from(value, from | 3u << bit);
+    const int more = (c1 >= need) + (c2 >= need) + (c3 >= need);
+    from |= uint32_t(more) << bit;
+    reach = more == 3 ? c3 : more == 2 ? c2 : more == 1 ? c1 : reach;
+  }
+  return from;
+}
+
+// What reaches the k best of the values `order` (0: none; LOW zero bits or as many ones in all of
+// them) with their different places below 2^place_bits (even): a value, and with that value a place
+// that is not later. With no more than k of them 0 is reached by all.
 struct Border {
   uint32_t value, place;
   __device__ inline bool reached(uint32_t order, uint32_t at) const {
     return order > value || (order == value && at <= place);
   }
 };
-template <int W, typename F>
-__device__ inline int count_of(F of) {
-  int c = 0;
-#pragma unroll
-  for (int w = 0; w < W; ++w) c += __popcll(__ballot(of(w)));
-  return c;
-}
-template <int W>
-__device__ inline Border border_of(const uint32_t (&order)[W], const uint32_t (&place)[W], int k) {
+template <int LOW, int W>
+__device__ inline Border border_of(const uint32_t (&order)[W], const uint32_t (&place)[W], int k,
+                                   int place_bits) {
   Border r{0u, ~0u};
-  int reach = count_of<W>([&](int w) { return order[w] > 0; });
+  int reach = count_from(order, 1u);
   if (reach <= k) return r;
   uint32_t most = 0, least = ~0u;
 #pragma unroll
   for (int w = 0; w < W; ++w) most = max(most, order[w]), least = min(least, order[w] - 1);  // not of 0
   most = wave_max(most);
   least = ~wave_max(~least) + 1;
-  int bit = (31 - __builtin_clz((most ^ least) | 1)) & ~1;  // the highest that they differ in
-  r.value = most & ~((4u << bit) - 1);
-  for (; bit >= 0 && reach != k; bit -= 2) {
-    const uint32_t one = r.value | 1u << bit, two = r.value | 2u << bit, three = r.value | 3u << bit;
-    const int c1 = count_of<W>([&](int w) { return order[w] >= one; });
-    const int c2 = count_of<W>([&](int w) { return order[w] >= two; });
-    const int c3 = count_of<W>([&](int w) { return order[w] >= three; });
-    if (c3 >= k) r.value = three, reach = c3;
-    else if (c2 >= k) r.value = two, reach = c2;
-    else if (c1 >= k) r.value = one, reach = c1;
-  }
-  if (reach > k) {
-    const int more = k - count_of<W>([&](int w) { return order[w] > r.value; });
-    r.place = 0;
-    for (int bit = 20; bit >= 0; --bit) {  // places are at most 2^20
-      const uint32_t below = r.place | ((1u << bit) - 1);
-      if (count_of<W>([&](int w) { return order[w] == r.value && place[w] <= below; }) < more)
-        r.place |= 1u << bit;
+  const int bit = (31 - __builtin_clz((most ^ least) | 1)) & ~1;  // the highest that they differ in
+  r.value = reached_by<LOW>(order, k, most & ~((4u << bit) - 1), bit, reach);
+  if (LOW > 0 && !(r.value >> 31)) r.value |= (1u << LOW) - 1;  // a negative value's low bits
+  if (reach > k) {  // equal ones: the earliest of them
+    uint32_t equal[W];
+    int above = 0;
+    reach = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const bool is = order[w] == r.value;
+      equal[w] = is ? (1u << place_bits) - place[w] : 0u;
+      above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(!is && order[w] > r.value));
+      reach += __builtin_popcountll(__builtin_amdgcn_ballot_w64(is));
     }
+    r.place = (1u << place_bits) - reached_by<0>(equal, k - above, 0u, place_bits, reach);
   }
   return r;
 }
@@ -248,6 +260,7 @@ template <typename T, int LANES, bool TOP>
 __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
   static_assert(!TOP || LANES >= 64, "alternatives are chosen by waves");
   constexpr int kStep = 8 * LANES, kSub = 256 / LANES, kWaves = LANES > 64 ? LANES / 64 : 1;
+  constexpr int kLow = sizeof(T) == 2 ? 16 : 0;
   __shared__ float red[kWaves][3];
   __shared__ uint32_t best_of[TOP && LANES > 64 ? 256 : 1], base_of[TOP && LANES > 64 ? 256 : 1];
   __shared__ int chosen[kSub][OPTIMA_TOP_MAX];
@@ -340,7 +353,7 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
     }
   }
   if constexpr (TOP) {
-    const uint32_t mine = 8 * t < len ? order_of(best) : 0u, from = uint32_t(p0 + base);
+    const uint32_t mine = 8 * t < len ? order_of(best) : 0u, from = uint32_t(base) >> 3;
     if constexpr (LANES > 64) {
       best_of[t] = mine;
       base_of[t] = from;
@@ -353,12 +366,13 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
         order[w] = LANES > 64 ? best_of[t + 64 * w] : mine;
         place[w] = LANES > 64 ? base_of[t + 64 * w] : from;
       }
-      const Border r = border_of(order, place, a.k);
+      const Border r = border_of<kLow>(order, place, a.k, 12);
+      static_assert(kPartLen / 8 <= 4096, "places of groups");
       int at = 0;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const bool in = order[w] > 0 && r.reached(order[w], place[w]);
-        const uint64_t mask = __ballot(in);
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(in);
         if (in) chosen[sub][at + __popcll(mask & ((uint64_t(1) << t) - 1))] = t + 64 * w;
         at += __popcll(mask);
       }
@@ -382,7 +396,7 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t o = order_of(v[e]);
-        if (g + e < len && limit.reached(o, uint32_t(p0 + g)))
+        if (g + e < len && limit.reached(o, uint32_t(g) >> 3))
           list[atomicAdd(&found[sub], 1)] = uint64_t(o) << 32 | uint32_t(~uint32_t(p0 + g + e));
       }
     }
@@ -405,7 +419,7 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
 // keys come from other XCDs, so that all loads of a thread go out together.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
-  constexpr int kSub = 256 / LANES, kEach = LANES > 64 ? 8 : 4;
+  constexpr int kSub = 256 / LANES, kEach = LANES > 64 ? 8 : 4, kLow = sizeof(T) == 2 ? 16 : 0;
   extern __shared__ uint64_t lists[];
   __shared__ int found[kSub];
   const int sub = row_of_thread<LANES>(), t = threadIdx.x % LANES, lane = threadIdx.x & 63;
@@ -430,7 +444,7 @@ __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
   if (t == 0) write_row<T>(a, row, s);
   if (!a.k) return;
   const uint32_t order[1] = {uint32_t(first >> 32)}, place[1] = {~uint32_t(first)};
-  const Border limit = border_of(order, place, a.k);
+  const Border limit = border_of<kLow>(order, place, a.k, 20);
   group_sync<LANES>();
   uint64_t* list = lists + sub * keys;
   for (int q = 0;;) {
