@@ -415,7 +415,8 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
 }
 
 // The parts of a row, by LANES threads (64 or 256): lane p of each wave has the sums of part p and
-// the first of its keys. Of all keys those that reach the k best of the parts' first are ranked. The
+// the m-th of its keys, which are sorted: m keys of k / m parts reach the k / m best of these (both
+// rounded up). Of all keys those that do are ranked; m is such that half of the parts do, not all. The
 // keys come from other XCDs, so that all loads of a thread go out together.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
@@ -428,7 +429,8 @@ __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
   const float c = a.scale * kLog2e;
   const int keys = a.parts * a.k;
   const uint64_t* all = a.keys + row * keys;
-  uint64_t key[kEach] = {}, first = 0;
+  uint64_t key[kEach] = {}, mth = 0;
+  const int m = a.k ? std::min((2 * a.k + a.parts - 1) / a.parts, a.k) : 1;
   if (a.k)
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
@@ -437,14 +439,14 @@ __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
   if (lane < a.parts) {
     const float* p = a.stat + (row * a.parts + lane) * 3;
     s = Sums{p[0], p[1], p[2]};
-    if (a.k) first = all[lane * a.k];
+    if (a.k) mth = all[lane * a.k + m - 1];
   }
   if (t == 0) found[sub] = 0;
   s = lanes_sums<64>(s, c);
   if (t == 0) write_row<T>(a, row, s);
   if (!a.k) return;
-  const uint32_t order[1] = {uint32_t(first >> 32)}, place[1] = {~uint32_t(first)};
-  const Border limit = border_of<kLow>(order, place, a.k, 20);
+  const uint32_t order[1] = {uint32_t(mth >> 32)}, place[1] = {~uint32_t(mth)};
+  const Border limit = border_of<kLow>(order, place, (a.k + m - 1) / m, 20);
   group_sync<LANES>();
   uint64_t* list = lists + sub * keys;
   for (int q = 0;;) {
@@ -516,18 +518,24 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
 
 constexpr int64_t kMostTasks = int64_t(1) << 22;  // of a launch, in workgroups
 
-// Lanes of a row: 16 for up to 128 values without alternatives, a wave, or a workgroup. Parts of a row
-// of a workgroup's: enough workgroups for the chip, of 2048 values at least, and with alternatives of
-// kPartLen at most.
+// Lanes of a row: 16 for up to 128 values without alternatives, a wave, or a workgroup.
+//
+// Parts of a workgroup's row: for few rows as many as give every second CU a workgroup, of 8192
+// values at least, since the join is a launch (one row of 128000 14.6 us in one part, 6.6 in 15; 100
+// of 9000 with 5 alternatives 9 and 13 in two); of 16384 where the last rows would otherwise leave CUs
+// idle for long (8192 rows of 128000 420 us in one, 374 in eight); and of kPartLen at most with
+// alternatives, whose list is kept for a part.
 struct LogprobPlan {
   int lanes, parts, len;
 };
+constexpr int64_t kFewRows = 512, kFewLen = 8192, kManyValues = int64_t(1) << 29, kManyLen = 16384;
 LogprobPlan plan(int64_t n, int64_t vocab, int k) {
   if (vocab <= 128 && !k) return {16, 1, int(vocab)};
   if (vocab <= (n >= 4096 ? 8192 : 2048)) return {64, 1, int(vocab)};
-  int64_t parts = std::min<int64_t>({ceil_div(2048, std::max<int64_t>(n, 1)), ceil_div(vocab, 2048), 64});
+  int64_t parts = std::min<int64_t>({kFewRows / std::max<int64_t>(n, 1), vocab / kFewLen, 64});
+  if (n * vocab >= kManyValues) parts = std::max(parts, vocab / kManyLen);
   if (k) parts = std::max(parts, ceil_div(vocab, kPartLen));
-  const int64_t len = round_up(ceil_div(vocab, parts), 8);
+  const int64_t len = round_up(ceil_div(vocab, std::max<int64_t>(parts, 1)), 8);
   return {256, int(ceil_div(vocab, len)), int(len)};
 }
 
@@ -582,16 +590,12 @@ void launch_grad(const LogprobGradArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t token_logprobs_workspace_bytes(int64_t n, int64_t vocab, int64_t k) {
-  // The most of any number of rows up to these, so that more need no less.
-  size_t most = 0;
-  auto of = [&](int64_t rows) {
-    const LogprobPlan p = plan(rows, vocab, int(k));
-    if (p.parts > 1) most = std::max(most, size_t(rows) * p.parts * size_t(12 + 8 * k));
-  };
-  for (int64_t parts = 2; parts <= 64; ++parts)  // the last rows of each number of parts
-    of(std::min<int64_t>(n, (2048 - 1) / (parts - 1)));
-  of(n);
-  return most;
+  // The parts of any number of rows up to these, so that more need no less.
+  int64_t parts = std::min(n, kFewRows) * (vocab / kFewLen);
+  parts = std::min(parts, kFewRows);
+  if (n * vocab >= kManyValues) parts = std::max(parts, n * (vocab / kManyLen));
+  if (k && vocab > kPartLen) parts = std::max(parts, n * ceil_div(vocab, kPartLen));
+  return size_t(parts) * size_t(12 + 8 * k);
 }
 
 optima_status token_logprobs(const void* X, int64_t ldx, int dtype, int64_t n, int64_t vocab,

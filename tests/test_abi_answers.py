@@ -118,8 +118,8 @@ def test_row_sizes(lib):
 
 
 def _logprobs(lib, **kw):
-    """optima_token_logprobs of 10 rows of 5000 bf16 logits, with changes."""
-    a = dict(X=1 * MB, ldx=5000, dtype=BF16, n=10, vocab=5000, tokens=2 * MB, scale=1.0,
+    """optima_token_logprobs of 10 rows of 20000 bf16 logits, with changes."""
+    a = dict(X=1 * MB, ldx=20000, dtype=BF16, n=10, vocab=20000, tokens=2 * MB, scale=1.0,
              logp=3 * MB, lse=4 * MB, entropy=5 * MB, k=4, index=6 * MB, top=7 * MB, ws=8 * MB,
              nbytes=MB)
     a.update(kw)
@@ -130,7 +130,7 @@ def _logprobs(lib, **kw):
 
 @pytest.mark.parametrize("change, status", [
     (dict(X=None), INVAL), (dict(tokens=None), INVAL), (dict(n=-1), INVAL), (dict(vocab=0), INVAL),
-    (dict(vocab=(1 << 20) + 1, ldx=1 << 21), INVAL), (dict(ldx=4999), INVAL),
+    (dict(vocab=(1 << 20) + 1, ldx=1 << 21), INVAL), (dict(ldx=19999), INVAL),
     (dict(dtype=I8), UNSUPPORTED), (dict(scale=0.0), INVAL), (dict(scale=-1.0), INVAL),
     (dict(scale=float("nan")), INVAL), (dict(scale=float("inf")), INVAL), (dict(k=-1), INVAL),
     (dict(k=33), UNSUPPORTED), (dict(k=0), INVAL), (dict(k=4, index=None, top=None), INVAL),
@@ -149,7 +149,7 @@ def test_logprobs_refusals(lib, change, status):
 def test_logprobs_workspace(lib):
     f = _sizes(lib).optima_token_logprobs_workspace_bytes
     f.argtypes = [i64, i64, i64]
-    assert f(1, 2048, 8) == 0 and f(1, 2049, 0) > 0
+    assert f(1, 8000, 8) == 0 and f(1, 20000, 0) > 0
     for vocab in (100, 2049, 5000, 32768, 50001, 128000, 1 << 20):
         for k in (0, 1, 32):
             last = 0
