@@ -8,6 +8,7 @@ importing this module without it raises, there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass, fields
 
@@ -754,8 +755,15 @@ def optima_w4_gated(X: torch.Tensor, Qg: torch.Tensor, scales_g: torch.Tensor, Q
                      nbytes, _launch_stream(stream)))
 
 
+@functools.lru_cache(maxsize=None)
+def _devices() -> int:
+    return torch.cuda.device_count()
+
+
 def _need_one_device(stream, *tensors):
     """A call launches on the current device, or its stream's: all its tensors are there."""
+    if _devices() < 2:
+        return
     at = _current_device() if stream is None else stream.device.index
     for t in tensors:
         if t is not None and t.is_cuda and t.get_device() != at:
@@ -771,12 +779,16 @@ def optima_mx4_scale_bytes(d: int) -> int:
 
 
 def _mx4_codes(q_name, Q, s_name, scales, n, d):
+    if Q.dtype == scales.dtype == torch.uint8 and Q.is_cuda and scales.is_cuda and \
+            Q.is_contiguous() and scales.is_contiguous() and \
+            Q.shape == (n, (d + 255) // 256 * 128) and scales.shape == (n, (d + 511) // 512 * 16):
+        return
     _need_shape(q_name, Q, (n, -(-d // 256) * 128), (torch.uint8,))
     _need_shape(s_name, scales, (n, -(-d // 512) * 16), (torch.uint8,))
 
 
 def _mx4_addr(t):
-    return t.data_ptr() if t.shape[0] else None
+    return t.data_ptr() or None  # an empty tensor may report a null address
 
 
 def optima_mx4_pack(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
@@ -804,6 +816,7 @@ def optima_mx4_unpack(Q: torch.Tensor, scales: torch.Tensor, Y: torch.Tensor,
     _check(_mx4_unpack(_mx4_addr(Q), _mx4_addr(scales), n, d, y, ldy, dt, _launch_stream(stream)))
 
 
+@functools.lru_cache(maxsize=4096)
 def optima_mx4_workspace_bytes(n_tok: int, d: int, d_out: int) -> int:
     return int(_mx4_ws(n_tok, d, d_out))
 
@@ -841,10 +854,9 @@ def optima_mx4_linear(X: torch.Tensor, Q: torch.Tensor, scales: torch.Tensor, Y:
 
 
 TOP_MAX = 32
-_I = (torch.int64,)
-_F32 = (torch.float32,)
 
 
+@functools.lru_cache(maxsize=4096)
 def optima_token_logprobs_workspace_bytes(n: int, vocab: int, top: int = 0) -> int:
     return int(_logprobs_ws(n, vocab, top))
 
@@ -856,11 +868,13 @@ def _logits(logits):
     return (n, vocab, *_take("logits", logits, (n, vocab), _F))
 
 
-def _opt_shape(name, t, shape, dtypes):
-    if t is not None:
-        _need_shape(name, t, shape, dtypes)
-        return t.data_ptr() if t.numel() else None
-    return None
+def _row_values(name, t, shape, dtype):
+    """The address of a contiguous tensor or None, NULL without elements."""
+    if t is None:
+        return None
+    if not (t.dtype == dtype and t.is_cuda and t.shape == shape and t.is_contiguous()):
+        _need_shape(name, t, shape, (dtype,))
+    return t.data_ptr() or None
 
 
 def optima_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None,
@@ -874,29 +888,31 @@ def optima_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None,
     logarithm of the sum of exponentials lse and the entropy, float32 [n]; and the k most probable
     alternatives, top_index int64 and top_logp float32 [n, k], equal ones by rising index."""
     n, vocab, x, ldx, dt = _logits(logits)
-    t = _opt_shape("tokens", tokens, (n,), _I)
+    rows = (n,)
+    t = _row_values("tokens", tokens, rows, torch.int64)
     if logp is not None and tokens is None:
         raise ValueError("logp goes with tokens")
-    k = 0
-    for name, o in (("top_index", top_index), ("top_logp", top_logp)):
-        if o is not None:
-            if o.dim() != 2 or (k and o.shape[1] != k):
-                raise ValueError("top_index and top_logp must be [n, k] of one k")
-            k = o.shape[1]
-            if not 0 < k <= min(vocab, TOP_MAX):
-                raise ValueError(f"k must be 1 to {min(vocab, TOP_MAX)}, got {k}")
-    outs = [_opt_shape(name, o, (n,), _F32)
-            for name, o in (("logp", logp), ("lse", lse), ("entropy", entropy))]
-    top = [_opt_shape("top_index", top_index, (n, k), _I),
-           _opt_shape("top_logp", top_logp, (n, k), _F32)]
-    if all(o is None for o in (logp, lse, entropy, top_index, top_logp)):
+    p = _row_values("logp", logp, rows, torch.float32)
+    s = _row_values("lse", lse, rows, torch.float32)
+    h = _row_values("entropy", entropy, rows, torch.float32)
+    k, index, top = 0, None, None
+    if top_index is not None or top_logp is not None:
+        shape = (top_logp if top_index is None else top_index).shape
+        if len(shape) != 2:
+            raise ValueError("top_index and top_logp must be [n, k]")
+        k = shape[1]
+        if not 0 < k <= min(vocab, TOP_MAX):
+            raise ValueError(f"k must be 1 to {min(vocab, TOP_MAX)}, got {k}")
+        index = _row_values("top_index", top_index, (n, k), torch.int64)
+        top = _row_values("top_logp", top_logp, (n, k), torch.float32)
+    elif logp is None and lse is None and entropy is None:
         raise ValueError("one output is needed")
     _need_one_device(stream, logits, tokens, logp, lse, entropy, top_index, top_logp, ws)
     need = optima_token_logprobs_workspace_bytes(n, vocab, k)
     nbytes = 0
     if need or ws is not None:
         ws, nbytes = _workspace(need, ws, logits.device, stream)
-    _check(_logprobs(x, ldx, dt, n, vocab, t, float(scale), *outs, k, *top, _addr(ws), nbytes,
+    _check(_logprobs(x, ldx, dt, n, vocab, t, float(scale), p, s, h, k, index, top, _addr(ws), nbytes,
                      _launch_stream(stream)))
 
 
@@ -912,7 +928,7 @@ def optima_token_logprobs_backward(logits: torch.Tensor, lse: torch.Tensor,
     optima_token_logprobs stored. dlogits may be the logits themselves."""
     n, vocab, x, ldx, dt = _logits(logits)
     dx, lddx, _ = _take("dlogits", dlogits, (n, vocab), (logits.dtype,))
-    t = _opt_shape("tokens", tokens, (n,), _I)
+    t = _row_values("tokens", tokens, (n,), torch.int64)
     if lse is None:
         raise ValueError("lse is required")
     if dlogp is None and dentropy is None and dlse is None:
@@ -921,7 +937,7 @@ def optima_token_logprobs_backward(logits: torch.Tensor, lse: torch.Tensor,
         raise ValueError("dlogp goes with tokens")
     if dentropy is not None and entropy is None:
         raise ValueError("dentropy goes with the entropy")
-    rows = [_opt_shape(name, o, (n,), _F32)
+    rows = [_row_values(name, o, (n,), torch.float32)
             for name, o in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp),
                             ("dentropy", dentropy), ("dlse", dlse))]
     _need_one_device(stream, logits, lse, dlogits, tokens, dlogp, entropy, dentropy, dlse)
