@@ -563,7 +563,7 @@ optima_status optima_w4_gated(const void* X, int64_t ldx, int x_dtype, const flo
  *   one in the low half; rows are padded to whole 256 values with zero codes.
  * scales: [n][optima_mx4_scale_bytes(d)], 4-byte aligned: the exponent plus 127, that of block b
  *   (0 .. 3) of the 128 values c at byte 16 (c / 4) + 4 b + c % 4; rows are padded with zeros.
- * The 256-value pieces, n ceil(d / 256), are below 2^27, here and in unpack. */
+ * The 256-value pieces, n ceil(d / 256), are at most 2^27 - 8, here and in unpack. */
 size_t optima_mx4_row_bytes(int64_t d);
 size_t optima_mx4_scale_bytes(int64_t d);
 optima_status optima_mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t d, void* Q,
@@ -576,8 +576,8 @@ optima_status optima_mx4_unpack(const void* Q, const void* scales, int64_t n, in
 
 /* Y = X W^T for packed weights W [d_out][d], as optima_mx4_pack lays them out.
  * X: [n_tok][d] of x_dtype BF16 with pitch ldx and x_scales NULL, or of MX4: packed tokens with
- * x_scales (ldx is not used). n_tok <= 2^21, d <= 2^20, d_out <= 2^24. Y: [n_tok][d_out] BF16 or F32. Products of
- * values are exact, their sums fp32. A zero weight adds exactly nothing, except to an infinite or
+ * x_scales (ldx is not used). n_tok <= 2^21, d <= 2^20, d_out <= 2^24, and fewer than 2^24 - 8 64 x 64
+ * tiles of outputs. Y: [n_tok][d_out] BF16 or F32. Products of values are exact, their sums fp32. A zero weight adds exactly nothing, except to an infinite or
  * NaN token (NaN).
  * ws: optima_mx4_workspace_bytes(n_tok, d, d_out) bytes: 0 up to 8 tokens, never less for more. */
 size_t optima_mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out);

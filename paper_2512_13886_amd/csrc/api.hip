@@ -171,14 +171,15 @@ optima_status w4_call(const void* X, int64_t ldx, int x_dtype, const float* x_sc
                            scales2, group, d_out, act, Y, ldy, y_dtype, ws, stream);
 }
 
-// Rows in pieces of 256 values, 32 threads each: a launch has fewer than 2^32 threads.
+// Rows in pieces of 256 values, 32 threads each, and 64 x 64 tiles of outputs of 256 threads: a launch
+// has fewer than 2^32 threads.
 bool mx4_rows(int64_t n, int64_t d) {
   return n >= 0 && n < (int64_t(1) << 27) && d >= 1 && d <= kMaxDim &&
-         n * ((d + 255) / 256) < (int64_t(1) << 27);
+         n * ((d + 255) / 256) <= (int64_t(1) << 27) - 8;
 }
 bool mx4_sizes(int64_t n_tok, int64_t d, int64_t d_out) {
   return n_tok >= 0 && n_tok <= (int64_t(1) << 21) && d >= 1 && d <= kMaxDim && d_out >= 1 &&
-         d_out <= kMaxCols;
+         d_out <= kMaxCols && ((n_tok + 63) / 64) * ((d_out + 63) / 64) < (int64_t(1) << 24) - 8;
 }
 // Codes and scales of n rows.
 Span mx4_codes(const void* Q, int64_t n, int64_t d) {

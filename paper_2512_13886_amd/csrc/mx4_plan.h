@@ -13,6 +13,9 @@ constexpr int kMx4TileM[kMx4Tiles] = {256, 128, 64, 64}, kMx4TileN[kMx4Tiles] = 
 
 constexpr int64_t kMx4PartBytes = int64_t(64) << 20;  // of split sums, at most
 
+constexpr int kMx4Few = 16;     // tokens of the few-token kernel, at most
+constexpr int kMx4Fewest = 8;   // up to which 16-bit ones always take it, and no sum is split: no room
+
 struct Mx4Plan {
   int tile, splits;
   int64_t tiles;
@@ -42,7 +45,9 @@ inline Mx4Plan mx4_plan(int64_t n_tok, int64_t d, int64_t d_out) {
   for (int t = 0; t < kMx4Tiles; ++t) {
     const int64_t tiles = mx4_tiles(t, round_up(n_tok, 64), d_out);
     for (const int splits : kMx4Splits) {
-      if (splits > pairs || mx4_part_bytes(t, splits, tiles) > kMx4PartBytes) break;
+      if (splits > pairs || mx4_part_bytes(t, splits, tiles) > kMx4PartBytes ||
+          (splits > 1 && n_tok <= kMx4Fewest))
+        break;
       const double each = double(std::min(2 * ceil_div(pairs, splits), stages));
       const double us = kAround[t] + each * std::max(kAlone[t], kEach[t] * double(ceil_div(tiles * splits, 256))) +
                         (splits > 1 ? 2.3 + double(mx4_part_bytes(t, splits, tiles)) * 2 / 8e6 : 0);
@@ -59,8 +64,6 @@ inline Mx4Plan mx4_plan(int64_t n_tok, int64_t d, int64_t d_out) {
 struct Mx4SlabPlan {
   int tokens, splits;
 };
-constexpr int kMx4Few = 16;      // tokens of the few-token kernel, at most
-constexpr int kMx4Fewest = 8;    // up to which 16-bit ones always take it
 constexpr int kMx4SlabRows = 256;
 constexpr int kMx4SlabSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24};
 

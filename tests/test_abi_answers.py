@@ -39,6 +39,7 @@ def _pack(lib, **kw):
     (dict(d=0), INVAL), (dict(d=(1 << 20) + 1, ldx=(1 << 20) + 1), INVAL), (dict(ldx=299), INVAL),
     (dict(dtype=I8), UNSUPPORTED), (dict(dtype=F64), UNSUPPORTED), (dict(Q=2 * MB + 8), INVAL),
     (dict(scales=3 * MB + 2), INVAL), (dict(X=1 * MB + 1), INVAL), (dict(n=1 << 27), INVAL),
+    (dict(n=(1 << 26) - 3, d=257, ldx=257, X=1 << 50, Q=1 << 52, scales=1 << 54), INVAL),
     (dict(Q=1 * MB), INVAL), (dict(scales=1 * MB + 64), INVAL), (dict(scales=2 * MB), INVAL),
     (dict(n=0), OK), (dict(n=0, X=None, Q=None, scales=None), OK),
 ])
@@ -79,7 +80,8 @@ PACKED = dict(x_dtype=MX4, xs=7 * MB)
 @pytest.mark.parametrize("change, status", [
     (dict(X=None), INVAL), (dict(Q=None), INVAL), (dict(scales=None), INVAL), (dict(Y=None), INVAL),
     (dict(n=-1), INVAL), (dict(n=(1 << 21) + 1), INVAL), (dict(d=0), INVAL), (dict(d_out=0), INVAL),
-    (dict(d_out=(1 << 24) + 1, ldy=1 << 25), INVAL), (dict(ldx=299), INVAL), (dict(ldy=499), INVAL),
+    (dict(d_out=(1 << 24) + 1, ldy=1 << 25), INVAL),
+    (dict(n=1 << 12, d_out=1 << 24, ldy=1 << 24, Y=1 << 50, Q=1 << 52, scales=1 << 54, X=1 << 56), INVAL), (dict(ldx=299), INVAL), (dict(ldy=499), INVAL),
     (dict(x_dtype=F32), UNSUPPORTED), (dict(x_dtype=I8), UNSUPPORTED), (dict(y_dtype=MX4), UNSUPPORTED),
     (dict(xs=7 * MB), INVAL), (dict(x_dtype=MX4), INVAL), (dict(PACKED, X=1 * MB + 8), INVAL),
     (dict(PACKED, xs=7 * MB + 2), INVAL), (dict(Q=2 * MB + 8), INVAL), (dict(scales=3 * MB + 1), INVAL),

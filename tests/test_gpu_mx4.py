@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from oracle import answers_oracle as O
+from test_mx4_plans_host import SLABS, TILES
 
 pytestmark = pytest.mark.gpu
 
@@ -164,6 +165,18 @@ def test_linear_of_many_packed_tokens(L, n, d, ff):
     Q, s, w = _weights(L, ff, d, 3)
     _check(L, _tokens(n, d, 4), Q, s, w, torch.bfloat16, True, pad=3)
     _check(L, _tokens(n, d, 5), Q, s, w, torch.float32, True)
+
+
+@pytest.mark.parametrize("n, d, ff", sorted(TILES))
+def test_every_tile(L, n, d, ff):
+    Q, s, w = _weights(L, ff, d, 5)
+    _check(L, _tokens(n, d, 6), Q, s, w, torch.float32, True, pad=1)
+
+
+@pytest.mark.parametrize("n, d, ff", sorted(SLABS))
+def test_every_slab(L, n, d, ff):
+    Q, s, w = _weights(L, ff, d, 5)
+    _check(L, _tokens(n, d, 6), Q, s, w, torch.float32, False, pad=1)
 
 
 @pytest.mark.parametrize("packed", (False, True))
