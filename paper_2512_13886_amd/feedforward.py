@@ -248,6 +248,8 @@ def main(argv=None) -> None:
     ap.add_argument("--sparsity", type=float, default=0.5)
     ap.add_argument("--steps", type=int, default=20)
     ap.add_argument("--group", type=int, default=128, choices=(32, 64, 128))
+    ap.add_argument("--vocab", type=int, default=8000,
+                    help="tokens of a synthetic output head that scores the blocks; 0: none")
     a = ap.parse_args(argv)
     dev = torch.device("cuda:0")
     g = torch.Generator(device=dev).manual_seed(1)
@@ -290,6 +292,32 @@ def main(argv=None) -> None:
     graph.replay()
     _, ms = timed(lambda: [graph.replay() for _ in range(100)])
     print(f"serve    {10 * ms:9.2f} us a token")
+    if a.vocab:
+        _print_scores(a.vocab, block, {"pruned": pruned, "recovered": better}, X, R)
+
+
+def _print_scores(vocab: int, dense: FeedForward, others: dict, X: torch.Tensor,
+                  R: torch.Tensor) -> None:
+    """How probable the dense block's first choices are behind each block, under one head, with it
+    in 16 and in 4 bits."""
+    from .scoring import PackedHead, score, synthetic_head
+
+    head = synthetic_head(X.shape[1], vocab)
+    n = min(2048, X.shape[0])
+    X, R = X[:n], R[:n]
+    packed = PackedHead(head, max_tokens=n, packed_tokens=True)
+
+    def states(block):
+        return (X.float() + R.float()).bfloat16(), output(block, X, R).bfloat16()
+
+    S, Y = states(dense)
+    tokens = score(head, Y, torch.full((n,), -1, device=X.device), S, top=1).top_index[:, 0].clone()
+    for name, block in {"dense": dense, **others}.items():
+        S, Y = states(block)
+        s = score(head, Y, tokens, S)
+        p = packed.step(Y, S, tokens)
+        print(f"score    {name:>9}  log p {float(s.logp.mean()):8.4f}  entropy "
+              f"{float(s.entropy.mean()):7.4f}  head in 4 bits {float(p.logp.mean()):8.4f}")
 
 
 if __name__ == "__main__":

@@ -1,0 +1,196 @@
+"""The output head, scored, pruned, recovered and served in 4 bits, against 64-bit forms of the same
+steps on the CPU.
+
+B is half a step of bf16, relative. The head's 16-bit products round W, a and (where kept in 16 bits)
+the logits once each; a sum of products of entries that are off by up to 2 B each is off by no more
+than 2 B times the sum of their absolute values, and its fp32 sum by d 2^-24 of that."""
+import pytest
+import torch
+
+from oracle import answers_oracle as O
+
+pytestmark = pytest.mark.gpu
+B = 2.0 ** -8
+
+
+@pytest.fixture(scope="module")
+def sc():
+    from paper_2512_13886_amd import scoring
+    return scoring
+
+
+def _states(n, d, seed, device="cuda:0"):
+    g = torch.Generator(device=device).manual_seed(seed)
+    spread = torch.exp(0.5 * torch.randn(d, generator=g, device=device))
+    return [(torch.randn((n, d), generator=g, device=device) * spread).bfloat16() for _ in range(2)]
+
+
+def _double(head, X, R):
+    """a and the logits in 64 bits, from the unrounded sum."""
+    s = X.double() + R.double()
+    a = s / (s.square().mean(1, keepdim=True) + head.eps).sqrt() * head.norm.double()
+    return a, torch.mm(a, head.weight.double().t().contiguous())
+
+
+def _logit_bound(head, a):
+    d = a.shape[1]
+    return torch.mm(a.abs(), head.weight.double().abs().t().contiguous()) * (2.02 * B + d * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("n, d, vocab, top", ((1, 128, 1000, 5), (70, 100, 999, 32), (300, 256, 9001, 3)))
+def test_score(sc, n, d, vocab, top):
+    head = sc.synthetic_head(d, vocab)
+    X, R = _states(n, d, 1)
+    tokens = torch.arange(n, device=X.device) * 7 % vocab
+    tokens[::5] = -1
+    s = sc.score(head, X, tokens, R, top=top, scale=0.8)
+    a, z = _double(head, X, R)
+    off = _logit_bound(head, a)
+    assert ((s.logits.double() - z).abs() <= off).all()
+    # log p moves by no more than twice its row's largest change of a logit; so do the others by what
+    # they are sums of.
+    most = 0.8 * off.amax(1)
+    lse, logp, _ = O.token_logprobs(z, tokens, 0.8)
+    assert ((s.lse.double() - lse).abs() <= most + 1e-5).all()
+    assert ((s.logp.double() - logp).abs() <= 2 * most + 1e-5).all()
+    # Of its own logits exactly what the call says.
+    lse, logp, entropy = O.token_logprobs(s.logits, tokens, 0.8)
+    assert (s.entropy.double() - entropy).abs().max() < 1e-4
+    assert torch.equal(s.top_index, O.top(s.logits, top))
+
+
+def test_gradients(sc):
+    n, d, vocab = 90, 64, 400
+    head = sc.synthetic_head(d, vocab, 3)
+    X, R = _states(n, d, 2)
+    tokens = torch.arange(n, device=X.device) * 11 % vocab
+    tokens[::4] = -100
+    mask = (torch.rand(vocab, d, generator=torch.Generator(device="cuda").manual_seed(1),
+                       device="cuda") < 0.5).to(torch.uint8)
+    loss, g, dX = sc.gradients(head, X, tokens, R, mask)
+
+    def f(x, norm, w):
+        s = x + R.double()
+        a = s / (s.square().mean(1, keepdim=True) + head.eps).sqrt() * norm
+        z = torch.mm(a, w.t().contiguous())
+        lp = torch.log_softmax(z, 1).gather(1, tokens.clamp(min=0).unsqueeze(1)).squeeze(1)
+        return -lp[tokens >= 0].mean()
+
+    a, z = _double(head, X, R)
+    most = 2 * float((_logit_bound(head, a) + B * z.abs()).amax())  # of a log probability
+    args = [t.double().cpu().requires_grad_() for t in (X, head.norm, head.weight)]
+    a, z, R, tokens = a.cpu(), z.cpu(), R.cpu(), tokens.cpu()
+    want = f(*args)
+    want.backward()
+    assert abs(loss - want.item()) <= most
+    dx, dn, dw = (t.grad for t in args)
+    # D, the logits' gradient: p moves by exp(most) - 1 of itself and is rounded; then each product
+    # by what its operands are off (spectral times Frobenius norms), and by its own rounding.
+    given = tokens >= 0
+    p = torch.softmax(z, 1) / given.sum()
+    D = p.clone()
+    D[torch.arange(n), tokens.clamp(min=0)] -= 1.0 / given.sum()
+    D[~given] = p[~given] = 0
+    dD = (p * torch.expm1(torch.tensor(most)) + B * D.abs()).norm()
+
+    def norms(t):
+        return torch.linalg.matrix_norm(t, 2), t.norm()
+
+    w2, wf = norms(args[2].detach())
+    a2, af = norms(a)
+    d2, df = norms(D)
+    dA = D @ args[2].detach()
+    off_A = dD * w2 + 1.1 * d2 * B * wf + B * dA.norm()
+    off_W = dD * a2 + 1.1 * d2 * 2 * B * af
+    s = X.double().cpu() + R.double()
+    rstd = 1 / (s.square().mean(1, keepdim=True) + head.eps).sqrt()
+    xh = s * rstd
+    # The norm's gradient: a Jacobian of at most 2 rstd |w|, the stored sum rounded once.
+    off_X = 2 * float(rstd.max() * head.norm.abs().max()) * (off_A + 4 * B * dA.norm()) + B * dx.norm()
+    off_n = float(xh.norm(dim=0).max()) * (off_A + 4 * B * dA.norm())
+    for got, ref, off in ((dX, dx, off_X), (g["norm"], dn, off_n), (g["weight"], dw * mask.cpu(), off_W)):
+        assert (got.double().cpu() - ref).norm() <= off, ((got.double().cpu() - ref).norm(), off, ref.norm())
+    assert (g["weight"][mask == 0] == 0).all()
+
+
+def test_prune_and_recover(sc):
+    n, d, vocab = 1024, 128, 500
+    head = sc.synthetic_head(d, vocab, 5)
+    X, R = _states(n, d, 6)
+    dense = sc.score(head, X, torch.full((n,), -1, device=X.device), R, top=1)
+    tokens = dense.top_index[:, 0].clone()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    pruned, mask, skipped = sc.prune_head(head, X, R,
+                                          lambda w: torch.randn((8, w), generator=g, device="cuda"))
+    assert not skipped and (pruned.weight[mask == 0] == 0).all()
+    assert abs(float(mask.float().mean()) - 0.5) < 0.02
+    out, losses = sc.recover(pruned, mask, X, tokens, R, steps=3)
+    assert len(losses) == 3 and all(v > 0 for v in losses)
+    assert (out.weight[mask == 0] == 0).all()
+    again, _ = sc.recover(pruned, mask, X, tokens, R, steps=3)
+    assert torch.equal(out.weight, again.weight) and torch.equal(out.norm, again.norm)
+
+
+@pytest.mark.parametrize("packed_tokens", (False, True))
+@pytest.mark.parametrize("n", (1, 20, 150))
+def test_packed_head(sc, n, packed_tokens):
+    d, vocab = 300, 9000
+    head = sc.synthetic_head(d, vocab, 7)
+    packed = sc.PackedHead(head, max_tokens=n + 3, top=4, packed_tokens=packed_tokens)
+    X, R = _states(n, d, 8)
+    tokens = torch.arange(n, device=X.device) * 13 % vocab
+    S = R.clone()
+    out = packed.step(X, S, tokens, scale=1.25)
+    assert torch.equal(S, (X.float() + R.float()).bfloat16())
+    a = _double(head, X, R)[0].bfloat16()  # within a step of what the norm stored
+    if packed_tokens:
+        a = O.mx4_values(packed.normed[:n])[0]
+    w = O.mx4_values(head.weight)[0]
+    z = torch.mm(a.double(), w.t().contiguous())
+    size = torch.mm(a.double().abs(), w.abs().t().contiguous())
+    assert ((out.logits.double() - z).abs() <= 2.02 * B * size + B * z.abs() * 1.02).all()
+    lse, logp, entropy = O.token_logprobs(out.logits, tokens, 1.25)
+    assert (out.lse.double() - lse).abs().max() < 1e-4
+    assert (out.logp.double() - logp).abs().max() < 1e-4
+    assert (out.entropy.double() - entropy).abs().max() < 1e-4
+    assert torch.equal(out.top_index, O.top(out.logits, 4))
+    with pytest.raises(ValueError):
+        packed.step(*_states(n + 4, d, 1), torch.zeros(n + 4, dtype=torch.int64, device=X.device))
+
+
+@pytest.mark.parametrize("n", (1, 12))
+def test_packed_head_in_graphs(sc, n):
+    """Two heads in graphs of their own, replayed in turn with eager steps between."""
+    d, vocab = 256, 20000
+    sets = []
+    for k in range(2):
+        packed = sc.PackedHead(sc.synthetic_head(d, vocab, k), max_tokens=n, top=3)
+        X, S = _states(n, d, 30 + k)
+        tokens = torch.arange(n, device=X.device)
+        packed.step(X, S, tokens)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = packed.step(X, S, tokens)
+        sets.append((packed, X, S, tokens, graph, out))
+    for trial in range(3):
+        wants = []
+        for k, (packed, X, S, tokens, graph, out) in enumerate(sets):
+            x, s = _states(n, d, 50 + 2 * trial + k)
+            X.copy_(x)
+            S.copy_(s)
+            got = packed.step(x, s, tokens)
+            wants.append([t.clone() for t in (got.logits, got.logp, got.entropy, got.top_index, got.top_logp)])
+        for one in sets:
+            one[4].replay()
+        torch.cuda.synchronize()
+        for (packed, X, S, tokens, graph, out), want in zip(sets, wants):
+            for a, b in zip((out.logits, out.logp, out.entropy, out.top_index, out.top_logp), want):
+                assert torch.equal(a, b)
+
+
+def test_command(capsys):
+    from paper_2512_13886_amd import feedforward
+    feedforward.main(["--d", "128", "--ff", "192", "--tokens", "512", "--steps", "2", "--vocab", "300"])
+    out = capsys.readouterr().out
+    assert out.count("score") == 3 and "nan" not in out
