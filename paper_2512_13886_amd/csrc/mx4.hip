@@ -149,12 +149,28 @@ __device__ inline void mfma_bf16(f4& c, const u32x4& w, uint32_t sw, const bf16x
     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(weights8(w[j], scale), x[j], c, 0, 0, 0);
 }
 
-// Values k .. k + 7 of a row of d 16-bit values; zeros past its end.
-__device__ inline u32x4 tokens8(const bf16_t* row, int k, int d) {
-  Raw8<bf16_t> r;
-  load_piece(r, row, k, d);
-  return r.w;
-}
+// Values k .. k + 7 of rows of d 16-bit values, zeros past their end: loaded as they lie or, of a row's
+// last piece, from eight values before its end, without a branch, so that the loads of several rows
+// go out together; and moved afterwards. (In load_piece each row's end waits for its own load: 13
+// tokens, 1001 -> 2731, 7.1 us and 5.7.)
+struct TokenPiece {
+  int at, shift, d;
+  __device__ inline TokenPiece(int k, int d) : at(max(min(k, d - 8), 0)), shift(k - at), d(d) {}
+  __device__ inline u32x4 load(const bf16_t* row) const {
+    Raw8<bf16_t> r;
+    if (d >= 8)
+      load8(r, row + at);
+    else
+      load_some(r, row, d);
+    return r.w;
+  }
+  __device__ inline u32x4 moved(const u32x4& v) const {
+    if (shift >= 8) return u32x4{0, 0, 0, 0};
+    Raw8<bf16_t> r{v};
+    shift_down(r, shift);
+    return r.w;
+  }
+};
 
 __device__ inline void store_y4(const Mx4Args& a, int64_t tok, int64_t n, const f4& v) {
   if (tok >= a.n_tok || n >= a.d_out) return;
@@ -208,8 +224,9 @@ __device__ inline void load_codes(u32x4 (&w)[kBatch], uint32_t& s, const uint8_t
   s = *reinterpret_cast<const uint32_t*>(sc + n * a.srow + batch * 16 + 4 * b);
 }
 
-// ROWS: tokens that a lane loads values of together; RB: blocks of 16 outputs.
-template <bool PACKED, int ROWS, int RB>
+// ROWS: tokens that a lane loads values of together; RB: blocks of 16 outputs; RAGGED: 16-bit tokens of
+// a width that is no multiple of 8.
+template <bool PACKED, int ROWS, int RB, bool RAGGED>
 __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   float* part = reinterpret_cast<float*>(lds);  // [wave][lane][4], at the end
@@ -241,12 +258,21 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
       }
     } else {
       // The tokens' values come through LDS: the operands would read each 16 times over.
-      const int k = batch * kBatchK + 8 * lane;
+      const TokenPiece piece(batch * kBatchK + 8 * lane, a.d);
       for (int r0 = 0; r0 < tokens; r0 += ROWS) {
         u32x4 v[ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
-          if (r0 + r < tokens) v[r] = tokens8(x + (r0 + r) * a.ldx, k, a.d);
+          if (r0 + r < tokens) {
+            const bf16_t* row = x + (r0 + r) * a.ldx;
+            if constexpr (RAGGED)
+              v[r] = piece.load(row);
+            else
+              v[r] = piece.shift ? u32x4{0, 0, 0, 0} : *reinterpret_cast<const u32x4_2*>(row + piece.at);
+          }
+        if (RAGGED && piece.shift)
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r) v[r] = piece.moved(v[r]);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
           if (r0 + r < tokens)
@@ -312,15 +338,19 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
 
   u32x4 xv[kEach];
   auto fetch_x = [&](int batch) {
+    static_assert(512 % kPieces == 0, "one place in all rows of a thread");
+    const TokenPiece piece(batch * kBatchK + 8 * (int(threadIdx.x) % kPieces), a.d);
 #pragma unroll
     for (int r = 0; r < kEach; ++r) {
-      const int at = threadIdx.x + 512 * r;
-      const int64_t t = t0 + std::min(at / kPieces, tokens - 1);
-      const int p = at % kPieces;
-      xv[r] = tokens8(static_cast<const bf16_t*>(a.x) + t * a.ldx, batch * kBatchK + 8 * p, a.d);
+      const int64_t t = t0 + std::min(int(threadIdx.x + 512 * r) / kPieces, tokens - 1);
+      xv[r] = piece.load(static_cast<const bf16_t*>(a.x) + t * a.ldx);
     }
   };
-  auto put_x = [&](int to) {
+  auto put_x = [&](int to, int batch) {
+    const TokenPiece piece(batch * kBatchK + 8 * (int(threadIdx.x) % kPieces), a.d);
+    if (piece.shift)
+#pragma unroll
+      for (int r = 0; r < kEach; ++r) xv[r] = piece.moved(xv[r]);
 #pragma unroll
     for (int r = 0; r < kEach; ++r) {
       const int at = threadIdx.x + 512 * r;
@@ -343,7 +373,7 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
   if (b0 < b1) {
     fetch_x(b0);
     fetch_w(b0);
-    put_x(0);
+    put_x(0, b0);
   }
   __syncthreads();
   for (int batch = b0; batch < b1; ++batch) {
@@ -382,7 +412,7 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
             sum[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[m][j], f, sum[m][t], 0, 0, 0);
         }
     }
-    if (batch + 1 < b1) put_x(cur ^ 1);
+    if (batch + 1 < b1) put_x(cur ^ 1, batch + 1);
     __syncthreads();
   }
   if (gridDim.y > 1) {  // [split][64 tokens][workgroup][wave][row block][token block][lane]
@@ -610,38 +640,42 @@ void launch_tile(const Mx4Args& a, hipStream_t s) {
                        int(p.tiles));
 }
 
-template <bool PACKED, int ROWS, int RB>
+template <bool PACKED, int ROWS, int RB, bool RAGGED>
 void launch_few(const Mx4Args& a, hipStream_t s) {
   // As many waves as there are batches, and as the CU's LDS holds tokens for.
   const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kFewPitch, RB * 1024);
   const int most = int(std::min<size_t>(kFewWaves, (size_t(160) << 10) / each));
   const int waves = int(std::min<int64_t>(ceil_div(a.chunks, kBatch), most));
-  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB>), dim3(unsigned(ceil_div(a.d_out, 16 * RB))),
+  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB, RAGGED>), dim3(unsigned(ceil_div(a.d_out, 16 * RB))),
                      dim3(64 * waves), waves * each, s, a);
+}
+template <int ROWS, int RB>
+void launch_few_16bit(const Mx4Args& a, hipStream_t s) {
+  if (a.d % 8) launch_few<false, 4, RB, true>(a, s);
+  else launch_few<false, ROWS, RB, false>(a, s);
 }
 // Two blocks of outputs where every CU still has a workgroup: they halve what is read of the
 // tokens. 16 tokens, 4096 -> 8192 12.4 to 9.3 us, -> 14336 22.3 to 16.8, but -> 1000 with d = 1000 5.9
 // to 6.8; one token, 14336 -> 4096 9.4 to 12.8.
-template <bool PACKED, int ROWS>
-void launch_few(const Mx4Args& a, hipStream_t s) {
-  if (a.d_out > 32 * 255) launch_few<PACKED, ROWS, 2>(a, s);
-  else launch_few<PACKED, ROWS, 1>(a, s);
-}
+bool two_blocks(const Mx4Args& a) { return a.d_out > 32 * 255; }
 
 void launch_packed(const Mx4Args& a, hipStream_t s) {
   // Every 16 or 32 outputs of the few-token kernel read all tokens again. us with it and in tiles: 16
   // tokens, 4096 -> 4096 5.6 and 9.6, -> 14336 12.6 and 11.5; 8 tokens, 4096 -> 14336 10.9 and 11.3,
   // -> 128000 70 and 55; one token, -> 128000 55 and 57.
   if (a.n_tok > kMx4Few || a.n_tok * a.d_out > 131072) launch_tile(a, s);
-  else launch_few<true, 4>(a, s);
+  else if (two_blocks(a)) launch_few<true, 4, 2, false>(a, s);
+  else launch_few<true, 4, 1, false>(a, s);
 }
 void launch_16bit(const Mx4Args& a, hipStream_t s) {
   const Mx4SlabPlan p = mx4_slab_plan(a.n_tok, a.d, a.d_out);
   if (p.tokens == 16) launch_slab<1>(a, p.splits, s);
   else if (p.tokens == 32) launch_slab<2>(a, p.splits, s);
   else if (p.tokens == 64) launch_slab<4>(a, p.splits, s);
-  else if (a.n_tok > 4) launch_few<false, 8>(a, s);
-  else launch_few<false, 4>(a, s);
+  else if (a.n_tok > 4 && two_blocks(a)) launch_few_16bit<8, 2>(a, s);
+  else if (a.n_tok > 4) launch_few_16bit<8, 1>(a, s);
+  else if (two_blocks(a)) launch_few_16bit<4, 2>(a, s);
+  else launch_few_16bit<4, 1>(a, s);
 }
 
 }  // namespace
