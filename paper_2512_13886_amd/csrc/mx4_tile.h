@@ -190,16 +190,21 @@ __device__ inline void ring_stage(f4 (&acc)[R::MB][R::NB], RingScales<R>& sc, co
     __builtin_amdgcn_s_waitcnt(0x0F70);
   t256::barrier();
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
-  if (U0 == 0 && s + 2 < n)
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(src.scales + 8 * (s + 2)),
-        (__attribute__((address_space(3))) void*)(next + wave * 1024), 16, 0, 0);
-  if (s + R::NBUF - 1 < n)
-#pragma unroll
-    for (int i = 0; i < R::kLoads; ++i)
+  auto fetch = [&] {
+    if (U0 == 0 && s + 2 < n)
       __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(src.row[i] + int64_t(s + R::NBUF - 1) * 128),
-          (__attribute__((address_space(3))) void*)(to + (i * 4 + wave) * 1024), 16, 0, 0);
+          (const __attribute__((address_space(1))) void*)(src.scales + 8 * (s + 2)),
+          (__attribute__((address_space(3))) void*)(next + wave * 1024), 16, 0, 0);
+    if (s + R::NBUF - 1 < n)
+  #pragma unroll
+      for (int i = 0; i < R::kLoads; ++i)
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(src.row[i] + int64_t(s + R::NBUF - 1) * 128),
+            (__attribute__((address_space(3))) void*)(to + (i * 4 + wave) * 1024), 16, 0, 0);
+  };
+  // With two buffers the next stage's loads have no time to lose; with four the reads go first, and the
+  // loads' addresses are worked out behind them (64 tokens, 4096 -> 14336 13.8 to 11.9 us).
+  if constexpr (R::NBUF == 2) fetch();
   const int ra = (wave / R::WN) * R::MB * 16 + (lane & 15);
   const int rb = R::TM + (wave % R::WN) * R::NB * 16 + (lane & 15);
   if constexpr (U0 == 0) {
@@ -210,26 +215,31 @@ __device__ inline void ring_stage(f4 (&acc)[R::MB][R::NB], RingScales<R>& sc, co
     for (int m = 0; m < R::NB; ++m)
       sc.b[m] = *reinterpret_cast<const uint32_t*>(now + (rb + 16 * m) * 16 + 4 * g);
   }
-  auto frag = [cur, g](int r, int k) {
-    return *reinterpret_cast<const bf16x8*>(cur + r * 128 + (((4 * k + g) ^ (r & 7)) * 16));
-  };
+  bf16x8 fa[2][R::MB], fb[2][R::NB];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    bf16x8 fa[R::MB], fb[R::NB];
+    auto frag = [cur, g, k](int r) {
+      return *reinterpret_cast<const bf16x8*>(cur + r * 128 + (((4 * k + g) ^ (r & 7)) * 16));
+    };
 #pragma unroll
-    for (int m = 0; m < R::MB; ++m) fa[m] = frag(ra + 16 * m, k);
+    for (int m = 0; m < R::NB; ++m) fb[k][m] = frag(rb + 16 * m);
 #pragma unroll
-    for (int m = 0; m < R::NB; ++m) fb[m] = frag(rb + 16 * m, k);
-#pragma unroll
-    for (int mi = 0; mi < R::MB; ++mi)
-#pragma unroll
-      for (int ni = 0; ni < R::NB; ++ni) {
-        if (k == 0)
-          mfma<U0>(acc[mi][ni], fb[ni], sc.b[ni], fa[mi], sc.a[mi]);
-        else
-          mfma<U0 + 1>(acc[mi][ni], fb[ni], sc.b[ni], fa[mi], sc.a[mi]);
-      }
+    for (int m = 0; m < R::MB; ++m) fa[k][m] = frag(ra + 16 * m);
   }
+  if constexpr (R::NBUF > 2) {
+    __builtin_amdgcn_sched_barrier(0);
+    fetch();
+  }
+#pragma unroll
+  for (int mi = 0; mi < R::MB; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < R::NB; ++ni)
+      mfma<U0>(acc[mi][ni], fb[0][ni], sc.b[ni], fa[0][mi], sc.a[mi]);
+#pragma unroll
+  for (int mi = 0; mi < R::MB; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < R::NB; ++ni)
+      mfma<U0 + 1>(acc[mi][ni], fb[1][ni], sc.b[ni], fa[1][mi], sc.a[mi]);
 }
 
 // n stages (n >= 1) from an even one on. b0 .. b3: the ring's buffers, the first NBUF of them.
