@@ -31,14 +31,14 @@ inline int64_t mx4_part_bytes(int tile, int splits, int64_t tiles) {
 constexpr int kMx4Splits[] = {1, 2, 3, 4, 6, 8, 12};
 
 // The least estimate, in microseconds: a stage (256 values) of one workgroup alone on its CU, or of
-// each of those that share it; what is around the stages; the operands and outputs at 6 TB/s; and
-// the join with its parts at 8 TB/s. The constants fit 75 sizes of 17 to 16287 tokens, 64 to 14336
-// wide, every tile and split timed with cold weights: the choice is 1.8 % off the best of them on
-// average, 19 % at most. 777 tokens, 4097 -> 5001: 128 x 128 27 us, 64 x 128 30, 64 x 64 32,
-// 256 x 256 35; 256 tokens, 1000 -> 768: 6.1, 5.0, 4.2, 11.6.
+// each of those that share it; what is around the stages; and the join with its parts at 10 TB/s.
+// (Operands and outputs take the same with every tile.) The constants fit 70 sizes of 17 to 16287
+// tokens, 64 to 14336 wide, every tile and split timed with weights from HBM and from the cache: the
+// choice is 1.7 % off the best of them on average, 26 % at most. 777 tokens, 4097 -> 5001: 128 x 128
+// 27 us, 64 x 128 30, 64 x 64 32, 256 x 256 35; 256 tokens, 1000 -> 768: 6.1, 5.0, 4.0, 11.6.
 inline Mx4Plan mx4_plan(int64_t n_tok, int64_t d, int64_t d_out) {
-  constexpr double kAlone[kMx4Tiles] = {1.31, 0.62, 0.51, 0.33}, kEach[kMx4Tiles] = {1.35, 0.55, 0.39, 0.27};
-  constexpr double kAround[kMx4Tiles] = {6.0, 3.7, 3.1, 3.1};
+  constexpr double kAlone[kMx4Tiles] = {1.23, 0.60, 0.49, 0.25}, kEach[kMx4Tiles] = {1.24, 0.57, 0.42, 0.25};
+  constexpr double kAround[kMx4Tiles] = {7.7, 3.5, 2.8, 2.8};
   const int64_t stages = ceil_div(d, 256), pairs = ceil_div(d, 512);
   Mx4Plan best{};
   double best_us = 1e30;
@@ -50,7 +50,7 @@ inline Mx4Plan mx4_plan(int64_t n_tok, int64_t d, int64_t d_out) {
         break;
       const double each = double(std::min(2 * ceil_div(pairs, splits), stages));
       const double us = kAround[t] + each * std::max(kAlone[t], kEach[t] * double(ceil_div(tiles * splits, 256))) +
-                        (splits > 1 ? 2.3 + double(mx4_part_bytes(t, splits, tiles)) * 2 / 8e6 : 0);
+                        (splits > 1 ? 2.6 + double(mx4_part_bytes(t, splits, tiles)) * 2 / 10.2e6 : 0);
       if (us < best_us) {
         best_us = us;
         best = Mx4Plan{t, splits, tiles};
