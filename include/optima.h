@@ -576,9 +576,9 @@ optima_status optima_mx4_unpack(const void* Q, const void* scales, int64_t n, in
 
 /* Y = X W^T for packed weights W [d_out][d], as optima_mx4_pack lays them out.
  * X: [n_tok][d] of x_dtype BF16 with pitch ldx and x_scales NULL, or of MX4: packed tokens with
- * x_scales (ldx is not used). n_tok <= 2^21, d <= 2^20, d_out <= 2^24, and fewer than 2^24 - 8 64 x 64
- * tiles of outputs. Y: [n_tok][d_out] BF16 or F32. Products of values are exact, their sums fp32. A zero weight adds exactly nothing, except to an infinite or
- * NaN token (NaN).
+ * x_scales (ldx is not used). n_tok <= 2^21, d <= 2^20, d_out <= 2^24, and fewer than 2^24 - 8
+ * tiles of 64 x 64 outputs. Y: [n_tok][d_out] BF16 or F32. Products of values are exact, their sums
+ * fp32. A zero weight adds exactly nothing, except to an infinite or NaN token (NaN).
  * ws: optima_mx4_workspace_bytes(n_tok, d, d_out) bytes: 0 up to 8 tokens, never less for more. */
 size_t optima_mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out);
 optima_status optima_mx4_linear(const void* X, int64_t ldx, int x_dtype, const void* x_scales,
@@ -611,8 +611,8 @@ optima_status optima_token_logprobs(const void* X, int64_t ldx, int dtype, int64
  * with p = exp(z - lse). dlogp (with tokens), dentropy (with entropy) and dlse: fp32 [n], each
  * nullable, one at least. A row without a token has no part of dlogp; one whose token is vocab or
  * more is NaN; one whose lse is below -1e30 (nothing but masks) has gradient 0. p is as exact as
- * lse, within |lse| 2^-24 of itself. dX: [n][lddx] of X's dtype, and may be X
- * itself (same pointer and pitch). */
+ * lse, within |lse| 2^-24 of itself. dX: [n][lddx] of X's dtype, and may be X itself (same pointer
+ * and pitch). */
 optima_status optima_token_logprobs_backward(const void* X, int64_t ldx, int dtype, int64_t n,
                                              int64_t vocab, const int64_t* tokens, float scale,
                                              const float* lse, const float* entropy,

@@ -41,7 +41,9 @@ __device__ inline uint32_t quad_max(uint32_t m) {
   return max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0x4E, 0xF, 0xF, true)));  // 2 3 0 1
 }
 
-// Thirty-two lanes for 256 values, one dword (eight codes) each.
+// Thirty-two lanes for 256 values, one dword (eight codes) each: a block's largest takes two exchanges of
+// neighbouring lanes, and its scale, a power of two, leaves the quotients exact, so that one rounding
+// is all there is. Bound by HBM: 14336 x 4096 fp32 in 54 us, 4.9 TB/s, the rate of a copy.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, uint32_t total,
                                                        uint32_t pieces, int d, uint8_t* Q,
@@ -85,6 +87,8 @@ __global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, 
   }
 }
 
+// The values, exact in either type. Bound by HBM's writes: 14336 x 4096 to bf16 in 23 us, 6.5 TB/s with
+// the codes partly in a cache.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_mx4_unpack(const uint8_t* Q, const uint8_t* scales,
                                                          int srow, uint32_t total, uint32_t pieces,
@@ -206,7 +210,9 @@ __device__ inline void wave_exchange() {
 }
 
 // Up to 16 tokens. A workgroup takes 16 outputs, its waves every waves-th batch of 512 values,
-// and the waves' sums are joined in LDS in their order.
+// and the waves' sums are joined in LDS in their order. Bound by the latency of one or two batches of
+// loads a wave, which nothing hides: one 16-bit token, 14336 -> 4096 (31 MB) 8.2 us, 3.8 TB/s; with
+// twice the outputs or the batches a wave it was no faster.
 constexpr int kFewWaves = 16;
 // Bytes of a token's batch in LDS, with 64 between rows.
 constexpr int kFewPitch = kBatchK * 2 + 64;
@@ -316,7 +322,10 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
 
 // More 16-bit tokens, 16 NT at a time. The tokens' values of a batch go through LDS, two batches in
 // turn, for all waves of a workgroup; a wave takes 32 outputs, whose codes it loads a batch
-// ahead. With few outputs the batches are split over blockIdx.y, and k_mx4_join adds the parts.
+// ahead. With few outputs the batches are split over blockIdx.y, and k_mx4_join adds the parts. Bound by
+// the conversion of codes, which every 64 tokens repeat, and its loads' latency: 64 tokens, 4096 ->
+// 128000 (279 MB) 99 us, 4096 -> 14336 23 us; packed tokens, whose codes need no conversion, take 54
+// and 12.
 constexpr int kSlabWaves = kMx4SlabRows / 32;
 
 template <int NT>

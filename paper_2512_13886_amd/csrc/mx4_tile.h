@@ -4,9 +4,17 @@
 // stage has two phases in place of four:
 //   1: read A0, B0, B1   A0 B0, A0 B1   fetch A1 of the next stage
 //   2: read A1           A1 B1, A1 B0   fetch A0, B0 and B1 of the stage after it
-// so that a memory part (up to 64 KiB of LDS reads for four waves, 512 cycles) and an MFMA part
-// (32 of 16 cycles) are of one length, with half the barriers. Every load has a stage's time: both
-// waits leave the newest four half tiles in flight, one phase's A1 and the other's three.
+// so that there are half the barriers, and an MFMA part (32 of 16 cycles) is longer than the other
+// group's LDS reads (up to 64 KiB). Every load has a stage's time: both waits leave the newest four
+// half tiles in flight, one phase's A1 and the other's three.
+//
+// Bound by the direct loads, 64 KiB a stage, 18 bytes a clock and CU, and what of the MFMAs does not run
+// beside them: 8192 tokens, 4096 -> 14336 250-270 us (3.6-3.8 PFLOP/s), 40 of them the outputs' stores at
+// the tiles' ends; 4096 tokens, 14336 -> 4096 109-112 us (4.3). Without its MFMAs the loop takes 195 and
+// 76 us, without its loads 224 and 89, without the scales 243 and 103. The matrix instructions are busy
+// for 47 and 54 % of the time at 1.9 GHz; alone in registers they reach 7.4 PFLOP/s with random codes and
+// 9.2 with constant ones. Four phases took the same time as two. All operands of the next half stage read
+// while one multiplies would need about 240 registers beside the addresses, and spilled.
 //
 // The scales of two stages are 16 bytes a row: one direct load a thread brings those of the 256
 // rows of X and of W into LDS, first in phase 1 of every even stage, for the two stages after the
