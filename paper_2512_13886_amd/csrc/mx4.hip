@@ -187,15 +187,32 @@ __device__ inline void store_y4(const Mx4Args& a, int64_t tok, int64_t n, const 
     store_upto4(static_cast<bf16_t*>(a.y) + at, w, left);
 }
 
-__device__ inline void store_y8(const Mx4Args& a, int64_t tok, int64_t n, const f4& v, const f4& w) {
-  if (tok >= a.n_tok || n >= a.d_out) return;
-  const float u[8] = {v[0], v[1], v[2], v[3], w[0], w[1], w[2], w[3]};
+// 16 tokens from tok0 on and 32 outputs from n0 on, of which lane (b, i) has those from 8 b on of token i.
+// They are stored by lane 4 i + b, so that neighbouring lanes store neighbouring bytes.
+__device__ inline void store_block(const Mx4Args& a, int64_t tok0, int64_t n0, const f4& v, const f4& w) {
+  const int lane = threadIdx.x & 63, from = ((lane & 3) * 16 + (lane >> 2)) * 4;
+  const int64_t tok = tok0 + (lane >> 2), n = n0 + 8 * (lane & 3);
+  auto moved = [from](uint32_t u) { return uint32_t(__builtin_amdgcn_ds_bpermute(from, int(u))); };
   const int left = int(std::min<int64_t>(a.d_out - n, 8));
+  const bool live = tok < a.n_tok && left > 0;
   const int64_t at = tok * a.ldy + n;
-  if (a.y_f32)
-    store_upto8(static_cast<float*>(a.y) + at, u, left);
-  else
-    store_upto8(static_cast<bf16_t*>(a.y) + at, u, left);
+  if (a.y_f32) {
+    float u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = __uint_as_float(moved(__float_as_uint(e < 4 ? v[e] : w[e - 4])));
+    if (live) store_upto8(static_cast<float*>(a.y) + at, u, left);
+  } else {
+    Raw8<bf16_t> r{u32x4{moved(pack_bf16(v[0], v[1])), moved(pack_bf16(v[2], v[3])),
+                         moved(pack_bf16(w[0], w[1])), moved(pack_bf16(w[2], w[3]))}};
+    bf16_t* y = static_cast<bf16_t*>(a.y) + at;
+    if (!live) return;
+    if (left == 8)
+      *reinterpret_cast<u32x4_2*>(y) = r.w;
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < left) y[e].bits = uint16_t(r.w[e >> 1] >> (16 * (e & 1)));
+  }
 }
 
 constexpr int kBatch = 4;                 // chunks that a wave's loads go out together for
@@ -511,6 +528,7 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_mx4_tile(Mx4Args a) {
   Acc256 acc;
   mx4::mainloop(acc, src, scales + 16 * p0, std::min(2 * p1, stages) - 2 * p0, l0, l1, l2, l3, l4, l5,
                 l6, l7, s0, s1);
+  const int wm = threadIdx.x >> 8, wn = (threadIdx.x >> 6) & 3;
   f4* part = gridDim.y > 1
                  ? a.part + ((size_t(blockIdx.y) * gridDim.x + blockIdx.x) * Tile256::kWaves +
                              (threadIdx.x >> 6)) * 32 * 64 + (threadIdx.x & 63)
@@ -526,7 +544,7 @@ __global__ void __launch_bounds__(Tile256::kThreads) k_mx4_tile(Mx4Args a) {
           part[((qa * 4 + mi) * 4 + 2 * qb) * 64] = c[0];
           part[((qa * 4 + mi) * 4 + 2 * qb + 1) * 64] = c[1];
         } else {
-          store_y8(a, m0 + t256_rows_row(qa, mi), n0 + t256_rows_col(qb), c[0], c[1]);
+          store_block(a, m0 + qa * 128 + wm * 64 + mi * 16, n0 + qb * 128 + wn * 32, c[0], c[1]);
         }
       }
 }
@@ -547,10 +565,10 @@ __global__ void __launch_bounds__(kThreads) k_mx4_tile_join(Mx4Args a, int split
   const int tiles_m = int((a.n_tok + 255) / 256);
   int tm, tn;
   tile_of_block(tile, tiles, tiles_m, tiles / tiles_m, &tm, &tn);
-  const int64_t tok = int64_t(tm) * 256 + qa * 128 + (wave >> 2) * 64 + mi * 16 + (lane & 15);
-  const int64_t n = int64_t(tn) * 256 + (wave & 3) * 32 + 8 * (lane >> 4);
-  store_y8(a, tok, n, c[0], c[1]);
-  store_y8(a, tok, n + 128, c[2], c[3]);
+  const int64_t tok = int64_t(tm) * 256 + qa * 128 + (wave >> 2) * 64 + mi * 16;
+  const int64_t n = int64_t(tn) * 256 + (wave & 3) * 32;
+  store_block(a, tok, n, c[0], c[1]);
+  store_block(a, tok, n + 128, c[2], c[3]);
 }
 
 // Smaller tiles. Workgroups of one XCD (index modulo 8) take consecutive tiles, the tiles of one
@@ -600,8 +618,8 @@ __global__ void __launch_bounds__(R::kThreads) k_mx4_ring(Mx4Args a) {
   for (int mi = 0; mi < R::MB; ++mi)
 #pragma unroll
     for (int ni = 0; ni < R::NB; ni += 2)
-      store_y8(a, m0 + ((wave / R::WN) * R::MB + mi) * 16 + (lane & 15),
-               n0 + (wave % R::WN) * R::NB * 16 + ni * 16 + 8 * (lane >> 4), acc[mi][ni], acc[mi][ni + 1]);
+      store_block(a, m0 + ((wave / R::WN) * R::MB + mi) * 16, n0 + (wave % R::WN) * R::NB * 16 + ni * 16,
+                  acc[mi][ni], acc[mi][ni + 1]);
 }
 
 template <typename R>
@@ -619,8 +637,8 @@ __global__ void __launch_bounds__(kThreads) k_mx4_ring_join(Mx4Args a, int split
     for (int q = 0; q < 2; ++q) c[q] += part[sp * step + q * 64];
   const int tile = int(at / (4 * kPairs)), wave = int(at / kPairs) & 3, pair = int(at % kPairs);
   const int tn = tile / tiles_m, mi = pair / (R::NB / 2), ni = pair % (R::NB / 2) * 2;
-  store_y8(a, int64_t(tile - tn * tiles_m) * R::TM + ((wave / R::WN) * R::MB + mi) * 16 + (lane & 15),
-           int64_t(tn) * R::TN + (wave % R::WN) * R::NB * 16 + ni * 16 + 8 * (lane >> 4), c[0], c[1]);
+  store_block(a, int64_t(tile - tn * tiles_m) * R::TM + ((wave / R::WN) * R::MB + mi) * 16,
+              int64_t(tn) * R::TN + (wave % R::WN) * R::NB * 16 + ni * 16, c[0], c[1]);
 }
 
 using Ring128x128 = mx4::Ring<128, 128, 2, 2, 2>;
