@@ -176,17 +176,6 @@ struct TokenPiece {
   }
 };
 
-__device__ inline void store_y4(const Mx4Args& a, int64_t tok, int64_t n, const f4& v) {
-  if (tok >= a.n_tok || n >= a.d_out) return;
-  const float w[4] = {v[0], v[1], v[2], v[3]};
-  const int left = int(std::min<int64_t>(a.d_out - n, 4));
-  const int64_t at = tok * a.ldy + n;
-  if (a.y_f32)
-    store_upto4(static_cast<float*>(a.y) + at, w, left);
-  else
-    store_upto4(static_cast<bf16_t*>(a.y) + at, w, left);
-}
-
 // 16 tokens from tok0 on and 32 outputs from n0 on, of which lane (b, i) has those from 8 b on of token i.
 // They are stored by lane 4 i + b, so that neighbouring lanes store neighbouring bytes.
 __device__ inline void store_block(const Mx4Args& a, int64_t tok0, int64_t n0, const f4& v, const f4& w) {
@@ -338,11 +327,13 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
 }
 
 // More 16-bit tokens, 16 NT at a time. The tokens' values of a batch go through LDS, two batches in
-// turn, for all waves of a workgroup; a wave takes 32 outputs, whose codes it loads a batch
-// ahead. With few outputs the batches are split over blockIdx.y, and k_mx4_join adds the parts. Bound by
-// the conversion of codes, which every 64 tokens repeat, and its loads' latency: 64 tokens, 4096 ->
-// 128000 (279 MB) 99 us, 4096 -> 14336 23 us; packed tokens, whose codes need no conversion, take 54
-// and 12.
+// turn, for all waves of a workgroup; a wave takes 32 outputs, whose codes it loads a batch ahead, in
+// the order in which a lane's sums of both blocks are eight consecutive outputs (stored as they
+// came out of the MFMA, four by four, 8192 tokens took 1126 us in place of 1083). With few outputs the
+// batches are split over blockIdx.y, and k_mx4_join adds the parts. Bound by the conversion of codes,
+// which every 64 tokens repeat, and its loads' latency: 64 tokens, 4096 -> 128000 (279 MB) 105 us, 4096
+// -> 14336 24 us, where packed tokens, whose codes need no conversion, take 54 and 12; 8192 tokens, 4096
+// -> 14336 0.89 PFLOP/s.
 constexpr int kSlabWaves = kMx4SlabRows / 32;
 
 template <int NT>
@@ -357,7 +348,7 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
   const int64_t n0 = int64_t(blockIdx.x) * kMx4SlabRows + wave * 32;
   int64_t n[2];
 #pragma unroll
-  for (int m = 0; m < 2; ++m) n[m] = std::min(n0 + 16 * m + i, a.d_out - 1);
+  for (int m = 0; m < 2; ++m) n[m] = std::min(n0 + 8 * (i >> 2) + 4 * m + (i & 3), a.d_out - 1);
   const int batches = (a.chunks + kBatch - 1) / kBatch;
   const int b0 = int(int64_t(batches) * blockIdx.y / gridDim.y);
   const int b1 = int(int64_t(batches) * (blockIdx.y + 1) / gridDim.y);
@@ -451,26 +442,26 @@ __global__ void __launch_bounds__(64 * kSlabWaves) k_mx4_slab(Mx4Args a) {
     return;
   }
 #pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) store_y4(a, t0 + 16 * t + i, n0 + 16 * m + 4 * b, sum[m][t]);
+  for (int t = 0; t < NT; ++t) store_block(a, t0 + 16 * t, n0, sum[0][t], sum[1][t]);
 }
 
-// The parts of the outputs, added in their order. blocks: 16 x 16 outputs, of all splits' one.
+// The parts of the outputs, added in their order. blocks: 16 x 32 outputs, of all splits' one.
 template <int NT>
 __global__ void __launch_bounds__(kThreads) k_mx4_join(Mx4Args a, int splits, int64_t blocks,
                                                        int64_t per) {
   const int lane = threadIdx.x & 63;
   const int64_t at = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
   if (at >= blocks) return;
-  const f4* part = a.part + at * 64 + lane;
-  f4 sum = {0.f, 0.f, 0.f, 0.f};
+  const int64_t z = at / per, in = at - z * per;  // of 16 NT tokens
+  const int64_t wave = at / NT;
+  const int t = int(in % NT);
+  const f4* part = a.part + (wave * 2 * NT + t) * 64 + lane;
+  f4 c[2] = {};
 #pragma unroll 8
-  for (int sp = 0; sp < splits; ++sp) sum += part[sp * blocks * 64];
-  const int64_t z = at / per, in = at - z * per;  // of 64 tokens
-  const int64_t wave = in / (2 * NT);
-  const int m = int(in / NT) & 1, t = int(in % NT);
-  store_y4(a, z * 16 * NT + 16 * t + (lane & 15), wave * 32 + 16 * m + 4 * (lane >> 4), sum);
+  for (int sp = 0; sp < splits; ++sp)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) c[m] += part[(sp * blocks * 2 + m * NT) * 64];
+  store_block(a, z * 16 * NT + 16 * t, in / NT * 32, c[0], c[1]);
 }
 
 template <int NT>
@@ -480,7 +471,7 @@ void launch_slab(const Mx4Args& a, int splits, hipStream_t s) {
   hipLaunchKernelGGL((k_mx4_slab<NT>), dim3(wgs, unsigned(splits), tiles),
                      dim3(64 * kSlabWaves), 0, s, a);
   if (splits > 1) {
-    const int64_t per = int64_t(wgs) * kSlabWaves * 2 * NT, blocks = per * tiles;
+    const int64_t per = int64_t(wgs) * kSlabWaves * NT, blocks = per * tiles;
     hipLaunchKernelGGL((k_mx4_join<NT>), dim3(unsigned(ceil_div(blocks, kThreads / 64))),
                        dim3(kThreads), 0, s, a, splits, blocks, per);
   }
