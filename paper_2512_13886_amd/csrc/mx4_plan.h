@@ -77,6 +77,8 @@ inline int64_t mx4_slab_parts(int tokens, int splits, int64_t n_tok, int64_t d_o
 // batches. The constants fit 90 sizes of 9 to 64 tokens; the choice is 1.7 % off the best on average.
 // 16 tokens, 4096 -> 14336: few 17.1 us, slabs of 16 16.2; -> 4096 6.9 and 10.0; 64 tokens,
 // 768 -> 14336 8.7 us in slabs of 16, 13.5 in slabs of 64; 4096 -> 14336 23 in slabs of 32, 22.4 of 64.
+// More tokens: slabs of 32 where those of 64 leave a round nearly empty (777 tokens, 4097 -> 5001 64 us and
+// 87; 128, 1000 -> 5000 9.9 and 13.1; but 1024, 4096 -> 14336 183 and 153).
 inline Mx4SlabPlan mx4_slab_plan(int64_t n_tok, int64_t d, int64_t d_out) {
   Mx4SlabPlan best{0, 1};
   if (n_tok <= kMx4Fewest) return best;
@@ -88,7 +90,7 @@ inline Mx4SlabPlan mx4_slab_plan(int64_t n_tok, int64_t d, int64_t d_out) {
     best_us = 1.35 + 2.9 * double(rounds) + 0.1 * double(n_tok) + bytes / 3.9e6;
   }
   for (const int tokens : {16, 32, 64}) {
-    if (n_tok > 64 ? tokens < 64 : tokens > 16 && n_tok <= tokens / 2) continue;
+    if (n_tok > 64 ? tokens < (n_tok > 16384 ? 64 : 32) : tokens > 16 && n_tok <= tokens / 2) continue;
     const double around = tokens == 16 ? 2.4 : tokens == 32 ? 3.2 : 4.0;
     const double batch = tokens == 16 ? 2.43 : tokens == 32 ? 2.66 : 3.62;
     const int64_t tiles = ceil_div(n_tok, tokens) * ceil_div(d_out, kMx4SlabRows);

@@ -33,7 +33,8 @@ TILES = {(4096, 2000, 4096): (0, False), (2000, 14336, 4096): (0, True), (1000, 
          (96, 2000, 256): (3, False), (96, 4096, 1000): (3, True), (8, 14336, 20000): (2, False)}
 SLABS = {(16, 4096, 14336): (0, False), (64, 1000, 14336): (16, False), (9, 14336, 4096): (16, True),
          (64, 200, 20000): (32, False), (17, 4096, 14336): (32, True), (64, 600, 70000): (64, False),
-         (33, 14336, 14336): (64, True), (100, 4096, 14336): (64, True)}
+         (33, 14336, 14336): (64, True), (100, 4096, 14336): (32, False), (300, 4096, 4096): (64, True),
+         (96, 4096, 4096): (32, True)}
 
 
 @pytest.fixture(scope="module")
