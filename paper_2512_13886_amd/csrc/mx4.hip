@@ -41,22 +41,8 @@ __device__ inline uint32_t quad_max(uint32_t m) {
   return max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0x4E, 0xF, 0xF, true)));  // 2 3 0 1
 }
 
-// Thirty-two lanes for 256 values, one dword (eight codes) each: a block's largest takes two exchanges of
-// neighbouring lanes, and its scale, a power of two, leaves the quotients exact, so that one rounding
-// is all there is. Bound by HBM: 14336 x 4096 fp32 in 54 us, 4.9 TB/s, the rate of a copy.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, uint32_t total,
-                                                       uint32_t pieces, int d, uint8_t* Q,
-                                                       uint8_t* scales, int srow) {
-  const uint32_t idx = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-  const bool live = idx < total;  // of all 32 lanes
-  const int64_t n = live ? idx / pieces : 0u;
-  const int h = live ? int(idx % pieces) : 0;
-  const int i = threadIdx.x & 31;
-  Raw8<T> raw;
-  load_piece(raw, X + n * ldx, 256 * h + 8 * i, live ? d : 0);
-  float v[8];
-  values8(raw, v);
+// Eight values to codes, by the four lanes of a block; s: the block's scale.
+__device__ inline uint32_t codes8(const float (&v)[8], uint32_t& s) {
   uint32_t m = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
@@ -65,7 +51,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, 
   // block has codes 0: NaN as values.
   const uint32_t top = m >> 23;
   const bool fine = top < 255u;
-  const uint32_t s = fine ? max(top, 2u) - 2u : 255u;
+  s = fine ? max(top, 2u) - 2u : 255u;
   const float inv = __uint_as_float((254u - s) << 23);  // 2^(127 - s): the quotients are exact
   uint32_t q = 0;
   if (fine) {
@@ -74,17 +60,56 @@ __global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, 
     q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4] * inv, v[5] * inv, 1.f, 2);
     q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6] * inv, v[7] * inv, 1.f, 3);
   }
-  // Lanes 0 .. 15 hold the first 128 values, 16 .. 31 the second, whose scales are neighbours.
-  const uint32_t both = s | uint32_t(__shfl_xor(int(s), 16, 64)) << 8;
-  if (!live) return;
-  *reinterpret_cast<uint32_t*>(Q + (n * pieces + h) * 128 + 4 * i) = q;
-  if (i < 16 && (i & 3) == 0) {
-    uint8_t* at = scales + n * srow + 16 * (h >> 1) + i + 2 * (h & 1);
-    if ((h & 1) == 0 && h + 1 == int(pieces))  // the row's padding
-      *reinterpret_cast<uint32_t*>(at) = both;
-    else
-      *reinterpret_cast<uint16_t*>(at) = uint16_t(both);
+  return q;
+}
+
+// Thirty-two lanes for H pieces of 256 values, eight codes of each a lane: a block's largest takes two
+// exchanges of neighbouring lanes, and its scale, a power of two, leaves the quotients exact, so that
+// one rounding is all there is. Bound by HBM: 14336 x 4096 in 52 us from fp32, 5.1 TB/s, and 28 from bf16,
+// 5.3 TB/s. Two pieces, for bf16 rows of more than one: 8192 x 4096 19.8 to 17.9 us; but fp32 at
+// 14336 x 4096 51.9 to 52.9, and 100000 x 64 13.9 to 17.6.
+template <typename T, int H>
+__global__ void __launch_bounds__(kThreads) k_mx4_pack(const T* X, int64_t ldx, uint32_t total,
+                                                       uint32_t each, int d, uint8_t* Q, int row,
+                                                       uint8_t* scales, int srow) {
+  const uint32_t idx = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const bool live = idx < total;  // of all 32 lanes
+  const int64_t n = live ? idx / each : 0u;
+  const int at = live ? int(idx % each) * H : 0, pieces = row / 128;
+  const int i = threadIdx.x & 31;
+  Raw8<T> raw[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) load_piece(raw[h], X + n * ldx, 256 * (at + h) + 8 * i, live ? d : 0);
+  uint32_t q[H], sc = 0;
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    float v[8];
+    values8(raw[h], v);
+    uint32_t s;
+    q[h] = codes8(v, s);
+    // Lanes 0 .. 15 hold the first 128 values, 16 .. 31 the second, whose scales are neighbours. A
+    // piece past the row's has the padding's scales of 0.
+    s |= uint32_t(__shfl_xor(int(s), 16, 64)) << 8;
+    if (at + h < pieces) sc |= s << (16 * h);
   }
+  if (!live) return;
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+    if (at + h < pieces) *reinterpret_cast<uint32_t*>(Q + n * row + (at + h) * 128 + 4 * i) = q[h];
+  if (i < 16 && (i & 3) == 0) {
+    uint8_t* to = scales + n * srow + 16 * (at >> 1) + i + 2 * (at & 1);
+    if (H == 2 || ((at & 1) == 0 && at + 1 == pieces))  // with the padding's
+      *reinterpret_cast<uint32_t*>(to) = sc;
+    else
+      *reinterpret_cast<uint16_t*>(to) = uint16_t(sc);
+  }
+}
+template <typename T, int H>
+void launch_pack(const void* X, int64_t ldx, int64_t n, int64_t d, void* Q, void* scales, hipStream_t s) {
+  const uint32_t each = uint32_t(ceil_div(d, 256 * H)), total = uint32_t(n * each);  // below 2^27
+  hipLaunchKernelGGL((k_mx4_pack<T, H>), dim3(unsigned(ceil_div(total, kThreads / 32))), dim3(kThreads), 0,
+                     s, static_cast<const T*>(X), ldx, total, each, int(d), static_cast<uint8_t*>(Q),
+                     int(row_bytes(d)), static_cast<uint8_t*>(scales), int(scale_bytes(d)));
 }
 
 // The values, exact in either type. Bound by HBM's writes: 14336 x 4096 to bf16 in 23 us, 6.5 TB/s with
@@ -703,16 +728,9 @@ size_t mx4_scale_bytes(int64_t d) { return size_t(scale_bytes(d)); }
 
 optima_status mx4_pack(const void* X, int64_t ldx, int dtype, int64_t n, int64_t d, void* Q,
                        void* scales, hipStream_t s) {
-  const uint32_t pieces = uint32_t(ceil_div(d, 256)), total = uint32_t(n * pieces);  // below 2^27
-  const int srow = int(scale_bytes(d));
-  const dim3 grid(unsigned(ceil_div(total, kThreads / 32)));
-  uint8_t *q = static_cast<uint8_t*>(Q), *sc = static_cast<uint8_t*>(scales);
-  if (dtype == OPTIMA_DTYPE_BF16)
-    hipLaunchKernelGGL(k_mx4_pack<bf16_t>, grid, dim3(kThreads), 0, s,
-                       static_cast<const bf16_t*>(X), ldx, total, pieces, int(d), q, sc, srow);
-  else
-    hipLaunchKernelGGL(k_mx4_pack<float>, grid, dim3(kThreads), 0, s, static_cast<const float*>(X),
-                       ldx, total, pieces, int(d), q, sc, srow);
+  if (dtype == OPTIMA_DTYPE_F32) launch_pack<float, 1>(X, ldx, n, d, Q, scales, s);
+  else if (d <= 256) launch_pack<bf16_t, 1>(X, ldx, n, d, Q, scales, s);
+  else launch_pack<bf16_t, 2>(X, ldx, n, d, Q, scales, s);
   OPTIMA_LAUNCH_CHECK();
   return OPTIMA_OK;
 }
