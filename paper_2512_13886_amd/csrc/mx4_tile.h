@@ -9,9 +9,9 @@
 // half tiles in flight, one phase's A1 and the other's three.
 //
 // Bound by the direct loads, 64 KiB a stage, 18 bytes a clock and CU, and what of the MFMAs does not run
-// beside them: 8192 tokens, 4096 -> 14336 250-270 us (3.6-3.8 PFLOP/s), 40 of them the outputs' stores at
-// the tiles' ends; 4096 tokens, 14336 -> 4096 109-112 us (4.3). Without its MFMAs the loop takes 195 and
-// 76 us, without its loads 224 and 89, without the scales 243 and 103. The matrix instructions are busy
+// beside them: 8192 tokens, 4096 -> 14336 250 us (3.8 PFLOP/s), 30 of them the outputs' stores at the
+// tiles' ends; 4096 tokens, 14336 -> 4096 105 us (4.6). Of 265 and 112 us it took 195 and 76 without its
+// MFMAs, 224 and 89 without its loads, 243 and 103 without the scales. The matrix instructions are busy
 // for 47 and 54 % of the time at 1.9 GHz; alone in registers they reach 7.4 PFLOP/s with random codes and
 // 9.2 with constant ones. Four phases took the same time as two. All operands of the next half stage read
 // while one multiplies would need about 240 registers beside the addresses, and spilled.
