@@ -242,8 +242,8 @@ __device__ inline void wave_exchange() {
 
 // Up to 16 tokens. A workgroup takes 16 outputs, its waves every waves-th batch of 512 values,
 // and the waves' sums are joined in LDS in their order. Bound by the latency of one or two batches of
-// loads a wave, which nothing hides: one 16-bit token, 14336 -> 4096 (31 MB) 8.2 us, 3.8 TB/s; with
-// twice the outputs or the batches a wave it was no faster.
+// loads a wave, which nothing hides: one 16-bit token, 14336 -> 4096 (31 MB) 8.2 us, 3.8 TB/s, with
+// weights that no cache holds 9.5. Twice the outputs a workgroup took 12.8, codes loaded a batch ahead 12.2.
 constexpr int kFewWaves = 16;
 // Bytes of a token's batch in LDS, with 64 between rows.
 constexpr int kFewPitch = kBatchK * 2 + 64;

@@ -171,12 +171,14 @@ def test_linear_of_many_packed_tokens(L, n, d, ff):
 def test_every_tile(L, n, d, ff):
     Q, s, w = _weights(L, ff, d, 5)
     _check(L, _tokens(n, d, 6), Q, s, w, torch.float32, True, pad=1)
+    _check(L, _tokens(n, d, 7), Q, s, w, torch.bfloat16, True)
 
 
 @pytest.mark.parametrize("n, d, ff", sorted(SLABS))
 def test_every_slab(L, n, d, ff):
     Q, s, w = _weights(L, ff, d, 5)
     _check(L, _tokens(n, d, 6), Q, s, w, torch.float32, False, pad=1)
+    _check(L, _tokens(n, d, 7), Q, s, w, torch.bfloat16, False)
 
 
 @pytest.mark.parametrize("packed", (False, True))
