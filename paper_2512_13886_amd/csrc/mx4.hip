@@ -685,22 +685,29 @@ void launch_tile(const Mx4Args& a, hipStream_t s) {
 
 template <bool PACKED, int ROWS, int RB, bool RAGGED>
 void launch_few(const Mx4Args& a, hipStream_t s) {
-  // As many waves as there are batches, and as the CU's LDS holds tokens for.
+  // As many waves as there are batches, and as the CU's LDS holds tokens for; eight where several
+  // workgroups of two blocks, or of more than four tokens, can share a CU (8 tokens, 8192 -> 10240 22.0 to 18.4 us;
+  // one block of one token, 8192 -> 9000 14.4 in place of 14.0).
+  const unsigned wgs = unsigned(ceil_div(a.d_out, 16 * RB));
   const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kFewPitch, RB * 1024);
-  const int most = int(std::min<size_t>(kFewWaves, (size_t(160) << 10) / each));
+  const int cap = wgs > 256 && (RB > 1 || a.n_tok > 4) ? 8 : kFewWaves;
+  const int most = int(std::min<size_t>(cap, (size_t(160) << 10) / each));
   const int waves = int(std::min<int64_t>(ceil_div(a.chunks, kBatch), most));
-  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB, RAGGED>), dim3(unsigned(ceil_div(a.d_out, 16 * RB))),
-                     dim3(64 * waves), waves * each, s, a);
+  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB, RAGGED>), dim3(wgs), dim3(64 * waves), waves * each, s, a);
 }
 template <int ROWS, int RB>
 void launch_few_16bit(const Mx4Args& a, hipStream_t s) {
   if (a.d % 8) launch_few<false, 4, RB, true>(a, s);
   else launch_few<false, ROWS, RB, false>(a, s);
 }
-// Two blocks of outputs where every CU still has a workgroup: they halve what is read of the
-// tokens. 16 tokens, 4096 -> 8192 12.4 to 9.3 us, -> 14336 22.3 to 16.8, but -> 1000 with d = 1000 5.9
-// to 6.8; one token, 14336 -> 4096 9.4 to 12.8.
-bool two_blocks(const Mx4Args& a) { return a.d_out > 32 * 255; }
+// Two blocks of outputs halve what is read of the tokens, where that outweighs fewer workgroups than CUs
+// can share evenly. us in one and two: 16 tokens, 4096 -> 9000 16.1 and 15.4, d = 1000 -> 1000 5.9 and 6.8; 8
+// tokens, 8192 -> 12288 19.6 and 20.4, -> 17000 28.5 and 27.7; 4 tokens, 4096 -> 12288 9.3 and 10.2, ->
+// 128000 65 and 60; one token, 8192 -> 10240 13.3 and 15.7, 4096 -> 128000 57 and 63.
+bool two_blocks(const Mx4Args& a) {
+  const int64_t wgs = ceil_div(a.d_out, 32);
+  return a.n_tok > 8 ? wgs > 255 : a.n_tok > 4 ? wgs > 384 : a.n_tok > 1 && wgs > 2048;
+}
 
 void launch_packed(const Mx4Args& a, hipStream_t s) {
   // Every 16 or 32 outputs of the few-token kernel read all tokens again. us with it and in tiles: 16
