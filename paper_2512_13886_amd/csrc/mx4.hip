@@ -244,9 +244,7 @@ __device__ inline void wave_exchange() {
 // and the waves' sums are joined in LDS in their order. Bound by the latency of one or two batches of
 // loads a wave, which nothing hides: one 16-bit token, 14336 -> 4096 (31 MB) 8.2 us, 3.8 TB/s, with
 // weights that no cache holds 9.5. Twice the outputs a workgroup took 12.8, codes loaded a batch ahead 12.2.
-constexpr int kFewWaves = 16;
-// Bytes of a token's batch in LDS, with 64 between rows.
-constexpr int kFewPitch = kBatchK * 2 + 64;
+static_assert(kMx4FewPitch == kBatchK * 2 + 64, "a token's batch, with 64 bytes between rows");
 
 // A batch's codes and scales of row n: zeros for chunks past the row's end.
 __device__ inline void load_codes(u32x4 (&w)[kBatch], uint32_t& s, const uint8_t* q,
@@ -264,7 +262,7 @@ __device__ inline void load_codes(u32x4 (&w)[kBatch], uint32_t& s, const uint8_t
 // ROWS: tokens that a lane loads values of together; RB: blocks of 16 outputs; RAGGED: 16-bit tokens of
 // a width that is no multiple of 8.
 template <bool PACKED, int ROWS, int RB, bool RAGGED>
-__global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
+__global__ void __launch_bounds__(64 * kMx4FewWaves) k_mx4_few(Mx4Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   float* part = reinterpret_cast<float*>(lds);  // [wave][lane][4], at the end
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -272,7 +270,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
   const int64_t n0 = int64_t(blockIdx.x) * 16 * RB;
   const int tok = std::min(i, tokens - 1), batches = (a.chunks + kBatch - 1) / kBatch;
   const bf16_t* x = static_cast<const bf16_t*>(a.x);
-  char* mine = lds + wave * tokens * kFewPitch;
+  char* mine = lds + wave * tokens * kMx4FewPitch;
   f4 sum[RB];
 #pragma unroll
   for (int m = 0; m < RB; ++m) sum[m] = f4{0.f, 0.f, 0.f, 0.f};
@@ -313,7 +311,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
           if (r0 + r < tokens)
-            *reinterpret_cast<u32x4*>(mine + (r0 + r) * kFewPitch + 16 * lane) = v[r];
+            *reinterpret_cast<u32x4*>(mine + (r0 + r) * kMx4FewPitch + 16 * lane) = v[r];
       }
       wave_exchange();
       auto chunk = [&](auto u) {
@@ -321,7 +319,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_mx4_few(Mx4Args a) {
         bf16x8 f[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          f[j] = *reinterpret_cast<const bf16x8*>(mine + tok * kFewPitch +
+          f[j] = *reinterpret_cast<const bf16x8*>(mine + tok * kMx4FewPitch +
                                                   (U * kChunk + 32 * b + 8 * j) * 2);
 #pragma unroll
         for (int m = 0; m < RB; ++m) mfma_bf16<U>(sum[m], w[m][U], s[m], f);
@@ -684,48 +682,36 @@ void launch_tile(const Mx4Args& a, hipStream_t s) {
 }
 
 template <bool PACKED, int ROWS, int RB, bool RAGGED>
-void launch_few(const Mx4Args& a, hipStream_t s) {
-  // As many waves as there are batches, and as the CU's LDS holds tokens for; eight where several
-  // workgroups of two blocks, or of more than four tokens, can share a CU (8 tokens, 8192 -> 10240 22.0 to 18.4 us;
-  // one block of one token, 8192 -> 9000 14.4 in place of 14.0).
-  const unsigned wgs = unsigned(ceil_div(a.d_out, 16 * RB));
-  const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kFewPitch, RB * 1024);
-  const int cap = wgs > 256 && (RB > 1 || a.n_tok > 4) ? 8 : kFewWaves;
-  const int most = int(std::min<size_t>(cap, (size_t(160) << 10) / each));
-  const int waves = int(std::min<int64_t>(ceil_div(a.chunks, kBatch), most));
-  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB, RAGGED>), dim3(wgs), dim3(64 * waves), waves * each, s, a);
+void launch_few(const Mx4Args& a, int waves, hipStream_t s) {
+  const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kMx4FewPitch, RB * 1024);
+  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB, RAGGED>), dim3(unsigned(ceil_div(a.d_out, 16 * RB))),
+                     dim3(64 * waves), waves * each, s, a);
 }
 template <int ROWS, int RB>
-void launch_few_16bit(const Mx4Args& a, hipStream_t s) {
-  if (a.d % 8) launch_few<false, 4, RB, true>(a, s);
-  else launch_few<false, ROWS, RB, false>(a, s);
-}
-// Two blocks of outputs halve what is read of the tokens, where that outweighs fewer workgroups than CUs
-// can share evenly. us in one and two: 16 tokens, 4096 -> 9000 16.1 and 15.4, d = 1000 -> 1000 5.9 and 6.8; 8
-// tokens, 8192 -> 12288 19.6 and 20.4, -> 17000 28.5 and 27.7; 4 tokens, 4096 -> 12288 9.3 and 10.2, ->
-// 128000 65 and 60; one token, 8192 -> 10240 13.3 and 15.7, 4096 -> 128000 57 and 63.
-bool two_blocks(const Mx4Args& a) {
-  const int64_t wgs = ceil_div(a.d_out, 32);
-  return a.n_tok > 8 ? wgs > 255 : a.n_tok > 4 ? wgs > 384 : a.n_tok > 1 && wgs > 2048;
+void launch_few_16bit(const Mx4Args& a, int waves, hipStream_t s) {
+  if (a.d % 8) launch_few<false, 4, RB, true>(a, waves, s);
+  else launch_few<false, ROWS, RB, false>(a, waves, s);
 }
 
 void launch_packed(const Mx4Args& a, hipStream_t s) {
   // Every 16 or 32 outputs of the few-token kernel read all tokens again. us with it and in tiles: 16
-  // tokens, 4096 -> 4096 5.6 and 9.6, -> 14336 12.6 and 11.5; 8 tokens, 4096 -> 14336 10.9 and 11.3,
-  // -> 128000 70 and 55; one token, -> 128000 55 and 57.
-  if (a.n_tok > kMx4Few || a.n_tok * a.d_out > 131072) launch_tile(a, s);
-  else if (two_blocks(a)) launch_few<true, 4, 2, false>(a, s);
-  else launch_few<true, 4, 1, false>(a, s);
+  // tokens, 4096 -> 4096 5.5 and 9.4, -> 9000 10.8 and 10.1, -> 60000 35 and 33; 8 tokens, 8192 -> 28672 33 and
+  // 41, 4096 -> 60000 31.4 and 29.8, -> 128000 60 and 55; one token, -> 128000 53 and 56.
+  const Mx4FewPlan p = mx4_few_plan(a.n_tok, a.d, a.d_out, true);
+  if (a.n_tok > kMx4Few || a.n_tok * a.d_out >= (a.n_tok > 8 ? 100000 : 240000)) launch_tile(a, s);
+  else if (p.blocks == 2) launch_few<true, 4, 2, false>(a, p.waves, s);
+  else launch_few<true, 4, 1, false>(a, p.waves, s);
 }
 void launch_16bit(const Mx4Args& a, hipStream_t s) {
   const Mx4SlabPlan p = mx4_slab_plan(a.n_tok, a.d, a.d_out);
+  const Mx4FewPlan few = mx4_few_plan(a.n_tok, a.d, a.d_out, false);
   if (p.tokens == 16) launch_slab<1>(a, p.splits, s);
   else if (p.tokens == 32) launch_slab<2>(a, p.splits, s);
   else if (p.tokens == 64) launch_slab<4>(a, p.splits, s);
-  else if (a.n_tok > 4 && two_blocks(a)) launch_few_16bit<8, 2>(a, s);
-  else if (a.n_tok > 4) launch_few_16bit<8, 1>(a, s);
-  else if (two_blocks(a)) launch_few_16bit<4, 2>(a, s);
-  else launch_few_16bit<4, 1>(a, s);
+  else if (a.n_tok > 4 && few.blocks == 2) launch_few_16bit<8, 2>(a, few.waves, s);
+  else if (a.n_tok > 4) launch_few_16bit<8, 1>(a, few.waves, s);
+  else if (few.blocks == 2) launch_few_16bit<4, 2>(a, few.waves, s);
+  else launch_few_16bit<4, 1>(a, few.waves, s);
 }
 
 }  // namespace

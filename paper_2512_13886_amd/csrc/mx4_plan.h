@@ -60,6 +60,38 @@ inline Mx4Plan mx4_plan(int64_t n_tok, int64_t d, int64_t d_out) {
   return best;
 }
 
+// The few-token kernel: blocks of 16 outputs that a workgroup takes, and its waves.
+struct Mx4FewPlan {
+  int blocks, waves;
+};
+constexpr int kMx4FewWaves = 16;
+constexpr int kMx4FewPitch = 512 * 2 + 64;  // bytes of a 16-bit token's 512 values in LDS
+
+// Two blocks halve what is read of the tokens, where that outweighs fewer workgroups than CUs can share
+// evenly. us in one and two: 16 tokens, 4096 -> 9000 16.1 and 15.4, d = 1000 -> 1000 5.9 and 6.8; 8 tokens,
+// 8192 -> 12288 19.6 and 20.4, -> 17000 28.5 and 27.7; 4 tokens, 4096 -> 12288 9.3 and 10.2, -> 128000 65
+// and 60; one token, 8192 -> 10240 13.3 and 15.7, 4096 -> 128000 57 and 63.
+// As many waves as there are batches of 512 values, and as the CU's LDS holds tokens for; eight where
+// several workgroups of two blocks, or of more than four tokens, can share a CU (8 tokens, 8192 -> 10240
+// 22.0 to 18.4 us; but one block of one token, 8192 -> 9000 14.4 in place of 14.0).
+inline Mx4FewPlan mx4_few_plan(int64_t n_tok, int64_t d, int64_t d_out, bool packed) {
+  const int64_t pairs = ceil_div(d_out, 32), batches = ceil_div(d, 512);
+  const bool two = n_tok > 8 ? pairs > 255 : n_tok > 4 ? pairs > 384 : n_tok > 1 && pairs > 2048;
+  const int cap = two || (ceil_div(d_out, 16) > 256 && n_tok > 4) ? 8 : kMx4FewWaves;
+  const int64_t lds = packed ? cap : 163840 / (n_tok * kMx4FewPitch);
+  return {two ? 2 : 1, int(std::min({batches, lds, int64_t(cap)}))};
+}
+// Of up to kMx4Few 16-bit tokens, in microseconds: rounds of the workgroups that the CUs hold, and the
+// batches that a CU takes. The constants fit 84 sizes of 9 to 16 tokens, 4.6 % off on average.
+inline double mx4_few_us(int64_t n_tok, int64_t d, int64_t d_out) {
+  const Mx4FewPlan p = mx4_few_plan(n_tok, d, d_out, false);
+  const int64_t batches = ceil_div(d, 512), each = ceil_div(ceil_div(d_out, 16 * p.blocks), 256);
+  const int64_t share = std::min<int64_t>({32 / p.waves, 163840 / (p.waves * n_tok * kMx4FewPitch), 8});
+  const double rounds = double(ceil_div(each, std::max<int64_t>(share, 1)));
+  return 2.1 + rounds * (1.36 + 0.58 * double(ceil_div(batches, p.waves))) +
+         (2.75 + 2.13 / 16 * double(n_tok)) * double(each * batches * p.blocks) / 16;
+}
+
 // 16-bit tokens: the few-token kernel (tokens 0), or slabs of 16, 32 or 64 tokens and 256 outputs.
 struct Mx4SlabPlan {
   int tokens, splits;
@@ -73,9 +105,9 @@ inline int64_t mx4_slab_parts(int tokens, int splits, int64_t n_tok, int64_t d_o
 }
 
 // The least estimate, in microseconds, as above: batches of 512 values of a slab's workgroup, one a
-// CU, 9 TB/s for operands and outputs, and the join; of the few-token kernel rounds of its waves'
-// batches. The constants fit 90 sizes of 9 to 64 tokens; the choice is 1.7 % off the best on average.
-// 16 tokens, 4096 -> 14336: few 17.1 us, slabs of 16 16.2; -> 4096 6.9 and 10.0; 64 tokens,
+// CU, 9 TB/s for operands and outputs, and the join. The constants fit 90 sizes of 9 to 64 tokens; the
+// choice is 1.7 % off the best on average, between slabs and the few-token kernel 0.2 % of 84 sizes of 9 to 16
+// tokens, 5 % at most. 16 tokens, 4096 -> 4096: few 6.8 us, slabs 10.9; -> 128000 118 and 73. 64 tokens,
 // 768 -> 14336 8.7 us in slabs of 16, 13.5 in slabs of 64; 4096 -> 14336 23 in slabs of 32, 22.4 of 64.
 // More tokens: slabs of 32 where those of 64 leave a round nearly empty (777 tokens, 4097 -> 5001 64 us and
 // 87; 128, 1000 -> 5000 9.9 and 13.1; but 1024, 4096 -> 14336 183 and 153).
@@ -85,10 +117,7 @@ inline Mx4SlabPlan mx4_slab_plan(int64_t n_tok, int64_t d, int64_t d_out) {
   const int64_t batches = ceil_div(d, 512);
   const double bytes = double(d) * double(d_out) * 0.53 + 2.0 * double(n_tok) * double(d + d_out);
   double best_us = 1e30;
-  if (n_tok <= kMx4Few) {
-    const int64_t rounds = ceil_div(batches, std::min<int64_t>(batches, 163840 / (n_tok * 1088)));
-    best_us = 1.35 + 2.9 * double(rounds) + 0.1 * double(n_tok) + bytes / 3.9e6;
-  }
+  if (n_tok <= kMx4Few) best_us = mx4_few_us(n_tok, d, d_out);
   for (const int tokens : {16, 32, 64}) {
     if (n_tok > 64 ? tokens < (n_tok > 16384 ? 64 : 32) : tokens > 16 && n_tok <= tokens / 2) continue;
     const double around = tokens == 16 ? 2.4 : tokens == 32 ? 3.2 : 4.0;

@@ -30,8 +30,9 @@ int main(int argc, char** argv) {
 # Sizes of tests/test_gpu_mx4.py: packed tokens (tile, whether split), and 16-bit ones (tokens of a slab).
 TILES = {(4096, 2000, 4096): (0, False), (2000, 14336, 4096): (0, True), (1000, 2000, 4096): (1, False),
          (272, 8192, 3651): (1, True), (400, 2000, 4096): (2, False), (392, 10000, 2897): (2, True),
-         (96, 2000, 256): (3, False), (96, 4096, 1000): (3, True), (8, 14336, 20000): (2, False)}
-SLABS = {(16, 4096, 14336): (0, False), (64, 1000, 14336): (16, False), (9, 14336, 4096): (16, True),
+         (96, 2000, 256): (3, False), (96, 4096, 1000): (3, True), (8, 600, 60000): (2, False),
+         (8, 4096, 40000): (3, False)}
+SLABS = {(16, 4096, 14336): (16, True), (64, 1000, 14336): (16, False), (9, 14336, 4096): (0, False),
          (64, 200, 20000): (32, False), (17, 4096, 14336): (32, True), (64, 600, 70000): (64, False),
          (33, 14336, 14336): (64, True), (100, 4096, 14336): (32, False), (300, 4096, 4096): (64, True),
          (96, 4096, 4096): (32, True)}
