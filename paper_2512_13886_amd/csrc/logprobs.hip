@@ -527,17 +527,20 @@ constexpr int64_t kMostTasks = int64_t(1) << 22;  // of a launch, in workgroups
 //
 // Parts of a workgroup's row: for few rows as many as give every second CU a workgroup, of 8192
 // values at least, since the join is a launch (one row of 128000 14.6 us in one part, 6.6 in 15; 100
-// of 9000 with 5 alternatives 9 and 13 in two); of 16384 where the last rows would otherwise leave CUs
+// of 9000 with 5 alternatives 9 and 13 in two), or of 16384 bf16 ones with alternatives, whose search
+// takes as long for fewer (64 rows of 32000 with 20 15.3 to 13.4, one of 20000 with 5 11.1 to 8.8; but one
+// of 128000 in fp32 with 32 14.9 to 17.5); of 16384 where the last rows would otherwise leave CUs
 // idle for long (8192 rows of 128000 420 us in one, 370 in seven); and of kPartLen at most with
 // alternatives, whose list is kept for a part.
 struct LogprobPlan {
   int lanes, parts, len;
 };
 constexpr int64_t kFewRows = 512, kFewLen = 8192, kManyValues = int64_t(1) << 29, kManyLen = 16384;
-LogprobPlan plan(int64_t n, int64_t vocab, int k) {
+LogprobPlan plan(int64_t n, int64_t vocab, int k, int dtype) {
   if (vocab <= 128 && !k) return {16, 1, int(vocab)};
   if (vocab <= (n >= 4096 ? 8192 : 2048)) return {64, 1, int(vocab)};
-  int64_t parts = std::min<int64_t>({kFewRows / std::max<int64_t>(n, 1), vocab / kFewLen, 64});
+  const int64_t least = k && dtype == OPTIMA_DTYPE_BF16 ? 2 * kFewLen : kFewLen;
+  int64_t parts = std::min<int64_t>({kFewRows / std::max<int64_t>(n, 1), vocab / least, 64});
   if (n * vocab >= kManyValues) parts = std::max(parts, vocab / kManyLen);
   if (k) parts = std::max(parts, ceil_div(vocab, kPartLen));
   const int64_t len = round_up(ceil_div(vocab, std::max<int64_t>(parts, 1)), 8);
@@ -607,7 +610,7 @@ optima_status token_logprobs(const void* X, int64_t ldx, int dtype, int64_t n, i
                              const int64_t* tokens, float scale, float* logp, float* lse,
                              float* entropy, int64_t k, int64_t* top_index, float* top_logp,
                              void* ws, hipStream_t s) {
-  const LogprobPlan p = plan(n, vocab, int(k));
+  const LogprobPlan p = plan(n, vocab, int(k), dtype);
   uint64_t* keys = static_cast<uint64_t*>(ws);
   float* stat = keys ? reinterpret_cast<float*>(keys + size_t(n) * p.parts * size_t(k)) : nullptr;
   LogprobArgs a{X, tokens, logp, lse, entropy, top_logp, top_index, stat, keys, ldx, n, 0,
