@@ -610,9 +610,10 @@ optima_status optima_token_logprobs(const void* X, int64_t ldx, int dtype, int64
  *   dX = scale * (dlogp (onehot(token) - p) - dentropy p (log p + entropy) + dlse p)
  * with p = exp(z - lse). dlogp (with tokens), dentropy (with entropy) and dlse: fp32 [n], each
  * nullable, one at least. A row without a token has no part of dlogp; one whose token is vocab or
- * more is NaN; one whose lse is below -1e30 (nothing but masks) has gradient 0. p is as exact as
- * lse, within |lse| 2^-24 of itself. dX: [n][lddx] of X's dtype, and may be X itself (same pointer
- * and pitch). */
+ * more is NaN; one whose lse is below -1e30 (nothing but masks) has gradient 0. Where |lse| is more
+ * than 256 and the row's own (within |lse| 2^-22), p is worked out from the row itself, so that common
+ * offsets, as a mask of -1e9 on all of a row, cost no accuracy; elsewhere it is as exact as lse, within
+ * |lse| 2^-24 of itself. dX: [n][lddx] of X's dtype, and may be X itself (same pointer and pitch). */
 optima_status optima_token_logprobs_backward(const void* X, int64_t ldx, int dtype, int64_t n,
                                              int64_t vocab, const int64_t* tokens, float scale,
                                              const float* lse, const float* entropy,

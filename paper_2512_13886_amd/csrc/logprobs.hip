@@ -477,9 +477,60 @@ struct LogprobGradArgs {
   float scale;
 };
 
+// p = exp(z - lse) has the error of lse, |lse| 2^-24 at least. Past this |lse| (2^-16 of p) it comes from
+// the row itself: z - lse = scale (x - m) - ln S.
+constexpr float kFarLse = 256.f;
+
+// m and S (in every lane) of a row of the gradient, read again.
+template <typename T, int LANES>
+__device__ inline Sums row_sums(const T* x, int vocab, int t, float c) {
+  constexpr int kStep = 8 * LANES, kMany = LANES > 64 ? kGroups / 2 : 1;
+  Sums s = {-__builtin_inff(), 0.f, 0.f};
+  for (int at = 8 * t; at - 8 * t < vocab; at += kMany * kStep) {
+    Raw8<T> raw[kMany];
+#pragma unroll
+    for (int u = 0; u < kMany; ++u) load_piece(raw[u], x, at + u * kStep, vocab);
+#pragma unroll
+    for (int u = 0; u < kMany; ++u) {
+      float v[8], m = s.m;
+      values8(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (at + u * kStep + e >= vocab) v[e] = -__builtin_inff();
+        m = max3(m, v[e], v[e]);
+      }
+      if (m > s.m) rebase(s, m, c);
+      const float ref = finite_max(m);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s.s += __builtin_amdgcn_exp2f((v[e] - ref) * c);
+    }
+  }
+  s = lanes_sums<(LANES < 64 ? LANES : 64)>(s, c);
+  if constexpr (LANES < 64) s.s = __shfl(s.s, 0, LANES);
+  if constexpr (LANES > 64) {
+    __shared__ float red[LANES / 64][2];
+    if ((t & 63) == 0) red[t >> 6][0] = s.m, red[t >> 6][1] = s.s;
+    __syncthreads();
+    float m = red[0][0];
+#pragma unroll
+    for (int w = 1; w < LANES / 64; ++w) m = max3(m, red[w][0], m);
+    Sums all = {m, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < LANES / 64; ++w) {
+      Sums one = {red[w][0], red[w][1], 0.f};
+      rebase(one, m, c);
+      all.s += one.s;
+    }
+    s = all;
+  }
+  return s;
+}
+
 // dx = scale (g at the token + p (dlse - g - dH (ln p + H))), p = exp(z - lse). A thread loads its 32
 // values before it uses any. Bound by HBM: 4096 x 128000 in bf16, read and written, 399 us, 5.3 TB/s, the
 // rate of a copy; 65536 x 100 11.5 us. 301 x 50001 fp32 out of wider rows takes 23 us (5.3 TB/s).
+// A row of large |lse| is one workgroup's alone, which reads all of it before it writes any: where all
+// rows are such, 4096 x 128000 takes 716 us, one row of 128000 44 in place of 8.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
   constexpr int kStep = 8 * LANES, kSub = 256 / LANES;
@@ -487,38 +538,59 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
   const uint32_t task = blockIdx.x * kSub + sub, parts = a.parts;
   const int64_t row = a.row0 + task / parts;
   if (row >= a.n) return;
-  const int at0 = int(task % parts) * kGroups * kStep + 8 * t;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   T* dx = static_cast<T*>(a.dx) + row * a.lddx;
+  Raw8<T> raw[kGroups];
+  auto load = [&](int part) {
+    const int first = part * kGroups * kStep;
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u)
+      if (first + u * kStep < a.vocab) load_piece(raw[u], x, first + 8 * t + u * kStep, a.vocab);
+  };
+  const int own_part = int(task % parts);
   const float lse = a.lse[row];
   const int64_t token = a.tokens ? a.tokens[row] : -1;
   float g = a.dlogp && token >= 0 ? a.dlogp[row] : 0.f;
   if (token >= a.vocab) g = __builtin_nanf("");
   const float gh = a.dentropy ? a.dentropy[row] : 0.f, h = a.dentropy ? a.entropy[row] : 0.f;
   const float gl = (a.dlse ? a.dlse[row] : 0.f) - g;
-  // Nothing left of the row: no gradient. A row of the lowest finite value counts as such: beside
-  // it lse cannot hold the logarithm of the vocabulary, and p would be 1 everywhere.
+  // Nothing left of the row: no gradient. A row of the lowest finite value counts as such.
   const bool none = lse < -1e30f;
-  Raw8<T> raw[kGroups];
+  // The loaded part's gradient, ln p = scale (x - ref) - rest.
+  auto store = [&](int part, float ref, float rest) {
+    const int at0 = part * kGroups * kStep + 8 * t;
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u)
-    if (at0 - 8 * t + u * kStep < a.vocab) load_piece(raw[u], x, at0 + u * kStep, a.vocab);
+    for (int u = 0; u < kGroups; ++u) {
+      const int at = at0 + u * kStep;
+      if (at >= a.vocab) break;
+      float v[8];
+      values8(raw[u], v);
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u) {
-    const int at = at0 + u * kStep;
-    if (at >= a.vocab) break;
-    float v[8];
-    values8(raw[u], v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float lp = v[e] * a.scale - lse;
-      const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
-      float d = p * (gl - gh * (max3(lp, -1e4f, -1e4f) + h));
-      if (at + e == token) d += g;
-      v[e] = none ? 0.f : d * a.scale;
+      for (int e = 0; e < 8; ++e) {
+        const float lp = (v[e] - ref) * a.scale - rest;
+        const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+        float d = p * (gl - gh * (max3(lp, -1e4f, -1e4f) + h));
+        if (at + e == token) d += g;
+        v[e] = none ? 0.f : d * a.scale;
+      }
+      store_upto8(dx + at, v, a.vocab - at);
     }
-    store_upto8(dx + at, v, a.vocab - at);
+  };
+  if (!none && (lse > kFarLse || lse < -kFarLse)) {
+    // Neighbouring rows take different places of theirs, which are on different XCDs.
+    if (own_part != int(uint32_t(row) % parts)) return;
+    const Sums s = row_sums<T, LANES>(x, a.vocab, t, a.scale * kLog2e);
+    // Not where the caller's lse is of more than this row: then it counts as it is.
+    const float ln = logf(s.s), own = a.scale * s.m + ln;
+    const bool is = own == lse || fabsf(own - lse) <= fabsf(lse) * 0x1p-22f;
+    for (int part = 0; part < int(parts); ++part) {
+      load(part);
+      store(part, is ? s.m : 0.f, is ? ln : lse);
+    }
+    return;
   }
+  load(own_part);
+  store(own_part, 0.f, lse);
 }
 
 constexpr int64_t kMostTasks = int64_t(1) << 22;  // of a launch, in workgroups
