@@ -85,9 +85,11 @@ __device__ inline float max3(float a, float b, float c) {
 struct Sums {
   float m, s, t;  // t in units of log 2: sum of 2^y y
 };
+// Of 2^((x - m) c) = exp(scale (x - m)); finite for every scale, so that the largest values have 2^0.
+__device__ inline float exponent_scale(float scale) { return fminf(scale * kLog2e, 3.4028235e38f); }
 // The reference of the exponents: any finite one for a row that has only -inf yet.
 __device__ inline float finite_max(float m) { return m > -__builtin_inff() ? m : 0.f; }
-// to the maximum m (not smaller). c: scale log2 e.
+// to the maximum m (not smaller). c: exponent_scale.
 __device__ inline void rebase(Sums& a, float m, float c) {
   // Above 0 only from -inf, with sums of 0.
   const float d = fminf(fmaxf((finite_max(a.m) - finite_max(m)) * c, -1e30f), 0.f);
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int list_len) {
   const int part = int(task % parts), p0 = part * a.part_len;
   const int len = std::min(a.part_len, a.vocab - p0);
   const T* x = static_cast<const T*>(a.x) + row * a.ldx + p0;
-  const float c = a.scale * kLog2e;
+  const float c = exponent_scale(a.scale);
 
   Sums s = {-__builtin_inff(), 0.f, 0.f};
   float best = -__builtin_inff();
@@ -429,7 +431,7 @@ __global__ void __launch_bounds__(256) k_logprobs_join(LogprobArgs a) {
   const int sub = row_of_thread<LANES>(), t = threadIdx.x % LANES, lane = threadIdx.x & 63;
   const int64_t row = a.row0 + int64_t(blockIdx.x) * kSub + sub;
   if (row >= a.n) return;
-  const float c = a.scale * kLog2e;
+  const float c = exponent_scale(a.scale);
   const int keys = a.parts * a.k;
   const uint64_t* all = a.keys + row * keys;
   uint64_t key[kEach] = {}, mth = 0;
@@ -579,7 +581,7 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobGradArgs a) {
   if (!none && (lse > kFarLse || lse < -kFarLse)) {
     // Neighbouring rows take different places of theirs, which are on different XCDs.
     if (own_part != int(uint32_t(row) % parts)) return;
-    const Sums s = row_sums<T, LANES>(x, a.vocab, t, a.scale * kLog2e);
+    const Sums s = row_sums<T, LANES>(x, a.vocab, t, exponent_scale(a.scale));
     // Not where the caller's lse is of more than this row: then it counts as it is.
     const float ln = logf(s.s), own = a.scale * s.m + ln;
     const bool is = own == lse || fabsf(own - lse) <= fabsf(lse) * 0x1p-22f;
