@@ -578,7 +578,9 @@ optima_status optima_mx4_unpack(const void* Q, const void* scales, int64_t n, in
  * X: [n_tok][d] of x_dtype BF16 with pitch ldx and x_scales NULL, or of MX4: packed tokens with
  * x_scales (ldx is not used). n_tok <= 2^21, d <= 2^20, d_out <= 2^24, and fewer than 2^24 - 8
  * tiles of 64 x 64 outputs. Y: [n_tok][d_out] BF16 or F32. Products of values are exact, their sums
- * fp32. A zero weight adds exactly nothing, except to an infinite or NaN token (NaN).
+ * fp32. A zero weight adds exactly nothing, except to an infinite or NaN token (NaN). More than 16
+ * packed tokens want both scales 16-byte aligned, as an allocation is: at other multiples of 4 bytes
+ * every 16 tokens read all weights again.
  * ws: optima_mx4_workspace_bytes(n_tok, d, d_out) bytes: 0 up to 8 tokens, never less for more. */
 size_t optima_mx4_workspace_bytes(int64_t n_tok, int64_t d, int64_t d_out);
 optima_status optima_mx4_linear(const void* X, int64_t ldx, int x_dtype, const void* x_scales,

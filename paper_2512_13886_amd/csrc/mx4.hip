@@ -240,8 +240,8 @@ __device__ inline void wave_exchange() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Up to 16 tokens. A workgroup takes 16 outputs, its waves every waves-th batch of 512 values,
-// and the waves' sums are joined in LDS in their order. Bound by the latency of one or two batches of
+// Up to 16 tokens (of packed ones blockIdx.y's). A workgroup takes 16 outputs, its waves every waves-th
+// batch of 512 values, and the waves' sums are joined in LDS in their order. Bound by the latency of one or two batches of
 // loads a wave, which nothing hides: one 16-bit token, 14336 -> 4096 (31 MB) 8.2 us, 3.8 TB/s, with
 // weights that no cache holds 9.5. Twice the outputs a workgroup took 12.8, codes loaded a batch ahead 12.2.
 static_assert(kMx4FewPitch == kBatchK * 2 + 64, "a token's batch, with 64 bytes between rows");
@@ -266,7 +266,8 @@ __global__ void __launch_bounds__(64 * kMx4FewWaves) k_mx4_few(Mx4Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   float* part = reinterpret_cast<float*>(lds);  // [wave][lane][4], at the end
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int b = lane >> 4, i = lane & 15, tokens = int(a.n_tok);
+  const int64_t t0 = PACKED ? int64_t(blockIdx.y) * kMx4Few : 0;
+  const int b = lane >> 4, i = lane & 15, tokens = int(std::min<int64_t>(a.n_tok - t0, kMx4Few));
   const int64_t n0 = int64_t(blockIdx.x) * 16 * RB;
   const int tok = std::min(i, tokens - 1), batches = (a.chunks + kBatch - 1) / kBatch;
   const bf16_t* x = static_cast<const bf16_t*>(a.x);
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(64 * kMx4FewWaves) k_mx4_few(Mx4Args a) {
     if constexpr (PACKED) {
       u32x4 f[kBatch];
       uint32_t sx;
-      load_codes(f, sx, static_cast<const uint8_t*>(a.x), a.xs, a, tok, batch, b);
+      load_codes(f, sx, static_cast<const uint8_t*>(a.x), a.xs, a, t0 + tok, batch, b);
 #pragma unroll
       for (int m = 0; m < RB; ++m) {
         mfma_mx4<0>(sum[m], w[m][0], s[m], f[0], sx);
@@ -341,7 +342,7 @@ __global__ void __launch_bounds__(64 * kMx4FewWaves) k_mx4_few(Mx4Args a) {
     const float* p = part + ((nn >> 4) * 64 + (nn >> 2 & 3) * 16 + t) * 4 + (nn & 3);
     float v = 0.f;
     for (int w = 0; w < waves; ++w) v += p[w * RB * 256];
-    const int64_t at = t * a.ldy + n0 + nn;
+    const int64_t at = (t0 + t) * a.ldy + n0 + nn;
     if (a.y_f32)
       static_cast<float*>(a.y)[at] = v;
     else
@@ -684,8 +685,8 @@ void launch_tile(const Mx4Args& a, hipStream_t s) {
 template <bool PACKED, int ROWS, int RB, bool RAGGED>
 void launch_few(const Mx4Args& a, int waves, hipStream_t s) {
   const size_t each = std::max<size_t>(PACKED ? 0 : size_t(a.n_tok) * kMx4FewPitch, RB * 1024);
-  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB, RAGGED>), dim3(unsigned(ceil_div(a.d_out, 16 * RB))),
-                     dim3(64 * waves), waves * each, s, a);
+  const dim3 grid(unsigned(ceil_div(a.d_out, 16 * RB)), unsigned(ceil_div(a.n_tok, kMx4Few)));
+  hipLaunchKernelGGL((k_mx4_few<PACKED, ROWS, RB, RAGGED>), grid, dim3(64 * waves), waves * each, s, a);
 }
 template <int ROWS, int RB>
 void launch_few_16bit(const Mx4Args& a, int waves, hipStream_t s) {
@@ -694,13 +695,18 @@ void launch_few_16bit(const Mx4Args& a, int waves, hipStream_t s) {
 }
 
 void launch_packed(const Mx4Args& a, hipStream_t s) {
-  // Every 16 or 32 outputs of the few-token kernel read all tokens again. us with it and in tiles: 16
-  // tokens, 4096 -> 4096 5.5 and 9.4, -> 9000 10.8 and 10.1, -> 60000 35 and 33; 8 tokens, 8192 -> 28672 33 and
-  // 41, 4096 -> 60000 31.4 and 29.8, -> 128000 60 and 55; one token, -> 128000 53 and 56.
-  const Mx4FewPlan p = mx4_few_plan(a.n_tok, a.d, a.d_out, true);
-  if (a.n_tok > kMx4Few || a.n_tok * a.d_out >= (a.n_tok > 8 ? 100000 : 240000)) launch_tile(a, s);
-  else if (p.blocks == 2) launch_few<true, 4, 2, false>(a, p.waves, s);
-  else launch_few<true, 4, 1, false>(a, p.waves, s);
+  if (mx4_packed_tiles(a.n_tok, a.d_out, aligned16(a.xs) && aligned16(a.s))) return launch_tile(a, s);
+  const int64_t most = int64_t(65535) * kMx4Few;  // of a launch
+  for (int64_t t = 0; t < a.n_tok; t += most) {
+    Mx4Args b = a;
+    b.x = static_cast<const uint8_t*>(a.x) + t * a.row;
+    b.xs = a.xs + t * a.srow;
+    b.y = static_cast<char*>(a.y) + t * a.ldy * (a.y_f32 ? 4 : 2);
+    b.n_tok = std::min(a.n_tok - t, most);
+    const Mx4FewPlan p = mx4_few_plan(std::min<int64_t>(b.n_tok, kMx4Few), a.d, a.d_out, true);
+    if (p.blocks == 2) launch_few<true, 4, 2, false>(b, p.waves, s);
+    else launch_few<true, 4, 1, false>(b, p.waves, s);
+  }
 }
 void launch_16bit(const Mx4Args& a, hipStream_t s) {
   const Mx4SlabPlan p = mx4_slab_plan(a.n_tok, a.d, a.d_out);

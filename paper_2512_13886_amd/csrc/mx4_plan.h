@@ -60,6 +60,16 @@ inline Mx4Plan mx4_plan(int64_t n_tok, int64_t d, int64_t d_out) {
   return best;
 }
 
+// Whether packed tokens go in tiles, or by 16 in the few-token kernel. Every 16 or 32 outputs of that one
+// read all tokens again. us with it and in tiles: 16 tokens, 4096 -> 4096 5.5 and 9.4, -> 9000 10.8 and 10.1,
+// -> 60000 35 and 33; 8 tokens, 8192 -> 28672 33 and 41, 4096 -> 60000 31.4 and 29.8, -> 128000 60 and 55;
+// one token, -> 128000 53 and 56.
+// Tiles bring scales into LDS by direct loads of 16 bytes, at multiples of 16; the other kernel takes them
+// by dwords, so that other scales (of 4 bytes' alignment) go there whatever their number.
+inline bool mx4_packed_tiles(int64_t n_tok, int64_t d_out, bool aligned) {
+  return aligned && (n_tok > kMx4Few || n_tok * d_out >= (n_tok > 8 ? 100000 : 240000));
+}
+
 // The few-token kernel: blocks of 16 outputs that a workgroup takes, and its waves.
 struct Mx4FewPlan {
   int blocks, waves;
