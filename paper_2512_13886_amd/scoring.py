@@ -91,15 +91,18 @@ def gradients(head: Head, X: torch.Tensor, tokens: torch.Tensor, R: torch.Tensor
     is), bfloat16 of the hidden states."""
     n, d = X.shape
     S, A = _normed(head, X, R)
-    s = _scores(_product(A, head.weight, torch.bfloat16), 0)
+    # float32, as in score: in bfloat16 logits near 16 are 1/8 apart, and the loss would not be the score.
+    s = _scores(_product(A, head.weight, torch.float32), 0)
     L.optima_token_logprobs(s.logits, tokens, s.logp, lse=s.lse)
     given = tokens >= 0
     count = given.sum().clamp_(min=1)
     dlogp = torch.where(given, -1.0 / count, 0.0).float()
-    # The logits are not needed again: their gradient takes their place.
+    # The logits are not needed again: their gradient takes their place. It is rounded once, for the
+    # 16-bit products.
     L.optima_token_logprobs_backward(s.logits, s.lse, s.logits, tokens=tokens, dlogp=dlogp)
-    dA = _product(s.logits, head.weight.t().contiguous(), torch.bfloat16)
-    g = {"weight": _product(s.logits.t().contiguous(), A.t().float().contiguous(), torch.float32),
+    D = s.logits.bfloat16()
+    dA = _product(D, head.weight.t().contiguous(), torch.bfloat16)
+    g = {"weight": _product(D.t().contiguous(), A.t().float().contiguous(), torch.float32),
          "norm": torch.empty_like(head.norm)}
     if mask is not None:
         g["weight"].mul_(mask)

@@ -194,3 +194,21 @@ def test_command(capsys):
     feedforward.main(["--d", "128", "--ff", "192", "--tokens", "512", "--steps", "2", "--vocab", "300"])
     out = capsys.readouterr().out
     assert out.count("score") == 3 and "nan" not in out
+
+
+def test_loss_is_the_score(sc):
+    """The loss that gradients and recover return is minus the mean of score's log probabilities, also
+    where logits are large: no 16-bit rounding of them between."""
+    n, d, vocab = 300, 128, 4001
+    head = sc.synthetic_head(d, vocab, 3)
+    head.weight *= 4
+    X, R = _states(n, d, 2)
+    tokens = torch.arange(n, device=X.device) * 11 % vocab
+    tokens[::4] = -100
+    logp = sc.score(head, X, tokens, R).logp
+    want = -float(logp.double().sum() / (tokens >= 0).sum())
+    mask = torch.ones(vocab, d, dtype=torch.uint8, device=X.device)
+    # A sum of 225 terms of one sign in fp32, and its quotient.
+    bound = abs(want) * 227 * 2.0 ** -24
+    assert abs(sc.gradients(head, X, tokens, R)[0] - want) <= bound
+    assert abs(sc.recover(head, mask, X, tokens, R, steps=1)[1][0] - want) <= bound
