@@ -13,6 +13,7 @@ This module sequences library calls and allocates with torch.
 """
 from __future__ import annotations
 
+import ctypes
 from dataclasses import dataclass, replace
 from typing import Callable
 
@@ -154,11 +155,21 @@ class PackedHead:
     def step(self, X: torch.Tensor, S: torch.Tensor, tokens: torch.Tensor,
              scale: float = 1.0) -> Scores:
         """S <- X + S, and the scores of `tokens` after it, in this object's buffers. X and S are
-        [n, d], bfloat16 or float32 of one type."""
+        [n, d], bfloat16 or float32 of one type. A call that is refused leaves S as it is."""
         n = X.shape[0]
         if n > self.normed.shape[0]:
             raise ValueError(f"{n} tokens, made for {self.normed.shape[0]}")
         A, o = self.normed[:n], self.out
+        # What the calls after the norm would refuse. The norm refuses X and S itself, before it writes.
+        L._need_one_device(None, X, S, tokens, A)
+        if not (tokens.dtype == torch.int64 and tokens.is_cuda and tokens.shape == (n,) and
+                tokens.is_contiguous()):
+            raise ValueError(f"tokens must be contiguous int64 [{n}] on the device")
+        if o.top_index is not None and \
+                tokens.untyped_storage().data_ptr() == o.top_index.untyped_storage().data_ptr():
+            raise ValueError("tokens lie in this object's alternatives, which the step writes")
+        if not 0.0 < ctypes.c_float(scale).value < float("inf"):
+            raise ValueError(f"scale must be positive and finite, got {scale}")
         out = Scores(o.logits[:n], o.logp[:n], o.lse[:n], o.entropy[:n],
                      None if o.top_index is None else o.top_index[:n],
                      None if o.top_logp is None else o.top_logp[:n])

@@ -212,3 +212,24 @@ def test_loss_is_the_score(sc):
     bound = abs(want) * 227 * 2.0 ** -24
     assert abs(sc.gradients(head, X, tokens, R)[0] - want) <= bound
     assert abs(sc.recover(head, mask, X, tokens, R, steps=1)[1][0] - want) <= bound
+
+
+def test_a_refused_step_changes_nothing(sc):
+    """S is updated in place by the step's first call: what a later one would refuse is refused before."""
+    from paper_2512_13886_amd import OptimaError
+    n, d, vocab = 5, 128, 900
+    packed = sc.PackedHead(sc.synthetic_head(d, vocab, 7), max_tokens=8, top=4)
+    X, R = _states(n, d, 8)
+    tokens = torch.arange(n, device=X.device)
+    for bad in (dict(tokens=tokens.int()), dict(tokens=tokens[:4]), dict(tokens=tokens.cpu()),
+                dict(tokens=torch.arange(2 * n, device=X.device)[::2]), dict(tokens=tokens.unsqueeze(0)),
+                dict(tokens=packed.out.top_index.view(-1)[:n]),
+                dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+                dict(scale=1e-60), dict(scale=1e60), dict(X=X[:4]), dict(X=X[:, :100]), dict(X=X.half())):
+        S = R.clone()
+        with pytest.raises((ValueError, OptimaError)):
+            packed.step(**dict(dict(X=X, S=S, tokens=tokens), **bad))
+        assert torch.equal(S, R)
+    S = R.clone()
+    packed.step(X, S, tokens)
+    assert not torch.equal(S, R)
