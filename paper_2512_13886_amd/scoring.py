@@ -131,10 +131,14 @@ def recover(head: Head, mask: torch.Tensor, X: torch.Tensor, tokens: torch.Tenso
 
 class PackedHead:
     """The head with W in microscaled 4-bit floating point, for up to max_tokens tokens a call, taken
-    in 16 bits, or with packed_tokens in 4 bits too. All buffers are made here: step only launches
-    and can be captured in a graph."""
+    in 16 bits, or with packed_tokens in 4 bits too. Logits are kept in logits_dtype: bfloat16 halves
+    what is written and read again of them, and its half step (1/16 at logits of 16 to 32) is below the
+    4-bit weights' own error; the log probabilities, lse and entropy are those of the logits as they
+    are kept. float32 keeps the products' sums as they are. All buffers are made here: step only
+    launches and can be captured in a graph."""
 
-    def __init__(self, head: Head, max_tokens: int = 1, top: int = 0, packed_tokens: bool = False):
+    def __init__(self, head: Head, max_tokens: int = 1, top: int = 0, packed_tokens: bool = False,
+                 logits_dtype: torch.dtype = torch.bfloat16):
         vocab, d = head.weight.shape
         dev = head.weight.device
         self.norm, self.eps = head.norm, head.eps
@@ -147,7 +151,7 @@ class PackedHead:
         L.optima_mx4_pack(head.weight, *self.packed)
         self.normed = torch.empty((max_tokens, d), dtype=torch.bfloat16, device=dev)
         self.codes = room(max_tokens) if packed_tokens else None
-        self.out = _scores(torch.empty((max_tokens, vocab), dtype=torch.bfloat16, device=dev), top)
+        self.out = _scores(torch.empty((max_tokens, vocab), dtype=logits_dtype, device=dev), top)
         space = max(L.optima_mx4_workspace_bytes(max_tokens, d, vocab),
                     L.optima_token_logprobs_workspace_bytes(max_tokens, vocab, top), 16)
         self.ws = torch.empty(space, dtype=torch.uint8, device=dev)

@@ -233,3 +233,32 @@ def test_a_refused_step_changes_nothing(sc):
     S = R.clone()
     packed.step(X, S, tokens)
     assert not torch.equal(S, R)
+
+
+@pytest.mark.parametrize("packed_tokens", (False, True))
+@pytest.mark.parametrize("n", (1, 20, 150))
+def test_packed_head_with_fp32_logits(sc, n, packed_tokens):
+    """float32 logits: the 4-bit products' own sums, without a 16-bit rounding."""
+    d, vocab = 300, 9000
+    head = sc.synthetic_head(d, vocab, 7)
+    head.weight *= 6
+    packed = sc.PackedHead(head, max_tokens=n, top=4, packed_tokens=packed_tokens,
+                           logits_dtype=torch.float32)
+    X, R = _states(n, d, 8)
+    tokens = torch.arange(n, device=X.device) * 13 % vocab
+    out = packed.step(X, R.clone(), tokens)
+    assert out.logits.dtype == torch.float32
+    a = packed.normed[:n]
+    x = O.mx4_values(a)[0] if packed_tokens else a.double()
+    w = O.mx4_values(head.weight)[0]
+    z = torch.mm(x, w.t().contiguous())
+    # Products are exact, their sum is rounded d times at most.
+    off = torch.mm(x.abs(), w.abs().t().contiguous()) * (d * 2.0 ** -24) * (1 + B)
+    assert ((out.logits.double() - z).abs() <= off).all()
+    lse, logp, entropy = O.token_logprobs(z, tokens)
+    # A row's log p moves by twice its logits' largest change at most; the call's own roundings are those
+    # of an fp32 lse near 40 and of sums of 9000 terms, 300 steps of 2^-24 of it at most.
+    most = 2 * off.amax(1) + 2.0 ** -24 * 300 * (1 + z.abs().amax(1))
+    for got, want in ((out.lse, lse), (out.logp, logp)):
+        assert ((got.double() - want).abs() <= most).all()
+    assert torch.equal(out.top_index, O.top(out.logits, 4))
