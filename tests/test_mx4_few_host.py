@@ -14,10 +14,19 @@ using namespace optima;
 int main(int argc, char** argv) {
   for (int i = 1; i + 2 < argc; i += 3) {
     const int64_t n = atoll(argv[i]), d = atoll(argv[i + 1]), ff = atoll(argv[i + 2]);
-    printf("%d %d\n", int(mx4_packed_tiles(n, ff, true)), int(mx4_packed_tiles(n, ff, false)));
+    const Mx4FewPlan f = mx4_few_plan(n, d, ff, false);
+    printf("%d %d %d %d %d\n", int(mx4_packed_tiles(n, ff, true)), int(mx4_packed_tiles(n, ff, false)),
+           mx4_slab_plan(n, d, ff).tokens, f.blocks, f.waves);
   }
 }
 """
+# Sizes of tests/test_gpu_mx4.py's kind for few 16-bit tokens, that slabs do not take: (blocks of 16 outputs,
+# waves). Widths that are no multiple of 8 take the kernel's ragged form, in four tokens at a time.
+FEW = {(1, 4097, 5001): (1, 9), (1, 4096, 5000): (1, 8), (3, 1001, 66000): (2, 2), (4, 1000, 66000): (2, 2),
+       (2, 14337, 66001): (2, 8), (8, 4097, 14336): (2, 8), (6, 1001, 13000): (2, 2), (5, 1000, 13000): (2, 2),
+       (7, 4097, 5001): (1, 8), (9, 1001, 9000): (2, 2), (16, 1001, 9000): (2, 2), (12, 1000, 9000): (2, 2),
+       (9, 14335, 4000): (1, 16), (16, 8191, 4000): (1, 9), (10, 8192, 4000): (1, 15),
+       (1, 7, 70000): (1, 1), (4, 7, 70000): (2, 1), (8, 5, 13000): (2, 1)}
 
 
 @pytest.fixture(scope="module")
@@ -48,3 +57,13 @@ def test_odd_scales_never_take_tiles(plans):
     assert all(p[1] == 0 for p in plans(sizes))
     assert [p[0] for p in plans([(16, 4096, 4096), (16, 4096, 9000), (8, 8192, 28672), (17, 64, 64)])] == [
         0, 1, 0, 1]
+
+
+@pytest.mark.slow
+def test_sizes_take_every_few_token_form(plans):
+    got = plans(FEW)
+    assert all(p[2] == 0 for p in got), [s for s, p in zip(FEW, got) if p[2]]
+    assert {s: (p[3], p[4]) for s, p in zip(FEW, got)} == FEW
+    # Up to 4 tokens and more, one block and two, widths of multiples of 8 and others.
+    assert {(n > 4, b, d % 8 > 0) for (n, d, _), (b, _) in FEW.items()} == {
+        (a, b, c) for a in (False, True) for b in (1, 2) for c in (False, True)}
