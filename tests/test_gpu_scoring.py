@@ -262,3 +262,38 @@ def test_packed_head_with_fp32_logits(sc, n, packed_tokens):
     for got, want in ((out.lse, lse), (out.logp, logp)):
         assert ((got.double() - want).abs() <= most).all()
     assert torch.equal(out.top_index, O.top(out.logits, 4))
+
+
+def _exact_loss(head, X, R, tokens):
+    a, z = _double(head, X, R)
+    logp = torch.log_softmax(z, 1).gather(1, tokens.clamp(min=0).unsqueeze(1)).squeeze(1)
+    return -float(logp[tokens >= 0].mean())
+
+
+def test_recover_moves_against_the_gradient(sc):
+    """One step against the definition: norm and kept entries move by lr times the gradient relative to its
+    largest entry times the largest value, in 64 bits of the gradients that gradients returns; and a
+    short step lowers the loss."""
+    n, d, vocab, lr = 512, 96, 400, 1e-3
+    head = sc.synthetic_head(d, vocab, 5)
+    X, R = _states(n, d, 6)
+    tokens = torch.arange(n, device=X.device) * 7 % vocab
+    tokens[::5] = -1
+    mask = (torch.rand(vocab, d, generator=torch.Generator(device="cuda").manual_seed(1),
+                       device="cuda") < 0.5).to(torch.uint8)
+    head.weight *= mask
+    loss, g, _ = sc.gradients(head, X, tokens, R, mask)
+    out, losses = sc.recover(head, mask, X, tokens, R, steps=1, lr=lr)
+    assert losses == [loss]
+    slope = 0.0
+    for name in ("norm", "weight"):
+        p, q, grad = (t.double() for t in (getattr(head, name), getattr(out, name), g[name]))
+        step = -lr * grad * p.abs().amax() / grad.abs().amax()
+        # The step has five roundings of its own, and the new value one.
+        assert ((q - p - step).abs() <= 2.0 ** -24 * (5 * step.abs() + q.abs())).all()
+        assert float((q - p).abs().amax()) > 0.5 * lr * float(p.abs().amax())
+        slope += float((grad * (q - p)).sum())
+    assert slope < 0
+    assert (out.weight[mask == 0] == 0).all()
+    # The loss itself, in 64 bits.
+    assert _exact_loss(out, X, R, tokens) < _exact_loss(head, X, R, tokens)
