@@ -44,9 +44,6 @@ __device__ inline uint32_t order_of(float x) {
 __device__ inline float value_of(uint32_t o) {
   return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
-__device__ inline uint64_t key_of(float x, uint32_t place) {
-  return uint64_t(order_of(x)) << 32 | uint32_t(~place);
-}
 
 // v of another lane of the same 16: rotated by 8, 4, 2 and 1 lanes in turn, every lane gets a sum or
 // maximum of all 16.
@@ -605,7 +602,8 @@ constexpr int64_t kMostTasks = int64_t(1) << 22;  // of a launch, in workgroups
 // takes as long for fewer (64 rows of 32000 with 20 15.3 to 13.4, one of 20000 with 5 11.1 to 8.8; but one
 // of 128000 in fp32 with 32 14.9 to 17.5); of 16384 where the last rows would otherwise leave CUs
 // idle for long (8192 rows of 128000 420 us in one, 370 in seven); and of kPartLen at most with
-// alternatives, whose list is kept for a part.
+// alternatives, whose groups of eight have places below 4096 and whose list (k ceil(len / 2048) 64 bytes
+// of LDS, 32 KB at k = 32) is kept for a part.
 struct LogprobPlan {
   int lanes, parts, len;
 };

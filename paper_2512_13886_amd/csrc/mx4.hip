@@ -354,10 +354,11 @@ __global__ void __launch_bounds__(64 * kMx4FewWaves) k_mx4_few(Mx4Args a) {
 // turn, for all waves of a workgroup; a wave takes 32 outputs, whose codes it loads a batch ahead, in
 // the order in which a lane's sums of both blocks are eight consecutive outputs (stored as they
 // came out of the MFMA, four by four, 8192 tokens took 1126 us in place of 1083). With few outputs the
-// batches are split over blockIdx.y, and k_mx4_join adds the parts. Bound by the conversion of codes,
-// which every 64 tokens repeat, and its loads' latency: 64 tokens, 4096 -> 128000 (279 MB) 105 us, 4096
-// -> 14336 24 us, where packed tokens, whose codes need no conversion, take 54 and 12; 8192 tokens, 4096
-// -> 14336 0.89 PFLOP/s.
+// batches are split over blockIdx.y, and k_mx4_join adds the parts. 64 tokens, 4096 -> 128000 (279 MB) 105
+// us, 4096 -> 14336 24 us, where packed tokens take 54 and 12; 8192 tokens, 4096 -> 14336 0.89 PFLOP/s. Bound
+// by waits: two waves a SIMD with a barrier a batch spend 39 to 46 % of their time on loads, LDS and
+// barriers, while the matrix instructions are busy for 28, 12 and 37 % of it, all vector instructions (the
+// conversion of codes, which every 64 tokens repeat, is a part) for 21, 14 and 27, and LDS for 32, 13 and 42.
 constexpr int kSlabWaves = kMx4SlabRows / 32;
 
 template <int NT>
